@@ -205,6 +205,130 @@ DP_API int dp_shared_table_cross_sqnorms(const int32_t* ids, const void* G_emb, 
                                          const void* h, int T_out, int d, int V, int dtype, float* sqnorm,
                                          void* cuda_stream);
 
+/* ---- Global norm over many tensors, and clipping --------------------------------------------------------------
+ * The clip of an aggregated gradient: of the noised mean of Algorithm 1 (post-processing, so it costs no privacy), or
+ * of the plain batch gradient in a non-private baseline.  (No counterpart in the paper.)
+ * A list is two HOST arrays, device pointers and element counts, of one dtype (DP_F32 or DP_BF16); entries with count 0
+ * are skipped and their pointers not looked at, and n_tensors may be 0.  Any element alignment is accepted.
+ * Lists of several dtypes, or the shards of several ranks, are combined with accumulate_into or by adding the sums. */
+
+/* Bytes of scratch for dp_global_sqnorm (fixed; 256-byte aligned). */
+DP_API size_t dp_global_norm_workspace_bytes(void);
+
+/* *sqsum (device double) = or += the sum over all tensors and elements of x^2.  Groups of at most 32 squares are summed
+ * in fp32 (in fp64 where they would leave its range), the groups in fp64, in an order that only the list and the device
+ * decide. */
+DP_API int dp_global_sqnorm(const void* const* tensors /*HOST*/, const int64_t* sizes /*HOST*/, int n_tensors, int dtype,
+                            int accumulate_into, double* sqsum, void* workspace, size_t workspace_bytes,
+                            void* cuda_stream);
+
+/* outs[k] = tensors[k] * f, f = min(1, max_norm / sqrt(*sqsum)), 1 where *sqsum = 0.  outs[k] may be tensors[k] itself
+ * (then nothing is written when f = 1); other overlaps are not allowed.  norm_and_factor (device float[2], or NULL)
+ * receives sqrt(*sqsum) and f.  An infinite norm gives f = 0 and a NaN one f = NaN: both show in the result. */
+DP_API int dp_clip_by_global_norm(const void* const* tensors /*HOST*/, void* const* outs /*HOST*/,
+                                  const int64_t* sizes /*HOST*/, int n_tensors, int dtype, const double* sqsum,
+                                  double max_norm, float* norm_and_factor, void* cuda_stream);
+
+/* dp_adamw_step on g * f with the factor f of dp_clip_by_global_norm, without writing the clipped gradient; with
+ * zero_g != 0 it also clears g. */
+DP_API int dp_clip_adamw_step(float* theta, float* m, float* v, float* g, int zero_g, int64_t n, const double* sqsum,
+                              double max_norm, double lr, double beta1, double beta2, double xi, double weight_decay,
+                              int64_t t, void* cuda_stream);
+
+/* ---- Tensors whose per-example gradient is given ------------------------------------------------------------------
+ * A small trainable tensor (a relative-position table, the gain of a head norm) for which the backward pass has formed
+ * every example's gradient: grad [B, width] fp32.  Its two steps beside those of dp_layer: */
+typedef struct dp_rows {
+  const float* grad;   /* [B, width] per-example gradients */
+  float* acc;          /* [width] accumulator (+=); may be NULL for dp_rows_sqnorms.  No two entries of a call share one */
+  int64_t width;
+} dp_rows;
+
+/* sqnorm[i] = or += sum over the tensors of |grad_i|^2 (the whole-model clip of Algorithm 1: call it with
+ * accumulate_into = 1 after dp_per_example_sqnorms, before dp_clip_factors). */
+DP_API int dp_rows_sqnorms(const dp_rows* rows /*HOST*/, int n_rows, int B, float* sqnorm, int accumulate_into,
+                           void* cuda_stream);
+
+/* acc += sum_i clip_i * grad_i for every tensor; fp32, in a fixed order. */
+DP_API int dp_rows_clipped_accumulate(const dp_rows* rows /*HOST*/, int n_rows, int B, const float* clip,
+                                      void* cuda_stream);
+
+/* ---- Learned relative position bias ---------------------------------------------------------------------------------
+ * bias[h][q][k] = table[bucket(k - q - offset)][h], table [num_buckets, n_heads].  (No counterpart in the paper, whose
+ * model has absolute positions; the table is one more trainable tensor for the per-example clip.)
+ * Let half = num_buckets, or num_buckets / 2 with `bidirectional`, where keys behind the query (k > q + offset) use the
+ * second half by their distance n = |k - q - offset|.  Without it a key behind its query counts as distance 0.
+ * exact = half / 2: distances below it have a bucket each; bucket exact + j holds the distances with
+ * (n / exact)^(half - exact) >= (max_distance / exact)^j, compared exactly, and the last bucket everything beyond.
+ * Needs 2 <= num_buckets <= 256 (even, >= 4, with bidirectional) and exact < max_distance <= 2^24; Tq, Tk <= 2^24. */
+typedef struct dp_relpos {
+  int32_t num_buckets, max_distance, bidirectional, n_heads;
+  int32_t Tq, Tk;
+  int64_t offset;      /* position of query 0 minus position of key 0 (Tk - 1 for the one query of a decoding step) */
+} dp_relpos;
+
+/* Host-only: starts[j] = smallest distance of bucket j of one side (`half` values, ascending; equal neighbours mean an
+ * empty bucket). */
+DP_API int dp_relpos_bucket_starts(int num_buckets, int max_distance, int bidirectional, int32_t* starts /*HOST*/);
+
+/* out[h * stride_h + q * stride_q + k] = the bias, rounded once to out_dtype.  table and out are DP_F32 or DP_BF16 each;
+ * strides in elements, stride_q >= Tk. */
+DP_API int dp_relpos_bias(const dp_relpos* p /*HOST*/, const void* table, int table_dtype, void* out, int out_dtype,
+                          int64_t stride_h, int64_t stride_q, void* cuda_stream);
+
+/* Bytes of scratch for dp_relpos_bias_grad over B examples; 0 on invalid sizes. */
+DP_API size_t dp_relpos_workspace_bytes(const dp_relpos* p /*HOST*/, int B);
+
+/* Every example's gradient of the table from the gradient G of the scores, G[b * stride_b + h * stride_h + q * stride_q
+ * + k] (DP_F32 or DP_BF16; strides in elements, 0 allowed):
+ *   rows[b][n][h] = or += sum over (q, k) with bucket(k - q - offset) = n of G[b][h][q][k],   rows fp32 [B, num_buckets, n_heads].
+ * q_len, k_len: int32 [B] device arrays or NULL; queries q >= q_len[b] and keys k >= k_len[b] do not count, and causal
+ * != 0 leaves out keys k > q + offset.  What does not count may hold anything, NaN included.  accumulate_into = 1 adds a
+ * further layer that shares the table.  fp32 sums in a fixed order. */
+DP_API int dp_relpos_bias_grad(const dp_relpos* p /*HOST*/, int B, int causal, const void* G, int dtype, int64_t stride_b,
+                               int64_t stride_h, int64_t stride_q, const int32_t* q_len, const int32_t* k_len, float* rows,
+                               int accumulate_into, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---- Norms of queries and keys per head, with the position rotation ---------------------------------------------------
+ * For each head x [dim] of each token:  y = R(p) (gain * x / sqrt(mean(x^2) + eps)),  R(p) turning pair j of the first
+ * `rot` elements by p * inv_freq[j]: (a, b) -> (a cos - b sin, b cos + a sin).  Pair j is elements (j, j + rot/2), or
+ * (2j, 2j + 1) with `interleaved`; elements beyond rot are not turned.  (No counterpart in the paper; the gains are
+ * trainable tensors for the per-example clip.) */
+typedef struct dp_qknorm {
+  int32_t dtype;               /* dp_dtype of queries, keys, outputs and their gradients */
+  int32_t B, T, n_q, n_k;      /* query and key heads; either may be 0, its tensors are then not looked at */
+  int32_t dim, rot;            /* even, dim <= 512, 0 <= rot <= dim */
+  int32_t interleaved;
+  double eps;                  /* >= 0 */
+  const float* gain_q;         /* [dim] fp32, or NULL for ones */
+  const float* gain_k;
+  const int32_t* positions;    /* [B, T], or NULL for 0 .. T-1 */
+  const int32_t* lengths;      /* [B] or NULL: tokens t >= lengths[b] are skipped and their outputs left as they were */
+  const double* inv_freq;      /* HOST [rot / 2], radians per position; read during the call.  The angle is kept modulo a
+                                  turn to 2^-32 at any position */
+} dp_qknorm;
+
+typedef struct dp_heads {      /* a [B, T, heads, dim] view, dim contiguous; strides in elements */
+  void* data;
+  int64_t stride_b, stride_t, stride_h;
+} dp_heads;
+
+/* An output may be its own input (same strides); other overlaps are not allowed.  16-byte vectors are used where dim and
+ * rot are multiples of 16 (bf16) or 8 (fp32, dim <= 256) elements and every head starts on a 16-byte boundary. */
+DP_API int dp_qknorm_rope(const dp_qknorm* p /*HOST*/, const dp_heads* q, const dp_heads* k, const dp_heads* out_q,
+                          const dp_heads* out_k, void* cuda_stream);
+
+/* Bytes of scratch for dp_qknorm_rope_backward (0 if none is needed, or on invalid sizes). */
+DP_API size_t dp_qknorm_workspace_bytes(const dp_qknorm* p /*HOST*/);
+
+/* Backward pass from the inputs q, k of dp_qknorm_rope and the gradients of its outputs: dq, dk, and every example's
+ * gradients of the gains, rows_q and rows_k (fp32 [B, dim], each may be NULL; = or += by accumulate_into).  dq may be q
+ * or dout_q itself (same strides), dk likewise.  Sums run in a fixed order. */
+DP_API int dp_qknorm_rope_backward(const dp_qknorm* p /*HOST*/, const dp_heads* q, const dp_heads* k,
+                                   const dp_heads* dout_q, const dp_heads* dout_k, const dp_heads* dq, const dp_heads* dk,
+                                   float* rows_q, float* rows_k, int accumulate_into, void* workspace,
+                                   size_t workspace_bytes, void* cuda_stream);
+
 /* Test utility: out[k] = the raw Philox word of element elem_offset + k (lane (e & 3) of block e >> 2). */
 DP_API int dp_philox_u32(uint32_t* out, int64_t n_words, int64_t elem_offset, uint64_t seed, uint64_t step,
                   void* cuda_stream);

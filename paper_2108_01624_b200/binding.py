@@ -27,7 +27,11 @@ EXPORTS = ["dp_workspace_bytes", "dp_per_example_sqnorms", "dp_clip_factors", "d
            "dp_clip_stats", "dp_philox_u32", "dp_shared_table_cross_sqnorms",
            "dp_token_equality_mask", "dp_layernorm_sqnorms_static", "dp_poll_status", "dp_last_timeout_info", "dp_launch_count",
            "dp_set_wait_limit_cycles", "dp_selftest_wait_timeout",
-           "dp_status_string", "dp_version"]
+           "dp_status_string", "dp_version",
+           "dp_global_norm_workspace_bytes", "dp_global_sqnorm", "dp_clip_by_global_norm", "dp_clip_adamw_step",
+           "dp_rows_sqnorms", "dp_rows_clipped_accumulate",
+           "dp_relpos_bucket_starts", "dp_relpos_bias", "dp_relpos_workspace_bytes", "dp_relpos_bias_grad",
+           "dp_qknorm_rope", "dp_qknorm_workspace_bytes", "dp_qknorm_rope_backward"]
 
 
 class dp_layer(C.Structure):
@@ -35,6 +39,26 @@ class dp_layer(C.Structure):
                 ("B", C.c_int32), ("T", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32),
                 ("A", C.c_void_p), ("ids", C.c_void_p), ("G", C.c_void_p),
                 ("acc_w", C.c_void_p), ("acc_b", C.c_void_p)]
+
+
+class dp_rows(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("acc", C.c_void_p), ("width", C.c_int64)]
+
+
+class dp_relpos(C.Structure):
+    _fields_ = [("num_buckets", C.c_int32), ("max_distance", C.c_int32), ("bidirectional", C.c_int32),
+                ("n_heads", C.c_int32), ("Tq", C.c_int32), ("Tk", C.c_int32), ("offset", C.c_int64)]
+
+
+class dp_qknorm(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("T", C.c_int32), ("n_q", C.c_int32), ("n_k", C.c_int32),
+                ("dim", C.c_int32), ("rot", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_double),
+                ("gain_q", C.c_void_p), ("gain_k", C.c_void_p), ("positions", C.c_void_p), ("lengths", C.c_void_p),
+                ("inv_freq", C.c_void_p)]
+
+
+class dp_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
 
 
 class DpError(RuntimeError):
@@ -75,6 +99,22 @@ def lib() -> C.CDLL:
         L.dp_token_equality_mask.argtypes = [vp, i32, i32, vp, vp]
         L.dp_shared_table_cross_sqnorms.argtypes = [vp, vp, i32, i32, vp, vp, i32, i32, i32, i32, vp, vp]
         L.dp_layernorm_sqnorms_static.argtypes = [vp, vp, i32, vp]
+        L.dp_global_norm_workspace_bytes.restype = sz
+        L.dp_global_norm_workspace_bytes.argtypes = []
+        L.dp_global_sqnorm.argtypes = [vp, vp, i32, i32, i32, vp, vp, sz, vp]
+        L.dp_clip_by_global_norm.argtypes = [vp, vp, vp, i32, i32, vp, f32, vp, vp]
+        L.dp_clip_adamw_step.argtypes = [vp, vp, vp, vp, i32, i64, vp, f32, f32, f32, f32, f32, f32, i64, vp]
+        L.dp_rows_sqnorms.argtypes = [vp, i32, i32, vp, i32, vp]
+        L.dp_rows_clipped_accumulate.argtypes = [vp, i32, i32, vp, vp]
+        L.dp_relpos_bucket_starts.argtypes = [i32, i32, i32, vp]
+        L.dp_relpos_bias.argtypes = [vp, vp, i32, vp, i32, i64, i64, vp]
+        L.dp_relpos_workspace_bytes.restype = sz
+        L.dp_relpos_workspace_bytes.argtypes = [vp, i32]
+        L.dp_relpos_bias_grad.argtypes = [vp, i32, i32, vp, i32, i64, i64, i64, vp, vp, vp, i32, vp, sz, vp]
+        L.dp_qknorm_rope.argtypes = [vp, vp, vp, vp, vp, vp]
+        L.dp_qknorm_workspace_bytes.restype = sz
+        L.dp_qknorm_workspace_bytes.argtypes = [vp]
+        L.dp_qknorm_rope_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
         L.dp_poll_status.argtypes = [vp]
         L.dp_set_wait_limit_cycles.argtypes = [C.c_longlong]
         L.dp_selftest_wait_timeout.argtypes = [vp]
@@ -351,3 +391,297 @@ def dp_selftest_wait_timeout(stream=None) -> None:
     """Enqueues the kernel whose waits nobody satisfies; dp_poll_status reports DP_ERR_TIMEOUT afterwards."""
     _check("dp_selftest_wait_timeout", lib().dp_selftest_wait_timeout(_stream(stream)))
 
+
+
+# ---- global norm over many tensors, rows, relative position bias, query/key norms -------------------------------------
+_DTYPES = {torch.float32: DP_F32, torch.bfloat16: DP_BF16}
+
+
+def _dtype(t: torch.Tensor) -> int:
+    try:
+        return _DTYPES[t.dtype]
+    except KeyError:
+        raise ValueError("fp32 or bf16 tensor expected") from None
+
+
+def _call(name: str, device: torch.device, stream, *args) -> None:
+    """The named entry point with the stream behind its arguments.  A launch goes to the CURRENT device, so one on
+    tensors of another device makes that device current for the call."""
+    if device.index == torch.cuda.current_device():
+        _check(name, getattr(lib(), name)(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(name, getattr(lib(), name)(*args, _stream(stream)))
+
+
+def _on(device: torch.device, dtype, t: Optional[torch.Tensor], what: str, shape=None, numel: Optional[int] = None):
+    """Address of an optional tensor after the checks that every argument gets: device, dtype, contiguity, size."""
+    if t is None:
+        return None
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device}, the other tensors are on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{what}: {dtype} expected, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{what}: {numel} elements expected, got {t.numel()}")
+    return _ptr(t)
+
+
+def _workspace(device: torch.device, workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return None, 0
+    if workspace.device != device:
+        raise ValueError(f"workspace: on {workspace.device}, the tensors are on {device}")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _tensor_list(tensors: Sequence[torch.Tensor]):
+    """(HOST array of addresses, HOST array of sizes, dtype, device) of a list of dense tensors."""
+    first = tensors[0]
+    device, dtype = first.device, first.dtype
+    n = len(tensors)
+    for t in tensors:
+        if t.dtype != dtype or t.device != device:
+            raise ValueError("the tensors of a list share one dtype and one device")
+        if not t.is_contiguous():
+            raise ValueError("contiguous tensor expected")
+    if not first.is_cuda:
+        raise ValueError("device tensor expected")
+    return ((C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int64 * n)(*[t.numel() for t in tensors]),
+            _dtype(first), device)
+
+
+def dp_global_norm_workspace_bytes() -> int:
+    return int(lib().dp_global_norm_workspace_bytes())
+
+
+def dp_global_sqnorm(tensors: Sequence[torch.Tensor], sqsum: torch.Tensor, accumulate_into: bool = False,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """sqsum (float64, one element) = or += the sum of squares over all tensors of the list (one dtype, fp32 or bf16)."""
+    if len(tensors) == 0:
+        ptrs, sizes, dtype, device = None, None, DP_F32, sqsum.device
+    else:
+        ptrs, sizes, dtype, device = _tensor_list(tensors)
+    out = _on(device, torch.float64, sqsum, "sqsum", numel=1)
+    ws_p, ws_n = _workspace(device, workspace)
+    _call("dp_global_sqnorm", device, stream, ptrs, sizes, len(tensors), dtype, int(accumulate_into), out, ws_p, ws_n)
+    return sqsum
+
+
+def dp_clip_by_global_norm(tensors: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]], sqsum: torch.Tensor,
+                           max_norm: float, norm_and_factor: Optional[torch.Tensor] = None, stream=None) -> None:
+    """outs[k] = tensors[k] * min(1, max_norm / sqrt(sqsum)); outs=None scales in place.  norm_and_factor: optional
+    float32 tensor with 2 elements that receives the norm and the factor."""
+    if len(tensors) == 0:
+        raise ValueError("at least one tensor expected")
+    ptrs, sizes, dtype, device = _tensor_list(tensors)
+    if outs is None:
+        optrs = ptrs
+    else:
+        if len(outs) != len(tensors):
+            raise ValueError("one output per tensor")
+        optrs, osizes, odtype, odevice = _tensor_list(outs)
+        if odtype != dtype or odevice != device or list(osizes) != list(sizes):
+            raise ValueError("outputs must have their tensors' sizes, dtype and device")
+    told = _on(device, torch.float32, norm_and_factor, "norm_and_factor", numel=2)
+    _call("dp_clip_by_global_norm", device, stream, ptrs, optrs, sizes, len(tensors), dtype,
+          _on(device, torch.float64, sqsum, "sqsum", numel=1), float(max_norm), told)
+
+
+def dp_clip_adamw_step(theta, m, v, g, zero_g, sqsum: torch.Tensor, max_norm: float, lr, beta1, beta2, xi, weight_decay,
+                       t, stream=None) -> None:
+    """dp_adamw_step on g * min(1, max_norm / sqrt(sqsum)); zero_g clears g in the same pass."""
+    device, n = theta.device, theta.numel()
+    th = _on(device, torch.float32, theta, "theta")
+    ptrs = [_on(device, torch.float32, x, what, numel=n) for x, what in ((m, "m"), (v, "v"), (g, "g"))]
+    _call("dp_clip_adamw_step", device, stream, th, *ptrs, int(bool(zero_g)), n,
+          _on(device, torch.float64, sqsum, "sqsum", numel=1), float(max_norm), float(lr), float(beta1), float(beta2),
+          float(xi), float(weight_decay), int(t))
+
+
+class RowList:
+    """A HOST array of dp_rows descriptors: (per-example gradients [B, ...], accumulator [...]) pairs, fp32, plus
+    references that keep the tensors alive.  The accumulator may be None where only the norms are wanted."""
+
+    def __init__(self, pairs: Sequence[tuple]):
+        self.pairs = list(pairs)
+        if not self.pairs:
+            raise ValueError("at least one tensor expected")
+        self.device = self.pairs[0][0].device
+        self.B = int(self.pairs[0][0].shape[0])
+        self.array = (dp_rows * len(self.pairs))()
+        for d, (grad, acc) in zip(self.array, self.pairs):
+            if grad.shape[0] != self.B:
+                raise ValueError("the tensors of a list share the number of examples")
+            d.grad = _on(self.device, torch.float32, grad, "per-example gradients")
+            d.width = grad.numel() // max(self.B, 1)
+            if acc is not None and tuple(acc.shape) != tuple(grad.shape[1:]):
+                raise ValueError(f"accumulator: shape {tuple(grad.shape[1:])} expected, got {tuple(acc.shape)}")
+            d.acc = _on(self.device, torch.float32, acc, "accumulator")
+
+    @property
+    def ptr(self):
+        return C.cast(self.array, C.c_void_p)
+
+    def __len__(self):
+        return len(self.pairs)
+
+
+def dp_rows_sqnorms(rows: RowList, sqnorm: torch.Tensor, accumulate_into: bool = False, stream=None) -> torch.Tensor:
+    _call("dp_rows_sqnorms", rows.device, stream, rows.ptr, len(rows), rows.B,
+          _on(rows.device, torch.float32, sqnorm, "sqnorm", numel=rows.B), int(accumulate_into))
+    return sqnorm
+
+
+def dp_rows_clipped_accumulate(rows: RowList, clip: torch.Tensor, stream=None) -> None:
+    _call("dp_rows_clipped_accumulate", rows.device, stream, rows.ptr, len(rows), rows.B,
+          _on(rows.device, torch.float32, clip, "clip", numel=rows.B))
+
+
+def dp_relpos_bucket_starts(num_buckets: int, max_distance: int, bidirectional: bool) -> List[int]:
+    """Smallest distance of each bucket of one side (host only)."""
+    half = num_buckets // 2 if bidirectional else num_buckets
+    out = (C.c_int32 * max(half, 1))()
+    _check("dp_relpos_bucket_starts",
+           lib().dp_relpos_bucket_starts(int(num_buckets), int(max_distance), int(bool(bidirectional)),
+                                         C.cast(out, C.c_void_p)))
+    return list(out)
+
+
+def dp_relpos_bias(table: torch.Tensor, out: torch.Tensor, max_distance: int = 128, bidirectional: bool = True,
+                   offset: int = 0, stream=None) -> torch.Tensor:
+    """out[h, q, k] = table[bucket(k - q - offset), h]; table [num_buckets, heads], out [heads, Tq, Tk] with unit stride
+    along the keys (fp32 or bf16 each)."""
+    device = table.device
+    nb, H = table.shape
+    if out.dim() != 3 or out.shape[0] != H or out.device != device:
+        raise ValueError(f"out: [{H}, Tq, Tk] on {device} expected, got {tuple(out.shape)} on {out.device}")
+    sh, sq, sk = out.stride()
+    Tq, Tk = int(out.shape[1]), int(out.shape[2])
+    if Tk > 1 and sk != 1:
+        raise ValueError("out: unit stride along the keys expected")
+    p = dp_relpos(nb, int(max_distance), int(bool(bidirectional)), H, Tq, Tk, int(offset))
+    _call("dp_relpos_bias", device, stream, C.byref(p), _ptr(table), _dtype(table), out.data_ptr(), _dtype(out), sh,
+          sq if Tq > 1 else max(sq, Tk))
+    return out
+
+
+def _relpos_of(G: torch.Tensor, num_buckets: int, max_distance: int, bidirectional: bool, offset: int) -> dp_relpos:
+    if G.dim() != 4:
+        raise ValueError("G: [B, heads, Tq, Tk] expected")
+    _, H, Tq, Tk = G.shape
+    return dp_relpos(int(num_buckets), int(max_distance), int(bool(bidirectional)), H, Tq, Tk, int(offset))
+
+
+def dp_relpos_workspace_bytes(G: torch.Tensor, num_buckets: int) -> int:
+    """Scratch for dp_relpos_bias_grad over G [B, heads, Tq, Tk] (at least 256, so that it can be allocated)."""
+    # the size depends on neither the distances nor the sides; two buckets' worth of distance is always valid
+    p = _relpos_of(G, num_buckets, num_buckets + 1, False, 0)
+    return max(256, int(lib().dp_relpos_workspace_bytes(C.byref(p), G.shape[0])))
+
+
+def dp_relpos_bias_grad(G: torch.Tensor, rows: torch.Tensor, max_distance: int = 128, bidirectional: bool = True,
+                        offset: int = 0, causal: bool = False, q_len: Optional[torch.Tensor] = None,
+                        k_len: Optional[torch.Tensor] = None, accumulate_into: bool = False,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """rows[b, n, h] = or += sum over the (q, k) of bucket n of G[b, h, q, k]: every example's gradient of the table.
+    G [B, heads, Tq, Tk] (fp32 or bf16) with unit stride along the keys, rows fp32 [B, num_buckets, heads]; q_len, k_len
+    int32 [B]."""
+    device = G.device
+    if not G.is_cuda:
+        raise ValueError("device tensor expected")
+    if rows.dim() != 3:
+        raise ValueError("rows: [B, num_buckets, heads] expected")
+    p = _relpos_of(G, rows.shape[1], max_distance, bidirectional, offset)
+    B = int(G.shape[0])
+    sb, sh, sq, sk = G.stride()
+    if G.shape[3] > 1 and sk != 1:
+        raise ValueError("G: unit stride along the keys expected")
+    ws_p, ws_n = _workspace(device, workspace)
+    _call("dp_relpos_bias_grad", device, stream, C.byref(p), B, int(bool(causal)), G.data_ptr(), _dtype(G), sb, sh, sq,
+          _on(device, torch.int32, q_len, "q_len", (B,)), _on(device, torch.int32, k_len, "k_len", (B,)),
+          _on(device, torch.float32, rows, "rows", (B, rows.shape[1], G.shape[1])), int(bool(accumulate_into)), ws_p, ws_n)
+    return rows
+
+
+def rope_frequencies(rot: int, base: float = 10000.0) -> torch.Tensor:
+    """inv_freq[j] = base^(-2j / rot), float64 on the host: radians per position of pair j."""
+    return float(base) ** (-torch.arange(rot // 2, dtype=torch.float64) / max(rot // 2, 1))
+
+
+class _Heads:
+    """Descriptors of one call over queries and keys [B, T, heads, dim] (either may be None)."""
+
+    def __init__(self, q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved):
+        x = q if q is not None else k
+        if x is None or x.dim() != 4:
+            raise ValueError("queries or keys [B, T, heads, dim] expected")
+        if not x.is_cuda:
+            raise ValueError("device tensor expected")
+        self.device, self.dtype = x.device, x.dtype
+        self.B, self.T, self.dim = int(x.shape[0]), int(x.shape[1]), int(x.shape[3])
+        n_q, n_k = (0 if y is None else int(y.shape[2]) for y in (q, k))
+        if inv_freq is None:
+            rot = 0
+        else:
+            if inv_freq.dtype != torch.float64 or inv_freq.is_cuda or not inv_freq.is_contiguous():
+                raise ValueError("inv_freq: contiguous float64 tensor on the host expected")
+            rot = 2 * inv_freq.numel()
+        on = lambda t, dt, what, shape: _on(self.device, dt, t, what, shape)  # noqa: E731
+        self.keep = inv_freq
+        self.p = dp_qknorm(_dtype(x), self.B, self.T, n_q, n_k, self.dim, rot, int(bool(interleaved)), float(eps),
+                           on(gain_q, torch.float32, "gain_q", (self.dim,)), on(gain_k, torch.float32, "gain_k", (self.dim,)),
+                           on(positions, torch.int32, "positions", (self.B, self.T)),
+                           on(lengths, torch.int32, "lengths", (self.B,)), inv_freq.data_ptr() if rot else None)
+
+    def view(self, t: Optional[torch.Tensor], like: Optional[torch.Tensor], what: str):
+        """dp_heads of a tensor with the shape of `like`; None where there are no such heads."""
+        if like is None:
+            return None
+        if t is None:
+            raise ValueError(f"{what} expected")
+        if t.dtype != self.dtype or t.device != self.device or t.shape != like.shape:
+            raise ValueError(f"{what}: {tuple(like.shape)} {self.dtype} on {self.device} expected")
+        if like.shape[0] != self.B or like.shape[1] != self.T or like.shape[3] != self.dim:
+            raise ValueError(f"{what}: queries and keys share examples, tokens and width")
+        sb, st, sh, sd = t.stride()
+        if sd != 1:
+            raise ValueError(f"{what}: unit stride along the width expected")
+        return C.byref(dp_heads(t.data_ptr(), sb, st, sh))
+
+
+def dp_qknorm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], out_q: Optional[torch.Tensor],
+                   out_k: Optional[torch.Tensor], gain_q: Optional[torch.Tensor], gain_k: Optional[torch.Tensor],
+                   eps: float, inv_freq: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                   lengths: Optional[torch.Tensor] = None, interleaved: bool = False, stream=None) -> None:
+    """RMS norm per head with gain, then the position rotation.  q, k [B, T, heads, dim] (any strides, unit along dim),
+    either None; gains fp32 [dim] or None; inv_freq float64 on the host (rope_frequencies), its length is rot / 2, None
+    for no rotation; positions int32 [B, T], lengths int32 [B]."""
+    H = _Heads(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
+    _call("dp_qknorm_rope", H.device, stream, C.byref(H.p), H.view(q, q, "q"), H.view(k, k, "k"),
+          H.view(out_q, q, "out_q"), H.view(out_k, k, "out_k"))
+
+
+def dp_qknorm_workspace_bytes(q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> int:
+    """Scratch for dp_qknorm_rope_backward (at least 256, so that it can be allocated)."""
+    H = _Heads(q, k, None, None, 0.0, None, None, None, False)
+    return max(256, int(lib().dp_qknorm_workspace_bytes(C.byref(H.p))))
+
+
+def dp_qknorm_rope_backward(q, k, dout_q, dout_k, dq, dk, gain_q: Optional[torch.Tensor], gain_k: Optional[torch.Tensor],
+                            rows_q: Optional[torch.Tensor], rows_k: Optional[torch.Tensor], eps: float,
+                            inv_freq: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                            lengths: Optional[torch.Tensor] = None, interleaved: bool = False,
+                            accumulate_into: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dq, dk and every example's gradients of the gains (rows_q, rows_k fp32 [B, dim], or None) from the inputs of
+    dp_qknorm_rope and the gradients of its outputs."""
+    H = _Heads(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
+    if (q is None and rows_q is not None) or (k is None and rows_k is not None):
+        raise ValueError("gradients of a gain need the heads that it scales")
+    ws_p, ws_n = _workspace(H.device, workspace)
+    _call("dp_qknorm_rope_backward", H.device, stream, C.byref(H.p), H.view(q, q, "q"), H.view(k, k, "k"),
+          H.view(dout_q, q, "dout_q"), H.view(dout_k, k, "dout_k"), H.view(dq, q, "dq"), H.view(dk, k, "dk"),
+          _on(H.device, torch.float32, rows_q, "rows_q", (H.B, H.dim)),
+          _on(H.device, torch.float32, rows_k, "rows_k", (H.B, H.dim)), int(bool(accumulate_into)), ws_p, ws_n)

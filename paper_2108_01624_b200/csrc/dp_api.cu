@@ -133,6 +133,18 @@ static int check_ws(const WsPlan& p, void* ws, size_t bytes) {
   return DP_OK;
 }
 
+int make_adam_args(double lr, double b1, double b2, double xi, double wd, int64_t t, AdamArgs* aa) {
+  if (t < 1) return DP_ERR_ARG;
+  if (!std::isfinite(lr) || !std::isfinite(xi) || !std::isfinite(wd) || xi < 0.0) return DP_ERR_ARG;
+  if (!(b1 >= 0.0 && b1 < 1.0) || !(b2 >= 0.0 && b2 < 1.0)) return DP_ERR_ARG;
+  aa->lr = (float)lr; aa->beta1 = (float)b1; aa->beta2 = (float)b2; aa->xi = (float)xi; aa->wd = (float)wd;
+  aa->one_m_beta1 = (float)(1.0 - b1);
+  aa->one_m_beta2 = (float)(1.0 - b2);
+  aa->bias1 = (float)(1.0 / (1.0 - std::pow(b1, (double)t)));
+  aa->bias2 = (float)(1.0 / (1.0 - std::pow(b2, (double)t)));
+  return DP_OK;
+}
+
 #define DP_CUDA(expr) do { if ((expr) != cudaSuccess) return DP_ERR_CUDA; } while (0)
 
 }  // namespace dpk
@@ -294,18 +306,6 @@ static int make_noise_args(int64_t n, int64_t elem_offset, double sigma, double 
   na->step0 = (uint32_t)step;
   na->step1 = (uint32_t)(step >> 32);
   na->elem_offset = elem_offset;
-  return DP_OK;
-}
-
-static int make_adam_args(double lr, double b1, double b2, double xi, double wd, int64_t t, AdamArgs* aa) {
-  if (t < 1) return DP_ERR_ARG;
-  if (!std::isfinite(lr) || !std::isfinite(xi) || !std::isfinite(wd) || xi < 0.0) return DP_ERR_ARG;
-  if (!(b1 >= 0.0 && b1 < 1.0) || !(b2 >= 0.0 && b2 < 1.0)) return DP_ERR_ARG;
-  aa->lr = (float)lr; aa->beta1 = (float)b1; aa->beta2 = (float)b2; aa->xi = (float)xi; aa->wd = (float)wd;
-  aa->one_m_beta1 = (float)(1.0 - b1);
-  aa->one_m_beta2 = (float)(1.0 - b2);
-  aa->bias1 = (float)(1.0 / (1.0 - std::pow(b1, (double)t)));
-  aa->bias2 = (float)(1.0 / (1.0 - std::pow(b2, (double)t)));
   return DP_OK;
 }
 

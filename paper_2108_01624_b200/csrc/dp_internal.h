@@ -2,6 +2,7 @@
 // Host-side launchers only; the C ABI in include/dp.h is implemented in dp_api.cu.
 #pragma once
 
+#include <cmath>
 #include <vector>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -41,6 +42,11 @@ cudaError_t launch_adamw(float* theta, float* m, float* v, const float* g, long 
 // sq_sums (optional, device double[2]): adds sum(acc^2) and sum((sigma C z)^2), the gradient-SNR terms.
 cudaError_t launch_noise_adamw(float* theta, float* m, float* v, float* acc, int zero_acc, long long n,
                                const NoiseArgs& na, const AdamArgs& aa, cudaStream_t s, double* sq_sums = nullptr);
+// AdamW on g * min(1, max_norm / sqrt(*sqsum)); zero_g clears g.
+cudaError_t launch_clip_adamw(float* theta, float* m, float* v, float* g, int zero_g, long long n, const double* sqsum,
+                              double max_norm, const AdamArgs& aa, cudaStream_t s);
+// Fills aa from the call's scalars; DP_ERR_ARG where they are out of range.
+int make_adam_args(double lr, double b1, double b2, double xi, double wd, int64_t t, AdamArgs* aa);
 // Fused cross-rank sum + noise + AdamW + replica update on one shard (elem_offset % 4 == 0, 16-byte aligned pointers).
 constexpr int kMaxRanks = 16;
 cudaError_t launch_reduce_update(float* theta, float* m, float* v, float* const* acc_of_rank,

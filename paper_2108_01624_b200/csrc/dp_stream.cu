@@ -1,6 +1,7 @@
 // Streaming kernels: clip factors, Philox4x32-10 noise + scaling, AdamW, and the fused pass.
 // All are bandwidth-bound: one thread owns one Philox block (4 consecutive elements, one 16-byte
 // vector per array), loads are fully coalesced, and the grid is a multiple of the SM count.
+#include "dp_clip.cuh"
 #include "dp_internal.h"
 
 namespace dpk {
@@ -238,6 +239,57 @@ cudaError_t launch_adamw(float* theta, float* m, float* v, const float* g, long 
 cudaError_t launch_noise_adamw(float* theta, float* m, float* v, float* acc, int zero_acc, long long n,
                                const NoiseArgs& na, const AdamArgs& aa, cudaStream_t s, double* sq_sums) {
   return launch_stream<2>(theta, m, v, acc, nullptr, zero_acc, n, na, aa, s, sq_sums);
+}
+
+// ---------------------------------------------------------------------------------------------
+// AdamW with the global-norm clip folded in: the gradient is multiplied by min(1, max_norm / sqrt(sqsum)) as it is
+// read, so the clipped gradient is never written.  28 bytes per element (32 with zero_g).
+// ---------------------------------------------------------------------------------------------
+template <bool VEC>
+__global__ void __launch_bounds__(256)
+k_clip_adamw(float* __restrict__ theta, float* __restrict__ m, float* __restrict__ v, float* __restrict__ g, int zero_g,
+             long long n, const double* __restrict__ sqsum, double max_norm, AdamArgs aa) {
+  __shared__ float f_shared;
+  if (threadIdx.x == 0) f_shared = clip_factor(*sqsum, max_norm);
+  __syncthreads();
+  const float f = f_shared;
+  const long long stride = (long long)gridDim.x * blockDim.x * 4;
+  for (long long k = ((long long)blockIdx.x * blockDim.x + threadIdx.x) * 4; k < n; k += stride) {
+    if (VEC && k + 4 <= n) {
+      const float4 g4 = *reinterpret_cast<const float4*>(g + k);
+      float4 t4 = *reinterpret_cast<const float4*>(theta + k);
+      float4 m4 = *reinterpret_cast<const float4*>(m + k);
+      float4 v4 = *reinterpret_cast<const float4*>(v + k);
+      adam_update(t4.x, m4.x, v4.x, g4.x * f, aa);
+      adam_update(t4.y, m4.y, v4.y, g4.y * f, aa);
+      adam_update(t4.z, m4.z, v4.z, g4.z * f, aa);
+      adam_update(t4.w, m4.w, v4.w, g4.w * f, aa);
+      *reinterpret_cast<float4*>(theta + k) = t4;
+      *reinterpret_cast<float4*>(m + k) = m4;
+      *reinterpret_cast<float4*>(v + k) = v4;
+      if (zero_g) *reinterpret_cast<float4*>(g + k) = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+#pragma unroll
+      for (int l = 0; l < 4; ++l) {
+        if (k + l >= n) break;
+        float t1 = theta[k + l], m1 = m[k + l], v1 = v[k + l];
+        adam_update(t1, m1, v1, g[k + l] * f, aa);
+        theta[k + l] = t1; m[k + l] = m1; v[k + l] = v1;
+        if (zero_g) g[k + l] = 0.0f;
+      }
+    }
+  }
+}
+
+cudaError_t launch_clip_adamw(float* theta, float* m, float* v, float* g, int zero_g, long long n, const double* sqsum,
+                              double max_norm, const AdamArgs& aa, cudaStream_t s) {
+  if (n <= 0) return cudaSuccess;
+  const int grid = stream_grid((unsigned long long)(n + 3) / 4);
+  if (aligned16(theta) && aligned16(m) && aligned16(v) && aligned16(g))
+    k_clip_adamw<true><<<grid, 256, 0, s>>>(theta, m, v, g, zero_g, n, sqsum, max_norm, aa);
+  else
+    k_clip_adamw<false><<<grid, 256, 0, s>>>(theta, m, v, g, zero_g, n, sqsum, max_norm, aa);
+  return counted(1);
 }
 
 // ---------------------------------------------------------------------------------------------
