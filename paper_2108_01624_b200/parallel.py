@@ -86,13 +86,25 @@ class ShardedUpdate:
 
     def __init__(self, state, dist, world: int, rank: int, update_fn: Optional[Callable] = None,
                  peer_acc=None, peer_theta=None, fused_fn: Optional[Callable] = None,
-                 poll_fn: Optional[Callable] = None):
+                 poll_fn: Optional[Callable] = None, noised_sqnorm_fn: Optional[Callable] = None,
+                 clipped_update_fn: Optional[Callable] = None):
         """peer_acc / peer_theta (optional, one entry per rank): every rank's full accumulator and full replica of
         theta as this GPU can address them (tensors from exchange_peer_buffers, or raw device addresses of
         peer-mapped memory).  With both given, the macro-batch ends with ONE kernel per rank that sums the shard
         over all ranks, applies noise + AdamW and writes theta into every replica (`fused_fn`, by default the
         library's dp_reduce_noise_adamw_step), between two barriers.
-        poll_fn() returns this rank's device status code (0 = clean); by default the library's dp_poll_status."""
+        poll_fn() returns this rank's device status code (0 = clean); by default the library's dp_poll_status.
+
+        A state with max_grad_norm clips the noised mean gradient by its global norm: every rank adds the noise to its
+        shard and sums its squares (`noised_sqnorm_fn(acc_shard, elem_offset, batch_size)` -> float64 [1], by default the
+        state's noised_sqnorm), the ranks add the sums (one all-reduce of 8 bytes), and the update of the shard scales by
+        the common factor (`clipped_update_fn(theta, m, v, acc)`, by default the state's clipped_update; `update_fn`
+        is not used then).  It needs the collectives: the one-kernel way sums over the ranks inside the update, when the norm would be too late."""
+        self.max_grad_norm = getattr(state, "max_grad_norm", None)
+        if self.max_grad_norm is not None and peer_acc is not None:
+            raise ValueError("max_grad_norm needs the collectives: leave peer_acc and peer_theta out")
+        self.noised_sqnorm_fn = noised_sqnorm_fn or getattr(state, "noised_sqnorm", None)
+        self.clipped_update_fn = clipped_update_fn or getattr(state, "clipped_update", None)
         self.state, self.dist, self.world, self.rank = state, dist, world, rank
         self.peer_acc, self.peer_theta = peer_acc, peer_theta
         self.fused_fn = fused_fn or self._fused_reduce_kernel
@@ -228,7 +240,17 @@ class ShardedUpdate:
         elif not self.nccl:
             dist.all_reduce(acc)
         self._mark(1)
-        if hi > lo:
+        if self.max_grad_norm is not None:
+            if hi > lo:
+                sqsum = self.noised_sqnorm_fn(acc[lo:hi], lo, s.examples_seen)
+            else:                                               # an empty shard still joins the sum
+                sqsum = torch.zeros(1, dtype=torch.float64, device=acc.device)
+            dist.all_reduce(sqsum)
+            if hi > lo:
+                self.clipped_update_fn(s.theta[lo:hi], s.m[lo:hi], s.v[lo:hi], acc[lo:hi])
+            else:
+                s.grad_sqsum = sqsum
+        elif hi > lo:
             self.update_fn(s.theta[lo:hi], s.m[lo:hi], s.v[lo:hi], acc[lo:hi], lo, s.examples_seen, s.t)
         self._mark(2)
         if self.nccl and self._in_place:

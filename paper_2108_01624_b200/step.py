@@ -6,12 +6,13 @@ the macro-batch size and the AdamW update run once per macro-batch (Section 5.3)
 """
 from __future__ import annotations
 
+import math
 from typing import List, Optional, Sequence
 
 import torch
 
 from . import binding as b
-from .synth import EMBEDDING, LAYERNORM, LINEAR, LayerData, LayerSpec
+from .synth import EMBEDDING, LAYERNORM, LINEAR, ROWS, LayerData, LayerSpec
 
 
 class DeviceStatusError(RuntimeError):
@@ -37,7 +38,8 @@ class DPStep:
 
     def __init__(self, specs: Sequence[LayerSpec], device, C: float, sigma: float, lr: float, beta1: float,
                  beta2: float, xi: float, weight_decay: float, seed: int = 0, theta: Optional[torch.Tensor] = None,
-                 track_snr: bool = False, shared_tables: Optional[dict] = None, shard_world: int = 1):
+                 track_snr: bool = False, shared_tables: Optional[dict] = None, shard_world: int = 1,
+                 max_grad_norm: Optional[float] = None):
         """shard_world: number of data-parallel ranks the macro-batch will be finished across (parallel.ShardedUpdate).
         The accumulator and theta are then allocated with room for `shard_world` equal shards (acc_store,
         theta_store; acc and theta are their first n_flat elements), so that the reduce-scatter and the all-gather
@@ -46,7 +48,21 @@ class DPStep:
         shared_tables maps the index of an output-projection spec (a bias-free LINEAR layer with d_in = V whose
         A is dlogits and whose G is the projection's input) to the index of the EMBEDDING spec whose [V, d] table it
         also trains (BERT's masked-LM decoder): the projection gets no storage of its own, both layers accumulate into
-        the table, and the per-example norm includes the inner product of their two contributions."""
+        the table, and the per-example norm includes the inner product of their two contributions.
+
+        max_grad_norm clips the noised mean gradient of a macro-batch to this global L2 norm, over all tensors, before
+        the AdamW update (post-processing of Algorithm 1's g_t, so it changes nothing about the privacy of a step).
+
+        A ROWS spec [d_in, d_out] is a tensor whose per-example gradients are formed elsewhere (dp_relpos_bias_grad,
+        dp_qknorm_rope_backward): pass them with every microbatch, accumulate_microbatch(..., rows=row_list(data))."""
+        if max_grad_norm is not None:
+            if not (max_grad_norm > 0.0 and math.isfinite(max_grad_norm)):
+                raise ValueError("max_grad_norm must be positive and finite")
+            if track_snr:
+                raise ValueError("track_snr reads its sums from the fused update, which max_grad_norm does not use")
+        self.max_grad_norm = max_grad_norm
+        self.grad_sqsum = None          # float64 [1]: squared norm of the last macro-batch's noised mean gradient
+        self._norm_ws = None
         self.specs = list(specs)
         self.shared_tables = dict(shared_tables or {})
         for p_li, e_li in self.shared_tables.items():
@@ -107,17 +123,39 @@ class DPStep:
         return flat[off:off + n].view(*shp)
 
     def layer_list(self, data: Sequence[LayerData], paths: Optional[Sequence[int]] = None) -> b.LayerList:
-        """Descriptors for one microbatch; data[k] must correspond to specs[k]."""
+        """Descriptors for one microbatch; data[k] must correspond to specs[k].  ROWS entries are left to row_list."""
         out = []
         for li, ld in enumerate(data):
             sp = self.specs[li]
             assert ld.spec.kind == sp.kind and ld.spec.d_out == sp.d_out
+            if sp.kind == ROWS:
+                continue
             acc_w = self.view(self.acc, li, 0)
             acc_b = self.view(self.acc, li, 1) if len(self.shapes[li]) > 1 else None
             out.append(b.Layer(kind=sp.kind, G=ld.G, A=ld.A, ids=ld.ids, acc_w=acc_w, acc_b=acc_b,
                                has_bias=sp.has_bias, vocab=sp.d_in if sp.kind == EMBEDDING else 0,
                                path=b.DP_PATH_AUTO if paths is None else paths[li]))
         return b.LayerList(out)
+
+    def row_list(self, data: Sequence[LayerData]) -> Optional[b.RowList]:
+        """Descriptors of the ROWS entries of one microbatch (None if there are none); data[k] corresponds to specs[k]."""
+        pairs = [(ld.G.view(ld.G.shape[0], sp.d_in, sp.d_out), self.view(self.acc, li, 0))
+                 for li, (sp, ld) in enumerate(zip(self.specs, data)) if sp.kind == ROWS]
+        return b.RowList(pairs) if pairs else None
+
+    def tensor_pieces(self, flat: torch.Tensor, lo: int = 0, hi: Optional[int] = None) -> List[torch.Tensor]:
+        """The tensors' elements among [lo, hi) of the flat vector, whose element lo is flat[0]: one 1-D view per tensor,
+        without the padding between tensors.  A shared table counts once."""
+        hi = self.n_flat if hi is None else hi
+        out = []
+        for li in range(len(self.specs)):
+            if li in self.shared_tables:
+                continue
+            for off, shp in zip(self.offsets[li], self.shapes[li]):
+                a, z = max(off, lo), min(off + math.prod(shp), hi)
+                if a < z:
+                    out.append(flat[a - lo:z - lo])
+        return out
 
     def layer_lists(self, data: Sequence[LayerData], paths: Optional[Sequence[int]] = None) -> List[b.LayerList]:
         """Descriptors for one microbatch whose layers do not all see the same number of tokens (encoder layers per
@@ -129,11 +167,21 @@ class DPStep:
             groups.setdefault(int(L.G.shape[1]), []).append(L)
         return [b.LayerList(ls) for ls in groups.values()]
 
-    def accumulate_microbatch(self, layers, stream=None):
+    def accumulate_microbatch(self, layers, stream=None, rows=None):
         """norms -> clip factors -> clipped accumulate for one microbatch (all enqueued, no sync).
-        `layers` is a LayerList, or a list of them (layer_lists) when token counts differ between layers."""
+        `layers` is a LayerList, or a list of them (layer_lists) when token counts differ between layers; `rows` is the
+        row_list of the microbatch, needed exactly when there are ROWS specs (an example's norm runs over ALL its
+        tensors: one left out would break the bound that the noise is calibrated to)."""
         lists = [layers] if isinstance(layers, b.LayerList) else list(layers)
-        B = lists[0].B
+        lists = [ll for ll in lists if len(ll)]
+        n_rows = sum(sp.kind == ROWS for sp in self.specs)
+        if (0 if rows is None else len(rows)) != n_rows:
+            raise ValueError(f"the model has {n_rows} ROWS tensors: pass row_list(data) of this microbatch as rows")
+        if not lists and rows is None:
+            raise ValueError("no layers")
+        B = lists[0].B if lists else rows.B
+        if rows is not None and rows.B != B:
+            raise ValueError(f"rows of {rows.B} examples, layers of {B}")
         if self._sqnorm is None or self._sqnorm.numel() != B:
             self._sqnorm = torch.empty(B, dtype=torch.float32, device=self.device)
             self._clip = torch.empty(B, dtype=torch.float32, device=self.device)
@@ -153,9 +201,13 @@ class DPStep:
                 if len(pair) == 2:
                     emb, proj = (pair[0], pair[1]) if pair[0].kind == EMBEDDING else (pair[1], pair[0])
                     b.dp_shared_table_cross_sqnorms(emb, proj, self._sqnorm, stream)
+        if rows is not None:
+            b.dp_rows_sqnorms(rows, self._sqnorm, bool(lists), stream)
         b.dp_clip_factors(self._sqnorm, self.C, self._clip, stream)
         for k, ll in enumerate(lists):
             b.dp_clipped_accumulate_after_sqnorms(ll, self._clip, self._ws[k], stream)
+        if rows is not None:
+            b.dp_rows_clipped_accumulate(rows, self._clip, stream)
         self.examples_seen += B
         return self._sqnorm, self._clip
 
@@ -184,7 +236,10 @@ class DPStep:
             self.check_device_status(stream)
         N = self.examples_seen if batch_size is None else batch_size
         self.t += 1
-        if fused and self.sq_sums is not None:
+        if self.max_grad_norm is not None:
+            self.noised_sqnorm(self.acc, 0, N, stream)
+            self.clipped_update(self.theta, self.m, self.v, self.acc, stream)
+        elif fused and self.sq_sums is not None:
             self.sq_sums.zero_()
             b.dp_noise_scale_adamw_step_snr(self.theta, self.m, self.v, self.acc, True, self.sigma, self.C, N,
                                             self.seed, self.t, self.lr, self.beta1, self.beta2, self.xi,
@@ -199,6 +254,28 @@ class DPStep:
                             self.weight_decay, self.t, stream)
             self.acc.zero_()
         self.examples_seen = 0
+
+    def noised_sqnorm(self, acc: torch.Tensor, elem_offset: int, batch_size: int, stream=None) -> torch.Tensor:
+        """acc (the flat vector from element elem_offset on) <- (acc + noise) / batch_size in place; returns the squared
+        norm of its tensors' elements in grad_sqsum."""
+        if self.grad_sqsum is None:
+            self.grad_sqsum = torch.zeros(1, dtype=torch.float64, device=self.device)
+            self._norm_ws = torch.empty(b.dp_global_norm_workspace_bytes(), dtype=torch.uint8, device=self.device)
+        b.dp_add_noise_and_scale(acc, self.sigma, self.C, batch_size, self.seed, self.t, elem_offset, stream)
+        b.dp_global_sqnorm(self.tensor_pieces(acc, elem_offset, elem_offset + acc.numel()), self.grad_sqsum, False,
+                           self._norm_ws, stream)
+        return self.grad_sqsum
+
+    def clipped_update(self, theta, m, v, acc, stream=None) -> None:
+        """AdamW on acc, clipped to max_grad_norm by the squared norm in grad_sqsum; acc is cleared."""
+        b.dp_clip_adamw_step(theta, m, v, acc, True, self.grad_sqsum, self.max_grad_norm, self.lr, self.beta1, self.beta2,
+                             self.xi, self.weight_decay, self.t, stream)
+
+    def grad_norm(self) -> float:
+        """Global norm of the last finished macro-batch's noised mean gradient before its clip (host sync)."""
+        if self.grad_sqsum is None:
+            raise RuntimeError("construct DPStep with max_grad_norm and finish a macro-batch")
+        return math.sqrt(float(self.grad_sqsum.item()))
 
     def state_dict(self) -> dict:
         """Everything a run needs to resume in the middle of a macro-batch: parameters, Adam moments, the partly

@@ -25,12 +25,13 @@ import numpy as np
 import torch
 
 LINEAR, LAYERNORM, EMBEDDING = "linear", "layernorm", "embedding"
+ROWS = "rows"           # a small tensor [d_in, d_out] whose per-example gradient is given
 
 
 @dataclass
 class LayerSpec:
     kind: str
-    d_in: int           # LINEAR: input width; LAYERNORM: d; EMBEDDING: vocab V
+    d_in: int           # LINEAR: input width; LAYERNORM: d; EMBEDDING: vocab V; ROWS: rows of the tensor
     d_out: int
     has_bias: bool = False
     name: str = ""
@@ -47,8 +48,8 @@ class LayerSpec:
 @dataclass
 class LayerData:
     spec: LayerSpec
-    G: torch.Tensor                       # [B, T, d_out]
-    A: Optional[torch.Tensor] = None      # [B, T, d_in]  (None for EMBEDDING)
+    G: torch.Tensor                       # [B, T, d_out]  (ROWS: fp32 per-example gradients, [B, d_in, d_out])
+    A: Optional[torch.Tensor] = None      # [B, T, d_in]  (None for EMBEDDING and ROWS)
     ids: Optional[torch.Tensor] = None    # [B, T] int32  (EMBEDDING only)
 
 
@@ -85,6 +86,13 @@ def encoder_layer_specs(hidden: int, ffn: int, tag: str = "") -> List[LayerSpec]
         LayerSpec(LINEAR, ffn, hidden, True, f"{tag}ffn2"),
         LayerSpec(LAYERNORM, hidden, hidden, False, f"{tag}ln2"),
     ]
+
+
+def attention_param_specs(heads: int, head_dim: int, buckets: int = 0, qk_norm: bool = True, tag: str = "") -> List[LayerSpec]:
+    """Trainables of an attention block beside its linears, each with a per-example gradient of its own: the gains of the
+    query and key norms [1, head_dim] and the relative position table [buckets, heads] (0: none)."""
+    out = [LayerSpec(ROWS, 1, head_dim, False, f"{tag}{n}_gain") for n in ("q", "k")] if qk_norm else []
+    return out + ([LayerSpec(ROWS, buckets, heads, False, f"{tag}relpos")] if buckets else [])
 
 
 def workload(name: str) -> Workload:
@@ -124,6 +132,8 @@ def kappa(specs: List[LayerSpec], T: int) -> float:
             s += T * sp.d_out * (sp.d_in + (1 if sp.has_bias else 0))
         elif sp.kind == LAYERNORM:
             s += 2 * T * sp.d_out
+        elif sp.kind == ROWS:
+            s += sp.d_in * sp.d_out
         else:
             s += T * sp.d_out
     return math.sqrt(s)
@@ -176,6 +186,10 @@ def generate(wl: Workload, seed: int = 0, device="cpu", microbatch: int = 0,
         if specs is not None and not any(sp is q for q in specs):
             continue
         gG = _gen(device, seed, microbatch, li, 1)
+        if sp.kind == ROWS:
+            G = torch.randn(B, sp.d_in, sp.d_out, generator=gG, device=device, dtype=torch.float32)
+            out.append(LayerData(sp, G=G if s is None else G * s.view(B, 1, 1)))
+            continue
         G = torch.randn(B, T, sp.d_out, generator=gG, device=device, dtype=torch.float32)
         if s is not None:
             G = G * s.view(B, 1, 1)
