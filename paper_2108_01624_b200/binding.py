@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -394,63 +395,90 @@ def dp_selftest_wait_timeout(stream=None) -> None:
 
 
 # ---- global norm over many tensors, rows, relative position bias, query/key norms -------------------------------------
+# These calls serve small tensors too, where the host side of a call is most of its time, so the checks below are made of
+# the cheapest queries that a tensor answers, and words for an error are looked for only where a check failed.
 _DTYPES = {torch.float32: DP_F32, torch.bfloat16: DP_BF16}
+_F32, _F64, _I32 = torch.float32, torch.float64, torch.int32
+_current_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _dtype(t: torch.Tensor) -> int:
     try:
         return _DTYPES[t.dtype]
     except KeyError:
-        raise ValueError("fp32 or bf16 tensor expected") from None
+        raise ValueError(f"fp32 or bf16 tensor expected, got {t.dtype}") from None
 
 
-def _call(name: str, device: torch.device, stream, *args) -> None:
+def _device(t: torch.Tensor) -> int:
+    """Index of the device that a call's first tensor is on."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    return t.get_device()
+
+
+def _call(name: str, device: int, stream, *args) -> None:
     """The named entry point with the stream behind its arguments.  A launch goes to the CURRENT device, so one on
     tensors of another device makes that device current for the call."""
-    if device.index == torch.cuda.current_device():
-        _check(name, getattr(lib(), name)(*args, _stream(stream)))
+    fn = getattr(_lib or lib(), name)
+    if device == _current_device():
+        rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(device):
-            _check(name, getattr(lib(), name)(*args, _stream(stream)))
+            rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError(name, rc)
 
 
-def _on(device: torch.device, dtype, t: Optional[torch.Tensor], what: str, shape=None, numel: Optional[int] = None):
+def _on(device: int, dtype, t: Optional[torch.Tensor], what: str, shape=None, numel: int = -1):
     """Address of an optional tensor after the checks that every argument gets: device, dtype, contiguity, size."""
     if t is None:
         return None
-    if t.device != device:
-        raise ValueError(f"{what}: on {t.device}, the other tensors are on {device}")
-    if t.dtype != dtype:
+    if (t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape)
+            and (numel < 0 or t.numel() == numel)):
+        return t.data_ptr()
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on {t.device}, the other tensors are on cuda:{device}")
+    if t.dtype is not dtype:
         raise ValueError(f"{what}: {dtype} expected, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
-    if numel is not None and t.numel() != numel:
-        raise ValueError(f"{what}: {numel} elements expected, got {t.numel()}")
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous tensor expected")
+    raise ValueError(f"{what}: {f'shape {tuple(shape)}' if shape is not None else f'{numel} elements'} expected, "
+                     f"got {tuple(t.shape)}")
 
 
-def _workspace(device: torch.device, workspace: Optional[torch.Tensor]):
+def _workspace(device: int, workspace: Optional[torch.Tensor]):
     if workspace is None:
         return None, 0
-    if workspace.device != device:
-        raise ValueError(f"workspace: on {workspace.device}, the tensors are on {device}")
-    return _ptr(workspace), workspace.numel() * workspace.element_size()
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous tensor on cuda:{device} expected")
+    return workspace.data_ptr(), workspace.nbytes
 
 
-def _tensor_list(tensors: Sequence[torch.Tensor]):
-    """(HOST array of addresses, HOST array of sizes, dtype, device) of a list of dense tensors."""
-    first = tensors[0]
-    device, dtype = first.device, first.dtype
-    n = len(tensors)
-    for t in tensors:
-        if t.dtype != dtype or t.device != device:
-            raise ValueError("the tensors of a list share one dtype and one device")
-        if not t.is_contiguous():
+_Tensor = torch.Tensor
+
+
+class _TensorArrays:
+    """HOST arrays of addresses and sizes of a list of dense tensors of one dtype on one device."""
+
+    def __init__(self, tensors: Sequence[torch.Tensor]):
+        first = tensors[0]
+        self.device, dtype = _device(first), first.dtype
+        if not all(map(_Tensor.is_contiguous, tensors)):
             raise ValueError("contiguous tensor expected")
-    if not first.is_cuda:
-        raise ValueError("device tensor expected")
-    return ((C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int64 * n)(*[t.numel() for t in tensors]),
-            _dtype(first), device)
+        if any([t.dtype is not dtype for t in tensors]) or set(map(_Tensor.get_device, tensors)) != {self.device}:
+            raise ValueError("the tensors of a list share one dtype and one device")
+        self.dtype, self.n = _dtype(first), len(tensors)
+        self.addresses = array("Q", map(_Tensor.data_ptr, tensors))
+        self.sizes = array("q", map(_Tensor.numel, tensors))
+
+    @property
+    def ptrs(self):
+        return self.addresses.buffer_info()[0]
+
+    @property
+    def counts(self):
+        return self.sizes.buffer_info()[0]
 
 
 def dp_global_norm_workspace_bytes() -> int:
@@ -460,13 +488,14 @@ def dp_global_norm_workspace_bytes() -> int:
 def dp_global_sqnorm(tensors: Sequence[torch.Tensor], sqsum: torch.Tensor, accumulate_into: bool = False,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """sqsum (float64, one element) = or += the sum of squares over all tensors of the list (one dtype, fp32 or bf16)."""
-    if len(tensors) == 0:
-        ptrs, sizes, dtype, device = None, None, DP_F32, sqsum.device
+    if len(tensors):
+        L = _TensorArrays(tensors)
+        device, args = L.device, (L.ptrs, L.counts, L.n, L.dtype)
     else:
-        ptrs, sizes, dtype, device = _tensor_list(tensors)
-    out = _on(device, torch.float64, sqsum, "sqsum", numel=1)
+        device, args = _device(sqsum), (None, None, 0, DP_F32)
     ws_p, ws_n = _workspace(device, workspace)
-    _call("dp_global_sqnorm", device, stream, ptrs, sizes, len(tensors), dtype, int(accumulate_into), out, ws_p, ws_n)
+    _call("dp_global_sqnorm", device, stream, *args, 1 if accumulate_into else 0,
+          _on(device, _F64, sqsum, "sqsum", None, 1), ws_p, ws_n)
     return sqsum
 
 
@@ -476,29 +505,22 @@ def dp_clip_by_global_norm(tensors: Sequence[torch.Tensor], outs: Optional[Seque
     float32 tensor with 2 elements that receives the norm and the factor."""
     if len(tensors) == 0:
         raise ValueError("at least one tensor expected")
-    ptrs, sizes, dtype, device = _tensor_list(tensors)
-    if outs is None:
-        optrs = ptrs
-    else:
-        if len(outs) != len(tensors):
-            raise ValueError("one output per tensor")
-        optrs, osizes, odtype, odevice = _tensor_list(outs)
-        if odtype != dtype or odevice != device or list(osizes) != list(sizes):
-            raise ValueError("outputs must have their tensors' sizes, dtype and device")
-    told = _on(device, torch.float32, norm_and_factor, "norm_and_factor", numel=2)
-    _call("dp_clip_by_global_norm", device, stream, ptrs, optrs, sizes, len(tensors), dtype,
-          _on(device, torch.float64, sqsum, "sqsum", numel=1), float(max_norm), told)
+    L = _TensorArrays(tensors)
+    O = L if outs is None else _TensorArrays(outs)
+    if O is not L and (O.n != L.n or O.dtype != L.dtype or O.device != L.device or O.sizes != L.sizes):
+        raise ValueError("outputs must have their tensors' number, sizes, dtype and device")
+    _call("dp_clip_by_global_norm", L.device, stream, L.ptrs, O.ptrs, L.counts, L.n, L.dtype,
+          _on(L.device, _F64, sqsum, "sqsum", None, 1), max_norm,
+          _on(L.device, _F32, norm_and_factor, "norm_and_factor", None, 2))
 
 
 def dp_clip_adamw_step(theta, m, v, g, zero_g, sqsum: torch.Tensor, max_norm: float, lr, beta1, beta2, xi, weight_decay,
                        t, stream=None) -> None:
     """dp_adamw_step on g * min(1, max_norm / sqrt(sqsum)); zero_g clears g in the same pass."""
-    device, n = theta.device, theta.numel()
-    th = _on(device, torch.float32, theta, "theta")
-    ptrs = [_on(device, torch.float32, x, what, numel=n) for x, what in ((m, "m"), (v, "v"), (g, "g"))]
-    _call("dp_clip_adamw_step", device, stream, th, *ptrs, int(bool(zero_g)), n,
-          _on(device, torch.float64, sqsum, "sqsum", numel=1), float(max_norm), float(lr), float(beta1), float(beta2),
-          float(xi), float(weight_decay), int(t))
+    device, n = _device(theta), theta.numel()
+    _call("dp_clip_adamw_step", device, stream, _on(device, _F32, theta, "theta"), _on(device, _F32, m, "m", None, n),
+          _on(device, _F32, v, "v", None, n), _on(device, _F32, g, "g", None, n), 1 if zero_g else 0, n,
+          _on(device, _F64, sqsum, "sqsum", None, 1), max_norm, lr, beta1, beta2, xi, weight_decay, t)
 
 
 class RowList:
@@ -509,35 +531,31 @@ class RowList:
         self.pairs = list(pairs)
         if not self.pairs:
             raise ValueError("at least one tensor expected")
-        self.device = self.pairs[0][0].device
-        self.B = int(self.pairs[0][0].shape[0])
+        first = self.pairs[0][0]
+        self.device, self.B = _device(first), first.shape[0]
         self.array = (dp_rows * len(self.pairs))()
         for d, (grad, acc) in zip(self.array, self.pairs):
-            if grad.shape[0] != self.B:
+            shape = grad.shape
+            if shape[0] != self.B:
                 raise ValueError("the tensors of a list share the number of examples")
-            d.grad = _on(self.device, torch.float32, grad, "per-example gradients")
+            d.grad = _on(self.device, _F32, grad, "per-example gradients")
             d.width = grad.numel() // max(self.B, 1)
-            if acc is not None and tuple(acc.shape) != tuple(grad.shape[1:]):
-                raise ValueError(f"accumulator: shape {tuple(grad.shape[1:])} expected, got {tuple(acc.shape)}")
-            d.acc = _on(self.device, torch.float32, acc, "accumulator")
-
-    @property
-    def ptr(self):
-        return C.cast(self.array, C.c_void_p)
+            d.acc = _on(self.device, _F32, acc, "accumulator", shape[1:])
+        self.ptr = C.addressof(self.array)
 
     def __len__(self):
         return len(self.pairs)
 
 
 def dp_rows_sqnorms(rows: RowList, sqnorm: torch.Tensor, accumulate_into: bool = False, stream=None) -> torch.Tensor:
-    _call("dp_rows_sqnorms", rows.device, stream, rows.ptr, len(rows), rows.B,
-          _on(rows.device, torch.float32, sqnorm, "sqnorm", numel=rows.B), int(accumulate_into))
+    _call("dp_rows_sqnorms", rows.device, stream, rows.ptr, len(rows.pairs), rows.B,
+          _on(rows.device, _F32, sqnorm, "sqnorm", None, rows.B), 1 if accumulate_into else 0)
     return sqnorm
 
 
 def dp_rows_clipped_accumulate(rows: RowList, clip: torch.Tensor, stream=None) -> None:
-    _call("dp_rows_clipped_accumulate", rows.device, stream, rows.ptr, len(rows), rows.B,
-          _on(rows.device, torch.float32, clip, "clip", numel=rows.B))
+    _call("dp_rows_clipped_accumulate", rows.device, stream, rows.ptr, len(rows.pairs), rows.B,
+          _on(rows.device, _F32, clip, "clip", None, rows.B))
 
 
 def dp_relpos_bucket_starts(num_buckets: int, max_distance: int, bidirectional: bool) -> List[int]:
@@ -554,32 +572,26 @@ def dp_relpos_bias(table: torch.Tensor, out: torch.Tensor, max_distance: int = 1
                    offset: int = 0, stream=None) -> torch.Tensor:
     """out[h, q, k] = table[bucket(k - q - offset), h]; table [num_buckets, heads], out [heads, Tq, Tk] with unit stride
     along the keys (fp32 or bf16 each)."""
-    device = table.device
+    device = _device(table)
     nb, H = table.shape
-    if out.dim() != 3 or out.shape[0] != H or out.device != device:
-        raise ValueError(f"out: [{H}, Tq, Tk] on {device} expected, got {tuple(out.shape)} on {out.device}")
+    if out.dim() != 3 or out.shape[0] != H or out.get_device() != device:
+        raise ValueError(f"out: [{H}, Tq, Tk] on cuda:{device} expected, got {tuple(out.shape)} on {out.device}")
+    _, Tq, Tk = out.shape
     sh, sq, sk = out.stride()
-    Tq, Tk = int(out.shape[1]), int(out.shape[2])
     if Tk > 1 and sk != 1:
         raise ValueError("out: unit stride along the keys expected")
-    p = dp_relpos(nb, int(max_distance), int(bool(bidirectional)), H, Tq, Tk, int(offset))
-    _call("dp_relpos_bias", device, stream, C.byref(p), _ptr(table), _dtype(table), out.data_ptr(), _dtype(out), sh,
-          sq if Tq > 1 else max(sq, Tk))
+    p = dp_relpos(nb, max_distance, 1 if bidirectional else 0, H, Tq, Tk, offset)
+    _call("dp_relpos_bias", device, stream, C.addressof(p), _on(device, table.dtype, table, "table"), _dtype(table),
+          out.data_ptr(), _dtype(out), sh if H > 1 else 0, sq if Tq > 1 else Tk)
     return out
-
-
-def _relpos_of(G: torch.Tensor, num_buckets: int, max_distance: int, bidirectional: bool, offset: int) -> dp_relpos:
-    if G.dim() != 4:
-        raise ValueError("G: [B, heads, Tq, Tk] expected")
-    _, H, Tq, Tk = G.shape
-    return dp_relpos(int(num_buckets), int(max_distance), int(bool(bidirectional)), H, Tq, Tk, int(offset))
 
 
 def dp_relpos_workspace_bytes(G: torch.Tensor, num_buckets: int) -> int:
     """Scratch for dp_relpos_bias_grad over G [B, heads, Tq, Tk] (at least 256, so that it can be allocated)."""
-    # the size depends on neither the distances nor the sides; two buckets' worth of distance is always valid
-    p = _relpos_of(G, num_buckets, num_buckets + 1, False, 0)
-    return max(256, int(lib().dp_relpos_workspace_bytes(C.byref(p), G.shape[0])))
+    B, H, Tq, Tk = G.shape
+    # the size depends on neither the distances nor the sides: one side and a distance that is always valid
+    p = dp_relpos(num_buckets, num_buckets + 1, 0, H, Tq, Tk, 0)
+    return max(256, (_lib or lib()).dp_relpos_workspace_bytes(C.addressof(p), B))
 
 
 def dp_relpos_bias_grad(G: torch.Tensor, rows: torch.Tensor, max_distance: int = 128, bidirectional: bool = True,
@@ -589,20 +601,19 @@ def dp_relpos_bias_grad(G: torch.Tensor, rows: torch.Tensor, max_distance: int =
     """rows[b, n, h] = or += sum over the (q, k) of bucket n of G[b, h, q, k]: every example's gradient of the table.
     G [B, heads, Tq, Tk] (fp32 or bf16) with unit stride along the keys, rows fp32 [B, num_buckets, heads]; q_len, k_len
     int32 [B]."""
-    device = G.device
-    if not G.is_cuda:
-        raise ValueError("device tensor expected")
-    if rows.dim() != 3:
-        raise ValueError("rows: [B, num_buckets, heads] expected")
-    p = _relpos_of(G, rows.shape[1], max_distance, bidirectional, offset)
-    B = int(G.shape[0])
+    device = _device(G)
+    if G.dim() != 4 or rows.dim() != 3:
+        raise ValueError("G [B, heads, Tq, Tk] and rows [B, num_buckets, heads] expected")
+    B, H, Tq, Tk = G.shape
+    nb = rows.shape[1]
     sb, sh, sq, sk = G.stride()
-    if G.shape[3] > 1 and sk != 1:
+    if Tk > 1 and sk != 1:
         raise ValueError("G: unit stride along the keys expected")
+    p = dp_relpos(nb, max_distance, 1 if bidirectional else 0, H, Tq, Tk, offset)
     ws_p, ws_n = _workspace(device, workspace)
-    _call("dp_relpos_bias_grad", device, stream, C.byref(p), B, int(bool(causal)), G.data_ptr(), _dtype(G), sb, sh, sq,
-          _on(device, torch.int32, q_len, "q_len", (B,)), _on(device, torch.int32, k_len, "k_len", (B,)),
-          _on(device, torch.float32, rows, "rows", (B, rows.shape[1], G.shape[1])), int(bool(accumulate_into)), ws_p, ws_n)
+    _call("dp_relpos_bias_grad", device, stream, C.addressof(p), B, 1 if causal else 0, G.data_ptr(), _dtype(G), sb, sh,
+          sq, _on(device, _I32, q_len, "q_len", (B,)), _on(device, _I32, k_len, "k_len", (B,)),
+          _on(device, _F32, rows, "rows", (B, nb, H)), 1 if accumulate_into else 0, ws_p, ws_n)
     return rows
 
 
@@ -611,45 +622,48 @@ def rope_frequencies(rot: int, base: float = 10000.0) -> torch.Tensor:
     return float(base) ** (-torch.arange(rot // 2, dtype=torch.float64) / max(rot // 2, 1))
 
 
-class _Heads:
-    """Descriptors of one call over queries and keys [B, T, heads, dim] (either may be None)."""
+def _qknorm(q, k, gain_q=None, gain_k=None, eps=0.0, inv_freq=None, positions=None, lengths=None, interleaved=False):
+    """(device, descriptor) of a call over queries and keys [B, T, heads, dim], either of which may be None."""
+    x = k if q is None else q
+    if x is None or x.dim() != 4 or (q is not None and k is not None and k.dim() != 4):
+        raise ValueError("queries or keys [B, T, heads, dim] expected")
+    device = _device(x)
+    B, T, heads, dim = x.shape
+    n_q = 0 if q is None else heads
+    n_k = 0 if k is None else k.shape[2]
+    if n_q and n_k and k.shape != (B, T, n_k, dim):
+        raise ValueError("queries and keys share examples, tokens and width")
+    if inv_freq is None:
+        rot, freq = 0, None
+    else:
+        if inv_freq.dtype is not _F64 or inv_freq.is_cuda or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq: contiguous float64 tensor on the host expected")
+        rot, freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
+    return device, dp_qknorm(_dtype(x), B, T, n_q, n_k, dim, rot, 1 if interleaved else 0, eps,
+                             _on(device, _F32, gain_q, "gain_q", (dim,)), _on(device, _F32, gain_k, "gain_k", (dim,)),
+                             _on(device, _I32, positions, "positions", (B, T)),
+                             _on(device, _I32, lengths, "lengths", (B,)), freq)
 
-    def __init__(self, q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved):
-        x = q if q is not None else k
-        if x is None or x.dim() != 4:
-            raise ValueError("queries or keys [B, T, heads, dim] expected")
-        if not x.is_cuda:
-            raise ValueError("device tensor expected")
-        self.device, self.dtype = x.device, x.dtype
-        self.B, self.T, self.dim = int(x.shape[0]), int(x.shape[1]), int(x.shape[3])
-        n_q, n_k = (0 if y is None else int(y.shape[2]) for y in (q, k))
-        if inv_freq is None:
-            rot = 0
-        else:
-            if inv_freq.dtype != torch.float64 or inv_freq.is_cuda or not inv_freq.is_contiguous():
-                raise ValueError("inv_freq: contiguous float64 tensor on the host expected")
-            rot = 2 * inv_freq.numel()
-        on = lambda t, dt, what, shape: _on(self.device, dt, t, what, shape)  # noqa: E731
-        self.keep = inv_freq
-        self.p = dp_qknorm(_dtype(x), self.B, self.T, n_q, n_k, self.dim, rot, int(bool(interleaved)), float(eps),
-                           on(gain_q, torch.float32, "gain_q", (self.dim,)), on(gain_k, torch.float32, "gain_k", (self.dim,)),
-                           on(positions, torch.int32, "positions", (self.B, self.T)),
-                           on(lengths, torch.int32, "lengths", (self.B,)), inv_freq.data_ptr() if rot else None)
 
-    def view(self, t: Optional[torch.Tensor], like: Optional[torch.Tensor], what: str):
-        """dp_heads of a tensor with the shape of `like`; None where there are no such heads."""
-        if like is None:
-            return None
+def _heads(device: int, like: Optional[torch.Tensor], what: str, *tensors):
+    """dp_heads of tensors with the shape and dtype of `like`, one HOST array; its entries' addresses (None where there are
+    no such heads) and the array, which must live until the call returns."""
+    n = len(tensors)
+    if like is None:
+        return (None,) * n + (None,)
+    shape, dtype = like.shape, like.dtype
+    out = (dp_heads * n)()
+    for d, t in zip(out, tensors):
         if t is None:
-            raise ValueError(f"{what} expected")
-        if t.dtype != self.dtype or t.device != self.device or t.shape != like.shape:
-            raise ValueError(f"{what}: {tuple(like.shape)} {self.dtype} on {self.device} expected")
-        if like.shape[0] != self.B or like.shape[1] != self.T or like.shape[3] != self.dim:
-            raise ValueError(f"{what}: queries and keys share examples, tokens and width")
-        sb, st, sh, sd = t.stride()
-        if sd != 1:
+            raise ValueError(f"{what}: a tensor is missing")
+        if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
+            raise ValueError(f"{what}: {tuple(shape)} {dtype} on cuda:{device} expected, got {tuple(t.shape)} {t.dtype} on {t.device}")
+        d.data = t.data_ptr()
+        d.stride_b, d.stride_t, d.stride_h, unit = t.stride()
+        if unit != 1:
             raise ValueError(f"{what}: unit stride along the width expected")
-        return C.byref(dp_heads(t.data_ptr(), sb, st, sh))
+    base = C.addressof(out)
+    return tuple(range(base, base + 32 * n, 32)) + (out,)
 
 
 def dp_qknorm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], out_q: Optional[torch.Tensor],
@@ -659,15 +673,18 @@ def dp_qknorm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], out_q: 
     """RMS norm per head with gain, then the position rotation.  q, k [B, T, heads, dim] (any strides, unit along dim),
     either None; gains fp32 [dim] or None; inv_freq float64 on the host (rope_frequencies), its length is rot / 2, None
     for no rotation; positions int32 [B, T], lengths int32 [B]."""
-    H = _Heads(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
-    _call("dp_qknorm_rope", H.device, stream, C.byref(H.p), H.view(q, q, "q"), H.view(k, k, "k"),
-          H.view(out_q, q, "out_q"), H.view(out_k, k, "out_k"))
+    device, p = _qknorm(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
+    q_in, q_out, keep_q = _heads(device, q, "queries", q, out_q)
+    k_in, k_out, keep_k = _heads(device, k, "keys", k, out_k)
+    if q is not None and k is not None and k.dtype is not q.dtype:
+        raise ValueError("queries and keys share one dtype")
+    _call("dp_qknorm_rope", device, stream, C.addressof(p), q_in, k_in, q_out, k_out)
 
 
 def dp_qknorm_workspace_bytes(q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> int:
     """Scratch for dp_qknorm_rope_backward (at least 256, so that it can be allocated)."""
-    H = _Heads(q, k, None, None, 0.0, None, None, None, False)
-    return max(256, int(lib().dp_qknorm_workspace_bytes(C.byref(H.p))))
+    _, p = _qknorm(q, k)
+    return max(256, (_lib or lib()).dp_qknorm_workspace_bytes(C.addressof(p)))
 
 
 def dp_qknorm_rope_backward(q, k, dout_q, dout_k, dq, dk, gain_q: Optional[torch.Tensor], gain_k: Optional[torch.Tensor],
@@ -677,11 +694,15 @@ def dp_qknorm_rope_backward(q, k, dout_q, dout_k, dq, dk, gain_q: Optional[torch
                             accumulate_into: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """dq, dk and every example's gradients of the gains (rows_q, rows_k fp32 [B, dim], or None) from the inputs of
     dp_qknorm_rope and the gradients of its outputs."""
-    H = _Heads(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
+    device, p = _qknorm(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
     if (q is None and rows_q is not None) or (k is None and rows_k is not None):
         raise ValueError("gradients of a gain need the heads that it scales")
-    ws_p, ws_n = _workspace(H.device, workspace)
-    _call("dp_qknorm_rope_backward", H.device, stream, C.byref(H.p), H.view(q, q, "q"), H.view(k, k, "k"),
-          H.view(dout_q, q, "dout_q"), H.view(dout_k, k, "dout_k"), H.view(dq, q, "dq"), H.view(dk, k, "dk"),
-          _on(H.device, torch.float32, rows_q, "rows_q", (H.B, H.dim)),
-          _on(H.device, torch.float32, rows_k, "rows_k", (H.B, H.dim)), int(bool(accumulate_into)), ws_p, ws_n)
+    if q is not None and k is not None and k.dtype is not q.dtype:
+        raise ValueError("queries and keys share one dtype")
+    q_in, q_dout, q_out, keep_q = _heads(device, q, "queries", q, dout_q, dq)
+    k_in, k_dout, k_out, keep_k = _heads(device, k, "keys", k, dout_k, dk)
+    ws_p, ws_n = _workspace(device, workspace)
+    shape = (p.B, p.dim)
+    _call("dp_qknorm_rope_backward", device, stream, C.addressof(p), q_in, k_in, q_dout, k_dout, q_out, k_out,
+          _on(device, _F32, rows_q, "rows_q", shape), _on(device, _F32, rows_k, "rows_k", shape),
+          1 if accumulate_into else 0, ws_p, ws_n)

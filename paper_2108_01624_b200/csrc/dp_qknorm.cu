@@ -10,6 +10,8 @@
 // The angle.  p * inv_freq loses its fractional turns in fp32 at far positions.  The host turns inv_freq[j] / (2 pi) into
 // a 64-bit binary fraction of a turn; p times that, modulo 2^64, is an ordinary wrapping integer product, and its upper
 // 32 bits are the angle in turns to 2^-32, at any 32-bit position, for the price of one multiplication.
+#include <type_traits>
+
 #include "dp_internal.h"
 
 namespace dpk {
@@ -40,6 +42,8 @@ struct QkArgs {
 
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float zero1(const float*) { return 0.0f; }
+__device__ __forceinline__ __nv_bfloat16 zero1(const __nv_bfloat16*) { return __float2bfloat16_rn(0.0f); }
 __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
@@ -73,20 +77,40 @@ struct Lane {
     if (!INTER && p < rot_pairs) { e1 = p; e2 = p + rot_pairs; }
     else { e1 = 2 * p; e2 = 2 * p + 1; }
   }
-  struct Raw { uint4 u1, u2; };
-  template <typename P>
-  __device__ __forceinline__ void read(const P* x, float (&f)[2 * NP]) const {     // f[i] = a, f[NP + i] = b
+  // A head in flight: fetch() issues the loads, unpack() makes fp32 of them (f[i] = a, f[NP + i] = b; 0 where nothing was
+  // fetched).
+  struct VecRaw { uint4 u1, u2; };
+  struct OneRaw { T x[2 * NP]; };
+  using Raw = std::conditional_t<VEC, VecRaw, OneRaw>;
+  __device__ __forceinline__ Raw fetch(const T* x, bool act) const {
+    Raw r;
     if constexpr (VEC) {
-      const uint4* q1 = reinterpret_cast<const uint4*>(x + o1);
-      const uint4* q2 = reinterpret_cast<const uint4*>(x + o2);
-      Raw r;
       r.u1 = r.u2 = make_uint4(0u, 0u, 0u, 0u);
-      if (on) { r.u1 = *q1; r.u2 = *q2; }
+      if (on && act) {
+        r.u1 = *reinterpret_cast<const uint4*>(x + o1);
+        r.u2 = *reinterpret_cast<const uint4*>(x + o2);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        r.x[i] = r.x[NP + i] = zero1(x);
+        if (act && has(i)) {
+          int e1, e2;
+          places(i, e1, e2);
+          r.x[i] = x[e1];
+          r.x[NP + i] = x[e2];
+        }
+      }
+    }
+    return r;
+  }
+  __device__ __forceinline__ void unpack(const Raw& r, float (&f)[2 * NP]) const {
+    if constexpr (VEC) {
       float t[2 * NP];
       const uint32_t w[8] = {r.u1.x, r.u1.y, r.u1.z, r.u1.w, r.u2.x, r.u2.y, r.u2.z, r.u2.w};
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        if constexpr (sizeof(P) == 4) {
+        if constexpr (sizeof(T) == 4) {
           t[k] = __uint_as_float(w[k]);
         } else {
           t[2 * k] = __uint_as_float(w[k] << 16);
@@ -100,19 +124,10 @@ struct Lane {
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        f[i] = f[NP + i] = 0.0f;
-        if (has(i)) {
-          int e1, e2;
-          places(i, e1, e2);
-          f[i] = load1(x + e1);
-          f[NP + i] = load1(x + e2);
-        }
-      }
+      for (int i = 0; i < 2 * NP; ++i) f[i] = load1(&r.x[i]);
     }
   }
-  template <typename P>
-  __device__ __forceinline__ void write(P* x, const float (&f)[2 * NP]) const {
+  __device__ __forceinline__ void write(T* x, const float (&f)[2 * NP]) const {
     if constexpr (VEC) {
       if (!on) return;
       float t[2 * NP];
@@ -124,7 +139,7 @@ struct Lane {
       uint32_t w[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        if constexpr (sizeof(P) == 4) {
+        if constexpr (sizeof(T) == 4) {
           w[k] = __float_as_uint(t[k]);
         } else {
           const __nv_bfloat162 h = __floats2bfloat162_rn(t[2 * k], t[2 * k + 1]);
@@ -169,7 +184,10 @@ struct Lane {
   }
 };
 
-template <int NP>
+// Sine and cosine of the angle of each pair.  EXACT (fp32 data): within 2 ulp.  Otherwise the hardware approximations on
+// [-pi, pi], off by at most 2^-21 of the pair's length: the data's own bf16 rounding is 2^12 times that, and the accurate
+// pair costs about ten times the instructions of the two.
+template <int NP, bool EXACT>
 __device__ __forceinline__ void angles(const unsigned long long* turn, int pos, const int (&pair)[NP], const bool (&turns)[NP],
                                        float (&cs)[NP], float (&sn)[NP]) {
 #pragma unroll
@@ -179,7 +197,64 @@ __device__ __forceinline__ void angles(const unsigned long long* turn, int pos, 
     if (turns[i]) {
       const unsigned long long t = turn[pair[i]] * (unsigned long long)(long long)pos;
       // signed, so that angles just below a whole turn are small negative ones; in units of pi
-      sincospif((float)(int)(unsigned int)(t >> 32) * 0x1p-31f, &sn[i], &cs[i]);
+      const float half_turns = (float)(int)(unsigned int)(t >> 32) * 0x1p-31f;
+      if (EXACT) {
+        sincospif(half_turns, &sn[i], &cs[i]);
+      } else {
+        sn[i] = __sinf(half_turns * 3.14159265f);
+        cs[i] = __cosf(half_turns * 3.14159265f);
+      }
+    }
+  }
+}
+
+// Two fp32 operations per instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+template <int N> __device__ __forceinline__ float2 at2(const float (&f)[N], int i) { return make_float2(f[i], f[i + 1]); }
+template <int N> __device__ __forceinline__ void put2(float (&f)[N], int i, float2 v) { f[i] = v.x; f[i + 1] = v.y; }
+
+template <int N>
+__device__ __forceinline__ float dot(const float (&a)[N], const float (&b)[N]) {      // N even
+  float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+  for (int i = 0; i < N; i += 2) s = fma2(at2(a, i), at2(b, i), s);
+  return s.x + s.y;
+}
+template <int N>
+__device__ __forceinline__ void scale(float (&a)[N], float r) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2) put2(a, i, mul2(at2(a, i), make_float2(r, r)));
+}
+// (a, b) <- (a c1 - b s1, b c2 + a s2) for each pair; f[i] = a, f[NP + i] = b.  s1n = -s1.
+template <int NP>
+__device__ __forceinline__ void turn_pairs(float (&f)[2 * NP], const float (&c1)[NP], const float (&s1n)[NP],
+                                           const float (&c2)[NP], const float (&s2)[NP]) {
+  if constexpr (NP % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < NP; i += 2) {
+      const float2 a = at2(f, i), b = at2(f, NP + i);
+      put2(f, i, fma2(a, at2(c1, i), mul2(b, at2(s1n, i))));
+      put2(f, NP + i, fma2(b, at2(c2, i), mul2(a, at2(s2, i))));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const float a = f[i], b = f[NP + i];
+      f[i] = fmaf(a, c1[i], b * s1n[i]);
+      f[NP + i] = fmaf(b, c2[i], a * s2[i]);
     }
   }
 }
@@ -190,10 +265,30 @@ __device__ __forceinline__ float group_sum(float s, int group) {
 }
 
 constexpr int kQkThreads = 256;
+#ifndef DP_QK_FWD_AHEAD
+#define DP_QK_FWD_AHEAD 2
+#endif
+#ifndef DP_QK_FWD_BLOCKS
+#define DP_QK_FWD_BLOCKS 2
+#endif
+#ifndef DP_QK_BWD_BLOCKS
+#define DP_QK_BWD_BLOCKS 2
+#endif
+#ifndef DP_QK_BWD_AHEAD
+#define DP_QK_BWD_AHEAD 1
+#endif
+#ifndef DP_QK_HP
+#define DP_QK_HP 8
+#endif
+#ifndef DP_QK_CHUNK
+#define DP_QK_CHUNK 128
+#endif
+constexpr int kHeadsPerItem = DP_QK_HP, kMaxChunk = DP_QK_CHUNK;
+constexpr int kFwdAhead = DP_QK_FWD_AHEAD, kBwdAhead = DP_QK_BWD_AHEAD;
 
 // Forward.  A group of lanes takes one item: a share of the query (or key) heads of one token, whose angles it forms once.
 template <typename T, int NP, bool VEC, bool INTER>
-__global__ void __launch_bounds__(kQkThreads)
+__global__ void __launch_bounds__(kQkThreads, VEC ? DP_QK_FWD_BLOCKS : 1)
 k_qknorm(const __grid_constant__ QkArgs a) {
   const int group = 1 << a.group_log;
   const int li = threadIdx.x & (group - 1);
@@ -219,30 +314,36 @@ k_qknorm(const __grid_constant__ QkArgs a) {
     pair[i] = L.pair(i);
     turns[i] = live && L.has(i) && pair[i] < a.rot_pairs;
   }
-  angles<NP>(a.turn, pos, pair, turns, cs, sn);
+  angles<NP, sizeof(T) == 4>(a.turn, pos, pair, turns, cs, sn);
   L.gains(v.gain, gain);
+  // the gain is folded into the rotation: y_a = r (a g_a cos - b g_b sin), y_b = r (b g_b cos + a g_a sin)
+  float c1[NP], s1n[NP], c2[NP], s2[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    c1[i] = gain[i] * cs[i];
+    s1n[i] = -gain[NP + i] * sn[i];
+    c2[i] = gain[NP + i] * cs[i];
+    s2[i] = gain[i] * sn[i];
+  }
   const T* x = static_cast<const T*>(v.in) + b * v.in_b + t * v.in_t + h0 * v.in_h;
   T* y = static_cast<T*>(v.out) + b * v.out_b + t * v.out_t + h0 * v.out_h;
   const int rounds = __reduce_max_sync(0xffffffffu, nh);
-#pragma unroll 2
-  for (int h = 0; h < rounds; ++h) {
-    const bool act = h < nh;
-    float f[2 * NP];
+  // kFwdAhead heads' loads are in flight while one is worked on
+  typename Lane<T, NP, VEC, INTER>::Raw raw[kFwdAhead];
 #pragma unroll
-    for (int i = 0; i < 2 * NP; ++i) f[i] = 0.0f;
-    if (act) L.read(x + h * v.in_h, f);
-    float s = 0.0f;
+  for (int k = 0; k < kFwdAhead; ++k) raw[k] = L.fetch(x + k * v.in_h, k < nh);
+  for (int h = 0; h < rounds; h += kFwdAhead) {
 #pragma unroll
-    for (int i = 0; i < 2 * NP; ++i) s = fmaf(f[i], f[i], s);
-    s = group_sum(s, group);
-    const float r = act ? rsqrtf(s * a.inv_dim + a.eps) : 0.0f;   // 0: idle heads add nothing, even with eps = 0
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const float p = f[i] * r * gain[i], q = f[NP + i] * r * gain[NP + i];
-      f[i] = p * cs[i] - q * sn[i];
-      f[NP + i] = q * cs[i] + p * sn[i];
+    for (int k = 0; k < kFwdAhead; ++k) {
+      const bool act = h + k < nh;
+      float f[2 * NP];
+      L.unpack(raw[k], f);
+      raw[k] = L.fetch(x + (h + k + kFwdAhead) * v.in_h, h + k + kFwdAhead < nh);
+      const float s = group_sum(dot(f, f), group);
+      scale(f, rsqrtf(s * a.inv_dim + a.eps));
+      turn_pairs<NP>(f, c1, s1n, c2, s2);
+      if (act) L.write(y + (h + k) * v.out_h, f);
     }
-    if (act) L.write(y + h * v.out_h, f);
   }
 }
 
@@ -250,7 +351,7 @@ k_qknorm(const __grid_constant__ QkArgs a) {
 // (token, head share) items.  Every lane adds u * xhat of its elements over all heads it meets; at the end the block's
 // sums go, in a fixed order, to the example's row or, where an example has several blocks, to a partial row.
 template <typename T, int NP, bool VEC, bool INTER>
-__global__ void __launch_bounds__(kQkThreads)
+__global__ void __launch_bounds__(kQkThreads, VEC ? DP_QK_BWD_BLOCKS : 1)
 k_qknorm_grad(const __grid_constant__ QkArgs a) {
   extern __shared__ float gsum[];                // [warps][D]
   const int group = 1 << a.group_log;
@@ -284,40 +385,45 @@ k_qknorm_grad(const __grid_constant__ QkArgs a) {
     float cs[NP], sn[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) turns[i] = live && L.has(i) && pair[i] < a.rot_pairs;
-    angles<NP>(a.turn, pos, pair, turns, cs, sn);
+    angles<NP, sizeof(T) == 4>(a.turn, pos, pair, turns, cs, sn);
+    float snn[NP];                               // R(-p): the sine with the other sign
+#pragma unroll
+    for (int i = 0; i < NP; ++i) snn[i] = -sn[i];
     const T* x = static_cast<const T*>(v.in) + b * v.in_b + t * v.in_t + h0 * v.in_h;
     const T* g = static_cast<const T*>(v.dout) + b * v.dout_b + t * v.dout_t + h0 * v.dout_h;
     T* y = static_cast<T*>(v.out) + b * v.out_b + t * v.out_t + h0 * v.out_h;
     const int rounds = __reduce_max_sync(0xffffffffu, nh);
-#pragma unroll 2
-    for (int h = 0; h < rounds; ++h) {
-      const bool act = h < nh;
-      float f[2 * NP], u[2 * NP];
+    typename Lane<T, NP, VEC, INTER>::Raw rx[kBwdAhead], rg[kBwdAhead];
 #pragma unroll
-      for (int i = 0; i < 2 * NP; ++i) f[i] = u[i] = 0.0f;
-      if (act) { L.read(x + h * v.in_h, f); L.read(g + h * v.dout_h, u); }
-      float s = 0.0f;
+    for (int k = 0; k < kBwdAhead; ++k) {
+      rx[k] = L.fetch(x + k * v.in_h, k < nh);
+      rg[k] = L.fetch(g + k * v.dout_h, k < nh);
+    }
+    for (int h = 0; h < rounds; h += kBwdAhead) {
 #pragma unroll
-      for (int i = 0; i < 2 * NP; ++i) s = fmaf(f[i], f[i], s);
-      s = group_sum(s, group);
-      const float r = act ? rsqrtf(s * a.inv_dim + a.eps) : 0.0f;   // 0: idle heads add nothing, even with eps = 0
-      float m = 0.0f;
+      for (int k = 0; k < kBwdAhead; ++k) {
+        const bool act = h + k < nh;
+        float f[2 * NP], u[2 * NP];
+        L.unpack(rx[k], f);
+        L.unpack(rg[k], u);
+        rx[k] = L.fetch(x + (h + k + kBwdAhead) * v.in_h, h + k + kBwdAhead < nh);
+        rg[k] = L.fetch(g + (h + k + kBwdAhead) * v.dout_h, h + k + kBwdAhead < nh);
+        turn_pairs<NP>(u, cs, sn, cs, snn);
+        const float s = group_sum(dot(f, f), group);
+        // 0 for idle heads, which then add nothing even with eps = 0
+        const float r = act ? rsqrtf(s * a.inv_dim + a.eps) : 0.0f;
+        // with u' = r u: sum += u' x (= u xhat), w' = gain u', dx = w' - x r^2 mean(w' x)
+        scale(u, r);
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const float p = u[i] * cs[i] + u[NP + i] * sn[i], q = u[NP + i] * cs[i] - u[i] * sn[i];
-        f[i] *= r;
-        f[NP + i] *= r;                          // xhat
-        sum[i] = fmaf(p, f[i], sum[i]);
-        sum[NP + i] = fmaf(q, f[NP + i], sum[NP + i]);
-        u[i] = p * gain[i];
-        u[NP + i] = q * gain[NP + i];            // w
-        m = fmaf(u[i], f[i], m);
-        m = fmaf(u[NP + i], f[NP + i], m);
+        for (int i = 0; i < 2 * NP; i += 2) {
+          put2(sum, i, fma2(at2(u, i), at2(f, i), at2(sum, i)));
+          put2(u, i, mul2(at2(u, i), at2(gain, i)));
+        }
+        const float m = -(group_sum(dot(u, f), group) * a.inv_dim) * r * r;
+#pragma unroll
+        for (int i = 0; i < 2 * NP; i += 2) put2(u, i, fma2(at2(f, i), make_float2(m, m), at2(u, i)));
+        if (act) L.write(y + (h + k) * v.out_h, u);
       }
-      m = group_sum(m, group) * a.inv_dim;
-#pragma unroll
-      for (int i = 0; i < 2 * NP; ++i) u[i] = r * (u[i] - f[i] * m);
-      if (act) L.write(y + h * v.out_h, u);
     }
   }
   if (!v.rows) return;                           // uniform over the block
@@ -409,14 +515,15 @@ static bool vec_heads(const dp_heads& x, int V) {
   return !misaligned(x.data, 16) && x.stride_b % V == 0 && x.stride_t % V == 0 && x.stride_h % V == 0;
 }
 
-// Tokens per block of the backward pass: enough blocks to fill the GPU several times over, so that the last round of
-// blocks costs little, but no more than 512 partial rows per example.
+// Tokens per block of the backward pass: a power of two, so that a block's items divide evenly among its groups, as large
+// as still gives enough blocks to fill the GPU several times over (the last round of blocks then costs little); at most 512
+// partial rows per example.
 static int grad_chunk(const dp_qknorm* p) {
-  const long long kinds = (p->n_q > 0) + (p->n_k > 0);
-  long long chunks = (148ll * 2 * 8 + (long long)p->B * kinds - 1) / ((long long)p->B * kinds);
-  if (chunks > 512) chunks = 512;
-  if (chunks > p->T) chunks = p->T;
-  return (int)((p->T + chunks - 1) / chunks);
+  const long long kinds = (p->n_q > 0) + (p->n_k > 0), per_token = (long long)p->B * kinds;
+  int chunk = kMaxChunk;
+  while (chunk > 1 && per_token * ceil_div(p->T, chunk) < 148ll * 2 * 6) chunk >>= 1;
+  while (ceil_div(p->T, chunk) > 512) chunk <<= 1;
+  return chunk;
 }
 
 static void fill_args(const dp_qknorm* p, QkArgs* a, bool backward) {
@@ -432,10 +539,10 @@ static void fill_args(const dp_qknorm* p, QkArgs* a, bool backward) {
   a->v[1].heads = p->n_k;
   a->v[0].gain = p->gain_q;
   a->v[1].gain = p->gain_k;
-  // Heads that share one set of angles: up to 8, fewer while there are too few items to fill the GPU.
-  const long long rows = (long long)p->B * p->T * (p->n_q + p->n_k);
-  int hp = 8;
-  while (hp > 1 && rows / hp < 148ll * 256) hp >>= 1;
+  // Heads that share one set of angles: up to kHeadsPerItem, fewer while the items would not fill the GPU's groups.
+  const long long rows = (long long)p->B * p->T * (p->n_q + p->n_k), fill = 148ll * 512 >> a->group_log;
+  int hp = kHeadsPerItem;
+  while (hp > 1 && rows < fill * hp) hp >>= 1;
   a->heads_per_item = hp;
   for (int k = 0; k < 2; ++k) a->v[k].slices = ceil_div(a->v[k].heads, hp);
   a->chunk = backward ? grad_chunk(p) : 0;
@@ -522,8 +629,8 @@ int dp_qknorm_rope(const dp_qknorm* p, const dp_heads* q, const dp_heads* k, con
     a.v[i].out = out[i]->data;
     a.v[i].out_b = out[i]->stride_b; a.v[i].out_t = out[i]->stride_t; a.v[i].out_h = out[i]->stride_h;
   }
+  a.group_log = group_log(p->dim / 2, vec, V);
   fill_args(p, &a, false);
-  a.group_log = group_log(a.pairs, vec, V);
   const Forward f{a, static_cast<cudaStream_t>(cuda_stream)};
   const bool inter = p->interleaved != 0;
   const cudaError_t e = p->dtype == DP_F32 ? pick<float>(a, vec, inter, f) : pick<__nv_bfloat16>(a, vec, inter, f);
@@ -566,8 +673,8 @@ int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_head
     a.v[i].out_b = out[i]->stride_b; a.v[i].out_t = out[i]->stride_t; a.v[i].out_h = out[i]->stride_h;
     a.v[i].rows = rows[i];
   }
+  a.group_log = group_log(p->dim / 2, vec, V);
   fill_args(p, &a, true);
-  a.group_log = group_log(a.pairs, vec, V);
   a.accumulate = accumulate_into ? 1 : 0;
   const bool want_rows = a.v[0].rows || a.v[1].rows;
   if (a.n_chunks > 1 && want_rows) {
