@@ -296,7 +296,7 @@ DP_API int dp_relpos_bias_grad(const dp_relpos* p /*HOST*/, int B, int causal, c
  * trainable tensors for the per-example clip.) */
 typedef struct dp_qknorm {
   int32_t dtype;               /* dp_dtype of queries, keys, outputs and their gradients */
-  int32_t B, T, n_q, n_k;      /* query and key heads; either may be 0, its tensors are then not looked at */
+  int32_t B, T, n_q, n_k;      /* B * T <= 2^30; query and key heads: either may be 0, its tensors are then not looked at */
   int32_t dim, rot;            /* even, dim <= 512, 0 <= rot <= dim */
   int32_t interleaved;
   double eps;                  /* >= 0 */

@@ -18,14 +18,23 @@ namespace dpk {
 
 constexpr int kMaxPairs = 256;                   // D <= 512
 
+// How the heads of one kind (queries or keys) are shared out.  A warp takes a unit: tokens_per_unit neighbouring tokens times
+// `heads_per_unit` heads.  Its groups of lanes stand as (tokens x heads) = 2^gt x 2^gh, and each walks down the tokens
+// with heads_per_group heads of every token, whose angles it forms once.
+struct Share {
+  int heads, heads_per_group, gh, gt, heads_per_unit, head_blocks, tokens_per_unit, chunks;
+  long long units;
+};
+
 struct View {                                    // [B, T, H, D], D contiguous; strides in elements
   const void* in;
   const void* dout;                              // backward: gradient of the output
   void* out;                                     // forward: the output; backward: gradient of the input
   const float* gain;                             // [D] or null (ones)
   float* rows;                                   // backward: [B][D] gain gradients, or null
+  float* partial;                                // backward: [B][chunks * head_blocks][D], or null (one unit per example)
   long long in_b, in_t, in_h, dout_b, dout_t, dout_h, out_b, out_t, out_h;
-  int heads, slices;                             // heads, and groups' shares of them per token
+  Share share;
 };
 
 struct QkArgs {
@@ -33,10 +42,8 @@ struct QkArgs {
   const int32_t* positions;                      // [B, T] or null: 0 .. T-1
   const int32_t* lengths;                        // [B] or null
   float eps, inv_dim;
-  int B, T, pairs, rot_pairs, heads_per_item, group_log;
-  int chunk, n_chunks;                           // backward: tokens per block, blocks per example and kind
+  int B, T, pairs, rot_pairs, group_log;
   int accumulate;
-  float* partial;                                // backward: [B][n_chunks][2][D], or null
   unsigned long long turn[kMaxPairs];            // fraction of a turn per position, 2^-64 units
 };
 
@@ -46,6 +53,14 @@ __device__ __forceinline__ float zero1(const float*) { return 0.0f; }
 __device__ __forceinline__ __nv_bfloat16 zero1(const __nv_bfloat16*) { return __float2bfloat16_rn(0.0f); }
 __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// 16 bytes to shared memory, asynchronously; with get = false the source is not read and zeros are written.
+__device__ __forceinline__ void copy16(uint4* slot, const void* src, bool get) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((unsigned)__cvta_generic_to_shared(slot)), "l"(src),
+               "r"(get ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_mark() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // How a lane holds its share of a head: NP pairs (a[i], b[i]).
 // VEC: NP neighbouring pairs fetched as two 16-byte vectors.  In the `halves` layout (pair j = elements j and
@@ -77,19 +92,24 @@ struct Lane {
     if (!INTER && p < rot_pairs) { e1 = p; e2 = p + rot_pairs; }
     else { e1 = 2 * p; e2 = 2 * p + 1; }
   }
-  // A head in flight: fetch() issues the loads, unpack() makes fp32 of them (f[i] = a, f[NP + i] = b; 0 where nothing was
-  // fetched).
+  // A head in flight.  VEC: copied asynchronously into the lane's own 32 bytes of shared memory (slot[0], slot[32]: the
+  // 16-byte words of a warp side by side), so that deep prefetch costs no registers; only the lane itself reads them, so its
+  // own wait is all the synchronisation there is.  Otherwise read directly when its turn comes.
   struct VecRaw { uint4 u1, u2; };
   struct OneRaw { T x[2 * NP]; };
   using Raw = std::conditional_t<VEC, VecRaw, OneRaw>;
-  __device__ __forceinline__ Raw fetch(const T* x, bool act) const {
+  __device__ __forceinline__ void issue(const T* x, bool act, uint4* slot) const {
+    if constexpr (VEC) {
+      const bool get = act && on;                // nothing is read otherwise, and the slot is filled with zeros
+      copy16(slot, x + o1, get);
+      copy16(slot + 32, x + o2, get);
+    }
+  }
+  __device__ __forceinline__ Raw take(const T* x, bool act, const uint4* slot) const {
     Raw r;
     if constexpr (VEC) {
-      r.u1 = r.u2 = make_uint4(0u, 0u, 0u, 0u);
-      if (on && act) {
-        r.u1 = *reinterpret_cast<const uint4*>(x + o1);
-        r.u2 = *reinterpret_cast<const uint4*>(x + o2);
-      }
+      r.u1 = slot[0];
+      r.u2 = slot[32];
     } else {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
@@ -173,7 +193,15 @@ struct Lane {
       }
     }
   }
-  // Elements that f[i] and f[NP + i] of read() hold.
+  // Fractions of a turn per position of the lane's pairs; 0 where nothing turns.
+  __device__ __forceinline__ void turns(const QkArgs& a, uint2 (&f)[NP]) const {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const unsigned long long x = has(i) && pair(i) < rot_pairs ? a.turn[pair(i)] : 0ull;
+      f[i] = make_uint2((unsigned)x, (unsigned)(x >> 32));
+    }
+  }
+  // Elements that f[i] and f[NP + i] of unpack() hold.
   __device__ __forceinline__ void element(int i, int& e1, int& e2) const {
     if (VEC) {
       e1 = INTER ? o1 + 2 * i : o1 + i;
@@ -184,28 +212,35 @@ struct Lane {
   }
 };
 
-// Sine and cosine of the angle of each pair.  EXACT (fp32 data): within 2 ulp.  Otherwise the hardware approximations on
-// [-pi, pi], off by at most 2^-21 of the pair's length: the data's own bf16 rounding is 2^12 times that, and the accurate
-// pair costs about ten times the instructions of the two.
-template <int NP, bool EXACT>
-__device__ __forceinline__ void angles(const unsigned long long* turn, int pos, const int (&pair)[NP], const bool (&turns)[NP],
-                                       float (&cs)[NP], float (&sn)[NP]) {
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    cs[i] = 1.0f;
-    sn[i] = 0.0f;
-    if (turns[i]) {
-      const unsigned long long t = turn[pair[i]] * (unsigned long long)(long long)pos;
-      // signed, so that angles just below a whole turn are small negative ones; in units of pi
-      const float half_turns = (float)(int)(unsigned int)(t >> 32) * 0x1p-31f;
-      if (EXACT) {
-        sincospif(half_turns, &sn[i], &cs[i]);
-      } else {
-        sn[i] = __sinf(half_turns * 3.14159265f);
-        cs[i] = __cosf(half_turns * 3.14159265f);
-      }
-    }
+// Sine and cosine of pos * turn (a 64-bit fraction of a turn per position; 0 for what does not turn, which gives exactly 0
+// and 1).  EXACT (fp32 data): within 2 ulp.  Otherwise the hardware approximations on [-pi, pi], off by at most 2^-21 of
+// the pair's length: the data's own bf16 rounding is 2^12 times that, and the accurate pair costs about ten times the
+// instructions of the two.
+template <bool EXACT>
+__device__ __forceinline__ void angle(uint2 turn, int pos, float& cs, float& sn) {
+  // bits 32..63 of turn * pos modulo 2^64, pos signed; as a signed number, so that angles just below a whole turn are small
+  // negative ones
+  unsigned h = turn.y * (unsigned)pos + __umulhi(turn.x, (unsigned)pos);
+  if (pos < 0) h -= turn.x;
+  const float half_turns = (float)(int)h * 0x1p-31f;
+  if (EXACT) {
+    sincospif(half_turns, &sn, &cs);
+  } else {
+    sn = __sinf(half_turns * 3.14159265f);
+    cs = __cosf(half_turns * 3.14159265f);
   }
+}
+
+// Sum over a group of 2^GL lanes (GL < 0: of `group` lanes, known at run time only).
+template <int GL>
+__device__ __forceinline__ float group_sum(float s, int group) {
+  if constexpr (GL >= 0) {
+#pragma unroll
+    for (int o = (1 << GL) >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  } else {
+    for (int o = group >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  }
+  return s;
 }
 
 // Two fp32 operations per instruction.
@@ -259,224 +294,268 @@ __device__ __forceinline__ void turn_pairs(float (&f)[2 * NP], const float (&c1)
   }
 }
 
-__device__ __forceinline__ float group_sum(float s, int group) {
-  for (int o = group >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return s;
+
+// Measured on the BERT-Large microbatch (forward 268 MB, backward 403 MB; device time of the main kernel):
+//   heads in flight per group   forward  2: 55 us, 4: 51, 8: 53        backward  2: 84, 4: 76
+//   warps resident per SM       forward 12: 51 us, 16: 51, 20: 55      backward  8: 82, 12: 76, 16: 100 (registers spill)
+//   warps per block             forward  1, 2, 4: 50 to 51 us; one token for each of 64 sequences 4.2, 4.8, 5.4 us
+// One warp a block, then: warps never wait for one another, and a finished one makes room at once.
+// Units: two waves of them (one: 51 / 75 us and 18.0 on few examples in fp32; two: 50 / 76 and 16.7; three: 53 / 80).
+constexpr int kFwdStages = 4, kBwdStages = 4;    // heads in flight per group (powers of two)
+constexpr int kFwdWarps = 16, kBwdWarps = 12;    // resident per SM
+constexpr int kWaves = 2, kHeadsPerGroup = 8;
+
+// Where one group of lanes is on its walk over its unit: heads_per_group heads of a token, then its next token.  Two of
+// these run over a unit, one that issues copies some heads ahead and one that computes.
+template <bool FLAT>
+struct Walk {
+  int token, tstep, end, b, t;
+  bool live;                                     // this group's token exists
+  // tokens [first, end) of the unit: of example b, or, FLAT, of all examples one behind another
+  __device__ __forceinline__ Walk(const Share& s, int gi, int first, int end_, int b_)
+      : token(first + (gi >> s.gh) - (1 << s.gt)), tstep(1 << s.gt), end(end_), b(b_), t(0), live(false) {}
+  __device__ __forceinline__ void next(const QkArgs& a) {
+    token += tstep;
+    live = token < end;
+    t = live ? token : 0;
+    if (FLAT && live) {
+      b = token / a.T;
+      t = token - b * a.T;
+      if (a.lengths && t >= a.lengths[b]) live = false;
+    }
+  }
+};
+
+// Which unit of which kind a block (one warp) has.
+__device__ __forceinline__ void unit_of(const QkArgs& a, int& kind, long long& unit) {
+  unit = blockIdx.x;
+  kind = unit >= a.v[0].share.units;
+  if (kind) unit -= a.v[0].share.units;
 }
 
-constexpr int kQkThreads = 256;
-#ifndef DP_QK_FWD_AHEAD
-#define DP_QK_FWD_AHEAD 2
-#endif
-#ifndef DP_QK_FWD_BLOCKS
-#define DP_QK_FWD_BLOCKS 2
-#endif
-#ifndef DP_QK_BWD_BLOCKS
-#define DP_QK_BWD_BLOCKS 2
-#endif
-#ifndef DP_QK_BWD_AHEAD
-#define DP_QK_BWD_AHEAD 1
-#endif
-#ifndef DP_QK_HP
-#define DP_QK_HP 8
-#endif
-#ifndef DP_QK_CHUNK
-#define DP_QK_CHUNK 128
-#endif
-constexpr int kHeadsPerItem = DP_QK_HP, kMaxChunk = DP_QK_CHUNK;
-constexpr int kFwdAhead = DP_QK_FWD_AHEAD, kBwdAhead = DP_QK_BWD_AHEAD;
-
-// Forward.  A group of lanes takes one item: a share of the query (or key) heads of one token, whose angles it forms once.
-template <typename T, int NP, bool VEC, bool INTER>
-__global__ void __launch_bounds__(kQkThreads, VEC ? DP_QK_FWD_BLOCKS : 1)
+// Forward.
+template <typename T, int NP, bool VEC, bool INTER, int GL>
+__global__ void __launch_bounds__(32, VEC ? kFwdWarps : 1)
 k_qknorm(const __grid_constant__ QkArgs a) {
-  const int group = 1 << a.group_log;
-  const int li = threadIdx.x & (group - 1);
-  const Lane<T, NP, VEC, INTER> L(li, group, a);
-  const int slices = a.v[0].slices + a.v[1].slices;
-  const long long item = ((long long)blockIdx.x * kQkThreads + threadIdx.x) >> a.group_log;
-  const long long tok = item / slices;
-  int sl = (int)(item - tok * slices);
-  bool live = tok < (long long)a.B * a.T;
-  const int b = live ? (int)(tok / a.T) : 0, t = live ? (int)(tok - (long long)b * a.T) : 0;
-  if (live && a.lengths && t >= a.lengths[b]) live = false;
-  const int kind = sl >= a.v[0].slices;
-  if (kind) sl -= a.v[0].slices;
+  __shared__ uint4 ring_all[VEC ? kFwdStages * 64 : 1];            // [stages][2][32]
+  int kind;
+  long long unit;
+  unit_of(a, kind, unit);
   const View& v = a.v[kind];
-  const int h0 = sl * a.heads_per_item;
-  const int nh = live ? min(a.heads_per_item, v.heads - h0) : 0;
-  const int pos = !live ? 0 : a.positions ? a.positions[tok] : t;
-  int pair[NP];
-  bool turns[NP];
-  float cs[NP], sn[NP], gain[2 * NP];
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    pair[i] = L.pair(i);
-    turns[i] = live && L.has(i) && pair[i] < a.rot_pairs;
-  }
-  angles<NP, sizeof(T) == 4>(a.turn, pos, pair, turns, cs, sn);
+  const Share& s = v.share;
+  const int glog = GL >= 0 ? GL : a.group_log, group = 1 << glog;
+  const int lane = threadIdx.x, li = lane & (group - 1), gi = lane >> glog;
+  const Lane<T, NP, VEC, INTER> L(li, group, a);
+  uint4* ring = ring_all + lane;
+  const int per = s.heads_per_group, hstep = 1 << s.gh;
+  const int h0 = (int)(unit % s.head_blocks) * s.heads_per_unit + (gi & (hstep - 1));
+  const int mine = h0 < s.heads ? min(per, (s.heads - h0 + hstep - 1) >> s.gh) : 0;      // heads of a token
+  const long long first = unit / s.head_blocks * s.tokens_per_unit;
+  const int end = (int)min((long long)a.B * a.T, first + s.tokens_per_unit);
+  const int walks = (int)((end - first + (1 << s.gt) - 1) >> s.gt), steps = walks * per;
+  Walk<true> ahead(s, gi, (int)first, end, 0), at = ahead;
+  const T* in = static_cast<const T*>(v.in) + h0 * v.in_h;
+  T* out = static_cast<T*>(v.out) + h0 * v.out_h;
+  const long long in_step = hstep * v.in_h, out_step = hstep * v.out_h;
+  const T* src = in;
+  int aj = per, an = 0;                          // ahead: head of the token, step
+  auto issue = [&]() {
+    if (VEC) {
+      if (an < steps) {
+        if (aj == per) {
+          ahead.next(a);
+          src = in + ahead.b * v.in_b + ahead.t * v.in_t;
+          aj = 0;
+        }
+        L.issue(src, ahead.live && aj < mine, ring + (an & (kFwdStages - 1)) * 64);
+        src += in_step;
+        ++aj;
+        ++an;
+      }
+      copies_mark();
+    }
+  };
+#pragma unroll 1
+  for (int n = 0; n < kFwdStages - 1; ++n) issue();
+  float gain[2 * NP];
   L.gains(v.gain, gain);
-  // the gain is folded into the rotation: y_a = r (a g_a cos - b g_b sin), y_b = r (b g_b cos + a g_a sin)
-  float c1[NP], s1n[NP], c2[NP], s2[NP];
+  uint2 turn[NP];
+  L.turns(a, turn);
+  int n = 0;
+  for (int w = 0; w < walks; ++w) {
+    at.next(a);
+    const int pos = !at.live ? 0 : a.positions ? a.positions[at.token] : at.t;
+    // the gain is folded into the rotation: y_a = r (a g_a cos - b g_b sin), y_b = r (b g_b cos + a g_a sin)
+    float c1[NP], s1n[NP], c2[NP], s2[NP];
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    c1[i] = gain[i] * cs[i];
-    s1n[i] = -gain[NP + i] * sn[i];
-    c2[i] = gain[NP + i] * cs[i];
-    s2[i] = gain[i] * sn[i];
-  }
-  const T* x = static_cast<const T*>(v.in) + b * v.in_b + t * v.in_t + h0 * v.in_h;
-  T* y = static_cast<T*>(v.out) + b * v.out_b + t * v.out_t + h0 * v.out_h;
-  const int rounds = __reduce_max_sync(0xffffffffu, nh);
-  // kFwdAhead heads' loads are in flight while one is worked on
-  typename Lane<T, NP, VEC, INTER>::Raw raw[kFwdAhead];
-#pragma unroll
-  for (int k = 0; k < kFwdAhead; ++k) raw[k] = L.fetch(x + k * v.in_h, k < nh);
-  for (int h = 0; h < rounds; h += kFwdAhead) {
-#pragma unroll
-    for (int k = 0; k < kFwdAhead; ++k) {
-      const bool act = h + k < nh;
+    for (int i = 0; i < NP; ++i) {
+      float cs, sn;
+      angle<sizeof(T) == 4>(turn[i], pos, cs, sn);
+      c1[i] = gain[i] * cs;
+      s1n[i] = -gain[NP + i] * sn;
+      c2[i] = gain[NP + i] * cs;
+      s2[i] = gain[i] * sn;
+    }
+    const T* x = in + at.b * v.in_b + at.t * v.in_t;
+    T* y = out + at.b * v.out_b + at.t * v.out_t;
+#pragma unroll 1
+    for (int j = 0; j < per; ++j, ++n) {
+      issue();
+      if (VEC) copies_wait<kFwdStages - 1>();
+      const bool act = at.live && j < mine;
       float f[2 * NP];
-      L.unpack(raw[k], f);
-      raw[k] = L.fetch(x + (h + k + kFwdAhead) * v.in_h, h + k + kFwdAhead < nh);
-      const float s = group_sum(dot(f, f), group);
-      scale(f, rsqrtf(s * a.inv_dim + a.eps));
+      L.unpack(L.take(x, act, ring + (n & (kFwdStages - 1)) * 64), f);
+      scale(f, rsqrtf(group_sum<GL>(dot(f, f), group) * a.inv_dim + a.eps));
       turn_pairs<NP>(f, c1, s1n, c2, s2);
-      if (act) L.write(y + (h + k) * v.out_h, f);
+      if (act) L.write(y, f);
+      if (!VEC) x += in_step;
+      y += out_step;
     }
   }
 }
 
-// Backward.  A block takes a run of one example's tokens for the queries or for the keys; its groups share the
-// (token, head share) items.  Every lane adds u * xhat of its elements over all heads it meets; at the end the block's
-// sums go, in a fixed order, to the example's row or, where an example has several blocks, to a partial row.
-template <typename T, int NP, bool VEC, bool INTER>
-__global__ void __launch_bounds__(kQkThreads, VEC ? DP_QK_BWD_BLOCKS : 1)
+// Backward.  Every lane adds u * xhat of its elements over all heads it meets; at the unit's end the groups' sums go, in a
+// fixed order, to the example's row or, where an example has several units, to a partial row.
+template <typename T, int NP, bool VEC, bool INTER, int GL>
+__global__ void __launch_bounds__(32, VEC ? kBwdWarps : 1)
 k_qknorm_grad(const __grid_constant__ QkArgs a) {
-  extern __shared__ float gsum[];                // [warps][D]
-  const int group = 1 << a.group_log;
-  const int li = threadIdx.x & (group - 1);
-  const Lane<T, NP, VEC, INTER> L(li, group, a);
-  const int kind = blockIdx.z;
+  __shared__ uint4 ring_all[VEC ? kBwdStages * 128 : 1];           // [stages][x, dy][2][32]
+  int kind;
+  long long unit;
+  unit_of(a, kind, unit);
   const View& v = a.v[kind];
-  const int b = blockIdx.y, D = 2 * a.pairs;
-  const int t0 = blockIdx.x * a.chunk;
-  int t1 = min(t0 + a.chunk, a.T);
-  if (a.lengths) t1 = min(t1, a.lengths[b]);
-  const int n_items = max(t1 - t0, 0) * v.slices;
-  const int groups = kQkThreads >> a.group_log, mine = threadIdx.x >> a.group_log;
+  const Share& s = v.share;
+  const int glog = GL >= 0 ? GL : a.group_log, group = 1 << glog;
+  const int lane = threadIdx.x, li = lane & (group - 1), gi = lane >> glog;
+  const Lane<T, NP, VEC, INTER> L(li, group, a);
+  uint4* ring = ring_all + lane;
+  const int parts = s.chunks * s.head_blocks, b = (int)(unit / parts), part = (int)(unit - (long long)b * parts);
+  const int chunk = part / s.head_blocks;
+  const int per = s.heads_per_group, hstep = 1 << s.gh;
+  const int h0 = (part - chunk * s.head_blocks) * s.heads_per_unit + (gi & (hstep - 1));
+  const int mine = h0 < s.heads ? min(per, (s.heads - h0 + hstep - 1) >> s.gh) : 0;      // heads of a token
+  const int first = chunk * s.tokens_per_unit;
+  int end = min(a.T, first + s.tokens_per_unit);
+  if (a.lengths) end = min(end, a.lengths[b]);
+  const int walks = (max(end - first, 0) + (1 << s.gt) - 1) >> s.gt, steps = walks * per;
+  Walk<false> ahead(s, gi, first, end, b), at = ahead;
+  const T* in = static_cast<const T*>(v.in) + b * v.in_b + h0 * v.in_h;
+  const T* dout = static_cast<const T*>(v.dout) + b * v.dout_b + h0 * v.dout_h;
+  T* out = static_cast<T*>(v.out) + b * v.out_b + h0 * v.out_h;
+  const long long in_step = hstep * v.in_h, dout_step = hstep * v.dout_h, out_step = hstep * v.out_h;
+  const T* src = in;
+  const T* gsrc = dout;
+  int aj = per, an = 0;
+  auto issue = [&]() {
+    if (VEC) {
+      if (an < steps) {
+        if (aj == per) {
+          ahead.next(a);
+          src = in + ahead.t * v.in_t;
+          gsrc = dout + ahead.t * v.dout_t;
+          aj = 0;
+        }
+        uint4* slot = ring + (an & (kBwdStages - 1)) * 128;
+        const bool act = ahead.live && aj < mine;
+        L.issue(src, act, slot);
+        L.issue(gsrc, act, slot + 64);
+        src += in_step;
+        gsrc += dout_step;
+        ++aj;
+        ++an;
+      }
+      copies_mark();
+    }
+  };
+#pragma unroll 1
+  for (int n = 0; n < kBwdStages - 1; ++n) issue();
   float gain[2 * NP], sum[2 * NP];
   L.gains(v.gain, gain);
 #pragma unroll
   for (int i = 0; i < 2 * NP; ++i) sum[i] = 0.0f;
-  int pair[NP];
-#pragma unroll
-  for (int i = 0; i < NP; ++i) pair[i] = L.pair(i);
-  // the groups of a warp walk together
-  const int walks = (n_items + groups - 1) / groups;
+  uint2 turn[NP];
+  L.turns(a, turn);
+  int n = 0;
   for (int w = 0; w < walks; ++w) {
-    const int item = w * groups + mine;
-    const bool live = item < n_items;
-    const int t = t0 + (live ? item / v.slices : 0), sl = live ? item % v.slices : 0;
-    const int h0 = sl * a.heads_per_item;
-    const int nh = live ? min(a.heads_per_item, v.heads - h0) : 0;
-    const int pos = !live ? 0 : a.positions ? a.positions[(long long)b * a.T + t] : t;
-    bool turns[NP];
-    float cs[NP], sn[NP];
+    at.next(a);
+    const int pos = !at.live ? 0 : a.positions ? a.positions[(long long)b * a.T + at.t] : at.t;
+    float cs[NP], sn[NP], snn[NP];               // R(-p): the sine with the other sign
 #pragma unroll
-    for (int i = 0; i < NP; ++i) turns[i] = live && L.has(i) && pair[i] < a.rot_pairs;
-    angles<NP, sizeof(T) == 4>(a.turn, pos, pair, turns, cs, sn);
-    float snn[NP];                               // R(-p): the sine with the other sign
-#pragma unroll
-    for (int i = 0; i < NP; ++i) snn[i] = -sn[i];
-    const T* x = static_cast<const T*>(v.in) + b * v.in_b + t * v.in_t + h0 * v.in_h;
-    const T* g = static_cast<const T*>(v.dout) + b * v.dout_b + t * v.dout_t + h0 * v.dout_h;
-    T* y = static_cast<T*>(v.out) + b * v.out_b + t * v.out_t + h0 * v.out_h;
-    const int rounds = __reduce_max_sync(0xffffffffu, nh);
-    typename Lane<T, NP, VEC, INTER>::Raw rx[kBwdAhead], rg[kBwdAhead];
-#pragma unroll
-    for (int k = 0; k < kBwdAhead; ++k) {
-      rx[k] = L.fetch(x + k * v.in_h, k < nh);
-      rg[k] = L.fetch(g + k * v.dout_h, k < nh);
+    for (int i = 0; i < NP; ++i) {
+      angle<sizeof(T) == 4>(turn[i], pos, cs[i], sn[i]);
+      snn[i] = -sn[i];
     }
-    for (int h = 0; h < rounds; h += kBwdAhead) {
+    const T* x = in + at.t * v.in_t;
+    const T* g = dout + at.t * v.dout_t;
+    T* y = out + at.t * v.out_t;
+#pragma unroll 1
+    for (int j = 0; j < per; ++j, ++n) {
+      issue();
+      if (VEC) copies_wait<kBwdStages - 1>();
+      const bool act = at.live && j < mine;
+      const uint4* slot = ring + (n & (kBwdStages - 1)) * 128;
+      float f[2 * NP], u[2 * NP];
+      L.unpack(L.take(x, act, slot), f);
+      L.unpack(L.take(g, act, slot + 64), u);
+      turn_pairs<NP>(u, cs, sn, cs, snn);
+      const float square = group_sum<GL>(dot(f, f), group);
+      // 0 for idle groups, which then add nothing even with eps = 0
+      const float r = act ? rsqrtf(square * a.inv_dim + a.eps) : 0.0f;
+      // with u' = r u: sum += u' x (= u xhat), w' = gain u', dx = w' - x r^2 mean(w' x)
+      scale(u, r);
 #pragma unroll
-      for (int k = 0; k < kBwdAhead; ++k) {
-        const bool act = h + k < nh;
-        float f[2 * NP], u[2 * NP];
-        L.unpack(rx[k], f);
-        L.unpack(rg[k], u);
-        rx[k] = L.fetch(x + (h + k + kBwdAhead) * v.in_h, h + k + kBwdAhead < nh);
-        rg[k] = L.fetch(g + (h + k + kBwdAhead) * v.dout_h, h + k + kBwdAhead < nh);
-        turn_pairs<NP>(u, cs, sn, cs, snn);
-        const float s = group_sum(dot(f, f), group);
-        // 0 for idle heads, which then add nothing even with eps = 0
-        const float r = act ? rsqrtf(s * a.inv_dim + a.eps) : 0.0f;
-        // with u' = r u: sum += u' x (= u xhat), w' = gain u', dx = w' - x r^2 mean(w' x)
-        scale(u, r);
-#pragma unroll
-        for (int i = 0; i < 2 * NP; i += 2) {
-          put2(sum, i, fma2(at2(u, i), at2(f, i), at2(sum, i)));
-          put2(u, i, mul2(at2(u, i), at2(gain, i)));
-        }
-        const float m = -(group_sum(dot(u, f), group) * a.inv_dim) * r * r;
-#pragma unroll
-        for (int i = 0; i < 2 * NP; i += 2) put2(u, i, fma2(at2(f, i), make_float2(m, m), at2(u, i)));
-        if (act) L.write(y + (h + k) * v.out_h, u);
+      for (int i = 0; i < 2 * NP; i += 2) {
+        put2(sum, i, fma2(at2(u, i), at2(f, i), at2(sum, i)));
+        put2(u, i, mul2(at2(u, i), at2(gain, i)));
       }
+      const float m = -(group_sum<GL>(dot(u, f), group) * a.inv_dim) * r * r;
+#pragma unroll
+      for (int i = 0; i < 2 * NP; i += 2) put2(u, i, fma2(at2(f, i), make_float2(m, m), at2(u, i)));
+      if (act) L.write(y, u);
+      if (!VEC) { x += in_step; g += dout_step; }
+      y += out_step;
     }
   }
-  if (!v.rows) return;                           // uniform over the block
-  // lanes with the same elements: first inside the warp, then over the warps
+  if (!v.rows) return;                           // uniform over the warp
 #pragma unroll
   for (int i = 0; i < 2 * NP; ++i)
     for (int o = 16; o >= group; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
-  const int warp = threadIdx.x >> 5;
-  if ((threadIdx.x & 31) < group) {
+  if (gi == 0) {
+    const int D = 2 * a.pairs;
+    float* row = v.partial ? v.partial + unit * D : v.rows + (long long)b * D;
+    const bool add = !v.partial && a.accumulate;
 #pragma unroll
     for (int i = 0; i < NP; ++i)
       if (L.has(i)) {
         int e1, e2;
         L.element(i, e1, e2);
-        gsum[warp * D + e1] = sum[i];
-        gsum[warp * D + e2] = sum[NP + i];
+        row[e1] = add ? row[e1] + sum[i] : sum[i];
+        row[e2] = add ? row[e2] + sum[NP + i] : sum[NP + i];
       }
-  }
-  __syncthreads();
-  for (int d = threadIdx.x; d < D; d += kQkThreads) {
-    float s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kQkThreads / 32; ++w) s += gsum[w * D + d];
-    if (a.partial) {
-      a.partial[(((long long)b * a.n_chunks + blockIdx.x) * 2 + kind) * D + d] = s;
-    } else {
-      float* o = v.rows + (long long)b * D + d;
-      *o = a.accumulate ? *o + s : s;
-    }
   }
 }
 
-// rows[b][d] (+)= sum over the chunks, in order.  One block per (example, kind); 256 / 32 chunk strands per 32 columns.
-__global__ void __launch_bounds__(256)
-k_qknorm_rows(const float* __restrict__ partial, int n_chunks, int D, float* __restrict__ rows_q, float* __restrict__ rows_k,
-              int add) {
-  __shared__ float part[8][32];
-  const int b = blockIdx.x, kind = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float* rows = kind ? rows_k : rows_q;
-  if (!rows) return;
-  const int d = blockIdx.y * 32 + lane;
+// rows[b][d] (+)= sum over an example's partial rows.  A block owns 32 columns of one example; its warps take every
+// (number of warps)-th partial row and their sums are added in warp order.
+struct RowSums { const float* partial[2]; float* rows[2]; int parts[2]; };
+__global__ void __launch_bounds__(1024)
+k_qknorm_rows(const RowSums R, int D, int add) {
+  __shared__ float part[32][32];
+  const int b = blockIdx.x, kind = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if (!R.partial[kind]) return;
+  const int d = blockIdx.y * 32 + lane, n = R.parts[kind];
+  const float* p = R.partial[kind] + (long long)b * n * D + d;
   float s = 0.0f;
   if (d < D) {
-#pragma unroll 4
-    for (int c = warp; c < n_chunks; c += 8) s += partial[(((long long)b * n_chunks + c) * 2 + kind) * D + d];
+#pragma unroll 8
+    for (int c = warp; c < n; c += warps) s += p[(long long)c * D];
   }
   part[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && d < D) {
     float t = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) t += part[w][lane];
-    float* o = rows + (long long)b * D + d;
+    for (int w = 0; w < warps; ++w) t += part[w][lane];
+    float* o = R.rows[kind] + (long long)b * D + d;
     *o = add ? *o + t : t;
   }
 }
@@ -491,7 +570,8 @@ static int check_qk(const dp_qknorm* p) {
   if (p->dtype != DP_F32 && p->dtype != DP_BF16) return DP_ERR_ARG;
   if ((p->dim & 1) || p->rot < 0 || (p->rot & 1) || p->rot > p->dim) return DP_ERR_ARG;
   if (!(p->eps >= 0.0) || !std::isfinite(p->eps)) return DP_ERR_ARG;
-  if (p->n_q > 65535 || p->n_k > 65535 || p->B > 65535 * 32 || p->T > 1 << 24) return DP_ERR_UNSUPPORTED;
+  if (p->n_q > 65535 || p->n_k > 65535 || p->T > 1 << 24 || (int64_t)p->B * p->T > 1 << 30)
+    return DP_ERR_UNSUPPORTED;
   if (p->dim > 2 * kMaxPairs) return DP_ERR_UNSUPPORTED;
   if (p->rot > 0 && !p->inv_freq) return DP_ERR_ARG;
   for (int j = 0; j < p->rot / 2; ++j)
@@ -515,15 +595,39 @@ static bool vec_heads(const dp_heads& x, int V) {
   return !misaligned(x.data, 16) && x.stride_b % V == 0 && x.stride_t % V == 0 && x.stride_h % V == 0;
 }
 
-// Tokens per block of the backward pass: a power of two, so that a block's items divide evenly among its groups, as large
-// as still gives enough blocks to fill the GPU several times over (the last round of blocks then costs little); at most 512
-// partial rows per example.
-static int grad_chunk(const dp_qknorm* p) {
-  const long long kinds = (p->n_q > 0) + (p->n_k > 0), per_token = (long long)p->B * kinds;
-  int chunk = kMaxChunk;
-  while (chunk > 1 && per_token * ceil_div(p->T, chunk) < 148ll * 2 * 6) chunk >>= 1;
-  while (ceil_div(p->T, chunk) > 512) chunk <<= 1;
-  return chunk;
+// Shares the heads out (see Share).  `warps` is about what the GPU holds at once.  While there is less than a head for each
+// of their groups, heads are spread as widely as they go; with more, a group takes up to kHeadsPerGroup heads of a token,
+// and tokens_per_unit grows until kWaves waves of units cover everything.
+static Share share_heads(const dp_qknorm* p, int heads, int group_log, long long warps, bool flat) {
+  Share s = {};
+  s.heads = heads;
+  if (heads == 0) return s;
+  const int groups_log = 5 - group_log;
+  const long long tokens = flat ? (long long)p->B * p->T : p->T, rows = (long long)p->B * p->T * (p->n_q + p->n_k);
+  s.heads_per_group = kHeadsPerGroup;
+  while (s.heads_per_group > 1 && (rows < ((warps * s.heads_per_group) << groups_log) || s.heads_per_group > heads)) s.heads_per_group >>= 1;
+  // neighbouring groups take neighbouring heads, as long as a token has them; the rest of the warp takes further tokens,
+  // as long as there are such
+  while (s.gh < groups_log && (s.heads_per_group << (s.gh + 1)) <= heads) ++s.gh;
+  s.gt = groups_log - s.gh;
+  while (s.gt > 0 && (1ll << (s.gt - 1)) >= tokens) { --s.gt; ++s.gh; }
+  s.heads_per_unit = s.heads_per_group << s.gh;
+  s.head_blocks = ceil_div(heads, s.heads_per_unit);
+  const long long strands = (flat ? 1 : p->B) * (long long)s.head_blocks;      // units per run of tokens
+  const long long share = warps * kWaves * heads / (p->n_q + p->n_k) + 1;
+  long long chunks = (share + strands / 2) / strands;
+  const long long most = (tokens + (1 << s.gt) - 1) >> s.gt;
+  chunks = chunks < 1 ? 1 : chunks > most ? most : chunks;
+  s.tokens_per_unit = (int)(((most + chunks - 1) / chunks) << s.gt);
+  s.chunks = (int)((tokens + s.tokens_per_unit - 1) / s.tokens_per_unit);
+  s.units = strands * s.chunks;
+  return s;
+}
+
+// Warps that an SM holds at once, as many as the registers of the kernels allow.
+constexpr long long kSms = 148;
+static Share backward_share(const dp_qknorm* p, int heads, int group_log) {
+  return share_heads(p, heads, group_log, kSms * kBwdWarps, false);
 }
 
 static void fill_args(const dp_qknorm* p, QkArgs* a, bool backward) {
@@ -535,18 +639,13 @@ static void fill_args(const dp_qknorm* p, QkArgs* a, bool backward) {
   a->T = p->T;
   a->pairs = p->dim / 2;
   a->rot_pairs = p->rot / 2;
-  a->v[0].heads = p->n_q;
-  a->v[1].heads = p->n_k;
   a->v[0].gain = p->gain_q;
   a->v[1].gain = p->gain_k;
-  // Heads that share one set of angles: up to kHeadsPerItem, fewer while the items would not fill the GPU's groups.
-  const long long rows = (long long)p->B * p->T * (p->n_q + p->n_k), fill = 148ll * 512 >> a->group_log;
-  int hp = kHeadsPerItem;
-  while (hp > 1 && rows < fill * hp) hp >>= 1;
-  a->heads_per_item = hp;
-  for (int k = 0; k < 2; ++k) a->v[k].slices = ceil_div(a->v[k].heads, hp);
-  a->chunk = backward ? grad_chunk(p) : 0;
-  a->n_chunks = backward ? ceil_div(p->T, a->chunk) : 0;
+  for (int k = 0; k < 2; ++k) {
+    const int heads = k ? p->n_k : p->n_q;
+    a->v[k].share = backward ? backward_share(p, heads, a->group_log)
+                             : share_heads(p, heads, a->group_log, kSms * kFwdWarps, true);
+  }
   // inv_freq / (2 pi) modulo one turn, as a 64-bit fraction (x87 arithmetic: 64 bits of mantissa)
   const long double two_pi = 6.283185307179586476925286766559005768L;
   for (int j = 0; j < p->rot / 2; ++j) {
@@ -557,40 +656,38 @@ static void fill_args(const dp_qknorm* p, QkArgs* a, bool backward) {
   }
 }
 
-// Calls fn.template run<T, NP, VEC, INTER>() for the form that the sizes and alignments allow.
+// Calls fn.template run<T, NP, VEC, INTER, GL>() for the form that the sizes and alignments allow.  The lanes per head are a
+// constant of the kernel at the usual widths (64 to 256 in bf16, 32 to 128 in fp32), where the sums over them unroll.
+template <typename T, bool INTER, typename F>
+static cudaError_t pick_form(const QkArgs& a, bool vec, F fn) {
+  constexpr int V = 16 / sizeof(T);
+  if (vec) {
+    if (a.group_log == 2) return fn.template run<T, V, true, INTER, 2>();
+    if (a.group_log == 3) return fn.template run<T, V, true, INTER, 3>();
+    if (a.group_log == 4) return fn.template run<T, V, true, INTER, 4>();
+    return fn.template run<T, V, true, INTER, -1>();
+  }
+  const int np = ceil_div(a.pairs, 32);
+  if (np <= 1) return fn.template run<T, 1, false, INTER, 5>();
+  if (np <= 2) return fn.template run<T, 2, false, INTER, 5>();
+  if (np <= 4) return fn.template run<T, 4, false, INTER, 5>();
+  return fn.template run<T, 8, false, INTER, 5>();
+}
 template <typename T, typename F>
 static cudaError_t pick(const QkArgs& a, bool vec, bool inter, F fn) {
-  constexpr int V = 16 / sizeof(T);
-  if (vec) return inter ? fn.template run<T, V, true, true>() : fn.template run<T, V, true, false>();
-  const int np = ceil_div(a.pairs, 32);
-  if (np <= 1) return inter ? fn.template run<T, 1, false, true>() : fn.template run<T, 1, false, false>();
-  if (np <= 2) return inter ? fn.template run<T, 2, false, true>() : fn.template run<T, 2, false, false>();
-  if (np <= 4) return inter ? fn.template run<T, 4, false, true>() : fn.template run<T, 4, false, false>();
-  return inter ? fn.template run<T, 8, false, true>() : fn.template run<T, 8, false, false>();
+  return inter ? pick_form<T, true>(a, vec, fn) : pick_form<T, false>(a, vec, fn);
 }
 
-struct Forward {
+template <bool BACKWARD>
+struct Launch {
   const QkArgs& a;
   cudaStream_t s;
-  template <typename T, int NP, bool VEC, bool INTER>
+  template <typename T, int NP, bool VEC, bool INTER, int GL>
   cudaError_t run() const {
-    const long long items = (long long)a.B * a.T * (a.v[0].slices + a.v[1].slices);
-    const int per = kQkThreads >> a.group_log;
-    const long long blocks = (items + per - 1) / per;
-    if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-    k_qknorm<T, NP, VEC, INTER><<<(unsigned)blocks, kQkThreads, 0, s>>>(a);
-    return counted(1);
-  }
-};
-
-struct Backward {
-  const QkArgs& a;
-  cudaStream_t s;
-  template <typename T, int NP, bool VEC, bool INTER>
-  cudaError_t run() const {
-    const size_t smem = (size_t)(kQkThreads / 32) * 2 * a.pairs * sizeof(float);
-    const dim3 grid(a.n_chunks, a.B, 2);
-    k_qknorm_grad<T, NP, VEC, INTER><<<grid, kQkThreads, smem, s>>>(a);
+    const long long units = a.v[0].share.units + a.v[1].share.units;
+    if (units > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    if constexpr (BACKWARD) k_qknorm_grad<T, NP, VEC, INTER, GL><<<(unsigned)units, 32, 0, s>>>(a);
+    else k_qknorm<T, NP, VEC, INTER, GL><<<(unsigned)units, 32, 0, s>>>(a);
     return counted(1);
   }
 };
@@ -631,16 +728,30 @@ int dp_qknorm_rope(const dp_qknorm* p, const dp_heads* q, const dp_heads* k, con
   }
   a.group_log = group_log(p->dim / 2, vec, V);
   fill_args(p, &a, false);
-  const Forward f{a, static_cast<cudaStream_t>(cuda_stream)};
+  const Launch<false> f{a, static_cast<cudaStream_t>(cuda_stream)};
   const bool inter = p->interleaved != 0;
   const cudaError_t e = p->dtype == DP_F32 ? pick<float>(a, vec, inter, f) : pick<__nv_bfloat16>(a, vec, inter, f);
   return e == cudaSuccess ? DP_OK : DP_ERR_CUDA;
 }
 
+// Partial rows of both kinds, for a given lane grouping.
+static size_t partial_bytes(const dp_qknorm* p, int glog, size_t* of_queries) {
+  size_t n[2];
+  for (int k = 0; k < 2; ++k) {
+    const Share s = backward_share(p, k ? p->n_k : p->n_q, glog);
+    n[k] = s.units > p->B ? (size_t)s.units * p->dim * sizeof(float) : 0;
+  }
+  if (of_queries) *of_queries = n[0];
+  return n[0] + n[1];
+}
+
 size_t dp_qknorm_workspace_bytes(const dp_qknorm* p) {
   if (check_qk(p) != DP_OK) return 0;
-  const size_t chunks = (size_t)ceil_div(p->T, grad_chunk(p));
-  return chunks > 1 ? chunks * (size_t)p->B * 2 * (size_t)p->dim * sizeof(float) : 0;
+  // the grouping depends on the tensors' alignment, which is not known here: the larger of the two
+  const int V = p->dtype == DP_F32 ? 4 : 8;
+  const size_t one = partial_bytes(p, group_log(p->dim / 2, false, V), nullptr);
+  const size_t vec = vec_dims(p, V) ? partial_bytes(p, group_log(p->dim / 2, true, V), nullptr) : 0;
+  return one > vec ? one : vec;
 }
 
 int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_heads* k, const dp_heads* dout_q,
@@ -677,18 +788,30 @@ int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_head
   fill_args(p, &a, true);
   a.accumulate = accumulate_into ? 1 : 0;
   const bool want_rows = a.v[0].rows || a.v[1].rows;
-  if (a.n_chunks > 1 && want_rows) {
+  size_t of_queries = 0;
+  const size_t need = want_rows ? partial_bytes(p, a.group_log, &of_queries) : 0;
+  if (need) {
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < dp_qknorm_workspace_bytes(p)) return DP_ERR_WORKSPACE;
-    a.partial = static_cast<float*>(workspace);
+    for (int k = 0; k < 2; ++k)
+      if (a.v[k].share.units > p->B) a.v[k].partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + (k ? of_queries : 0));
   }
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const Backward f{a, s};
+  const Launch<true> f{a, s};
   const bool inter = p->interleaved != 0;
   const cudaError_t e = p->dtype == DP_F32 ? pick<float>(a, vec, inter, f) : pick<__nv_bfloat16>(a, vec, inter, f);
   if (e != cudaSuccess) return DP_ERR_CUDA;
-  if (a.partial) {
-    k_qknorm_rows<<<dim3(p->B, ceil_div(p->dim, 32), 2), 256, 0, s>>>(a.partial, a.n_chunks, p->dim, a.v[0].rows,
-                                                                      a.v[1].rows, a.accumulate);
+  if (need) {
+    RowSums R = {};
+    int most = 1;
+    for (int k = 0; k < 2; ++k) {
+      if (!a.v[k].partial || !a.v[k].rows) continue;
+      R.partial[k] = a.v[k].partial;
+      R.rows[k] = a.v[k].rows;
+      R.parts[k] = a.v[k].share.chunks * a.v[k].share.head_blocks;
+      if (R.parts[k] > most) most = R.parts[k];
+    }
+    const int warps = most <= 8 ? 4 : most <= 64 ? 8 : 32;     // a few loads per warp, all in flight together
+    k_qknorm_rows<<<dim3(p->B, ceil_div(p->dim, 32), 2), 32 * warps, 0, s>>>(R, p->dim, a.accumulate);
     if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
   }
   return DP_OK;
