@@ -104,18 +104,25 @@ k_relpos_bias(const TT* __restrict__ table, const __grid_constant__ Buckets bk, 
 }
 
 // ---------------------------------------------------------------------------------------------
-// Per-example gradient.  A group of LG lanes (a warp or a part of one) takes a unit: up to R rows of one (example, head)
-// times LG * V neighbouring columns, V columns a lane.  Walking down the rows, a diagonal moves one column to the right
-// per row: inside a lane that is another register of its V sums (renamed by unrolling the rows V at a time), at the
-// lane's right edge the sum is handed to the next lane, and the one that leaves the last lane is complete and goes to
-// shared memory.  That costs one add per element and one shuffle per V of them, with no atomic.  After the rows the
-// group sums its line of diagonals by buckets, in a fixed order.
+// Per-example gradient.  A block takes a tile of one (example, head), LG * V neighbouring columns wide; its groups of LG lanes
+// (a warp or a part of one) take strands of RG rows below one another, V columns a lane.  Walking down the rows, a diagonal
+// moves one column to the right per row: inside a lane that is another register of its V sums (renamed by unrolling the
+// rows), at the lane's right edge the sum is handed to the next lane, and the one that leaves the last lane is complete and
+// goes to the strand's line in shared memory.  That costs one add per element and one shuffle per V of them, with no atomic.
+// Then the warps add the strands' lines into one line of the tile's diagonals and sum that by buckets, each sum in a fixed
+// order.  A tile behind an example's lengths (or above the diagonal) only writes its zeros.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int V> struct Strip;
 template <> struct Strip<__nv_bfloat16, 8> {
   uint4 u;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcs(reinterpret_cast<const uint4*>(p)); }
   __device__ __forceinline__ void clear() { u = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void keep(int n) {          // the first n values; selected, so that the others may be NaN
+    u.x = n >= 2 ? u.x : n == 1 ? u.x & 0xffffu : 0u;
+    u.y = n >= 4 ? u.y : n == 3 ? u.y & 0xffffu : 0u;
+    u.z = n >= 6 ? u.z : n == 5 ? u.z & 0xffffu : 0u;
+    u.w = n >= 8 ? u.w : n == 7 ? u.w & 0xffffu : 0u;
+  }
   __device__ __forceinline__ float get(int j) const {
     const uint32_t w = j < 2 ? u.x : j < 4 ? u.y : j < 6 ? u.z : u.w;
     return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
@@ -125,123 +132,186 @@ template <> struct Strip<__nv_bfloat16, 2> {
   uint32_t u;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcs(reinterpret_cast<const unsigned int*>(p)); }
   __device__ __forceinline__ void clear() { u = 0u; }
+  __device__ __forceinline__ void keep(int n) { u = n >= 2 ? u : u & 0xffffu; }
   __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? u & 0xffff0000u : u << 16); }
 };
 template <> struct Strip<__nv_bfloat16, 1> {
   unsigned short u;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcs(reinterpret_cast<const unsigned short*>(p)); }
   __device__ __forceinline__ void clear() { u = 0; }
+  __device__ __forceinline__ void keep(int) {}
   __device__ __forceinline__ float get(int) const { return __uint_as_float((uint32_t)u << 16); }
 };
 template <> struct Strip<float, 4> {
   float4 u;
   __device__ __forceinline__ void load(const float* p) { u = __ldcs(reinterpret_cast<const float4*>(p)); }
   __device__ __forceinline__ void clear() { u = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void keep(int n) {
+    u.y = n >= 2 ? u.y : 0.f;
+    u.z = n >= 3 ? u.z : 0.f;
+    u.w = n >= 4 ? u.w : 0.f;
+  }
   __device__ __forceinline__ float get(int j) const { return j == 0 ? u.x : j == 1 ? u.y : j == 2 ? u.z : u.w; }
 };
 template <> struct Strip<float, 1> {
   float u;
   __device__ __forceinline__ void load(const float* p) { u = __ldcs(p); }
   __device__ __forceinline__ void clear() { u = 0.f; }
+  __device__ __forceinline__ void keep(int) {}
   __device__ __forceinline__ float get(int) const { return u; }
 };
 
-constexpr int kGradWarps = 8;
+// Measured (256 x 16 scores of 128 x 128; 64 x 16 of 512 x 512 padded at random; bf16, whole chain of calls):
+//   rows per strand at most  16: 41 / 69 us, 32: 37 / 57, 64: 37 / 58      threads at most  64: 37 / 65 us, 128: 37 / 57, 256: 37 / 58
+constexpr int kGradThreads = 128, kGradMaxRows = 5;   // threads per block at most; log2 of the rows per strand at most
 constexpr int kGradRowBlock = 8;                 // rows whose loads are issued together
 
 struct GradArgs {
   long long stride_b, stride_h, stride_q;
   int B, H, Tq, Tk, offset, causal;
-  int lg_log, R, n_ct, n_rt;                     // log2 of lanes per group, rows per unit, column and row units
-  long long units;
+  int rg_log, n_ct, tiles;                       // log2 of the rows per strand; tiles of a head, side by side and all
   int accumulate;
 };
 
-template <typename T, int V>
-__global__ void __launch_bounds__(32 * kGradWarps)
+template <typename T, int V, int LGL>
+__global__ void __launch_bounds__(kGradThreads)
 k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const __grid_constant__ GradArgs a,
               const int32_t* __restrict__ q_len, const int32_t* __restrict__ k_len, float* __restrict__ partial,
               float* __restrict__ rows) {
-  extern __shared__ float diag_smem[];
-  const int LG = 1 << a.lg_log, CW = LG * V;
+  extern __shared__ float grad_smem[];
+  constexpr int LG = 1 << LGL, CW = LG * V;
+  const int RG = 1 << a.rg_log, LINE = RG + CW;  // a strand's line: diagonals -RG .. CW - 1
   const int lane = threadIdx.x & 31, li = lane & (LG - 1);
-  const int group = threadIdx.x >> a.lg_log;     // within the block
-  const int groups = (32 * kGradWarps) >> a.lg_log;
-  float* buf = diag_smem + (long long)group * (a.R + CW);
-  const long long unit = (long long)blockIdx.x * groups + group;
-  const bool live = unit < a.units;
-  const int per_bh = a.n_ct * a.n_rt;
-  const long long bh = live ? unit / per_bh : 0;
-  const int u_in = live ? (int)(unit - bh * per_bh) : 0;
-  const int rt = u_in / a.n_ct, ct = u_in - rt * a.n_ct;
-  const int b = (int)(bh / a.H), h = (int)(bh - (long long)b * a.H);
+  const int gyi = threadIdx.x >> LGL, gy = blockDim.x >> LGL;
+  float* buf = grad_smem + gyi * LINE;
+  float* line = grad_smem + gy * LINE;           // the tile's: diagonals -(nr - 1) .. nc - 1
+  const unsigned unit = blockIdx.x, bh = unit / (unsigned)a.tiles, u_in = unit - bh * (unsigned)a.tiles;
+  const int rt = (int)(u_in / (unsigned)a.n_ct), ct = (int)u_in - rt * a.n_ct;
+  const int b = (int)(bh / (unsigned)a.H), h = (int)bh - b * a.H;
   const int q_end = q_len ? min(max(q_len[b], 0), a.Tq) : a.Tq;
   const int k_end = k_len ? min(max(k_len[b], 0), a.Tk) : a.Tk;
-  const int c0 = ct * CW, c = c0 + li * V;
-  int q0 = rt * a.R;
-  const int r_hi = min(q0 + a.R, q_end);
-  // a causal unit starts at the first row that sees its first column
-  if (a.causal) q0 = max(q0, c0 - a.offset);
-  int n = live && c0 < k_end ? max(r_hi - q0, 0) : 0;
-  const int valid = min(max(k_end - c, 0), V);   // of this lane's columns
+  const int nb = bk.both ? 2 * bk.half : bk.half;
+  const int R0 = rt * RG * gy, C0 = ct * CW;     // the tile's first row and column
+  const int nr = min(RG * gy, q_end - R0), nc = min(CW, k_end - C0);           // what counts of it
+  if (nr <= 0 || nc <= 0 || (a.causal && C0 > R0 + nr - 1 + a.offset)) {
+    for (int k = threadIdx.x; k < nb; k += blockDim.x) {
+      if (partial) partial[(long long)unit * nb + k] = 0.0f;
+      else if (!a.accumulate) rows[((long long)b * nb + k) * a.H + h] = 0.0f;
+    }
+    return;
+  }
+  // the buckets' first and last diagonals, as places in the tile's line
+  const int rel = C0 - R0 - a.offset - (nr - 1);           // relative position of line[0]
+  const int n_line = nr + nc - 1;
+  const int n_seen = a.causal ? min(n_line, 1 - rel) : n_line;      // causal: up to relative position 0
+  int2* ends = reinterpret_cast<int2*>(line + ((RG * gy + CW + 31) & ~31));
+  for (int k = threadIdx.x; k < nb; k += blockDim.x) {
+    int lo, hi;
+    bk.range(k, lo, hi);
+    ends[k] = make_int2(max(lo - rel, 0), min(hi - rel, n_seen - 1));
+  }
+  const int q0 = R0 + gyi * RG, c = C0 + li * V;
+  const int n = min(max(q_end - q0, 0), RG);     // rows of this strand
+  const int valid = min(max(k_end - c, 0), V);   // columns of this lane
+  // rows that this lane reads: [from, to); a causal lane starts where its first column is seen
+  const int to = valid > 0 ? n : 0, from = a.causal ? max(c - a.offset - q0, 0) : 0;
   const T* p = G + (long long)b * a.stride_b + (long long)h * a.stride_h + (long long)q0 * a.stride_q + c;
 
   float acc[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) acc[j] = 0.0f;
-  // the groups of a warp walk together: as many rounds as the longest of them
-  int rounds = (n + kGradRowBlock - 1) / kGradRowBlock;
-  rounds = __reduce_max_sync(0xffffffffu, rounds);
-  for (int t = 0; t < rounds; ++t) {
-    const int r0 = t * kGradRowBlock;
-    Strip<T, V> x[kGradRowBlock];
+  // the strands of a warp walk together: blocks of rows [skip, rounds)
+  const int rounds = (int)__reduce_max_sync(0xffffffffu, (unsigned)((n + kGradRowBlock - 1) / kGradRowBlock));
+  const int skip = min(rounds, (int)__reduce_min_sync(0xffffffffu, (unsigned)from / kGradRowBlock));
+  p += (long long)(skip * kGradRowBlock) * a.stride_q;
+  const unsigned span = (unsigned)max(to - from, 0);
+  const bool whole = __all_sync(0xffffffffu, valid == V);  // no lane of the warp is cut by the last key
+  // kGradRowBlock rows are in flight: a row's successor is fetched into its registers as soon as they are added up.  Where
+  // the whole warp's next rows count, that takes no conditions.
+  Strip<T, V> x[kGradRowBlock];
+  int row = skip * kGradRowBlock - from;
 #pragma unroll
-    for (int r = 0; r < kGradRowBlock; ++r) {
-      x[r].clear();
-      const bool seen = r0 + r < n && valid > 0 && (!a.causal || c <= q0 + r0 + r + a.offset);
-      if (seen) x[r].load(p + (long long)(r0 + r) * a.stride_q);
-    }
+  for (int r = 0; r < kGradRowBlock; ++r) {
+    x[r].clear();
+    if ((unsigned)(row + r) < span) x[r].load(p);
+    p += a.stride_q;
+  }
+  float* edge = buf + (CW - 1 - skip * kGradRowBlock + RG);
+  auto add_row = [&](const int r) {
 #pragma unroll
-    for (int r = 0; r < kGradRowBlock; ++r) {
+    for (int j = 0; j < V; ++j) acc[(j + kGradRowBlock * V - r) % V] += x[r].get(j);     // the register of column j's diagonal
+  };
+  auto hand_on = [&](const int r) {
+    const int s = (V - 1 + kGradRowBlock * V - r) % V;
+    const float out = acc[s];
+    const float in = __shfl_up_sync(0xffffffffu, out, 1, LG);
+    if (li == LG - 1) edge[-r] = out;
+    acc[s] = li == 0 ? 0.0f : in;
+  };
+  for (int t = skip; t < rounds; ++t) {
+    row += kGradRowBlock;
+    if (whole && __all_sync(0xffffffffu, row >= 0 && row + kGradRowBlock <= (int)span)) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int s = (j + kGradRowBlock * V - r) % V;       // the register that holds column j's diagonal in row r
-        acc[s] += j < valid ? x[r].get(j) : 0.0f;            // selected, never multiplied: a masked place may hold NaN
+      for (int r = 0; r < kGradRowBlock; ++r) {
+        add_row(r);
+        x[r].load(p);
+        p += a.stride_q;
+        hand_on(r);
       }
-      const int s = (V - 1 + kGradRowBlock * V - r) % V;
-      const float out = acc[s];
-      const float in = __shfl_up_sync(0xffffffffu, out, 1, LG);
-      if (li == LG - 1 && r0 + r < a.R) buf[CW - 1 - (r0 + r) + a.R] = out;
-      acc[s] = li == 0 ? 0.0f : in;
-    }
-  }
-  // buf[d + R]: diagonal d = (column - c0) - (row - q0), -walked <= d < CW.  (kGradRowBlock is a multiple of V.)
-  const int walked = rounds * kGradRowBlock;
+    } else {
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int d = li * V + j - walked;
-    if (d + a.R >= 0) buf[d + a.R] = acc[j];
+      for (int r = 0; r < kGradRowBlock; ++r) {
+        if (!whole) x[r].keep(valid);
+        add_row(r);
+        x[r].clear();
+        if ((unsigned)(row + r) < span) x[r].load(p);
+        p += a.stride_q;
+        hand_on(r);
+      }
+    }
+    edge -= kGradRowBlock;
   }
-  __syncwarp();
-  const int rel = c0 - q0 - a.offset;            // relative position of diagonal 0
-  const int d_lo = max(-walked, -a.R), d_hi = a.causal ? min(CW - 1, -rel) : CW - 1;
-  const int nb = bk.both ? 2 * bk.half : bk.half;
-  for (int k = 0; k < nb; ++k) {
-    int lo, hi;
-    const bool some = bk.range(k, lo, hi);
-    lo = max(lo - rel, d_lo);
-    hi = min(hi - rel, d_hi);
+  // buf[d + RG]: diagonal d = column - row, both from the strand's first; those in [-walked, CW - skipped) are there, the
+  // others of the line are 0.  (kGradRowBlock is a multiple of V.)
+  const int walked = rounds * kGradRowBlock, skipped = skip * kGradRowBlock;
+#pragma unroll
+  for (int j = 0; j < V; ++j) buf[li * V + j - walked + RG] = acc[j];
+  for (int i = li; i < RG - walked; i += LG) buf[i] = 0.0f;
+  for (int i = LINE - skipped + li; i < LINE; i += LG) buf[i] = 0.0f;
+  __syncthreads();
+  // The tile's line, 32 diagonals per warp at a time: the strands' lines added up, then inside the 32 every diagonal is
+  // summed with those before it that share its bucket, so that the last one of a bucket there holds their sum.
+  const int my_lo = lane < nb ? ends[lane].x : 0x7fffffff, my_hi = lane < nb ? ends[lane].y : -1;
+  for (int i0 = threadIdx.x & ~31; i0 < n_seen; i0 += blockDim.x) {
+    const int i = i0 + lane, d = i - (nr - 1);
+    // strand y has it as diagonal d + y RG, if that lies in [-RG, CW)
+    const int y0 = d < -RG ? (-d - 1) >> a.rg_log : 0, y1 = min(gy, d < CW ? ((CW - 1 - d) >> a.rg_log) + 1 : 0);
     float s = 0.0f;
-    if (some && n > 0)
-      for (int d = lo + li; d <= hi; d += LG) s += buf[d + a.R];
-    for (int o = LG >> 1; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o, LG);
-    if (live && li == 0) {
-      if (partial) {
-        partial[unit * nb + k] = s;
-      } else {
-        float* w = rows + ((long long)b * nb + k) * a.H + h;
-        *w = a.accumulate ? *w + s : s;
-      }
+    for (int y = y0; y < y1; ++y) s += grad_smem[y * (LINE + RG) + d + RG];
+    // where buckets begin among the 32
+    unsigned begins = __reduce_or_sync(0xffffffffu, my_lo <= my_hi && my_lo >= i0 && my_lo < i0 + 32 ? 1u << (my_lo - i0) : 0u);
+    for (int k = 32; k < nb; k += 32) {
+      const int2 e = k + lane < nb ? ends[k + lane] : make_int2(0, -1);
+      begins |= __reduce_or_sync(0xffffffffu, e.x <= e.y && e.x >= i0 && e.x < i0 + 32 ? 1u << (e.x - i0) : 0u);
+    }
+    const int head = 31 - __clz((int)(begins << (31 - lane) >> (31 - lane) | 1u));       // lane of this bucket's first here
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float other = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane - o >= head) s += other;
+    }
+    line[i] = s;                                 // the line has room for whole warps
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < nb; k += blockDim.x) {
+    const int lo = ends[k].x, hi = ends[k].y;
+    float s = 0.0f;
+    for (int i = lo; i <= hi; i = (i | 31) + 1) s += line[min(i | 31, hi)];
+    if (partial) {
+      partial[(long long)unit * nb + k] = s;
+    } else {
+      float* w = rows + ((long long)b * nb + k) * a.H + h;
+      *w = a.accumulate ? *w + s : s;
     }
   }
 }
@@ -342,22 +412,31 @@ static cudaError_t launch_bias(const dp_relpos& p, const Buckets& bk, const void
   return counted(1);
 }
 
-// How G is cut: V columns a lane, LG lanes a group, R rows a unit.  Many rows per unit amortise the sum over buckets;
-// few give every warp slot of the GPU a unit.
-struct GradPlan { int V, lg_log, R, n_ct, n_rt; long long units; };
+// How G is cut: V columns a lane, 2^lg lanes a strand, RG rows a strand, strands below one another in `threads` threads.
+struct GradPlan { int V, lg, rg_log, threads, n_ct, n_rt; long long units; size_t smem; };
 static GradPlan plan_grad(int B, const dp_relpos& p, int V) {
   GradPlan g;
   g.V = V;
-  int lanes = ceil_div(p.Tk, V);
-  g.lg_log = 2;
-  while (g.lg_log < 5 && (1 << g.lg_log) < lanes) ++g.lg_log;
-  const int CW = V << g.lg_log;
+  const int lanes = ceil_div(p.Tk, V);
+  g.lg = 3;
+  while (g.lg < 5 && (1 << g.lg) < lanes) ++g.lg;
+  const int CW = V << g.lg;
   g.n_ct = ceil_div(p.Tk, CW);
-  g.R = (512 << g.lg_log) >> 5;                  // bounds the shared memory of a warp's groups
-  const long long want = 148ll * 32 * (32 >> g.lg_log);
-  while (g.R > 32 && (long long)B * p.n_heads * g.n_ct * ceil_div(p.Tq, g.R) < want) g.R >>= 1;
-  g.n_rt = ceil_div(p.Tq, g.R);
+  // Long strands amortise a tile's sums over diagonals and buckets, few of them leave warps without work: halved while the
+  // GPU's warp slots would not be filled, or while a warp's strands reach far beyond the rows.
+  g.rg_log = kGradMaxRows;
+  while ((1 << g.rg_log) > kGradRowBlock &&
+         ((((long long)B * p.n_heads * g.n_ct * ceil_div(p.Tq, 1 << g.rg_log)) << g.lg) < 148ll * 32 * 32 ||
+          (1 << g.rg_log) * (32 >> g.lg) >= 2 * p.Tq))
+    --g.rg_log;
+  const int RG = 1 << g.rg_log;
+  // then as many strands as there are rows, in at most 4 warps
+  g.threads = 32;
+  while (g.threads < kGradThreads && (g.threads >> g.lg) * RG < p.Tq) g.threads <<= 1;
+  const int gy = g.threads >> g.lg;
+  g.n_rt = ceil_div(p.Tq, gy * RG);
   g.units = (long long)B * p.n_heads * g.n_ct * g.n_rt;
+  g.smem = ((size_t)gy * (RG + CW) + align_up((size_t)gy * RG + CW, 32)) * sizeof(float) + (size_t)p.num_buckets * sizeof(int2);
   return g;
 }
 
@@ -372,14 +451,13 @@ static int grad_vec(const void* G, int dtype, int Tk, long long sb, long long sh
 }
 
 template <typename T, int V>
-static cudaError_t launch_grad(const void* G, const Buckets& bk, const GradArgs& a, const int32_t* q_len,
+static cudaError_t launch_grad(const void* G, const Buckets& bk, const GradArgs& a, const GradPlan& g, const int32_t* q_len,
                                const int32_t* k_len, float* partial, float* rows, cudaStream_t s) {
-  const int groups = (32 * kGradWarps) >> a.lg_log;
-  const size_t smem = (size_t)groups * (a.R + (V << a.lg_log)) * sizeof(float);
-  const long long blocks = (a.units + groups - 1) / groups;
-  if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  k_relpos_grad<T, V><<<(unsigned)blocks, 32 * kGradWarps, smem, s>>>(static_cast<const T*>(G), bk, a, q_len, k_len,
-                                                                      partial, rows);
+  const T* p = static_cast<const T*>(G);
+  const unsigned n = (unsigned)g.units;
+  if (g.lg == 3) k_relpos_grad<T, V, 3><<<n, g.threads, g.smem, s>>>(p, bk, a, q_len, k_len, partial, rows);
+  else if (g.lg == 4) k_relpos_grad<T, V, 4><<<n, g.threads, g.smem, s>>>(p, bk, a, q_len, k_len, partial, rows);
+  else k_relpos_grad<T, V, 5><<<n, g.threads, g.smem, s>>>(p, bk, a, q_len, k_len, partial, rows);
   return counted(1);
 }
 
@@ -449,17 +527,17 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
       return DP_ERR_WORKSPACE;
     partial = static_cast<float*>(workspace);
   }
-  GradArgs a = {stride_b, stride_h, stride_q, B, p->n_heads, p->Tq, p->Tk, (int)p->offset, causal ? 1 : 0,
-                g.lg_log, g.R, g.n_ct, g.n_rt, g.units, accumulate_into ? 1 : 0};
+  const GradArgs a = {stride_b, stride_h, stride_q, B, p->n_heads, p->Tq, p->Tk, (int)p->offset, causal ? 1 : 0,
+                      g.rg_log, g.n_ct, g.n_ct * g.n_rt, accumulate_into ? 1 : 0};
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
   if (dtype == DP_F32)
-    e = V == 4 ? launch_grad<float, 4>(G, bk, a, q_len, k_len, partial, rows, s)
-               : launch_grad<float, 1>(G, bk, a, q_len, k_len, partial, rows, s);
+    e = V == 4 ? launch_grad<float, 4>(G, bk, a, g, q_len, k_len, partial, rows, s)
+               : launch_grad<float, 1>(G, bk, a, g, q_len, k_len, partial, rows, s);
   else
-    e = V == 8   ? launch_grad<__nv_bfloat16, 8>(G, bk, a, q_len, k_len, partial, rows, s)
-        : V == 2 ? launch_grad<__nv_bfloat16, 2>(G, bk, a, q_len, k_len, partial, rows, s)
-                 : launch_grad<__nv_bfloat16, 1>(G, bk, a, q_len, k_len, partial, rows, s);
+    e = V == 8   ? launch_grad<__nv_bfloat16, 8>(G, bk, a, g, q_len, k_len, partial, rows, s)
+        : V == 2 ? launch_grad<__nv_bfloat16, 2>(G, bk, a, g, q_len, k_len, partial, rows, s)
+                 : launch_grad<__nv_bfloat16, 1>(G, bk, a, g, q_len, k_len, partial, rows, s);
   if (e != cudaSuccess) return DP_ERR_CUDA;
   if (partial) {
     const long long n = (long long)B * p->n_heads * nb;
