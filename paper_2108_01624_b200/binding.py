@@ -149,8 +149,11 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream(stream=None) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if not torch.cuda.is_initialized():
+        torch.cuda.init()
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 @dataclass
@@ -455,30 +458,21 @@ def _workspace(device: int, workspace: Optional[torch.Tensor]):
     return workspace.data_ptr(), workspace.nbytes
 
 
-_Tensor = torch.Tensor
-
-
 class _TensorArrays:
     """HOST arrays of addresses and sizes of a list of dense tensors of one dtype on one device."""
 
     def __init__(self, tensors: Sequence[torch.Tensor]):
         first = tensors[0]
-        self.device, dtype = _device(first), first.dtype
-        if not all(map(_Tensor.is_contiguous, tensors)):
-            raise ValueError("contiguous tensor expected")
-        if any([t.dtype is not dtype for t in tensors]) or set(map(_Tensor.get_device, tensors)) != {self.device}:
-            raise ValueError("the tensors of a list share one dtype and one device")
-        self.dtype, self.n = _dtype(first), len(tensors)
-        self.addresses = array("Q", map(_Tensor.data_ptr, tensors))
-        self.sizes = array("q", map(_Tensor.numel, tensors))
-
-    @property
-    def ptrs(self):
-        return self.addresses.buffer_info()[0]
-
-    @property
-    def counts(self):
-        return self.sizes.buffer_info()[0]
+        device, dtype = _device(first), first.dtype
+        for t in tensors:
+            if t.dtype is not dtype or t.get_device() != device:
+                raise ValueError("the tensors of a list share one dtype and one device")
+            if not t.is_contiguous():
+                raise ValueError("contiguous tensor expected")
+        self.device, self.dtype, self.n = device, _dtype(first), len(tensors)
+        self.addresses = array("Q", [t.data_ptr() for t in tensors])
+        self.sizes = array("q", [t.numel() for t in tensors])
+        self.ptrs, self.counts = self.addresses.buffer_info()[0], self.sizes.buffer_info()[0]
 
 
 def dp_global_norm_workspace_bytes() -> int:
