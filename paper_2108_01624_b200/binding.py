@@ -1,13 +1,14 @@
 """ctypes binding of libdp_b200.so: the same entry points as include/dp.h, taking torch tensors.
 
 Argument marshalling only -- every step runs in the library's CUDA kernels.  There is no CPU or
-PyTorch fallback: if the shared library is missing or a call fails, an exception is raised.
+PyTorch fallback: if the shared library is missing or a call fails, an exception is raised.  The calls for small
+tensors marshal through a CPython module (_dp_tensors.so) instead of ctypes.
 """
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
-from array import array
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -398,81 +399,28 @@ def dp_selftest_wait_timeout(stream=None) -> None:
 
 
 # ---- global norm over many tensors, rows, relative position bias, query/key norms -------------------------------------
-# These calls serve small tensors too, where the host side of a call is most of its time, so the checks below are made of
-# the cheapest queries that a tensor answers, and words for an error are looked for only where a check failed.
-_DTYPES = {torch.float32: DP_F32, torch.bfloat16: DP_BF16}
-_F32, _F64, _I32 = torch.float32, torch.float64, torch.int32
-_current_device = torch._C._cuda_getDevice
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# These calls serve small tensors too, where the host side of a call is most of its time: the CPython module _dp_tensors
+# (csrc/dp_tensors.cpp) checks the tensors, fills the descriptors and calls the library's entry points.  It takes what the
+# functions below take, in their order, and returns the status; a tensor that does not fit raises ValueError.
+MODULE_PATH = os.path.join(_HERE, "_dp_tensors.so")
+_BOUND = ["dp_global_sqnorm", "dp_clip_by_global_norm", "dp_clip_adamw_step", "dp_rows_sqnorms", "dp_rows_clipped_accumulate",
+          "dp_relpos_bias", "dp_relpos_workspace_bytes", "dp_relpos_bias_grad", "dp_qknorm_rope",
+          "dp_qknorm_workspace_bytes", "dp_qknorm_rope_backward"]       # in the order of its bind()
+_module = None
 
 
-def _dtype(t: torch.Tensor) -> int:
-    try:
-        return _DTYPES[t.dtype]
-    except KeyError:
-        raise ValueError(f"fp32 or bf16 tensor expected, got {t.dtype}") from None
-
-
-def _device(t: torch.Tensor) -> int:
-    """Index of the device that a call's first tensor is on."""
-    if not t.is_cuda:
-        raise ValueError("device tensor expected")
-    return t.get_device()
-
-
-def _call(name: str, device: int, stream, *args) -> None:
-    """The named entry point with the stream behind its arguments.  A launch goes to the CURRENT device, so one on
-    tensors of another device makes that device current for the call."""
-    fn = getattr(_lib or lib(), name)
-    if device == _current_device():
-        rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
-    else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
-    if rc:
-        raise DpError(name, rc)
-
-
-def _on(device: int, dtype, t: Optional[torch.Tensor], what: str, shape=None, numel: int = -1):
-    """Address of an optional tensor after the checks that every argument gets: device, dtype, contiguity, size."""
-    if t is None:
-        return None
-    if (t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape)
-            and (numel < 0 or t.numel() == numel)):
-        return t.data_ptr()
-    if t.get_device() != device:
-        raise ValueError(f"{what}: on {t.device}, the other tensors are on cuda:{device}")
-    if t.dtype is not dtype:
-        raise ValueError(f"{what}: {dtype} expected, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous tensor expected")
-    raise ValueError(f"{what}: {f'shape {tuple(shape)}' if shape is not None else f'{numel} elements'} expected, "
-                     f"got {tuple(t.shape)}")
-
-
-def _workspace(device: int, workspace: Optional[torch.Tensor]):
-    if workspace is None:
-        return None, 0
-    if workspace.get_device() != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace: contiguous tensor on cuda:{device} expected")
-    return workspace.data_ptr(), workspace.nbytes
-
-
-class _TensorArrays:
-    """HOST arrays of addresses and sizes of a list of dense tensors of one dtype on one device."""
-
-    def __init__(self, tensors: Sequence[torch.Tensor]):
-        first = tensors[0]
-        device, dtype = _device(first), first.dtype
-        for t in tensors:
-            if t.dtype is not dtype or t.get_device() != device:
-                raise ValueError("the tensors of a list share one dtype and one device")
-            if not t.is_contiguous():
-                raise ValueError("contiguous tensor expected")
-        self.device, self.dtype, self.n = device, _dtype(first), len(tensors)
-        self.addresses = array("Q", [t.data_ptr() for t in tensors])
-        self.sizes = array("q", [t.numel() for t in tensors])
-        self.ptrs, self.counts = self.addresses.buffer_info()[0], self.sizes.buffer_info()[0]
+def _native():
+    global _module
+    if _module is None:
+        if not os.path.exists(MODULE_PATH):
+            raise ImportError(f"{MODULE_PATH} not found: run `python -m paper_2108_01624_b200.build` (needs nvcc and g++). "
+                              "There is no fallback implementation.")
+        spec = importlib.util.spec_from_file_location("_dp_tensors", MODULE_PATH)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        m.bind(*[C.cast(getattr(lib(), name), C.c_void_p).value for name in _BOUND])
+        _module = m
+    return _module
 
 
 def dp_global_norm_workspace_bytes() -> int:
@@ -482,14 +430,10 @@ def dp_global_norm_workspace_bytes() -> int:
 def dp_global_sqnorm(tensors: Sequence[torch.Tensor], sqsum: torch.Tensor, accumulate_into: bool = False,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """sqsum (float64, one element) = or += the sum of squares over all tensors of the list (one dtype, fp32 or bf16)."""
-    if len(tensors):
-        L = _TensorArrays(tensors)
-        device, args = L.device, (L.ptrs, L.counts, L.n, L.dtype)
-    else:
-        device, args = _device(sqsum), (None, None, 0, DP_F32)
-    ws_p, ws_n = _workspace(device, workspace)
-    _call("dp_global_sqnorm", device, stream, *args, 1 if accumulate_into else 0,
-          _on(device, _F64, sqsum, "sqsum", None, 1), ws_p, ws_n)
+    rc = (_module or _native()).global_sqnorm(tensors, sqsum, accumulate_into, workspace,
+                                              None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_global_sqnorm", rc)
     return sqsum
 
 
@@ -497,24 +441,19 @@ def dp_clip_by_global_norm(tensors: Sequence[torch.Tensor], outs: Optional[Seque
                            max_norm: float, norm_and_factor: Optional[torch.Tensor] = None, stream=None) -> None:
     """outs[k] = tensors[k] * min(1, max_norm / sqrt(sqsum)); outs=None scales in place.  norm_and_factor: optional
     float32 tensor with 2 elements that receives the norm and the factor."""
-    if len(tensors) == 0:
-        raise ValueError("at least one tensor expected")
-    L = _TensorArrays(tensors)
-    O = L if outs is None else _TensorArrays(outs)
-    if O is not L and (O.n != L.n or O.dtype != L.dtype or O.device != L.device or O.sizes != L.sizes):
-        raise ValueError("outputs must have their tensors' number, sizes, dtype and device")
-    _call("dp_clip_by_global_norm", L.device, stream, L.ptrs, O.ptrs, L.counts, L.n, L.dtype,
-          _on(L.device, _F64, sqsum, "sqsum", None, 1), max_norm,
-          _on(L.device, _F32, norm_and_factor, "norm_and_factor", None, 2))
+    rc = (_module or _native()).clip_by_global_norm(tensors, outs, sqsum, max_norm, norm_and_factor,
+                                                    None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_clip_by_global_norm", rc)
 
 
 def dp_clip_adamw_step(theta, m, v, g, zero_g, sqsum: torch.Tensor, max_norm: float, lr, beta1, beta2, xi, weight_decay,
                        t, stream=None) -> None:
     """dp_adamw_step on g * min(1, max_norm / sqrt(sqsum)); zero_g clears g in the same pass."""
-    device, n = _device(theta), theta.numel()
-    _call("dp_clip_adamw_step", device, stream, _on(device, _F32, theta, "theta"), _on(device, _F32, m, "m", None, n),
-          _on(device, _F32, v, "v", None, n), _on(device, _F32, g, "g", None, n), 1 if zero_g else 0, n,
-          _on(device, _F64, sqsum, "sqsum", None, 1), max_norm, lr, beta1, beta2, xi, weight_decay, t)
+    rc = (_module or _native()).clip_adamw_step(theta, m, v, g, zero_g, sqsum, max_norm, lr, beta1, beta2, xi, weight_decay,
+                                                t, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_clip_adamw_step", rc)
 
 
 class RowList:
@@ -523,33 +462,28 @@ class RowList:
 
     def __init__(self, pairs: Sequence[tuple]):
         self.pairs = list(pairs)
-        if not self.pairs:
-            raise ValueError("at least one tensor expected")
-        first = self.pairs[0][0]
-        self.device, self.B = _device(first), first.shape[0]
-        self.array = (dp_rows * len(self.pairs))()
-        for d, (grad, acc) in zip(self.array, self.pairs):
-            shape = grad.shape
-            if shape[0] != self.B:
-                raise ValueError("the tensors of a list share the number of examples")
-            d.grad = _on(self.device, _F32, grad, "per-example gradients")
-            d.width = grad.numel() // max(self.B, 1)
-            d.acc = _on(self.device, _F32, acc, "accumulator", shape[1:])
-        self.ptr = C.addressof(self.array)
+        self.native = (_module or _native()).rows_list(self.pairs)
+
+    @property
+    def B(self) -> int:
+        return self.native[1]
 
     def __len__(self):
         return len(self.pairs)
 
 
 def dp_rows_sqnorms(rows: RowList, sqnorm: torch.Tensor, accumulate_into: bool = False, stream=None) -> torch.Tensor:
-    _call("dp_rows_sqnorms", rows.device, stream, rows.ptr, len(rows.pairs), rows.B,
-          _on(rows.device, _F32, sqnorm, "sqnorm", None, rows.B), 1 if accumulate_into else 0)
+    rc = (_module or _native()).rows_sqnorms(rows.native, sqnorm, accumulate_into,
+                                             None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_rows_sqnorms", rc)
     return sqnorm
 
 
 def dp_rows_clipped_accumulate(rows: RowList, clip: torch.Tensor, stream=None) -> None:
-    _call("dp_rows_clipped_accumulate", rows.device, stream, rows.ptr, len(rows.pairs), rows.B,
-          _on(rows.device, _F32, clip, "clip", None, rows.B))
+    rc = (_module or _native()).rows_clipped_accumulate(rows.native, clip, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_rows_clipped_accumulate", rc)
 
 
 def dp_relpos_bucket_starts(num_buckets: int, max_distance: int, bidirectional: bool) -> List[int]:
@@ -566,26 +500,16 @@ def dp_relpos_bias(table: torch.Tensor, out: torch.Tensor, max_distance: int = 1
                    offset: int = 0, stream=None) -> torch.Tensor:
     """out[h, q, k] = table[bucket(k - q - offset), h]; table [num_buckets, heads], out [heads, Tq, Tk] with unit stride
     along the keys (fp32 or bf16 each)."""
-    device = _device(table)
-    nb, H = table.shape
-    if out.dim() != 3 or out.shape[0] != H or out.get_device() != device:
-        raise ValueError(f"out: [{H}, Tq, Tk] on cuda:{device} expected, got {tuple(out.shape)} on {out.device}")
-    _, Tq, Tk = out.shape
-    sh, sq, sk = out.stride()
-    if Tk > 1 and sk != 1:
-        raise ValueError("out: unit stride along the keys expected")
-    p = dp_relpos(nb, max_distance, 1 if bidirectional else 0, H, Tq, Tk, offset)
-    _call("dp_relpos_bias", device, stream, C.addressof(p), _on(device, table.dtype, table, "table"), _dtype(table),
-          out.data_ptr(), _dtype(out), sh if H > 1 else 0, sq if Tq > 1 else Tk)
+    rc = (_module or _native()).relpos_bias(table, out, max_distance, bidirectional, offset,
+                                            None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_relpos_bias", rc)
     return out
 
 
 def dp_relpos_workspace_bytes(G: torch.Tensor, num_buckets: int) -> int:
     """Scratch for dp_relpos_bias_grad over G [B, heads, Tq, Tk] (at least 256, so that it can be allocated)."""
-    B, H, Tq, Tk = G.shape
-    # the size depends on neither the distances nor the sides: one side and a distance that is always valid
-    p = dp_relpos(num_buckets, num_buckets + 1, 0, H, Tq, Tk, 0)
-    return max(256, (_lib or lib()).dp_relpos_workspace_bytes(C.addressof(p), B))
+    return (_module or _native()).relpos_workspace_bytes(G, num_buckets)
 
 
 def dp_relpos_bias_grad(G: torch.Tensor, rows: torch.Tensor, max_distance: int = 128, bidirectional: bool = True,
@@ -595,69 +519,16 @@ def dp_relpos_bias_grad(G: torch.Tensor, rows: torch.Tensor, max_distance: int =
     """rows[b, n, h] = or += sum over the (q, k) of bucket n of G[b, h, q, k]: every example's gradient of the table.
     G [B, heads, Tq, Tk] (fp32 or bf16) with unit stride along the keys, rows fp32 [B, num_buckets, heads]; q_len, k_len
     int32 [B]."""
-    device = _device(G)
-    if G.dim() != 4 or rows.dim() != 3:
-        raise ValueError("G [B, heads, Tq, Tk] and rows [B, num_buckets, heads] expected")
-    B, H, Tq, Tk = G.shape
-    nb = rows.shape[1]
-    sb, sh, sq, sk = G.stride()
-    if Tk > 1 and sk != 1:
-        raise ValueError("G: unit stride along the keys expected")
-    p = dp_relpos(nb, max_distance, 1 if bidirectional else 0, H, Tq, Tk, offset)
-    ws_p, ws_n = _workspace(device, workspace)
-    _call("dp_relpos_bias_grad", device, stream, C.addressof(p), B, 1 if causal else 0, G.data_ptr(), _dtype(G), sb, sh,
-          sq, _on(device, _I32, q_len, "q_len", (B,)), _on(device, _I32, k_len, "k_len", (B,)),
-          _on(device, _F32, rows, "rows", (B, nb, H)), 1 if accumulate_into else 0, ws_p, ws_n)
+    rc = (_module or _native()).relpos_bias_grad(G, rows, max_distance, bidirectional, offset, causal, q_len, k_len,
+                                                 accumulate_into, workspace, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_relpos_bias_grad", rc)
     return rows
 
 
 def rope_frequencies(rot: int, base: float = 10000.0) -> torch.Tensor:
     """inv_freq[j] = base^(-2j / rot), float64 on the host: radians per position of pair j."""
     return float(base) ** (-torch.arange(rot // 2, dtype=torch.float64) / max(rot // 2, 1))
-
-
-def _qknorm(q, k, gain_q=None, gain_k=None, eps=0.0, inv_freq=None, positions=None, lengths=None, interleaved=False):
-    """(device, descriptor) of a call over queries and keys [B, T, heads, dim], either of which may be None."""
-    x = k if q is None else q
-    if x is None or x.dim() != 4 or (q is not None and k is not None and k.dim() != 4):
-        raise ValueError("queries or keys [B, T, heads, dim] expected")
-    device = _device(x)
-    B, T, heads, dim = x.shape
-    n_q = 0 if q is None else heads
-    n_k = 0 if k is None else k.shape[2]
-    if n_q and n_k and k.shape != (B, T, n_k, dim):
-        raise ValueError("queries and keys share examples, tokens and width")
-    if inv_freq is None:
-        rot, freq = 0, None
-    else:
-        if inv_freq.dtype is not _F64 or inv_freq.is_cuda or not inv_freq.is_contiguous():
-            raise ValueError("inv_freq: contiguous float64 tensor on the host expected")
-        rot, freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
-    return device, dp_qknorm(_dtype(x), B, T, n_q, n_k, dim, rot, 1 if interleaved else 0, eps,
-                             _on(device, _F32, gain_q, "gain_q", (dim,)), _on(device, _F32, gain_k, "gain_k", (dim,)),
-                             _on(device, _I32, positions, "positions", (B, T)),
-                             _on(device, _I32, lengths, "lengths", (B,)), freq)
-
-
-def _heads(device: int, like: Optional[torch.Tensor], what: str, *tensors):
-    """dp_heads of tensors with the shape and dtype of `like`, one HOST array; its entries' addresses (None where there are
-    no such heads) and the array, which must live until the call returns."""
-    n = len(tensors)
-    if like is None:
-        return (None,) * n + (None,)
-    shape, dtype = like.shape, like.dtype
-    out = (dp_heads * n)()
-    for d, t in zip(out, tensors):
-        if t is None:
-            raise ValueError(f"{what}: a tensor is missing")
-        if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
-            raise ValueError(f"{what}: {tuple(shape)} {dtype} on cuda:{device} expected, got {tuple(t.shape)} {t.dtype} on {t.device}")
-        d.data = t.data_ptr()
-        d.stride_b, d.stride_t, d.stride_h, unit = t.stride()
-        if unit != 1:
-            raise ValueError(f"{what}: unit stride along the width expected")
-    base = C.addressof(out)
-    return tuple(range(base, base + 32 * n, 32)) + (out,)
 
 
 def dp_qknorm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], out_q: Optional[torch.Tensor],
@@ -667,18 +538,15 @@ def dp_qknorm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], out_q: 
     """RMS norm per head with gain, then the position rotation.  q, k [B, T, heads, dim] (any strides, unit along dim),
     either None; gains fp32 [dim] or None; inv_freq float64 on the host (rope_frequencies), its length is rot / 2, None
     for no rotation; positions int32 [B, T], lengths int32 [B]."""
-    device, p = _qknorm(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
-    q_in, q_out, keep_q = _heads(device, q, "queries", q, out_q)
-    k_in, k_out, keep_k = _heads(device, k, "keys", k, out_k)
-    if q is not None and k is not None and k.dtype is not q.dtype:
-        raise ValueError("queries and keys share one dtype")
-    _call("dp_qknorm_rope", device, stream, C.addressof(p), q_in, k_in, q_out, k_out)
+    rc = (_module or _native()).qknorm_rope(q, k, out_q, out_k, gain_q, gain_k, eps, inv_freq, positions, lengths,
+                                            interleaved, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_qknorm_rope", rc)
 
 
 def dp_qknorm_workspace_bytes(q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> int:
     """Scratch for dp_qknorm_rope_backward (at least 256, so that it can be allocated)."""
-    _, p = _qknorm(q, k)
-    return max(256, (_lib or lib()).dp_qknorm_workspace_bytes(C.addressof(p)))
+    return (_module or _native()).qknorm_workspace_bytes(q, k)
 
 
 def dp_qknorm_rope_backward(q, k, dout_q, dout_k, dq, dk, gain_q: Optional[torch.Tensor], gain_k: Optional[torch.Tensor],
@@ -688,15 +556,8 @@ def dp_qknorm_rope_backward(q, k, dout_q, dout_k, dq, dk, gain_q: Optional[torch
                             accumulate_into: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """dq, dk and every example's gradients of the gains (rows_q, rows_k fp32 [B, dim], or None) from the inputs of
     dp_qknorm_rope and the gradients of its outputs."""
-    device, p = _qknorm(q, k, gain_q, gain_k, eps, inv_freq, positions, lengths, interleaved)
-    if (q is None and rows_q is not None) or (k is None and rows_k is not None):
-        raise ValueError("gradients of a gain need the heads that it scales")
-    if q is not None and k is not None and k.dtype is not q.dtype:
-        raise ValueError("queries and keys share one dtype")
-    q_in, q_dout, q_out, keep_q = _heads(device, q, "queries", q, dout_q, dq)
-    k_in, k_dout, k_out, keep_k = _heads(device, k, "keys", k, dout_k, dk)
-    ws_p, ws_n = _workspace(device, workspace)
-    shape = (p.B, p.dim)
-    _call("dp_qknorm_rope_backward", device, stream, C.addressof(p), q_in, k_in, q_dout, k_dout, q_out, k_out,
-          _on(device, _F32, rows_q, "rows_q", shape), _on(device, _F32, rows_k, "rows_k", shape),
-          1 if accumulate_into else 0, ws_p, ws_n)
+    rc = (_module or _native()).qknorm_rope_backward(q, k, dout_q, dout_k, dq, dk, gain_q, gain_k, rows_q, rows_k, eps,
+                                                     inv_freq, positions, lengths, interleaved, accumulate_into, workspace,
+                                                     None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_qknorm_rope_backward", rc)

@@ -1,4 +1,4 @@
-"""Builds libdp_b200.so (sm_100a) in-tree with nvcc.  `python -m paper_2108_01624_b200.build`."""
+"""Builds libdp_b200.so (sm_100a, nvcc) and the CPython module _dp_tensors.so (g++) in-tree.  `python -m paper_2108_01624_b200.build`."""
 from __future__ import annotations
 
 import os
@@ -8,6 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdp_b200.so")
+MODULE = os.path.join(HERE, "_dp_tensors.so")          # CPython module: torch tensors into the C ABI
 SOURCES = ["dp_api.cu", "dp_stream.cu", "dp_generic.cu", "dp_umma.cu", "dp_noalloc.cu",
            "dp_clip.cu", "dp_rows.cu", "dp_relpos.cu", "dp_qknorm.cu"]
 
@@ -20,9 +21,9 @@ def _nvcc() -> str:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(MODULE):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(MODULE))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "dp.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -43,7 +44,28 @@ def build(force: bool = False, verbose: bool = False, defines=(), out: str = LIB
         raise RuntimeError("nvcc failed:\n" + proc.stdout + proc.stderr)
     if verbose:
         print(proc.stderr)
+    if out == LIB:
+        build_module()
     return out
+
+
+def build_module() -> str:
+    """The CPython module, host code only, against the installed torch's headers."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(os.path.abspath(torch.__file__))
+    cuda = os.path.dirname(os.path.dirname(os.path.abspath(_nvcc()))) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"),
+           os.path.join(CSRC, "dp_tensors.cpp"), "-o", MODULE, "-L", os.path.join(base, "lib"),
+           "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{os.path.join(base, 'lib')}"]
+    proc = subprocess.run(cmd, capture_output=True, text=True)
+    if proc.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + proc.stdout + proc.stderr)
+    return MODULE
 
 
 if __name__ == "__main__":

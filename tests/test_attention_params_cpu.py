@@ -178,3 +178,26 @@ def test_rope_frequencies():
     assert f.dtype == torch.float64
     torch.testing.assert_close(f, torch.tensor([1.0, 0.1, 0.01, 0.001], dtype=torch.float64), rtol=1e-14, atol=0)
     assert b.rope_frequencies(0).numel() == 0
+
+
+def test_missing_module_fails_loudly(lib, monkeypatch, tmp_path):
+    monkeypatch.setattr(b, "_module", None)
+    monkeypatch.setattr(b, "MODULE_PATH", str(tmp_path / "nope.so"))
+    with pytest.raises(ImportError):
+        b.RowList([(torch.zeros(2, 3), None)])
+
+
+def test_module_refuses_what_is_no_tensor_or_number(lib):
+    with pytest.raises(ValueError):
+        b.dp_global_sqnorm([1.0], torch.zeros(1, dtype=torch.float64))
+    with pytest.raises(TypeError):
+        b.dp_global_sqnorm(3, torch.zeros(1, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        b.RowList([torch.zeros(2, 3)])
+    with pytest.raises(TypeError):
+        b._native().global_sqnorm(1)
+    with pytest.raises(TypeError):
+        b._native().bind(1)
+    with pytest.raises(ValueError):
+        b.dp_relpos_workspace_bytes(torch.zeros(2, 3), 32)
+    assert b.dp_relpos_workspace_bytes(torch.empty(2, 4, 512, 512), 32) >= 256          # host arithmetic: any device
