@@ -161,9 +161,17 @@ template <> struct Strip<float, 1> {
   __device__ __forceinline__ float get(int) const { return u; }
 };
 
+// (a, b) + (x, y), two fp32 additions in one instruction.
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
+  asm("{.reg .b64 s, t, u;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 t, {%2, %3};\n\tadd.rn.f32x2 u, s, t;\n\tmov.b64 {%0, %1}, u;}"
+      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+
 // Measured (256 x 16 scores of 128 x 128; 64 x 16 of 512 x 512 padded at random; bf16, whole chain of calls):
 //   rows per strand at most  16: 41 / 69 us, 32: 37 / 57, 64: 37 / 58      threads at most  64: 37 / 65 us, 128: 37 / 57, 256: 37 / 58
+//   blocks per SM  8: 37 / 58 us, 9: 35 / 56, 10: 47 / 91 (registers spill); without the two-wide additions 36 / 57
 constexpr int kGradThreads = 128, kGradMaxRows = 5;   // threads per block at most; log2 of the rows per strand at most
+constexpr int kGradBlocks = 9;
 constexpr int kGradRowBlock = 8;                 // rows whose loads are issued together
 
 struct GradArgs {
@@ -174,7 +182,7 @@ struct GradArgs {
 };
 
 template <typename T, int V, int LGL>
-__global__ void __launch_bounds__(kGradThreads)
+__global__ void __launch_bounds__(kGradThreads, kGradBlocks)
 k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const __grid_constant__ GradArgs a,
               const int32_t* __restrict__ q_len, const int32_t* __restrict__ k_len, float* __restrict__ partial,
               float* __restrict__ rows) {
@@ -238,8 +246,14 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
   }
   float* edge = buf + (CW - 1 - skip * kGradRowBlock + RG);
   auto add_row = [&](const int r) {
+    // register i has, in row r, the diagonal of column (i + r) mod V
+    if constexpr (V % 2 == 0) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[(j + kGradRowBlock * V - r) % V] += x[r].get(j);     // the register of column j's diagonal
+      for (int i = 0; i < V; i += 2) add2(acc[i], acc[i + 1], x[r].get((i + r) % V), x[r].get((i + 1 + r) % V));
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] += x[r].get((i + r) % V);
+    }
   };
   auto hand_on = [&](const int r) {
     const int s = (V - 1 + kGradRowBlock * V - r) % V;

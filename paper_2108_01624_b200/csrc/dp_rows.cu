@@ -38,9 +38,9 @@ k_rows_sqnorm(const __grid_constant__ RowSet R, float* __restrict__ sqnorm, int 
   }
 }
 
-// acc[j] += sum_i clip[i] * grad[i][j].  A block owns 32 columns of one tensor; its 16 warps take every 16th example
+// acc[j] += sum_i clip[i] * grad[i][j].  A block owns 32 columns of one tensor; its 32 warps take every 32nd example
 // each (8 loads in flight) and their sums are added in warp order.
-constexpr int kAccWarps = 16;
+constexpr int kAccWarps = 32;
 __global__ void __launch_bounds__(32 * kAccWarps)
 k_rows_accum(const __grid_constant__ RowSet R, int B, const float* __restrict__ clip) {
   __shared__ float part[kAccWarps][32];
