@@ -16,7 +16,8 @@
  *     the default stream).  They do not synchronise the host, except dp_poll_status.
  *   - The library allocates no device memory.  Kernels that need scratch take it from the
  *     caller's `workspace` (size from dp_workspace_bytes, 256-byte aligned).  The contents
- *     of the workspace carry no meaning between calls.
+ *     of the workspace carry no meaning between calls.  Calls that may overlap on the GPU (other
+ *     streams, graphs replayed side by side) need workspaces of their own.
  *   - Return value: DP_OK (0) or a negative dp_status.  Arguments are validated on the
  *     host before anything is launched; nothing throws, aborts or traps.
  *   - Matrices are row-major with the feature index fastest.  bf16 tensors must be
@@ -209,7 +210,8 @@ DP_API int dp_shared_table_cross_sqnorms(const int32_t* ids, const void* G_emb, 
  * The clip of an aggregated gradient: of the noised mean of Algorithm 1 (post-processing, so it costs no privacy), or
  * of the plain batch gradient in a non-private baseline.  (No counterpart in the paper.)
  * A list is two HOST arrays, device pointers and element counts, of one dtype (DP_F32 or DP_BF16); entries with count 0
- * are skipped and their pointers not looked at, and n_tensors may be 0.  Any element alignment is accepted.
+ * are skipped and their pointers not looked at, and n_tensors may be 0.  Any element alignment is accepted.  Entries do
+ * not overlap one another.
  * Lists of several dtypes, or the shards of several ranks, are combined with accumulate_into or by adding the sums. */
 
 /* Bytes of scratch for dp_global_sqnorm (fixed; 256-byte aligned). */

@@ -581,8 +581,10 @@ static int check_qk(const dp_qknorm* p) {
   return DP_OK;
 }
 
-static int check_heads(const dp_heads* x, size_t es) {
+// Copies x to *h after the checks; the stride of an extent of one, which nothing depends on, becomes 0.
+static int take_heads(const dp_qknorm* p, int heads, const dp_heads* x, size_t es, dp_heads* h) {
   if (!x || !x->data || x->stride_b < 0 || x->stride_t < 0 || x->stride_h < 0) return DP_ERR_ARG;
+  *h = {x->data, p->B > 1 ? x->stride_b : 0, p->T > 1 ? x->stride_t : 0, heads > 1 ? x->stride_h : 0};
   return misaligned(x->data, es) ? DP_ERR_ALIGN : DP_OK;
 }
 
@@ -719,12 +721,13 @@ int dp_qknorm_rope(const dp_qknorm* p, const dp_heads* q, const dp_heads* k, con
   bool vec = vec_dims(p, V);
   for (int i = 0; i < 2; ++i) {
     if (heads[i] == 0) continue;
-    if ((rc = check_heads(in[i], es)) != DP_OK || (rc = check_heads(out[i], es)) != DP_OK) return rc;
-    vec = vec && vec_heads(*in[i], V) && vec_heads(*out[i], V);
-    a.v[i].in = in[i]->data;
-    a.v[i].in_b = in[i]->stride_b; a.v[i].in_t = in[i]->stride_t; a.v[i].in_h = in[i]->stride_h;
-    a.v[i].out = out[i]->data;
-    a.v[i].out_b = out[i]->stride_b; a.v[i].out_t = out[i]->stride_t; a.v[i].out_h = out[i]->stride_h;
+    dp_heads x, y;
+    if ((rc = take_heads(p, heads[i], in[i], es, &x)) != DP_OK || (rc = take_heads(p, heads[i], out[i], es, &y)) != DP_OK)
+      return rc;
+    vec = vec && vec_heads(x, V) && vec_heads(y, V);
+    View& v = a.v[i];
+    v.in = x.data; v.in_b = x.stride_b; v.in_t = x.stride_t; v.in_h = x.stride_h;
+    v.out = y.data; v.out_b = y.stride_b; v.out_t = y.stride_t; v.out_h = y.stride_h;
   }
   a.group_log = group_log(p->dim / 2, vec, V);
   fill_args(p, &a, false);
@@ -759,7 +762,6 @@ int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_head
                             int accumulate_into, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   int rc = check_qk(p);
   if (rc != DP_OK) return rc;
-  if (p->B > 65535) return DP_ERR_UNSUPPORTED;
   const size_t es = p->dtype == DP_F32 ? 4 : 2;
   const int V = (int)(16 / es);
   const dp_heads* in[2] = {q, k};
@@ -771,18 +773,17 @@ int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_head
   bool vec = vec_dims(p, V);
   for (int i = 0; i < 2; ++i) {
     if (heads[i] == 0) continue;
-    if ((rc = check_heads(in[i], es)) != DP_OK || (rc = check_heads(dout[i], es)) != DP_OK ||
-        (rc = check_heads(out[i], es)) != DP_OK)
+    dp_heads x, g, y;
+    if ((rc = take_heads(p, heads[i], in[i], es, &x)) != DP_OK || (rc = take_heads(p, heads[i], dout[i], es, &g)) != DP_OK ||
+        (rc = take_heads(p, heads[i], out[i], es, &y)) != DP_OK)
       return rc;
     if (misaligned(rows[i], 4)) return DP_ERR_ALIGN;
-    vec = vec && vec_heads(*in[i], V) && vec_heads(*dout[i], V) && vec_heads(*out[i], V);
-    a.v[i].in = in[i]->data;
-    a.v[i].in_b = in[i]->stride_b; a.v[i].in_t = in[i]->stride_t; a.v[i].in_h = in[i]->stride_h;
-    a.v[i].dout = dout[i]->data;
-    a.v[i].dout_b = dout[i]->stride_b; a.v[i].dout_t = dout[i]->stride_t; a.v[i].dout_h = dout[i]->stride_h;
-    a.v[i].out = out[i]->data;
-    a.v[i].out_b = out[i]->stride_b; a.v[i].out_t = out[i]->stride_t; a.v[i].out_h = out[i]->stride_h;
-    a.v[i].rows = rows[i];
+    vec = vec && vec_heads(x, V) && vec_heads(g, V) && vec_heads(y, V);
+    View& v = a.v[i];
+    v.in = x.data; v.in_b = x.stride_b; v.in_t = x.stride_t; v.in_h = x.stride_h;
+    v.dout = g.data; v.dout_b = g.stride_b; v.dout_t = g.stride_t; v.dout_h = g.stride_h;
+    v.out = y.data; v.out_b = y.stride_b; v.out_t = y.stride_t; v.out_h = y.stride_h;
+    v.rows = rows[i];
   }
   a.group_log = group_log(p->dim / 2, vec, V);
   fill_args(p, &a, true);

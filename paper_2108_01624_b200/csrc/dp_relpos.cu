@@ -531,6 +531,9 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
   if (dtype != DP_F32 && dtype != DP_BF16) return DP_ERR_ARG;
   if (misaligned(G, dtype == DP_F32 ? 4 : 2) || misaligned(rows, 4) || misaligned(q_len, 4) || misaligned(k_len, 4))
     return DP_ERR_ALIGN;
+  if (B == 1) stride_b = 0;                      // the stride of an extent of one, which nothing depends on
+  if (p->n_heads == 1) stride_h = 0;
+  if (p->Tq == 1) stride_q = 0;
   const int V = grad_vec(G, dtype, p->Tk, stride_b, stride_h, stride_q);
   const GradPlan g = plan_grad(B, *p, V);
   const int nb = p->num_buckets, per_bh = g.n_ct * g.n_rt;
