@@ -112,53 +112,41 @@ k_relpos_bias(const TT* __restrict__ table, const __grid_constant__ Buckets bk, 
 // Then the warps add the strands' lines into one line of the tile's diagonals and sum that by buckets, each sum in a fixed
 // order.  A tile behind an example's lengths (or above the diagonal) only writes its zeros.
 // ---------------------------------------------------------------------------------------------
-template <typename T, int V> struct Strip;
-template <> struct Strip<__nv_bfloat16, 8> {
-  uint4 u;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcs(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void clear() { u = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ __forceinline__ void keep(int n) {          // the first n values; selected, so that the others may be NaN
-    u.x = n >= 2 ? u.x : n == 1 ? u.x & 0xffffu : 0u;
-    u.y = n >= 4 ? u.y : n == 3 ? u.y & 0xffffu : 0u;
-    u.z = n >= 6 ? u.z : n == 5 ? u.z & 0xffffu : 0u;
-    u.w = n >= 8 ? u.w : n == 7 ? u.w & 0xffffu : 0u;
+// V neighbouring values of a row, as they lie in memory: kWords 32-bit words.
+template <typename T, int V>
+struct Strip {
+  static constexpr int kWords = V * sizeof(T) >= 4 ? V * sizeof(T) / 4 : 1;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kWords == 4) {
+      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p));
+      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+    } else if constexpr (V * sizeof(T) == 4) {
+      w[0] = __ldcs(reinterpret_cast<const unsigned int*>(p));
+    } else {
+      w[0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0u;
+  }
+  // All bits of the first n values: what the mask takes away may be NaN.
+  __device__ __forceinline__ void first(int n) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = n > i ? ~0u : 0u;
+      else w[i] = n >= 2 * i + 2 ? ~0u : n == 2 * i + 1 ? 0xffffu : 0u;
+    }
+  }
+  __device__ __forceinline__ void keep(const Strip& mask) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] &= mask.w[i];
   }
   __device__ __forceinline__ float get(int j) const {
-    const uint32_t w = j < 2 ? u.x : j < 4 ? u.y : j < 6 ? u.z : u.w;
-    return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+    else return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
   }
-};
-template <> struct Strip<__nv_bfloat16, 2> {
-  uint32_t u;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcs(reinterpret_cast<const unsigned int*>(p)); }
-  __device__ __forceinline__ void clear() { u = 0u; }
-  __device__ __forceinline__ void keep(int n) { u = n >= 2 ? u : u & 0xffffu; }
-  __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? u & 0xffff0000u : u << 16); }
-};
-template <> struct Strip<__nv_bfloat16, 1> {
-  unsigned short u;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcs(reinterpret_cast<const unsigned short*>(p)); }
-  __device__ __forceinline__ void clear() { u = 0; }
-  __device__ __forceinline__ void keep(int) {}
-  __device__ __forceinline__ float get(int) const { return __uint_as_float((uint32_t)u << 16); }
-};
-template <> struct Strip<float, 4> {
-  float4 u;
-  __device__ __forceinline__ void load(const float* p) { u = __ldcs(reinterpret_cast<const float4*>(p)); }
-  __device__ __forceinline__ void clear() { u = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void keep(int n) {
-    u.y = n >= 2 ? u.y : 0.f;
-    u.z = n >= 3 ? u.z : 0.f;
-    u.w = n >= 4 ? u.w : 0.f;
-  }
-  __device__ __forceinline__ float get(int j) const { return j == 0 ? u.x : j == 1 ? u.y : j == 2 ? u.z : u.w; }
-};
-template <> struct Strip<float, 1> {
-  float u;
-  __device__ __forceinline__ void load(const float* p) { u = __ldcs(p); }
-  __device__ __forceinline__ void clear() { u = 0.f; }
-  __device__ __forceinline__ void keep(int) {}
-  __device__ __forceinline__ float get(int) const { return u; }
 };
 
 // (a, b) + (x, y), two fp32 additions in one instruction.
@@ -168,10 +156,11 @@ __device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
 }
 
 // Measured (256 x 16 scores of 128 x 128; 64 x 16 of 512 x 512 padded at random; bf16, whole chain of calls):
-//   rows per strand at most  16: 41 / 69 us, 32: 37 / 57, 64: 37 / 58      threads at most  64: 37 / 65 us, 128: 37 / 57, 256: 37 / 58
-//   blocks per SM  8: 37 / 58 us, 9: 35 / 56, 10: 47 / 91 (registers spill); without the two-wide additions 36 / 57
+//   (before the last steps)  rows per strand at most  16: 41 / 69 us, 32: 37 / 57, 64: 37 / 58
+//                            threads at most  64: 37 / 65 us, 128: 37 / 57, 256: 37 / 58
+//   blocks per SM  7: 38 / 56 us, 8: 37 / 53, 9: 37 / 53, 10: 47 / 91 (registers spill)
 constexpr int kGradThreads = 128, kGradMaxRows = 5;   // threads per block at most; log2 of the rows per strand at most
-constexpr int kGradBlocks = 9;
+constexpr int kGradBlocks = 8;
 constexpr int kGradRowBlock = 8;                 // rows whose loads are issued together
 
 struct GradArgs {
@@ -221,9 +210,10 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
   const int q0 = R0 + gyi * RG, c = C0 + li * V;
   const int n = min(max(q_end - q0, 0), RG);     // rows of this strand
   const int valid = min(max(k_end - c, 0), V);   // columns of this lane
-  // rows that this lane reads: [from, to); a causal lane starts where its first column is seen
-  const int to = valid > 0 ? n : 0, from = a.causal ? max(c - a.offset - q0, 0) : 0;
-  const T* p = G + (long long)b * a.stride_b + (long long)h * a.stride_h + (long long)q0 * a.stride_q + c;
+  // rows that this lane reads: [from, n); a causal lane starts where its first column is seen.  A lane behind the last key
+  // reads what the last lane before it reads, and masks it.
+  const int from = a.causal ? max(c - a.offset - q0, 0) : 0;
+  const T* p = G + (long long)b * a.stride_b + (long long)h * a.stride_h + (long long)q0 * a.stride_q + min(c, (k_end - 1) / V * V);
 
   float acc[V];
 #pragma unroll
@@ -232,10 +222,12 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
   const int rounds = (int)__reduce_max_sync(0xffffffffu, (unsigned)((n + kGradRowBlock - 1) / kGradRowBlock));
   const int skip = min(rounds, (int)__reduce_min_sync(0xffffffffu, (unsigned)from / kGradRowBlock));
   p += (long long)(skip * kGradRowBlock) * a.stride_q;
-  const unsigned span = (unsigned)max(to - from, 0);
-  const bool whole = __all_sync(0xffffffffu, valid == V);  // no lane of the warp is cut by the last key
+  const unsigned span = (unsigned)max(n - from, 0);
+  const bool whole = __all_sync(0xffffffffu, valid == V);  // no lane of the warp reaches beyond the last key
+  Strip<T, V> mask;
+  mask.first(valid);
   // kGradRowBlock rows are in flight: a row's successor is fetched into its registers as soon as they are added up.  Where
-  // the whole warp's next rows count, that takes no conditions.
+  // all the warp's next rows count, that takes no conditions.
   Strip<T, V> x[kGradRowBlock];
   int row = skip * kGradRowBlock - from;
 #pragma unroll
@@ -264,9 +256,19 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
   };
   for (int t = skip; t < rounds; ++t) {
     row += kGradRowBlock;
-    if (whole && __all_sync(0xffffffffu, row >= 0 && row + kGradRowBlock <= (int)span)) {
+    const bool full = __all_sync(0xffffffffu, row >= 0 && row + kGradRowBlock <= (int)span);
+    if (full && whole) {
 #pragma unroll
       for (int r = 0; r < kGradRowBlock; ++r) {
+        add_row(r);
+        x[r].load(p);
+        p += a.stride_q;
+        hand_on(r);
+      }
+    } else if (full) {
+#pragma unroll
+      for (int r = 0; r < kGradRowBlock; ++r) {
+        x[r].keep(mask);
         add_row(r);
         x[r].load(p);
         p += a.stride_q;
@@ -275,7 +277,7 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
     } else {
 #pragma unroll
       for (int r = 0; r < kGradRowBlock; ++r) {
-        if (!whole) x[r].keep(valid);
+        x[r].keep(mask);
         add_row(r);
         x[r].clear();
         if ((unsigned)(row + r) < span) x[r].load(p);
