@@ -7,6 +7,7 @@
 // every query reads at another place, and the gradient is a sum along diagonals first, over buckets last.  Both kernels
 // are bound by memory: the bias by writing [H][Tq][Tk], the gradient by reading G once.
 #include <cstring>
+#include <type_traits>
 
 #include "dp_internal.h"
 
@@ -112,40 +113,88 @@ k_relpos_bias(const TT* __restrict__ table, const __grid_constant__ Buckets bk, 
 // Then the warps add the strands' lines into one line of the tile's diagonals and sum that by buckets, each sum in a fixed
 // order.  A tile behind an example's lengths (or above the diagonal) only writes its zeros.
 // ---------------------------------------------------------------------------------------------
-// V neighbouring values of a row, as they lie in memory: kWords 32-bit words.
-template <typename T, int V>
+// 16 bytes of neighbouring values of a row.
+template <typename T>
 struct Strip {
-  static constexpr int kWords = V * sizeof(T) >= 4 ? V * sizeof(T) / 4 : 1;
-  uint32_t w[kWords];
+  static constexpr int V = 16 / sizeof(T);
+  uint32_t w[4];
   __device__ __forceinline__ void load(const T* p) {
-    if constexpr (kWords == 4) {
-      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p));
-      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-    } else if constexpr (V * sizeof(T) == 4) {
-      w[0] = __ldcs(reinterpret_cast<const unsigned int*>(p));
-    } else {
-      w[0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
-    }
+    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p));
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
   }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = 0u;
-  }
+  __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
   // All bits of the first n values: what the mask takes away may be NaN.
   __device__ __forceinline__ void first(int n) {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if constexpr (sizeof(T) == 4) w[i] = n > i ? ~0u : 0u;
       else w[i] = n >= 2 * i + 2 ? ~0u : n == 2 * i + 1 ? 0xffffu : 0u;
     }
   }
   __device__ __forceinline__ void keep(const Strip& mask) {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] &= mask.w[i];
+    for (int i = 0; i < 4; ++i) w[i] &= mask.w[i];
   }
   __device__ __forceinline__ float get(int j) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
     else return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+  }
+};
+
+// The same where rows start anywhere: the two 16-byte words of memory that the values lie in.
+template <typename T>
+struct Wide {
+  uint32_t w[8];
+  static __device__ __forceinline__ const uint4* words(const T* p) {
+    return reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+  }
+  // Both words lie inside the scores, [lo, hi).  Only the first and last few values of the whole array ever fail this.
+  static __device__ __forceinline__ bool inside(const T* p, const T* lo, const T* hi) {
+    return reinterpret_cast<const T*>(words(p)) >= lo && reinterpret_cast<const T*>(words(p) + 2) <= hi;
+  }
+  __device__ __forceinline__ void load(const T* p) {
+    const uint4 u = __ldcs(words(p)), v = __ldcs(words(p) + 1);
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+    w[4] = v.x; w[5] = v.y; w[6] = v.z; w[7] = v.w;
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 0u;
+  }
+  __device__ __noinline__ static void gather(const T* p, const T* lo, const T* hi, uint32_t* out) {
+    const T* q = reinterpret_cast<const T*>(words(p));
+    for (int i = 0; i < 8; ++i) {
+      uint32_t u = 0u;
+      if constexpr (sizeof(T) == 4) {
+        if (q + i >= lo && q + i < hi) u = *reinterpret_cast<const uint32_t*>(q + i);
+      } else {
+        for (int k = 0; k < 2; ++k)
+          if (q + 2 * i + k >= lo && q + 2 * i + k < hi)
+            u |= (uint32_t)*reinterpret_cast<const unsigned short*>(q + 2 * i + k) << (16 * k);
+      }
+      out[i] = u;
+    }
+  }
+  // The strip that starts `s` values behind the first word's first.
+  __device__ __forceinline__ Strip<T> at(int s) const {
+    Strip<T> x;
+    if constexpr (sizeof(T) == 4) {
+      uint32_t t[5];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) t[i] = s & 2 ? w[i + 2] : w[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x.w[i] = s & 1 ? t[i + 1] : t[i];
+    } else {
+      uint32_t t[6], u[5];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) t[i] = s & 4 ? w[i + 2] : w[i];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) u[i] = s & 2 ? t[i + 1] : t[i];
+      const uint32_t pick = s & 1 ? 0x5432u : 0x3210u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x.w[i] = __byte_perm(u[i], u[i + 1], pick);
+    }
+    return x;
   }
 };
 
@@ -164,19 +213,20 @@ constexpr int kGradBlocks = 8;
 constexpr int kGradRowBlock = 8;                 // rows whose loads are issued together
 
 struct GradArgs {
-  long long stride_b, stride_h, stride_q;
+  long long stride_b, stride_h, stride_q, extent;          // extent: from the first score to behind the last, in elements
   int B, H, Tq, Tk, offset, causal;
   int rg_log, n_ct, tiles;                       // log2 of the rows per strand; tiles of a head, side by side and all
   int accumulate;
 };
 
-template <typename T, int V, int LGL>
+// SHIFT: the rows do not all start and end on 16-byte boundaries.
+template <typename T, int LGL, bool SHIFT>
 __global__ void __launch_bounds__(kGradThreads, kGradBlocks)
 k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const __grid_constant__ GradArgs a,
               const int32_t* __restrict__ q_len, const int32_t* __restrict__ k_len, float* __restrict__ partial,
               float* __restrict__ rows) {
   extern __shared__ float grad_smem[];
-  constexpr int LG = 1 << LGL, CW = LG * V;
+  constexpr int V = Strip<T>::V, LG = 1 << LGL, CW = LG * V;
   const int RG = 1 << a.rg_log, LINE = RG + CW;  // a strand's line: diagonals -RG .. CW - 1
   const int lane = threadIdx.x & 31, li = lane & (LG - 1);
   const int gyi = threadIdx.x >> LGL, gy = blockDim.x >> LGL;
@@ -224,28 +274,48 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
   p += (long long)(skip * kGradRowBlock) * a.stride_q;
   const unsigned span = (unsigned)max(n - from, 0);
   const bool whole = __all_sync(0xffffffffu, valid == V);  // no lane of the warp reaches beyond the last key
-  Strip<T, V> mask;
+  Strip<T> mask;
   mask.first(valid);
-  // kGradRowBlock rows are in flight: a row's successor is fetched into its registers as soon as they are added up.  Where
-  // all the warp's next rows count, that takes no conditions.
-  Strip<T, V> x[kGradRowBlock];
-  int row = skip * kGradRowBlock - from;
+  // kAhead rows are in flight: a later row is fetched into a row's registers as soon as that is added up.  Where all the
+  // warp's rows to be fetched count (and, shifted, lie well inside the scores), that takes no conditions.
+  constexpr int kAhead = SHIFT ? kGradRowBlock / 2 : kGradRowBlock;
+  std::conditional_t<SHIFT, Wide<T>, Strip<T>> x[kAhead];
+  const T *lo_end = G, *hi_end = G + a.extent;
+  int shift = SHIFT ? (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T)) : 0;       // of the row that is added next
+  const int shift_step = (int)(a.stride_q & (V - 1));
+  auto fetch = [&](const int r, bool counts) {
+    x[r % kAhead].clear();
+    if constexpr (SHIFT) {
+      if (counts && Wide<T>::inside(p, lo_end, hi_end)) {
+        x[r % kAhead].load(p);
+      } else if (counts) {
+        uint32_t t[8];
+        Wide<T>::gather(p, lo_end, hi_end, t);
 #pragma unroll
-  for (int r = 0; r < kGradRowBlock; ++r) {
-    x[r].clear();
-    if ((unsigned)(row + r) < span) x[r].load(p);
-    p += a.stride_q;
-  }
-  float* edge = buf + (CW - 1 - skip * kGradRowBlock + RG);
-  auto add_row = [&](const int r) {
-    // register i has, in row r, the diagonal of column (i + r) mod V
-    if constexpr (V % 2 == 0) {
-#pragma unroll
-      for (int i = 0; i < V; i += 2) add2(acc[i], acc[i + 1], x[r].get((i + r) % V), x[r].get((i + 1 + r) % V));
+        for (int i = 0; i < 8; ++i) x[r % kAhead].w[i] = t[i];
+      }
     } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) acc[i] += x[r].get((i + r) % V);
+      if (counts) x[r % kAhead].load(p);
     }
+    p += a.stride_q;
+  };
+  int row = skip * kGradRowBlock - from;         // the next row to be fetched, from the first that this lane reads
+#pragma unroll
+  for (int r = 0; r < kAhead; ++r) fetch(r, (unsigned)(row + r) < span);
+  row += kAhead;
+  float* edge = buf + (CW - 1 - skip * kGradRowBlock + RG);
+  auto add_row = [&](const int r, bool masked) {
+    Strip<T> y;
+    if constexpr (SHIFT) {
+      y = x[r % kAhead].at(shift);
+      shift = (shift + shift_step) & (V - 1);
+    } else {
+      y = x[r % kAhead];
+    }
+    if (masked) y.keep(mask);
+    // register i has, in row r, the diagonal of column (i + r) mod V
+#pragma unroll
+    for (int i = 0; i < V; i += 2) add2(acc[i], acc[i + 1], y.get((i + r) % V), y.get((i + 1 + r) % V));
   };
   auto hand_on = [&](const int r) {
     const int s = (V - 1 + kGradRowBlock * V - r) % V;
@@ -255,36 +325,34 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
     acc[s] = li == 0 ? 0.0f : in;
   };
   for (int t = skip; t < rounds; ++t) {
-    row += kGradRowBlock;
-    const bool full = __all_sync(0xffffffffu, row >= 0 && row + kGradRowBlock <= (int)span);
+    bool mine = row >= 0 && row + kGradRowBlock <= (int)span;
+    if (SHIFT) mine = mine && Wide<T>::inside(p, lo_end, hi_end) && Wide<T>::inside(p + (kGradRowBlock - 1) * a.stride_q, lo_end, hi_end);
+    const bool full = __all_sync(0xffffffffu, mine);
     if (full && whole) {
 #pragma unroll
       for (int r = 0; r < kGradRowBlock; ++r) {
-        add_row(r);
-        x[r].load(p);
+        add_row(r, false);
+        x[r % kAhead].load(p);
         p += a.stride_q;
         hand_on(r);
       }
     } else if (full) {
 #pragma unroll
       for (int r = 0; r < kGradRowBlock; ++r) {
-        x[r].keep(mask);
-        add_row(r);
-        x[r].load(p);
+        add_row(r, true);
+        x[r % kAhead].load(p);
         p += a.stride_q;
         hand_on(r);
       }
     } else {
 #pragma unroll
       for (int r = 0; r < kGradRowBlock; ++r) {
-        x[r].keep(mask);
-        add_row(r);
-        x[r].clear();
-        if ((unsigned)(row + r) < span) x[r].load(p);
-        p += a.stride_q;
+        add_row(r, true);
+        fetch(r, (unsigned)(row + r) < span);
         hand_on(r);
       }
     }
+    row += kGradRowBlock;
     edge -= kGradRowBlock;
   }
   // buf[d + RG]: diagonal d = column - row, both from the strand's first; those in [-walked, CW - skipped) are there, the
@@ -429,10 +497,9 @@ static cudaError_t launch_bias(const dp_relpos& p, const Buckets& bk, const void
 }
 
 // How G is cut: V columns a lane, 2^lg lanes a strand, RG rows a strand, strands below one another in `threads` threads.
-struct GradPlan { int V, lg, rg_log, threads, n_ct, n_rt; long long units; size_t smem; };
+struct GradPlan { int lg, rg_log, threads, n_ct, n_rt; long long units; size_t smem; };
 static GradPlan plan_grad(int B, const dp_relpos& p, int V) {
   GradPlan g;
-  g.V = V;
   const int lanes = ceil_div(p.Tk, V);
   g.lg = 3;
   while (g.lg < 5 && (1 << g.lg) < lanes) ++g.lg;
@@ -456,24 +523,23 @@ static GradPlan plan_grad(int B, const dp_relpos& p, int V) {
   return g;
 }
 
-// Columns per lane: 16 bytes of them where every row starts on a 16-byte boundary and ends on one, else 4, else one.
-static int grad_vec(const void* G, int dtype, int Tk, long long sb, long long sh, long long sq) {
-  const int es = dtype == DP_F32 ? 4 : 2;
-  for (int bytes : {16, 4}) {
-    const int V = bytes / es;
-    if (!misaligned(G, bytes) && Tk % V == 0 && sb % V == 0 && sh % V == 0 && sq % V == 0) return V;
-  }
-  return 1;
+template <typename T, int LGL>
+static void launch_grad_form(bool shift, const T* G, const Buckets& bk, const GradArgs& a, const GradPlan& g,
+                             const int32_t* q_len, const int32_t* k_len, float* partial, float* rows, cudaStream_t s) {
+  const unsigned n = (unsigned)g.units;
+  if (shift) k_relpos_grad<T, LGL, true><<<n, g.threads, g.smem, s>>>(G, bk, a, q_len, k_len, partial, rows);
+  else k_relpos_grad<T, LGL, false><<<n, g.threads, g.smem, s>>>(G, bk, a, q_len, k_len, partial, rows);
 }
 
-template <typename T, int V>
+template <typename T>
 static cudaError_t launch_grad(const void* G, const Buckets& bk, const GradArgs& a, const GradPlan& g, const int32_t* q_len,
                                const int32_t* k_len, float* partial, float* rows, cudaStream_t s) {
   const T* p = static_cast<const T*>(G);
-  const unsigned n = (unsigned)g.units;
-  if (g.lg == 3) k_relpos_grad<T, V, 3><<<n, g.threads, g.smem, s>>>(p, bk, a, q_len, k_len, partial, rows);
-  else if (g.lg == 4) k_relpos_grad<T, V, 4><<<n, g.threads, g.smem, s>>>(p, bk, a, q_len, k_len, partial, rows);
-  else k_relpos_grad<T, V, 5><<<n, g.threads, g.smem, s>>>(p, bk, a, q_len, k_len, partial, rows);
+  constexpr int V = Strip<T>::V;
+  const bool shift = misaligned(G, 16) || a.Tk % V || a.stride_b % V || a.stride_h % V || a.stride_q % V;
+  if (g.lg == 3) launch_grad_form<T, 3>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
+  else if (g.lg == 4) launch_grad_form<T, 4>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
+  else launch_grad_form<T, 5>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
   return counted(1);
 }
 
@@ -515,8 +581,8 @@ int dp_relpos_bias(const dp_relpos* p, const void* table, int table_dtype, void*
 size_t dp_relpos_workspace_bytes(const dp_relpos* p, int B) {
   Buckets bk;
   if (check_relpos(p, &bk) != DP_OK || B <= 0) return 0;
-  long long most = 0;                            // over the ways to cut G, which depend on its alignment
-  for (int V : {8, 4, 2, 1}) {
+  long long most = 0;                            // bf16 and fp32 are cut differently
+  for (int V : {8, 4}) {
     const GradPlan g = plan_grad(B, *p, V);
     if (g.units > most) most = g.units;
   }
@@ -536,8 +602,7 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
   if (B == 1) stride_b = 0;                      // the stride of an extent of one, which nothing depends on
   if (p->n_heads == 1) stride_h = 0;
   if (p->Tq == 1) stride_q = 0;
-  const int V = grad_vec(G, dtype, p->Tk, stride_b, stride_h, stride_q);
-  const GradPlan g = plan_grad(B, *p, V);
+  const GradPlan g = plan_grad(B, *p, dtype == DP_F32 ? 4 : 8);
   const int nb = p->num_buckets, per_bh = g.n_ct * g.n_rt;
   if (g.units > 0x7fffffffll || (long long)B * p->n_heads * nb > 0x7fffffffll * 128) return DP_ERR_UNSUPPORTED;
   float* partial = nullptr;
@@ -546,17 +611,13 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
       return DP_ERR_WORKSPACE;
     partial = static_cast<float*>(workspace);
   }
-  const GradArgs a = {stride_b, stride_h, stride_q, B, p->n_heads, p->Tq, p->Tk, (int)p->offset, causal ? 1 : 0,
+  const GradArgs a = {stride_b, stride_h, stride_q, (B - 1) * stride_b + (p->n_heads - 1) * stride_h + (p->Tq - 1) * stride_q + p->Tk,
+                      B, p->n_heads, p->Tq, p->Tk, (int)p->offset, causal ? 1 : 0,
                       g.rg_log, g.n_ct, g.n_ct * g.n_rt, accumulate_into ? 1 : 0};
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (dtype == DP_F32)
-    e = V == 4 ? launch_grad<float, 4>(G, bk, a, g, q_len, k_len, partial, rows, s)
-               : launch_grad<float, 1>(G, bk, a, g, q_len, k_len, partial, rows, s);
-  else
-    e = V == 8   ? launch_grad<__nv_bfloat16, 8>(G, bk, a, g, q_len, k_len, partial, rows, s)
-        : V == 2 ? launch_grad<__nv_bfloat16, 2>(G, bk, a, g, q_len, k_len, partial, rows, s)
-                 : launch_grad<__nv_bfloat16, 1>(G, bk, a, g, q_len, k_len, partial, rows, s);
+  if (dtype == DP_F32) e = launch_grad<float>(G, bk, a, g, q_len, k_len, partial, rows, s);
+  else e = launch_grad<__nv_bfloat16>(G, bk, a, g, q_len, k_len, partial, rows, s);
   if (e != cudaSuccess) return DP_ERR_CUDA;
   if (partial) {
     const long long n = (long long)B * p->n_heads * nb;

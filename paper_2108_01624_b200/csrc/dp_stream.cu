@@ -286,6 +286,21 @@ k_clip_adamw(float* __restrict__ theta, float* __restrict__ m, float* __restrict
       for (int u = 0; u < kClipAhead; ++u) {
         const long long k = (it - u * stride) * 4;
         if (k < 0) break;
+        if (VEC && k + 4 <= n) {
+          const float4 g4 = *reinterpret_cast<const float4*>(g + k);
+          float4 t4 = *reinterpret_cast<const float4*>(theta + k);
+          float4 m4 = *reinterpret_cast<const float4*>(m + k);
+          float4 v4 = *reinterpret_cast<const float4*>(v + k);
+          adam_update(t4.x, m4.x, v4.x, g4.x * f, aa);
+          adam_update(t4.y, m4.y, v4.y, g4.y * f, aa);
+          adam_update(t4.z, m4.z, v4.z, g4.z * f, aa);
+          adam_update(t4.w, m4.w, v4.w, g4.w * f, aa);
+          *reinterpret_cast<float4*>(theta + k) = t4;
+          *reinterpret_cast<float4*>(m + k) = m4;
+          *reinterpret_cast<float4*>(v + k) = v4;
+          if (zero_g) *reinterpret_cast<float4*>(g + k) = make_float4(0.f, 0.f, 0.f, 0.f);
+          continue;
+        }
         for (int l = 0; l < 4 && k + l < n; ++l) {
           float t1 = theta[k + l], m1 = m[k + l], v1 = v[k + l];
           adam_update(t1, m1, v1, g[k + l] * f, aa);
