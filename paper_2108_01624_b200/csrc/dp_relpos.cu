@@ -400,20 +400,26 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
   }
 }
 
-// rows[b][n][h] (+)= sum over the units of (b, h), in order.
-__global__ void __launch_bounds__(256)
-k_relpos_units(const float* __restrict__ partial, int B, int H, int nb, int units, float* __restrict__ rows, int add) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (long long)B * H * nb) return;
-  const int n = (int)(i % nb);                   // neighbours read neighbouring words
-  const long long bh = i / nb;
+// rows[b][n][h] (+)= sum over the tiles of (b, h).  A block owns one (b, h); its threads stand as strands x buckets, a strand
+// takes every (number of strands)-th tile and the strands are added in order.
+__global__ void __launch_bounds__(1024)
+k_relpos_units(const float* __restrict__ partial, int H, int nb, int units, float* __restrict__ rows, int add) {
+  __shared__ float part[1024];
+  const int strands = blockDim.x / nb, n = threadIdx.x % nb, strand = threadIdx.x / nb;
+  const long long bh = blockIdx.x, b = bh / H, h = bh - b * H;
   const float* p = partial + bh * units * nb + n;
   float s = 0.0f;
-#pragma unroll 4
-  for (int u = 0; u < units; ++u) s += p[(long long)u * nb];
-  const long long b = bh / H, h = bh - b * H;
-  float* w = rows + (b * nb + n) * H + h;
-  *w = add ? *w + s : s;
+  if (strand < strands) {
+#pragma unroll 8
+    for (int u = strand; u < units; u += strands) s += p[(long long)u * nb];
+  }
+  part[threadIdx.x] = s;
+  __syncthreads();
+  if (strand == 0) {
+    for (int k = 1; k < strands; ++k) s += part[k * nb + n];
+    float* w = rows + (b * nb + n) * H + h;
+    *w = add ? *w + s : s;
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -604,7 +610,7 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
   if (p->Tq == 1) stride_q = 0;
   const GradPlan g = plan_grad(B, *p, dtype == DP_F32 ? 4 : 8);
   const int nb = p->num_buckets, per_bh = g.n_ct * g.n_rt;
-  if (g.units > 0x7fffffffll || (long long)B * p->n_heads * nb > 0x7fffffffll * 128) return DP_ERR_UNSUPPORTED;
+  if (g.units > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
   float* partial = nullptr;
   if (per_bh > 1) {
     if (!workspace || misaligned(workspace, 256) || workspace_bytes < (size_t)g.units * nb * sizeof(float))
@@ -620,8 +626,10 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
   else e = launch_grad<__nv_bfloat16>(G, bk, a, g, q_len, k_len, partial, rows, s);
   if (e != cudaSuccess) return DP_ERR_CUDA;
   if (partial) {
-    const long long n = (long long)B * p->n_heads * nb;
-    k_relpos_units<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(partial, B, p->n_heads, nb, per_bh, rows, a.accumulate);
+    // enough strands that each has a handful of tiles, whose loads are all in flight
+    const int strands = per_bh <= 8 ? 1 : 1024 / nb < (per_bh + 7) / 8 ? 1024 / nb : (per_bh + 7) / 8;
+    const int threads = (strands * nb + 31) / 32 * 32;
+    k_relpos_units<<<B * p->n_heads, threads, 0, s>>>(partial, p->n_heads, nb, per_bh, rows, a.accumulate);
     if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
   }
   return DP_OK;
