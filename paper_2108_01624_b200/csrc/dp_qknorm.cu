@@ -94,32 +94,26 @@ struct Lane {
   }
   // A head in flight.  VEC: copied asynchronously into the lane's own 32 bytes of shared memory (slot[0], slot[32]: the
   // 16-byte words of a warp side by side), so that deep prefetch costs no registers; only the lane itself reads them, so its
-  // own wait is all the synchronisation there is.  Otherwise read directly when its turn comes.
+  // own wait is all the synchronisation there is.  Otherwise fetched into registers, one head ahead.  0 without `act`.
   struct VecRaw { uint4 u1, u2; };
   struct OneRaw { T x[2 * NP]; };
   using Raw = std::conditional_t<VEC, VecRaw, OneRaw>;
   __device__ __forceinline__ void issue(const T* x, bool act, uint4* slot) const {
-    if constexpr (VEC) {
-      const bool get = act && on;                // nothing is read otherwise, and the slot is filled with zeros
-      copy16(slot, x + o1, get);
-      copy16(slot + 32, x + o2, get);
-    }
+    const bool get = act && on;
+    copy16(slot, x + o1, get);
+    copy16(slot + 32, x + o2, get);
   }
-  __device__ __forceinline__ Raw take(const T* x, bool act, const uint4* slot) const {
+  __device__ __forceinline__ Raw take(const uint4* slot) const { return {slot[0], slot[32]}; }
+  __device__ __forceinline__ Raw fetch(const T* x, bool act) const {
     Raw r;
-    if constexpr (VEC) {
-      r.u1 = slot[0];
-      r.u2 = slot[32];
-    } else {
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        r.x[i] = r.x[NP + i] = zero1(x);
-        if (act && has(i)) {
-          int e1, e2;
-          places(i, e1, e2);
-          r.x[i] = x[e1];
-          r.x[NP + i] = x[e2];
-        }
+    for (int i = 0; i < NP; ++i) {
+      r.x[i] = r.x[NP + i] = zero1(x);
+      if (act && has(i)) {
+        int e1, e2;
+        places(i, e1, e2);
+        r.x[i] = x[e1];
+        r.x[NP + i] = x[e2];
       }
     }
     return r;
@@ -359,24 +353,24 @@ k_qknorm(const __grid_constant__ QkArgs a) {
   const long long in_step = hstep * v.in_h, out_step = hstep * v.out_h;
   const T* src = in;
   int aj = per, an = 0;                          // ahead: head of the token, step
+  typename Lane<T, NP, VEC, INTER>::Raw pending;
   auto issue = [&]() {
-    if (VEC) {
-      if (an < steps) {
-        if (aj == per) {
-          ahead.next(a);
-          src = in + ahead.b * v.in_b + ahead.t * v.in_t;
-          aj = 0;
-        }
-        L.issue(src, ahead.live && aj < mine, ring + (an & (kFwdStages - 1)) * 64);
-        src += in_step;
-        ++aj;
-        ++an;
+    if (an < steps) {
+      if (aj == per) {
+        ahead.next(a);
+        src = in + ahead.b * v.in_b + ahead.t * v.in_t;
+        aj = 0;
       }
-      copies_mark();
+      if constexpr (VEC) L.issue(src, ahead.live && aj < mine, ring + (an & (kFwdStages - 1)) * 64);
+      else pending = L.fetch(src, ahead.live && aj < mine);
+      src += in_step;
+      ++aj;
+      ++an;
     }
+    if (VEC) copies_mark();
   };
 #pragma unroll 1
-  for (int n = 0; n < kFwdStages - 1; ++n) issue();
+  for (int n = 0; n < (VEC ? kFwdStages - 1 : 1); ++n) issue();
   float gain[2 * NP];
   L.gains(v.gain, gain);
   uint2 turn[NP];
@@ -396,19 +390,22 @@ k_qknorm(const __grid_constant__ QkArgs a) {
       c2[i] = gain[NP + i] * cs;
       s2[i] = gain[i] * sn;
     }
-    const T* x = in + at.b * v.in_b + at.t * v.in_t;
     T* y = out + at.b * v.out_b + at.t * v.out_t;
 #pragma unroll 1
     for (int j = 0; j < per; ++j, ++n) {
-      issue();
-      if (VEC) copies_wait<kFwdStages - 1>();
       const bool act = at.live && j < mine;
       float f[2 * NP];
-      L.unpack(L.take(x, act, ring + (n & (kFwdStages - 1)) * 64), f);
+      if constexpr (VEC) {
+        issue();
+        copies_wait<kFwdStages - 1>();
+        L.unpack(L.take(ring + (n & (kFwdStages - 1)) * 64), f);
+      } else {
+        L.unpack(pending, f);
+        issue();
+      }
       scale(f, rsqrtf(group_sum<GL>(dot(f, f), group) * a.inv_dim + a.eps));
       turn_pairs<NP>(f, c1, s1n, c2, s2);
       if (act) L.write(y, f);
-      if (!VEC) x += in_step;
       y += out_step;
     }
   }
@@ -446,29 +443,33 @@ k_qknorm_grad(const __grid_constant__ QkArgs a) {
   const T* src = in;
   const T* gsrc = dout;
   int aj = per, an = 0;
+  typename Lane<T, NP, VEC, INTER>::Raw pending, gpending;
   auto issue = [&]() {
-    if (VEC) {
-      if (an < steps) {
-        if (aj == per) {
-          ahead.next(a);
-          src = in + ahead.t * v.in_t;
-          gsrc = dout + ahead.t * v.dout_t;
-          aj = 0;
-        }
+    if (an < steps) {
+      if (aj == per) {
+        ahead.next(a);
+        src = in + ahead.t * v.in_t;
+        gsrc = dout + ahead.t * v.dout_t;
+        aj = 0;
+      }
+      const bool act = ahead.live && aj < mine;
+      if constexpr (VEC) {
         uint4* slot = ring + (an & (kBwdStages - 1)) * 128;
-        const bool act = ahead.live && aj < mine;
         L.issue(src, act, slot);
         L.issue(gsrc, act, slot + 64);
-        src += in_step;
-        gsrc += dout_step;
-        ++aj;
-        ++an;
+      } else {
+        pending = L.fetch(src, act);
+        gpending = L.fetch(gsrc, act);
       }
-      copies_mark();
+      src += in_step;
+      gsrc += dout_step;
+      ++aj;
+      ++an;
     }
+    if (VEC) copies_mark();
   };
 #pragma unroll 1
-  for (int n = 0; n < kBwdStages - 1; ++n) issue();
+  for (int n = 0; n < (VEC ? kBwdStages - 1 : 1); ++n) issue();
   float gain[2 * NP], sum[2 * NP];
   L.gains(v.gain, gain);
 #pragma unroll
@@ -485,18 +486,22 @@ k_qknorm_grad(const __grid_constant__ QkArgs a) {
       angle<sizeof(T) == 4>(turn[i], pos, cs[i], sn[i]);
       snn[i] = -sn[i];
     }
-    const T* x = in + at.t * v.in_t;
-    const T* g = dout + at.t * v.dout_t;
     T* y = out + at.t * v.out_t;
 #pragma unroll 1
     for (int j = 0; j < per; ++j, ++n) {
-      issue();
-      if (VEC) copies_wait<kBwdStages - 1>();
       const bool act = at.live && j < mine;
-      const uint4* slot = ring + (n & (kBwdStages - 1)) * 128;
       float f[2 * NP], u[2 * NP];
-      L.unpack(L.take(x, act, slot), f);
-      L.unpack(L.take(g, act, slot + 64), u);
+      if constexpr (VEC) {
+        issue();
+        copies_wait<kBwdStages - 1>();
+        const uint4* slot = ring + (n & (kBwdStages - 1)) * 128;
+        L.unpack(L.take(slot), f);
+        L.unpack(L.take(slot + 64), u);
+      } else {
+        L.unpack(pending, f);
+        L.unpack(gpending, u);
+        issue();
+      }
       turn_pairs<NP>(u, cs, sn, cs, snn);
       const float square = group_sum<GL>(dot(f, f), group);
       // 0 for idle groups, which then add nothing even with eps = 0
@@ -512,7 +517,6 @@ k_qknorm_grad(const __grid_constant__ QkArgs a) {
 #pragma unroll
       for (int i = 0; i < 2 * NP; i += 2) put2(u, i, fma2(at2(f, i), make_float2(m, m), at2(u, i)));
       if (act) L.write(y, u);
-      if (!VEC) { x += in_step; g += dout_step; }
       y += out_step;
     }
   }
@@ -669,11 +673,7 @@ static cudaError_t pick_form(const QkArgs& a, bool vec, F fn) {
     if (a.group_log == 4) return fn.template run<T, V, true, INTER, 4>();
     return fn.template run<T, V, true, INTER, -1>();
   }
-  const int np = ceil_div(a.pairs, 32);
-  if (np <= 1) return fn.template run<T, 1, false, INTER, 5>();
-  if (np <= 2) return fn.template run<T, 2, false, INTER, 5>();
-  if (np <= 4) return fn.template run<T, 4, false, INTER, 5>();
-  return fn.template run<T, 8, false, INTER, 5>();
+  return a.pairs <= 4 * 32 ? fn.template run<T, 4, false, INTER, -1>() : fn.template run<T, 8, false, INTER, 5>();
 }
 template <typename T, typename F>
 static cudaError_t pick(const QkArgs& a, bool vec, bool inter, F fn) {
@@ -694,11 +694,11 @@ struct Launch {
   }
 };
 
-// Lanes per head.
+// Lanes per head: V pairs a lane in vectors, else 4, or 8 where 32 lanes of 4 do not hold a head.
 static int group_log(int pairs, bool vec, int V) {
-  if (!vec) return 5;
+  const int per = vec ? V : pairs <= 4 * 32 ? 4 : 8;
   int g = 0;
-  while ((V << g) < pairs) ++g;
+  while ((per << g) < pairs) ++g;
   return g;
 }
 
