@@ -5,6 +5,7 @@
 //
 // Work is cut into chunks of 32 KB that never cross a tensor, and block b takes the chunks b, b + grid, ...; every
 // block's sum is written to its own word and the words are added in one order, so a sum does not depend on timing.
+#include "dp_chain.cuh"
 #include "dp_clip.cuh"
 #include "dp_internal.h"
 
@@ -125,6 +126,8 @@ __global__ void __launch_bounds__(kNormThreads * TEAMS)
 k_list_sqsum(const __grid_constant__ TensorSet<N> S, double* __restrict__ partial, int add) {
   constexpr int V = Vec16<T>::kN;
   __shared__ double red[kNormThreads * TEAMS / 32];
+  wait_for_predecessor();
+  let_successor_in();
   const unsigned int chunks = S.chunk0[S.n];
   const int tid = threadIdx.x % kNormThreads;
   double sum = 0.0;
@@ -170,6 +173,8 @@ k_list_sqsum(const __grid_constant__ TensorSet<N> S, double* __restrict__ partia
 __global__ void __launch_bounds__(1024)
 k_partials_sum(const double* __restrict__ partial, int n, double* __restrict__ sqsum, int add) {
   __shared__ double red[32];
+  wait_for_predecessor();
+  let_successor_in();
   double a = 0.0;
   for (int i = threadIdx.x; i < n; i += blockDim.x) a += partial[i];
   const double t = block_sum(a, red);
@@ -184,6 +189,7 @@ k_list_scale(const __grid_constant__ TensorSet<N> S, const double* __restrict__ 
              float* __restrict__ told) {
   constexpr int V = Vec16<T>::kN;
   __shared__ float f_shared;
+  wait_for_predecessor();
   if (threadIdx.x == 0) {
     float norm;
     f_shared = clip_factor(*sqsum, max_norm, &norm);
@@ -234,6 +240,11 @@ k_list_scale(const __grid_constant__ TensorSet<N> S, const double* __restrict__ 
     if (last && cut.tail0 + threadIdx.x < n)
       Vec16<T>::store(o + cut.tail0 + threadIdx.x, Vec16<T>::load(p + cut.tail0 + threadIdx.x) * f);
   }
+}
+
+static int chained(cudaError_t e) {
+  note_launch(1);
+  return e == cudaSuccess ? DP_OK : DP_ERR_CUDA;
 }
 
 static int norm_grid(unsigned long long chunks) {
@@ -292,19 +303,16 @@ static int list_sqsum(const void* const* in, const int64_t* sizes, int n, double
   if (n <= N && total <= kOneBlockChunks) {      // little work: one block, whose sum is the answer
     TensorSet<N> S;
     fill_set<N>(S, in, nullptr, sizes, 0, n, sizeof(T));
-    k_list_sqsum<T, N, 4><<<1, 4 * kNormThreads, 0, s>>>(S, sqsum, add);
-    return counted(1) == cudaSuccess ? DP_OK : DP_ERR_CUDA;
+    return chained(launch_chained(k_list_sqsum<T, N, 4>, 1, 4 * kNormThreads, 0, s, S, sqsum, add));
   }
   const int grid = norm_grid(total);
   do {
     TensorSet<N> S;
     k = fill_set<N>(S, in, nullptr, sizes, k, n, sizeof(T));
-    k_list_sqsum<T, N, 1><<<grid, kNormThreads, 0, s>>>(S, partial, add_partial);
-    if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
+    if (const int rc = chained(launch_chained(k_list_sqsum<T, N, 1>, grid, kNormThreads, 0, s, S, partial, add_partial))) return rc;
     add_partial = 1;
   } while (k < n);
-  k_partials_sum<<<1, 1024, 0, s>>>(partial, grid, sqsum, add);
-  return counted(1) == cudaSuccess ? DP_OK : DP_ERR_CUDA;
+  return chained(launch_chained(k_partials_sum, 1, 1024, 0, s, partial, grid, sqsum, add));
 }
 
 template <typename T, int N>
@@ -314,8 +322,7 @@ static int list_scale(const void* const* in, void* const* out, const int64_t* si
   do {
     TensorSet<N> S;
     k = fill_set<N>(S, in, out, sizes, k, n, sizeof(T));
-    k_list_scale<T, N><<<norm_grid(S.chunk0[S.n]), kNormThreads, 0, s>>>(S, sqsum, max_norm, told);
-    if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
+    if (const int rc = chained(launch_chained(k_list_scale<T, N>, norm_grid(S.chunk0[S.n]), kNormThreads, 0, s, S, sqsum, max_norm, told))) return rc;
   } while (k < n);
   return DP_OK;
 }

@@ -12,6 +12,7 @@
 // 32 bits are the angle in turns to 2^-32, at any 32-bit position, for the price of one multiplication.
 #include <type_traits>
 
+#include "dp_chain.cuh"
 #include "dp_internal.h"
 
 namespace dpk {
@@ -332,6 +333,8 @@ template <typename T, int NP, bool VEC, bool INTER, int GL>
 __global__ void __launch_bounds__(32, VEC ? kFwdWarps : 1)
 k_qknorm(const __grid_constant__ QkArgs a) {
   __shared__ uint4 ring_all[VEC ? kFwdStages * 64 : 1];            // [stages][2][32]
+  wait_for_predecessor();
+  let_successor_in();
   int kind;
   long long unit;
   unit_of(a, kind, unit);
@@ -417,6 +420,8 @@ template <typename T, int NP, bool VEC, bool INTER, int GL>
 __global__ void __launch_bounds__(32, VEC ? kBwdWarps : 1)
 k_qknorm_grad(const __grid_constant__ QkArgs a) {
   __shared__ uint4 ring_all[VEC ? kBwdStages * 128 : 1];           // [stages][x, dy][2][32]
+  wait_for_predecessor();
+  let_successor_in();
   int kind;
   long long unit;
   unit_of(a, kind, unit);
@@ -545,6 +550,7 @@ struct RowSums { const float* partial[2]; float* rows[2]; int parts[2]; };
 __global__ void __launch_bounds__(1024)
 k_qknorm_rows(const RowSums R, int D, int add) {
   __shared__ float part[32][32];
+  wait_for_predecessor();
   const int b = blockIdx.x, kind = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   if (!R.partial[kind]) return;
   const int d = blockIdx.y * 32 + lane, n = R.parts[kind];
@@ -688,9 +694,9 @@ struct Launch {
   cudaError_t run() const {
     const long long units = a.v[0].share.units + a.v[1].share.units;
     if (units > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-    if constexpr (BACKWARD) k_qknorm_grad<T, NP, VEC, INTER, GL><<<(unsigned)units, 32, 0, s>>>(a);
-    else k_qknorm<T, NP, VEC, INTER, GL><<<(unsigned)units, 32, 0, s>>>(a);
-    return counted(1);
+    note_launch(1);
+    if constexpr (BACKWARD) return launch_chained(k_qknorm_grad<T, NP, VEC, INTER, GL>, (unsigned)units, 32, 0, s, a);
+    else return launch_chained(k_qknorm<T, NP, VEC, INTER, GL>, (unsigned)units, 32, 0, s, a);
   }
 };
 
@@ -812,8 +818,9 @@ int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_head
       if (R.parts[k] > most) most = R.parts[k];
     }
     const int warps = most <= 8 ? 4 : most <= 64 ? 8 : 32;     // a few loads per warp, all in flight together
-    k_qknorm_rows<<<dim3(p->B, ceil_div(p->dim, 32), 2), 32 * warps, 0, s>>>(R, p->dim, a.accumulate);
-    if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
+    const cudaError_t er = launch_chained(k_qknorm_rows, dim3(p->B, ceil_div(p->dim, 32), 2), 32 * warps, 0, s, R, p->dim, a.accumulate);
+    note_launch(1);
+    if (er != cudaSuccess) return DP_ERR_CUDA;
   }
   return DP_OK;
 }

@@ -9,6 +9,7 @@
 #include <cstring>
 #include <type_traits>
 
+#include "dp_chain.cuh"
 #include "dp_internal.h"
 
 namespace dpk {
@@ -66,6 +67,8 @@ k_relpos_bias(const TT* __restrict__ table, const __grid_constant__ Buckets bk, 
               T* __restrict__ out, long long stride_h, long long stride_q, int warps_x) {
   constexpr int V = 16 / sizeof(T);
   extern __shared__ __align__(16) unsigned char bias_smem[];
+  wait_for_predecessor();
+  let_successor_in();
   T* line = reinterpret_cast<T*>(bias_smem);
   const int warps_y = 8 / warps_x;
   const int cols = kBiasCols * warps_x, rows = kBiasRowsPerWarp * warps_y;
@@ -226,6 +229,8 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
               const int32_t* __restrict__ q_len, const int32_t* __restrict__ k_len, float* __restrict__ partial,
               float* __restrict__ rows) {
   extern __shared__ float grad_smem[];
+  wait_for_predecessor();
+  let_successor_in();
   constexpr int V = Strip<T>::V, LG = 1 << LGL, CW = LG * V;
   const int RG = 1 << a.rg_log, LINE = RG + CW;  // a strand's line: diagonals -RG .. CW - 1
   const int lane = threadIdx.x & 31, li = lane & (LG - 1);
@@ -405,6 +410,8 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
 __global__ void __launch_bounds__(1024)
 k_relpos_units(const float* __restrict__ partial, int H, int nb, int units, float* __restrict__ rows, int add) {
   __shared__ float part[1024];
+  wait_for_predecessor();
+  let_successor_in();
   const int strands = blockDim.x / nb, n = threadIdx.x % nb, strand = threadIdx.x / nb;
   const long long bh = blockIdx.x, b = bh / H, h = bh - b * H;
   const float* p = partial + bh * units * nb + n;
@@ -493,13 +500,9 @@ static cudaError_t launch_bias(const dp_relpos& p, const Buckets& bk, const void
   const dim3 grid(ceil_div(p.Tk, cols), ceil_div(p.Tq, rows), p.n_heads);
   const size_t smem = (size_t)(cols + rows) * sizeof(T);
   const bool vec = !misaligned(out, 16) && p.Tk % V == 0 && sh % V == 0 && sq % V == 0;
-  if (vec)
-    k_relpos_bias<T, TT, true><<<grid, 256, smem, s>>>(static_cast<const TT*>(table), bk, p.n_heads, p.Tq, p.Tk,
-                                                       (int)p.offset, static_cast<T*>(out), sh, sq, wx);
-  else
-    k_relpos_bias<T, TT, false><<<grid, 256, smem, s>>>(static_cast<const TT*>(table), bk, p.n_heads, p.Tq, p.Tk,
-                                                        (int)p.offset, static_cast<T*>(out), sh, sq, wx);
-  return counted(1);
+  note_launch(1);
+  return launch_chained(vec ? k_relpos_bias<T, TT, true> : k_relpos_bias<T, TT, false>, grid, 256, smem, s,
+                        static_cast<const TT*>(table), bk, p.n_heads, p.Tq, p.Tk, (int)p.offset, static_cast<T*>(out), sh, sq, wx);
 }
 
 // How G is cut: V columns a lane, 2^lg lanes a strand, RG rows a strand, strands below one another in `threads` threads.
@@ -530,11 +533,12 @@ static GradPlan plan_grad(int B, const dp_relpos& p, int V) {
 }
 
 template <typename T, int LGL>
-static void launch_grad_form(bool shift, const T* G, const Buckets& bk, const GradArgs& a, const GradPlan& g,
+static cudaError_t launch_grad_form(bool shift, const T* G, const Buckets& bk, const GradArgs& a, const GradPlan& g,
                              const int32_t* q_len, const int32_t* k_len, float* partial, float* rows, cudaStream_t s) {
   const unsigned n = (unsigned)g.units;
-  if (shift) k_relpos_grad<T, LGL, true><<<n, g.threads, g.smem, s>>>(G, bk, a, q_len, k_len, partial, rows);
-  else k_relpos_grad<T, LGL, false><<<n, g.threads, g.smem, s>>>(G, bk, a, q_len, k_len, partial, rows);
+  note_launch(1);
+  return launch_chained(shift ? k_relpos_grad<T, LGL, true> : k_relpos_grad<T, LGL, false>, n, g.threads, g.smem, s, G, bk, a,
+                        q_len, k_len, partial, rows);
 }
 
 template <typename T>
@@ -543,10 +547,9 @@ static cudaError_t launch_grad(const void* G, const Buckets& bk, const GradArgs&
   const T* p = static_cast<const T*>(G);
   constexpr int V = Strip<T>::V;
   const bool shift = misaligned(G, 16) || a.Tk % V || a.stride_b % V || a.stride_h % V || a.stride_q % V;
-  if (g.lg == 3) launch_grad_form<T, 3>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
-  else if (g.lg == 4) launch_grad_form<T, 4>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
-  else launch_grad_form<T, 5>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
-  return counted(1);
+  if (g.lg == 3) return launch_grad_form<T, 3>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
+  if (g.lg == 4) return launch_grad_form<T, 4>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
+  return launch_grad_form<T, 5>(shift, p, bk, a, g, q_len, k_len, partial, rows, s);
 }
 
 }  // namespace dpk
@@ -629,8 +632,9 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
     // enough strands that each has a handful of tiles, whose loads are all in flight
     const int strands = per_bh <= 8 ? 1 : 1024 / nb < (per_bh + 7) / 8 ? 1024 / nb : (per_bh + 7) / 8;
     const int threads = (strands * nb + 31) / 32 * 32;
-    k_relpos_units<<<B * p->n_heads, threads, 0, s>>>(partial, p->n_heads, nb, per_bh, rows, a.accumulate);
-    if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
+    e = launch_chained(k_relpos_units, B * p->n_heads, threads, 0, s, partial, p->n_heads, nb, per_bh, rows, a.accumulate);
+    note_launch(1);
+    if (e != cudaSuccess) return DP_ERR_CUDA;
   }
   return DP_OK;
 }

@@ -2,6 +2,7 @@
 // gain of a head norm) for which a layer's own kernel has already formed every example's gradient.  The two steps that
 // the whole-model clip needs of them: the squared norm of every example's row, and the clipped sum over the examples.
 // Both are bound by reading the rows once (a few MB at most, so mostly by latency); sums run in a fixed order.
+#include "dp_chain.cuh"
 #include "dp_internal.h"
 
 namespace dpk {
@@ -19,6 +20,8 @@ struct RowSet {
 __global__ void __launch_bounds__(256)
 k_rows_sqnorm(const __grid_constant__ RowSet R, float* __restrict__ sqnorm, int add) {
   __shared__ float red[8];
+  wait_for_predecessor();
+  let_successor_in();
   const long long i = blockIdx.x;
   float s = 0.0f;
   for (int k = 0; k < R.n; ++k) {
@@ -44,6 +47,8 @@ constexpr int kAccWarps = 32;
 __global__ void __launch_bounds__(32 * kAccWarps)
 k_rows_accum(const __grid_constant__ RowSet R, int B, const float* __restrict__ clip) {
   __shared__ float part[kAccWarps][32];
+  wait_for_predecessor();
+  let_successor_in();
   int k = 0;
   while (R.col0[k + 1] <= (int)blockIdx.x) ++k;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -106,8 +111,9 @@ int dp_rows_sqnorms(const dp_rows* rows, int n_rows, int B, float* sqnorm, int a
     RowSet R;
     const int add = accumulate_into || k > 0;
     k = fill_rows(R, rows, k, n_rows);
-    k_rows_sqnorm<<<B, 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(R, sqnorm, add);
-    if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
+    const cudaError_t e = launch_chained(k_rows_sqnorm, B, 256, 0, static_cast<cudaStream_t>(cuda_stream), R, sqnorm, add);
+    note_launch(1);
+    if (e != cudaSuccess) return DP_ERR_CUDA;
   }
   return DP_OK;
 }
@@ -120,8 +126,9 @@ int dp_rows_clipped_accumulate(const dp_rows* rows, int n_rows, int B, const flo
   for (int k = 0; k < n_rows;) {
     RowSet R;
     k = fill_rows(R, rows, k, n_rows);
-    k_rows_accum<<<R.col0[R.n], 32 * kAccWarps, 0, static_cast<cudaStream_t>(cuda_stream)>>>(R, B, clip);
-    if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
+    const cudaError_t e = launch_chained(k_rows_accum, R.col0[R.n], 32 * kAccWarps, 0, static_cast<cudaStream_t>(cuda_stream), R, B, clip);
+    note_launch(1);
+    if (e != cudaSuccess) return DP_ERR_CUDA;
   }
   return DP_OK;
 }

@@ -1,6 +1,7 @@
 // Streaming kernels: clip factors, Philox4x32-10 noise + scaling, AdamW, and the fused pass.
 // All are bandwidth-bound: one thread owns one Philox block (4 consecutive elements, one 16-byte
 // vector per array), loads are fully coalesced, and the grid is a multiple of the SM count.
+#include "dp_chain.cuh"
 #include "dp_clip.cuh"
 #include "dp_internal.h"
 
@@ -253,6 +254,7 @@ __global__ void __launch_bounds__(256)
 k_clip_adamw(float* __restrict__ theta, float* __restrict__ m, float* __restrict__ v, float* __restrict__ g, int zero_g,
              long long n, const double* __restrict__ sqsum, double max_norm, AdamArgs aa) {
   __shared__ float f_shared;
+  wait_for_predecessor();
   if (threadIdx.x == 0) f_shared = clip_factor(*sqsum, max_norm);
   __syncthreads();
   const float f = f_shared;
@@ -316,11 +318,11 @@ cudaError_t launch_clip_adamw(float* theta, float* m, float* v, float* g, int ze
                               double max_norm, const AdamArgs& aa, cudaStream_t s) {
   if (n <= 0) return cudaSuccess;
   const int grid = stream_grid((unsigned long long)(n + 3) / 4);
-  if (aligned16(theta) && aligned16(m) && aligned16(v) && aligned16(g))
-    k_clip_adamw<true><<<grid, 256, 0, s>>>(theta, m, v, g, zero_g, n, sqsum, max_norm, aa);
-  else
-    k_clip_adamw<false><<<grid, 256, 0, s>>>(theta, m, v, g, zero_g, n, sqsum, max_norm, aa);
-  return counted(1);
+  const bool vec = aligned16(theta) && aligned16(m) && aligned16(v) && aligned16(g);
+  const cudaError_t e = launch_chained(vec ? k_clip_adamw<true> : k_clip_adamw<false>, grid, 256, 0, s, theta, m, v, g, zero_g,
+                                       n, sqsum, max_norm, aa);
+  note_launch(1);
+  return e;
 }
 
 // ---------------------------------------------------------------------------------------------
