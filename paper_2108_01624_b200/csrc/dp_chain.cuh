@@ -26,7 +26,9 @@ static cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, s
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+  if (e != cudaSuccess) cudaGetLastError();      // reported to the caller here, not to whoever asks next
+  return e;
 }
 
 }  // namespace dpk

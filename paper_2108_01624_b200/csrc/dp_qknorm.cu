@@ -274,23 +274,14 @@ __device__ __forceinline__ void scale(float (&a)[N], float r) {
 template <int NP>
 __device__ __forceinline__ void turn_pairs(float (&f)[2 * NP], const float (&c1)[NP], const float (&s1n)[NP],
                                            const float (&c2)[NP], const float (&s2)[NP]) {
-  if constexpr (NP % 2 == 0) {
+  static_assert(NP % 2 == 0, "pairs are turned two at a time");
 #pragma unroll
-    for (int i = 0; i < NP; i += 2) {
-      const float2 a = at2(f, i), b = at2(f, NP + i);
-      put2(f, i, fma2(a, at2(c1, i), mul2(b, at2(s1n, i))));
-      put2(f, NP + i, fma2(b, at2(c2, i), mul2(a, at2(s2, i))));
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const float a = f[i], b = f[NP + i];
-      f[i] = fmaf(a, c1[i], b * s1n[i]);
-      f[NP + i] = fmaf(b, c2[i], a * s2[i]);
-    }
+  for (int i = 0; i < NP; i += 2) {
+    const float2 a = at2(f, i), b = at2(f, NP + i);
+    put2(f, i, fma2(a, at2(c1, i), mul2(b, at2(s1n, i))));
+    put2(f, NP + i, fma2(b, at2(c2, i), mul2(a, at2(s2, i))));
   }
 }
-
 
 // Measured on the BERT-Large microbatch (forward 268 MB, backward 403 MB; device time of the main kernel):
 //   heads in flight per group   forward  2: 55 us, 4: 51, 8: 53        backward  2: 84, 4: 76

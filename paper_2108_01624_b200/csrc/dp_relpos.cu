@@ -49,75 +49,6 @@ struct Buckets {
   }
 };
 
-// ---------------------------------------------------------------------------------------------
-// Forward.  A block of 8 warps writes a tile of columns x rows of one head; the line of bias values that the tile
-// needs is looked up once into shared memory (in the output's type).  VEC: a lane owns 16 bytes of neighbouring columns
-// and walks down the rows: from one row to the next its window of the line moves by one value, so it shifts its
-// registers and reads a single new value.  Otherwise a lane owns every 32nd column, one element per store.
-// ---------------------------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ T to_type(float x);
-template <> __device__ __forceinline__ float to_type<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 to_type<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-
-constexpr int kBiasCols = 256, kBiasRowsPerWarp = 16;
-
-template <typename T, typename TT, bool VEC>
-__global__ void __launch_bounds__(256)
-k_relpos_bias(const TT* __restrict__ table, const __grid_constant__ Buckets bk, int n_heads, int Tq, int Tk, int offset,
-              T* __restrict__ out, long long stride_h, long long stride_q, int warps_x) {
-  constexpr int V = 16 / sizeof(T);
-  extern __shared__ __align__(16) unsigned char bias_smem[];
-  wait_for_predecessor();
-  let_successor_in();
-  T* line = reinterpret_cast<T*>(bias_smem);
-  const int warps_y = 8 / warps_x;
-  const int cols = kBiasCols * warps_x, rows = kBiasRowsPerWarp * warps_y;
-  const int c0 = blockIdx.x * cols, q0 = blockIdx.y * rows, h = blockIdx.z;
-  const int n_line = cols + rows - 1;
-  // line[i]: relative position (c0 - q0 - offset) + i - (rows - 1)
-  const int rel0 = c0 - q0 - offset - (rows - 1);
-  for (int i = threadIdx.x; i < n_line; i += 256)
-    line[i] = to_type<T>(to_float(table[(long long)bk.of(rel0 + i) * n_heads + h]));
-  __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int wx = warp % warps_x, wy = warp / warps_x;
-  const int r0 = wy * kBiasRowsPerWarp;
-  const int r1 = min(r0 + kBiasRowsPerWarp, Tq - q0);
-  T* o = out + (long long)h * stride_h + (long long)q0 * stride_q + c0;
-  if (VEC) {
-    for (int cc = wx * kBiasCols + lane * V; cc < (wx + 1) * kBiasCols; cc += 32 * V) {
-      if (c0 + cc >= Tk) break;
-      T w[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) w[j] = line[cc + j - r0 + rows - 1];
-      for (int r = r0; r < r1; ++r) {
-        uint4 u;
-        memcpy(&u, w, 16);
-        *reinterpret_cast<uint4*>(o + (long long)r * stride_q + cc) = u;
-#pragma unroll
-        for (int j = V - 1; j > 0; --j) w[j] = w[j - 1];
-        if (r + 1 < r1) w[0] = line[cc - (r + 1) + rows - 1];
-      }
-    }
-  } else {
-    for (int r = r0; r < r1; ++r)
-#pragma unroll 4
-      for (int cc = wx * kBiasCols + lane; cc < (wx + 1) * kBiasCols; cc += 32)
-        if (c0 + cc < Tk) o[(long long)r * stride_q + cc] = line[cc - r + rows - 1];
-  }
-}
-
-// ---------------------------------------------------------------------------------------------
-// Per-example gradient.  A block takes a tile of one (example, head), LG * V neighbouring columns wide; its groups of LG lanes
-// (a warp or a part of one) take strands of RG rows below one another, V columns a lane.  Walking down the rows, a diagonal
-// moves one column to the right per row: inside a lane that is another register of its V sums (renamed by unrolling the
-// rows), at the lane's right edge the sum is handed to the next lane, and the one that leaves the last lane is complete and
-// goes to the strand's line in shared memory.  That costs one add per element and one shuffle per V of them, with no atomic.
-// Then the warps add the strands' lines into one line of the tile's diagonals and sum that by buckets, each sum in a fixed
-// order.  A tile behind an example's lengths (or above the diagonal) only writes its zeros.
-// ---------------------------------------------------------------------------------------------
 // 16 bytes of neighbouring values of a row.
 template <typename T>
 struct Strip {
@@ -203,6 +134,106 @@ struct Wide {
   }
 };
 
+// ---------------------------------------------------------------------------------------------
+// Forward.  A block of 8 warps writes a tile of columns x rows of one head; the line of bias values that the tile
+// needs is looked up once into shared memory (in the output's type).  VEC: a lane owns 16 bytes of neighbouring columns
+// and walks down the rows: from one row to the next its window of the line moves by one value, so it shifts its
+// registers and reads a single new value.  Otherwise rows start anywhere: of each, the aligned 16-byte words are written
+// whole, out of copies of the line that begin at every place of a word, and the few values before and behind them one by
+// one (16 x 2047 x 2047: bf16 34 us value by value, 27 so; 2048 x 2048 23; fp32 51, 47 and 43).
+// ---------------------------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ T to_type(float x);
+template <> __device__ __forceinline__ float to_type<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 to_type<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+constexpr int kBiasCols = 256, kBiasRowsPerWarp = 16;
+
+template <typename T, typename TT, bool VEC>
+__global__ void __launch_bounds__(256)
+k_relpos_bias(const TT* __restrict__ table, const __grid_constant__ Buckets bk, int n_heads, int Tq, int Tk, int offset,
+              T* __restrict__ out, long long stride_h, long long stride_q, int warps_x) {
+  constexpr int V = 16 / sizeof(T);
+  extern __shared__ __align__(16) unsigned char bias_smem[];
+  wait_for_predecessor();
+  let_successor_in();
+  T* line = reinterpret_cast<T*>(bias_smem);
+  const int warps_y = 8 / warps_x;
+  const int cols = kBiasCols * warps_x, rows = kBiasRowsPerWarp * warps_y;
+  const int c0 = blockIdx.x * cols, q0 = blockIdx.y * rows, h = blockIdx.z;
+  const int n_line = cols + rows - 1 + (VEC ? 0 : V);      // words may end behind the tile's columns
+  const int pitch = (n_line + V - 1) / V * V;
+  // line[i]: relative position (c0 - q0 - offset) + i - (rows - 1)
+  const int rel0 = c0 - q0 - offset - (rows - 1);
+  T* o = out + (long long)h * stride_h + (long long)q0 * stride_q + c0;
+  // Otherwise V copies of the line, copy s without its first s values, so that a row's words are words of one of them; which
+  // ones occur repeats every V rows.
+  const int off0 = (int)((reinterpret_cast<uintptr_t>(o) & 15) / sizeof(T));
+  auto offset_of = [&](int r) { return (off0 + r * (int)(stride_q & (V - 1))) & (V - 1); };  // of a row's first column in its word
+  unsigned need = 1u;
+  if (!VEC)
+    for (int r = 0; r < min(V, Tq - q0); ++r) need |= 1u << ((rows - 1 - r - offset_of(r)) & (V - 1));
+  for (int i = threadIdx.x; i < n_line; i += 256) {
+    const T x = to_type<T>(to_float(table[(long long)bk.of(rel0 + i) * n_heads + h]));
+    line[i] = x;
+    if (!VEC) {
+#pragma unroll
+      for (int s = 1; s < V; ++s)
+        if ((need >> s & 1u) && i >= s) line[s * pitch + i - s] = x;
+    }
+  }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int wx = warp % warps_x, wy = warp / warps_x;
+  const int r0 = wy * kBiasRowsPerWarp;
+  const int r1 = min(r0 + kBiasRowsPerWarp, Tq - q0);
+  if (VEC) {
+    for (int cc = wx * kBiasCols + lane * V; cc < (wx + 1) * kBiasCols; cc += 32 * V) {
+      if (c0 + cc >= Tk) break;
+      T w[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) w[j] = line[cc + j - r0 + rows - 1];
+      for (int r = r0; r < r1; ++r) {
+        uint4 u;
+        memcpy(&u, w, 16);
+        *reinterpret_cast<uint4*>(o + (long long)r * stride_q + cc) = u;
+#pragma unroll
+        for (int j = V - 1; j > 0; --j) w[j] = w[j - 1];
+        if (r + 1 < r1) w[0] = line[cc - (r + 1) + rows - 1];
+      }
+    }
+  } else {
+    const int seg = c0 + wx * kBiasCols, left = Tk - seg;            // the warp's first column, columns from there on
+    if (left <= 0) return;
+#pragma unroll 4
+    for (int r = r0; r < r1; ++r) {
+      T* row = o + (long long)r * stride_q + wx * kBiasCols;
+      const int off = offset_of(r), head = off ? V - off : 0;          // columns before the first aligned word
+      const int from = wx * kBiasCols - r + rows - 1, place = from + head, s = place & (V - 1);
+      // the words that begin in the warp's columns, the last of which may end behind them; what a row has before its first
+      // word and behind its last is written value by value
+      const int most = (kBiasCols - head + V - 1) / V, have = left > head ? (left - head) / V : 0, words = min(most, have);
+      const uint4* q = reinterpret_cast<const uint4*>(line + s * pitch + place - s);
+#pragma unroll
+      for (int k = lane; k < kBiasCols / V; k += 32)
+        if (k < words) *reinterpret_cast<uint4*>(row + head + k * V) = q[k];
+      const int before = seg == 0 ? min(head, left) : 0, behind = have < most ? max(left - head - have * V, 0) : 0;
+      if (lane < before) row[lane] = line[from + lane];
+      if (lane < behind) row[head + have * V + lane] = line[place + have * V + lane];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Per-example gradient.  A block takes a tile of one (example, head), LG * V neighbouring columns wide; its groups of LG lanes
+// (a warp or a part of one) take strands of RG rows below one another, V columns a lane.  Walking down the rows, a diagonal
+// moves one column to the right per row: inside a lane that is another register of its V sums (renamed by unrolling the
+// rows), at the lane's right edge the sum is handed to the next lane, and the one that leaves the last lane is complete and
+// goes to the strand's line in shared memory.  That costs one add per element and one shuffle per V of them, with no atomic.
+// Then the warps add the strands' lines into one line of the tile's diagonals and sum that by buckets, each sum in a fixed
+// order.  A tile behind an example's lengths (or above the diagonal) only writes its zeros.
+// ---------------------------------------------------------------------------------------------
 // (a, b) + (x, y), two fp32 additions in one instruction.
 __device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
   asm("{.reg .b64 s, t, u;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 t, {%2, %3};\n\tadd.rn.f32x2 u, s, t;\n\tmov.b64 {%0, %1}, u;}"
@@ -500,8 +531,8 @@ static cudaError_t launch_bias(const dp_relpos& p, const Buckets& bk, const void
   const int wx = p.Tq <= kBiasRowsPerWarp ? 8 : 1, wy = 8 / wx;
   const int cols = kBiasCols * wx, rows = kBiasRowsPerWarp * wy;
   const dim3 grid(ceil_div(p.Tk, cols), ceil_div(p.Tq, rows), p.n_heads);
-  const size_t smem = (size_t)(cols + rows) * sizeof(T);
   const bool vec = !misaligned(out, 16) && p.Tk % V == 0 && sh % V == 0 && sq % V == 0;
+  const size_t smem = (vec ? cols + rows : (size_t)V * (cols + rows + 2 * V)) * sizeof(T);
   note_launch(1);
   return launch_chained(vec ? k_relpos_bias<T, TT, true> : k_relpos_bias<T, TT, false>, grid, 256, smem, s,
                         static_cast<const TT*>(table), bk, p.n_heads, p.Tq, p.Tk, (int)p.offset, static_cast<T*>(out), sh, sq, wx);
