@@ -537,27 +537,34 @@ k_qknorm_grad(const __grid_constant__ QkArgs a) {
   }
 }
 
-// rows[b][d] (+)= sum over an example's partial rows.  A block owns 32 columns of one example; its warps take every
-// (number of warps)-th partial row and their sums are added in warp order.
+// rows[b][d] (+)= sum over an example's partial rows.  A block owns COLS columns of one example; its threads stand as strands
+// x columns, a strand takes every (number of strands)-th partial row, and the strands are added in a fixed order.  Many
+// partial rows get more strands on fewer columns.
 struct RowSums { const float* partial[2]; float* rows[2]; int parts[2]; };
+template <int COLS>
 __global__ void __launch_bounds__(1024)
 k_qknorm_rows(const RowSums R, int D, int add) {
-  __shared__ float part[32][32];
+  __shared__ float part[32][COLS];
   wait_for_predecessor();
   const int b = blockIdx.x, kind = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   if (!R.partial[kind]) return;
-  const int d = blockIdx.y * 32 + lane, n = R.parts[kind];
+  const int d = blockIdx.y * COLS + (lane & (COLS - 1)), n = R.parts[kind];
   const float* p = R.partial[kind] + (long long)b * n * D + d;
   float s = 0.0f;
   if (d < D) {
 #pragma unroll 8
-    for (int c = warp; c < n; c += warps) s += p[(long long)c * D];
+    for (int c = threadIdx.x / COLS; c < n; c += blockDim.x / COLS) s += p[(long long)c * D];
   }
-  part[warp][lane] = s;
+#pragma unroll
+  for (int o = 16; o >= COLS; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane < COLS) part[warp][lane] = s;
   __syncthreads();
-  if (warp == 0 && d < D) {
-    float t = 0.0f;
-    for (int w = 0; w < warps; ++w) t += part[w][lane];
+  if (warp) return;
+  float t = 0.0f;
+  for (int w = lane / COLS; w < warps; w += 32 / COLS) t += part[w][lane & (COLS - 1)];
+#pragma unroll
+  for (int o = 16; o >= COLS; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  if (lane < COLS && d < D) {
     float* o = R.rows[kind] + (long long)b * D + d;
     *o = add ? *o + t : t;
   }
@@ -810,8 +817,12 @@ int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_head
       R.parts[k] = a.v[k].share.chunks * a.v[k].share.head_blocks;
       if (R.parts[k] > most) most = R.parts[k];
     }
-    const int warps = most <= 8 ? 4 : most <= 64 ? 8 : 32;     // a few loads per warp, all in flight together
-    const cudaError_t er = launch_chained(k_qknorm_rows, dim3(p->B, ceil_div(p->dim, 32), 2), 32 * warps, 0, s, R, p->dim, a.accumulate);
+    // a handful of partial rows per strand, whose loads are all in flight
+    const int warps = most <= 8 ? 4 : most <= 64 ? 8 : 32;
+    const bool narrow = most > 256;
+    const cudaError_t er = launch_chained(narrow ? k_qknorm_rows<8> : k_qknorm_rows<32>,
+                                          dim3(p->B, ceil_div(p->dim, narrow ? 8 : 32), 2), 32 * warps, 0, s, R, p->dim,
+                                          a.accumulate);
     note_launch(1);
     if (er != cudaSuccess) return DP_ERR_CUDA;
   }
