@@ -7,7 +7,7 @@
 // every query reads at another place, and the gradient is a sum along diagonals first, over buckets last.  Both kernels
 // are bound by memory: the bias by writing [H][Tq][Tk] (16 x 4096 x 4096 in bf16: 75 us, 7.2 TB/s), the gradient by reading
 // G once (256 x 16 x 128 x 128 in bf16: 29 us, 4.6 TB/s; 64 x 16 x 512 x 512 padded at random: 45 us, 4.8 TB/s of what
-// counts), where its instructions hold it back.
+// counts; launches that short spend several microseconds on filling and draining the GPU).
 #include <cstring>
 #include <type_traits>
 
