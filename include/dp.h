@@ -285,8 +285,9 @@ DP_API size_t dp_relpos_workspace_bytes(const dp_relpos* p /*HOST*/, int B);
  * + k] (DP_F32 or DP_BF16; strides in elements, 0 allowed):
  *   rows[b][n][h] = or += sum over (q, k) with bucket(k - q - offset) = n of G[b][h][q][k],   rows fp32 [B, num_buckets, n_heads].
  * q_len, k_len: int32 [B] device arrays or NULL; queries q >= q_len[b] and keys k >= k_len[b] do not count, and causal
- * != 0 leaves out keys k > q + offset.  What does not count may hold anything, NaN included.  accumulate_into = 1 adds a
- * further layer that shares the table.  fp32 sums in a fixed order. */
+ * != 0 leaves out keys k > q + offset.  What does not count may hold anything, NaN included; bytes between the rows of G
+ * may be read, none before its first score or behind its last.  accumulate_into = 1 adds a further layer that shares the
+ * table.  fp32 sums in a fixed order. */
 DP_API int dp_relpos_bias_grad(const dp_relpos* p /*HOST*/, int B, int causal, const void* G, int dtype, int64_t stride_b,
                                int64_t stride_h, int64_t stride_q, const int32_t* q_len, const int32_t* k_len, float* rows,
                                int accumulate_into, void* workspace, size_t workspace_bytes, void* cuda_stream);

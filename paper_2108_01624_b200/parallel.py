@@ -105,6 +105,8 @@ class ShardedUpdate:
             raise ValueError("max_grad_norm needs the collectives: leave peer_acc and peer_theta out")
         self.noised_sqnorm_fn = noised_sqnorm_fn or getattr(state, "noised_sqnorm", None)
         self.clipped_update_fn = clipped_update_fn or getattr(state, "clipped_update", None)
+        if self.max_grad_norm is not None and (self.noised_sqnorm_fn is None or self.clipped_update_fn is None):
+            raise ValueError("a state with max_grad_norm needs noised_sqnorm and clipped_update")
         self.state, self.dist, self.world, self.rank = state, dist, world, rank
         self.peer_acc, self.peer_theta = peer_acc, peer_theta
         self.fused_fn = fused_fn or self._fused_reduce_kernel
