@@ -152,3 +152,55 @@ def test_sharded_end_with_the_global_clip_equals_the_single_one(tmp_path):
         assert float(steps[1].acc.abs().max()) == 0.0 and float(steps[1].theta.abs().max()) > 0
     finally:
         dist.destroy_process_group()
+
+
+def test_captured_calls_behind_copies_and_fills():
+    """The calls' kernels may be set up before their predecessors end: behind copies, fills and torch's own kernels, eager
+    and in a replayed graph, they still see what those wrote."""
+    g = gen(7)
+    B, P, n = 64, 512, 3_000_000
+    src, grad, clip = randn(g, P), randn(g, B, P), torch.rand(B, generator=g, device=DEV)
+    acc, sq, total = torch.empty(P, device=DEV), torch.empty(B, device=DEV), torch.empty(1, dtype=torch.float64, device=DEV)
+    big, out, t = randn(g, n), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    x, y = randn(g, 32, 64, 8, 64, dtype=BF16), torch.empty(32, 64, 8, 64, dtype=BF16, device=DEV)
+    w, freq = work(b.dp_global_norm_workspace_bytes()), b.rope_frequencies(64)
+    rl = b.RowList([(grad, acc)])
+
+    def chain():
+        acc.copy_(src)                                                 # a copy, then the call that adds to it
+        b.dp_rows_clipped_accumulate(rl, clip)
+        sq.zero_()
+        b.dp_rows_sqnorms(rl, sq, True)
+        t.copy_(big)
+        t.mul_(2.0)                                                    # a kernel of torch's, then the norm of what it wrote
+        b.dp_global_sqnorm([t], total, False, w)
+        b.dp_clip_by_global_norm([t], [out], total, 1.0)
+        y.zero_()
+        b.dp_qknorm_rope(x, None, y, None, None, None, 1e-6, freq)
+        y.add_(1.0)
+
+    def check():
+        terms = grad.double() * clip.double()[:, None]
+        within(acc, src.double() + terms.sum(0), (terms.abs().sum(0) + src.double().abs()) * 40 * HALF[F32])
+        ref = grad.double().square().sum(1)
+        within(sq, ref, ref * 40 * HALF[F32])
+        norm2 = float((big.double() * 2).square().sum())
+        assert float(total) == pytest.approx(norm2, rel=34 * 2.0 ** -24)
+        want = big.double() * 2 / norm2 ** 0.5
+        within(out, want, want.abs() * 40 * HALF[F32])
+        z = torch.empty_like(y)
+        b.dp_qknorm_rope(x, None, z, None, None, None, 1e-6, freq)
+        torch.cuda.synchronize()
+        assert torch.equal(y, z + 1.0)
+    for _ in range(20):
+        chain()
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for seed in range(3):
+        h = gen(70 + seed)
+        src.copy_(randn(h, P)), grad.copy_(randn(h, B, P)), big.copy_(randn(h, n)), x.copy_(randn(h, 32, 64, 8, 64, dtype=BF16))
+        for _ in range(10):
+            graph.replay()
+        check()
