@@ -5,6 +5,10 @@
 // predecessor has completed and what it wrote is visible.  Since no thread of such a kernel ends before that, its own
 // successor may in turn rely on everything before it.  let_successor_in() only permits the early set-up (it takes
 // effect once every block of the grid has said it or ended); a successor that was launched the ordinary way ignores it.
+//
+// Such a kernel's pointer parameters are not __restrict__, and it uses no non-coherent loads: both promise that nobody else
+// writes the data while the kernel runs, which begins here while the predecessor still writes, and would let the compiler
+// move a load in front of the wait.
 #pragma once
 
 #include <cuda_runtime.h>

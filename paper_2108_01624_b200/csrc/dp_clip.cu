@@ -124,7 +124,7 @@ __device__ __forceinline__ double block_sum(double a, double* red) {
 // more teams of kNormThreads, each with chunks of its own.
 template <typename T, int N, int TEAMS>
 __global__ void __launch_bounds__(kNormThreads * TEAMS)
-k_list_sqsum(const __grid_constant__ TensorSet<N> S, double* __restrict__ partial, int add) {
+k_list_sqsum(const __grid_constant__ TensorSet<N> S, double* partial, int add) {
   constexpr int V = Vec16<T>::kN;
   __shared__ double red[kNormThreads * TEAMS / 32];
   wait_for_predecessor();
@@ -172,7 +172,7 @@ k_list_sqsum(const __grid_constant__ TensorSet<N> S, double* __restrict__ partia
 
 // sqsum (+)= sum of the partial sums, in index order per thread and then by a fixed tree.
 __global__ void __launch_bounds__(1024)
-k_partials_sum(const double* __restrict__ partial, int n, double* __restrict__ sqsum, int add) {
+k_partials_sum(const double* partial, int n, double* sqsum, int add) {
   __shared__ double red[32];
   wait_for_predecessor();
   let_successor_in();
@@ -186,8 +186,8 @@ k_partials_sum(const double* __restrict__ partial, int n, double* __restrict__ s
 // last ones in L2.  With f = 1 and out = in a tensor is left alone.
 template <typename T, int N>
 __global__ void __launch_bounds__(kNormThreads)
-k_list_scale(const __grid_constant__ TensorSet<N> S, const double* __restrict__ sqsum, double max_norm,
-             float* __restrict__ told) {
+k_list_scale(const __grid_constant__ TensorSet<N> S, const double* sqsum, double max_norm,
+             float* told) {
   constexpr int V = Vec16<T>::kN;
   __shared__ float f_shared;
   wait_for_predecessor();

@@ -152,8 +152,8 @@ constexpr int kBiasCols = 256, kBiasRowsPerWarp = 16;
 
 template <typename T, typename TT, bool VEC>
 __global__ void __launch_bounds__(256)
-k_relpos_bias(const TT* __restrict__ table, const __grid_constant__ Buckets bk, int n_heads, int Tq, int Tk, int offset,
-              T* __restrict__ out, long long stride_h, long long stride_q, int warps_x) {
+k_relpos_bias(const TT* table, const __grid_constant__ Buckets bk, int n_heads, int Tq, int Tk, int offset,
+              T* out, long long stride_h, long long stride_q, int warps_x) {
   constexpr int V = 16 / sizeof(T);
   extern __shared__ __align__(16) unsigned char bias_smem[];
   wait_for_predecessor();
@@ -258,9 +258,9 @@ struct GradArgs {
 // SHIFT: the rows do not all start and end on 16-byte boundaries.
 template <typename T, int LGL, bool SHIFT>
 __global__ void __launch_bounds__(kGradThreads, kGradBlocks)
-k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const __grid_constant__ GradArgs a,
-              const int32_t* __restrict__ q_len, const int32_t* __restrict__ k_len, float* __restrict__ partial,
-              float* __restrict__ rows) {
+k_relpos_grad(const T* G, const __grid_constant__ Buckets bk, const __grid_constant__ GradArgs a,
+              const int32_t* q_len, const int32_t* k_len, float* partial,
+              float* rows) {
   extern __shared__ float grad_smem[];
   wait_for_predecessor();
   let_successor_in();
@@ -441,7 +441,7 @@ k_relpos_grad(const T* __restrict__ G, const __grid_constant__ Buckets bk, const
 // rows[b][n][h] (+)= sum over the tiles of (b, h).  A block owns one (b, h); its threads stand as strands x buckets, a strand
 // takes every (number of strands)-th tile and the strands are added in order.
 __global__ void __launch_bounds__(1024)
-k_relpos_units(const float* __restrict__ partial, int H, int nb, int units, float* __restrict__ rows, int add) {
+k_relpos_units(const float* partial, int H, int nb, int units, float* rows, int add) {
   __shared__ float part[1024];
   wait_for_predecessor();
   let_successor_in();

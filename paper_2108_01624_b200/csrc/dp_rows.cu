@@ -18,7 +18,7 @@ struct RowSet {
 
 // One block per example: all tensors' rows, fp32 products summed per thread, then a fixed tree.
 __global__ void __launch_bounds__(256)
-k_rows_sqnorm(const __grid_constant__ RowSet R, float* __restrict__ sqnorm, int add) {
+k_rows_sqnorm(const __grid_constant__ RowSet R, float* sqnorm, int add) {
   __shared__ float red[8];
   wait_for_predecessor();
   let_successor_in();
@@ -45,7 +45,7 @@ k_rows_sqnorm(const __grid_constant__ RowSet R, float* __restrict__ sqnorm, int 
 // each (8 loads in flight) and their sums are added in warp order.
 constexpr int kAccWarps = 32;
 __global__ void __launch_bounds__(32 * kAccWarps)
-k_rows_accum(const __grid_constant__ RowSet R, int B, const float* __restrict__ clip) {
+k_rows_accum(const __grid_constant__ RowSet R, int B, const float* clip) {
   __shared__ float part[kAccWarps][32];
   wait_for_predecessor();
   let_successor_in();

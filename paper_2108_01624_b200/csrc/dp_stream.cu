@@ -251,8 +251,8 @@ cudaError_t launch_noise_adamw(float* theta, float* m, float* v, float* acc, int
 constexpr int kClipAhead = 4;
 template <bool VEC>
 __global__ void __launch_bounds__(256)
-k_clip_adamw(float* __restrict__ theta, float* __restrict__ m, float* __restrict__ v, float* __restrict__ g, int zero_g,
-             long long n, const double* __restrict__ sqsum, double max_norm, AdamArgs aa) {
+k_clip_adamw(float* theta, float* m, float* v, float* g, int zero_g,
+             long long n, const double* sqsum, double max_norm, AdamArgs aa) {
   __shared__ float f_shared;
   wait_for_predecessor();
   if (threadIdx.x == 0) f_shared = clip_factor(*sqsum, max_norm);
