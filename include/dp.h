@@ -247,7 +247,8 @@ typedef struct dp_rows {
 } dp_rows;
 
 /* sqnorm[i] = or += sum over the tensors of |grad_i|^2 (the whole-model clip of Algorithm 1: call it with
- * accumulate_into = 1 after dp_per_example_sqnorms, before dp_clip_factors). */
+ * accumulate_into = 1 after dp_per_example_sqnorms, before dp_clip_factors).  fp64 sums in a fixed order, rounded to fp32 once for
+ * every 128 tensors. */
 DP_API int dp_rows_sqnorms(const dp_rows* rows /*HOST*/, int n_rows, int B, float* sqnorm, int accumulate_into,
                            void* cuda_stream);
 
