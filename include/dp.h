@@ -308,8 +308,9 @@ typedef struct dp_qknorm {
   const float* gain_k;
   const int32_t* positions;    /* [B, T], or NULL for 0 .. T-1 */
   const int32_t* lengths;      /* [B] or NULL: tokens t >= lengths[b] are skipped and their outputs left as they were */
-  const double* inv_freq;      /* HOST [rot / 2], radians per position; read during the call.  The angle is kept modulo a
-                                  turn to 2^-32 at any position */
+  const double* inv_freq;      /* HOST [rot / 2], radians per position; read during the call.  The angle is formed modulo a
+                                  turn to 1.6 * 2^-32 turns at any position (frequencies up to 1); fp32 sines and cosines add 3 ulp
+                                  of their own, bf16 heads use ones within 2^-20 of the pair's length */
 } dp_qknorm;
 
 typedef struct dp_heads {      /* a [B, T, heads, dim] view, dim contiguous; strides in elements */

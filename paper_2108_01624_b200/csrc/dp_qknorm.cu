@@ -11,7 +11,7 @@
 //
 // The angle.  p * inv_freq loses its fractional turns in fp32 at far positions.  The host turns inv_freq[j] / (2 pi) into
 // a 64-bit binary fraction of a turn; p times that, modulo 2^64, is an ordinary wrapping integer product, and its upper
-// 32 bits are the angle in turns to 2^-32, at any 32-bit position, for the price of one multiplication.
+// 32 bits are the angle in units of 2^-32 turns, at any 32-bit position, for the price of one multiplication.
 #include <type_traits>
 
 #include "dp_chain.cuh"
@@ -210,19 +210,28 @@ struct Lane {
 };
 
 // Sine and cosine of pos * turn (a 64-bit fraction of a turn per position; 0 for what does not turn, which gives exactly 0
-// and 1).  EXACT (fp32 data): within 2 ulp.  Otherwise the hardware approximations on [-pi, pi], off by at most 2^-21 of
-// the pair's length: the data's own bf16 rounding is 2^12 times that, and the accurate pair costs about ten times the
-// instructions of the two.
+// and 1).  A float holds 24 of the angle's 32 bits.
+// EXACT (fp32 data): the nearest quarter turn is taken off in whole numbers first, so that those 24 bits count from the nearest
+// zero of the sine or cosine: each is off by 2^-24 and the function's 2 ulp of itself, and by 1.6 units of 2^-32 turns.
+// Otherwise the hardware approximations on [-pi, pi]: the angle in 24 bits and its product with pi are off by up to 3.0e-7, the sine
+// by 2^-21.4 and the cosine by 2^-21.2, together below 2^-20 of the pair's length.  The data's own bf16 rounding is 2^12 times
+// that, and the accurate pair costs about ten times the instructions of the two.
 template <bool EXACT>
 __device__ __forceinline__ void angle(uint2 turn, int pos, float& cs, float& sn) {
-  // bits 32..63 of turn * pos modulo 2^64, pos signed; as a signed number, so that angles just below a whole turn are small
-  // negative ones
+  // bits 32..63 of turn * pos modulo 2^64, pos signed
   unsigned h = turn.y * (unsigned)pos + __umulhi(turn.x, (unsigned)pos);
   if (pos < 0) h -= turn.x;
-  const float half_turns = (float)(int)h * 0x1p-31f;
   if (EXACT) {
-    sincospif(half_turns, &sn, &cs);
+    const unsigned quarter = (h + 0x20000000u) >> 30;
+    float s, c;
+    sincospif((float)(int)(h - (quarter << 30)) * 0x1p-31f, &s, &c);
+    sn = quarter & 1u ? c : s;
+    cs = quarter & 1u ? s : c;
+    if (quarter & 2u) sn = -sn;
+    if ((quarter + 1u) & 2u) cs = -cs;
   } else {
+    // as a signed number, so that angles just below a whole turn are small negative ones
+    const float half_turns = (float)(int)h * 0x1p-31f;
     sn = __sinf(half_turns * 3.14159265f);
     cs = __cosf(half_turns * 3.14159265f);
   }
