@@ -275,7 +275,8 @@ typedef struct dp_relpos {
 DP_API int dp_relpos_bucket_starts(int num_buckets, int max_distance, int bidirectional, int32_t* starts /*HOST*/);
 
 /* out[h * stride_h + q * stride_q + k] = the bias, rounded once to out_dtype.  table and out are DP_F32 or DP_BF16 each;
- * strides in elements, stride_q >= Tk. */
+ * strides in elements, stride_q >= Tk.  Rows do not overlap: of the heads' and the queries' stride (where there are several) the
+ * larger reaches past all that the smaller one covers; others are refused. */
 DP_API int dp_relpos_bias(const dp_relpos* p /*HOST*/, const void* table, int table_dtype, void* out, int out_dtype,
                           int64_t stride_h, int64_t stride_q, void* cuda_stream);
 
@@ -318,8 +319,11 @@ typedef struct dp_heads {      /* a [B, T, heads, dim] view, dim contiguous; str
   int64_t stride_b, stride_t, stride_h;
 } dp_heads;
 
-/* An output may be its own input (same strides); other overlaps are not allowed.  16-byte vectors are used where dim and
- * rot are multiples of 16 (bf16) or 8 (fp32, dim <= 256) elements and every head starts on a 16-byte boundary. */
+/* An output may be its own input (same strides); other overlaps are not allowed.  An output's heads do not overlap one
+ * another: its strides (of extents above 1) nest in some order, each reaching past all that the smaller ones cover; others are
+ * refused.  Strides of inputs may be 0.
+ * 16-byte vectors are used where dim and rot are multiples of 16 (bf16) or 8 (fp32, dim <= 256) elements and every head
+ * starts on a 16-byte boundary. */
 DP_API int dp_qknorm_rope(const dp_qknorm* p /*HOST*/, const dp_heads* q, const dp_heads* k, const dp_heads* out_q,
                           const dp_heads* out_k, void* cuda_stream);
 

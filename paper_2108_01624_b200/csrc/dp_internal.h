@@ -17,6 +17,24 @@ namespace dpk {
 static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// No two elements of a view coincide: `width` neighbouring elements, repeated extent[i] times at stride[i] >= 0 (i < n <= 4), with
+// the dimensions nested in some order, each stride reaching past all that the smaller ones cover.  (Dimensions that are
+// interleaved in another way and happen not to meet are not recognised.)
+static inline bool lies_apart(long long width, int n, const long long* extent, const long long* stride) {
+  bool used[4] = {};
+  __int128 covered = width;
+  for (int k = 0; k < n; ++k) {
+    int at = -1;
+    for (int i = 0; i < n; ++i)
+      if (!used[i] && extent[i] > 1 && (at < 0 || stride[i] < stride[at])) at = i;
+    if (at < 0) break;
+    if (stride[at] < covered) return false;
+    covered += (__int128)(extent[at] - 1) * stride[at];
+    used[at] = true;
+  }
+  return true;
+}
+
 // Launch accounting: every kernel launch of the library is counted (read back by dp_launch_count).
 void note_launch(int n);
 static inline cudaError_t counted(int n) { note_launch(n); return cudaGetLastError(); }

@@ -600,9 +600,12 @@ static int check_qk(const dp_qknorm* p) {
   return DP_OK;
 }
 
-// Copies x to *h after the checks; the stride of an extent of one, which nothing depends on, becomes 0.
-static int take_heads(const dp_qknorm* p, int heads, const dp_heads* x, size_t es, dp_heads* h) {
+// Copies x to *h after the checks; the stride of an extent of one, which nothing depends on, becomes 0.  Heads that are written
+// do not overlap one another.
+static int take_heads(const dp_qknorm* p, int heads, const dp_heads* x, size_t es, bool written, dp_heads* h) {
   if (!x || !x->data || x->stride_b < 0 || x->stride_t < 0 || x->stride_h < 0) return DP_ERR_ARG;
+  const long long extent[3] = {p->B, p->T, heads}, stride[3] = {x->stride_b, x->stride_t, x->stride_h};
+  if (written && !lies_apart(p->dim, 3, extent, stride)) return DP_ERR_ARG;
   *h = {x->data, p->B > 1 ? x->stride_b : 0, p->T > 1 ? x->stride_t : 0, heads > 1 ? x->stride_h : 0};
   return misaligned(x->data, es) ? DP_ERR_ALIGN : DP_OK;
 }
@@ -737,7 +740,7 @@ int dp_qknorm_rope(const dp_qknorm* p, const dp_heads* q, const dp_heads* k, con
   for (int i = 0; i < 2; ++i) {
     if (heads[i] == 0) continue;
     dp_heads x, y;
-    if ((rc = take_heads(p, heads[i], in[i], es, &x)) != DP_OK || (rc = take_heads(p, heads[i], out[i], es, &y)) != DP_OK)
+    if ((rc = take_heads(p, heads[i], in[i], es, false, &x)) != DP_OK || (rc = take_heads(p, heads[i], out[i], es, true, &y)) != DP_OK)
       return rc;
     vec = vec && vec_heads(x, V) && vec_heads(y, V);
     View& v = a.v[i];
@@ -789,8 +792,8 @@ int dp_qknorm_rope_backward(const dp_qknorm* p, const dp_heads* q, const dp_head
   for (int i = 0; i < 2; ++i) {
     if (heads[i] == 0) continue;
     dp_heads x, g, y;
-    if ((rc = take_heads(p, heads[i], in[i], es, &x)) != DP_OK || (rc = take_heads(p, heads[i], dout[i], es, &g)) != DP_OK ||
-        (rc = take_heads(p, heads[i], out[i], es, &y)) != DP_OK)
+    if ((rc = take_heads(p, heads[i], in[i], es, false, &x)) != DP_OK || (rc = take_heads(p, heads[i], dout[i], es, false, &g)) != DP_OK ||
+        (rc = take_heads(p, heads[i], out[i], es, true, &y)) != DP_OK)
       return rc;
     if (misaligned(rows[i], 4)) return DP_ERR_ALIGN;
     vec = vec && vec_heads(x, V) && vec_heads(g, V) && vec_heads(y, V);

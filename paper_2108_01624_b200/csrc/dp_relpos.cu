@@ -606,6 +606,8 @@ int dp_relpos_bias(const dp_relpos* p, const void* table, int table_dtype, void*
   const int rc = check_relpos(p, &bk);
   if (rc != DP_OK) return rc;
   if (!table || !out || stride_h < 0 || stride_q < p->Tk) return DP_ERR_ARG;
+  const long long extent[2] = {p->n_heads, p->Tq}, stride[2] = {stride_h, stride_q};
+  if (!lies_apart(p->Tk, 2, extent, stride)) return DP_ERR_ARG;
   if ((table_dtype != DP_F32 && table_dtype != DP_BF16) || (out_dtype != DP_F32 && out_dtype != DP_BF16)) return DP_ERR_ARG;
   if (p->n_heads > 65535 || ceil_div(p->Tq, kBiasRowsPerWarp * 8) > 65535) return DP_ERR_UNSUPPORTED;
   if (misaligned(table, table_dtype == DP_F32 ? 4 : 2) || misaligned(out, out_dtype == DP_F32 ? 4 : 2)) return DP_ERR_ALIGN;

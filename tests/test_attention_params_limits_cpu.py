@@ -1,5 +1,6 @@
 """Host side, without a GPU, of what the calls for the global norm, rows, relative position bias and query/key norms
 promise at their limits: which calls they refuse, and the rules that their kernels' sources keep."""
+import ctypes as C
 import os
 import re
 
@@ -9,7 +10,6 @@ from paper_2108_01624_b200 import binding as b
 from paper_2108_01624_b200 import build as builder
 
 ARG, ALIGN, UNSUPPORTED, WORKSPACE = -1, -2, -3, -6
-OK, NO_DEVICE = 0, -4               # a call that was accepted: launched, or no device to launch on
 
 
 @pytest.fixture(scope="module")
@@ -60,3 +60,44 @@ def test_kernels_that_start_early_promise_nothing_about_their_pointers():
             assert "__ldg" not in body and ".nc." not in body and "__restrict__" not in body, (f, name)
             before = body[1:body.index("wait_for_predecessor()")]
             assert all(re.match(r"(constexpr|(extern\s+)?__shared__)\b", s.strip()) for s in before.split(";") if s.strip()), (f, name)
+
+
+# An accepted layout is recognised by the next check's answer: its pointer is off the grid, so that nothing is launched.
+def test_a_bias_that_would_overlap_itself_is_refused(lib):
+    def bias(sh, sq, H=4, Tq=16, Tk=24):
+        return lib.dp_relpos_bias(C.byref(b.dp_relpos(32, 128, 1, H, Tq, Tk, 0)), 4096, 0, 8193, 1, sh, sq, None)
+    assert bias(16 * 24, 24) == ALIGN and bias(24, 4 * 24) == ALIGN                  # heads outside, queries outside
+    assert bias(1 << 40, 24) == ALIGN and bias(30, 4 * 30) == ALIGN and bias(16 * 24 + 5, 24) == ALIGN      # with gaps
+    assert bias(16 * 30 - 6, 30) == ALIGN                                            # no gap behind a head's last row
+    for sh, sq in ((0, 24), (23, 4 * 24), (24, 24), (16 * 24 - 1, 24), (24, 4 * 24 - 1), (96, 24), (0, 1 << 40)):
+        assert bias(sh, sq) == ARG, (sh, sq)
+    assert bias(0, 24, H=1) == ALIGN and bias(24, 24, Tq=1) == ALIGN                 # the stride of an extent of one
+
+
+def test_heads_that_would_overlap_themselves_are_refused(lib):
+    B, T, H, D = 2, 8, 4, 64
+
+    def heads(ptr, sb, st, sh):
+        return C.byref(b.dp_heads(ptr, sb, st, sh))
+    good = heads(4096, T * H * D, H * D, D)
+
+    def p(B=B, T=T, H=H):
+        return C.byref(b.dp_qknorm(1, B, T, H, 0, D, 0, 0, 1e-6, None, None, None, None, None))
+
+    def fwd(strides, x=good, **k):
+        return lib.dp_qknorm_rope(p(**k), x, None, heads(8193, *strides), None, None)
+
+    def bwd(strides, x=good, g=good, **k):
+        return lib.dp_qknorm_rope_backward(p(**k), x, None, g, None, heads(8193, *strides), None, None, None, 0, None, 0, None)
+    for call in (fwd, bwd):
+        for strides in ((T * H * D, H * D, D), (T * H * D, D, T * D), (D, B * H * D, B * D), (3 * T * H * D, 3 * H * D, 3 * D),
+                        (T * (H * D + 1), H * D + 1, D), (1 << 50, 1 << 30, 1 << 20)):
+            assert call(strides) == ALIGN, strides
+        for strides in ((0, H * D, D), (T * H * D, 0, D), (T * H * D, H * D, 0), (0, 0, 0), (T * H * D, H * D, D - 1),
+                        (T * H * D, H * D - 1, D), (T * H * D - 1, H * D, D), (H * D, H * D, D), (D, H * D, D)):
+            assert call(strides) == ARG, strides
+        assert call((0, H * D, D), B=1) == ALIGN and call((H * D, 0, D), T=1) == ALIGN and call((T * D, D, 0), H=1) == ALIGN
+        # inputs may be read several times
+        wide = heads(4096, 0, 0, 0)
+        assert call((T * H * D, H * D, D), x=wide) == ALIGN
+    assert bwd((T * H * D, H * D, D), g=heads(4096, 0, H * D, 0)) == ALIGN

@@ -8,7 +8,7 @@ import torch
 
 from paper_2108_01624_b200 import binding as b
 
-from .test_attention_params_gpu import BF16, DEV, F32, HALF, gen, randn, within
+from .test_attention_params_gpu import BF16, DEV, F32, HALF, QK_REL, gen, randn, within
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +116,57 @@ def test_angles_of_any_position(dtype, dim, rot, inter):
                                   (rows[:, p], cos[:, j], False), (rows[:, q], -sin[:, j], False)):
             rel = FP32_REL + (HALF[dtype] * 1.01 if rounded and dtype != F32 else 0.0)
             within(got, ref, ref.abs() * rel + absolute * (1 + rel), f"pair {j}")
+
+
+# ---- layouts of outputs -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_outputs_in_any_nested_layout_and_none_that_overlaps(dtype):
+    g = gen(2)
+    H, Tq, Tk = 3, 40, 56
+    table = randn(g, 32, H)
+    want = torch.empty(H, Tq, Tk, dtype=dtype, device=DEV)
+    b.dp_relpos_bias(table, want)
+    for room, cut in ((torch.empty(Tq, H, Tk, dtype=dtype, device=DEV), lambda r: r.transpose(0, 1)),
+                      (torch.empty(H, Tq + 3, Tk + 5, dtype=dtype, device=DEV), lambda r: r[:, 2:Tq + 2, 1:Tk + 1]),
+                      (torch.empty(Tq, 2, H, Tk, dtype=dtype, device=DEV), lambda r: r[:, 1].transpose(0, 1))):
+        room.fill_(9.0)
+        out = cut(room)
+        b.dp_relpos_bias(table, out)
+        assert torch.equal(out, want)
+        out.fill_(9.0)
+        assert bool((room == 9).all())                                 # nothing beside it was written
+    for bad in (torch.empty(1, Tq, Tk, dtype=dtype, device=DEV).expand(H, Tq, Tk),
+                torch.empty(2 * Tq * Tk, dtype=dtype, device=DEV).as_strided((H, Tq, Tk), (Tq * Tk // 2, Tk, 1))):
+        with pytest.raises(b.DpError):
+            b.dp_relpos_bias(table, bad)
+    B, T, n, D = 2, 9, 3, 64
+    x, dy = randn(g, B, T, n, D, dtype=dtype), randn(g, B, T, n, D, dtype=dtype)
+    freq, work = b.rope_frequencies(D), torch.empty(b.dp_qknorm_workspace_bytes(x, None), dtype=torch.uint8, device=DEV)
+    want, dwant = torch.empty_like(x), torch.empty_like(x)
+
+    def backward(dx, dout=dy):
+        b.dp_qknorm_rope_backward(x, None, dout, None, dx, None, None, None, None, None, 1e-6, freq, workspace=work)
+    b.dp_qknorm_rope(x, None, want, None, None, None, 1e-6, freq)
+    backward(dwant)
+    # another form of the kernel may serve a layout: both are within QK_REL of a pair's length (at most sqrt(D) = 8, a normed
+    # head's) and a rounding of the definition, the backward pass within 2 QK_REL of r (|u| + |hat| mean |u hat|) <= r |u| (1 + 8)
+    size = 8 * QK_REL
+    r = x.double().square().mean(-1, keepdim=True).rsqrt()
+    dsize = 2 * QK_REL * r * 2 ** 0.5 * float(dy.double().abs().max()) * 9
+    for room, cut in ((torch.empty(B, n, T, D, dtype=dtype, device=DEV), lambda r: r.transpose(1, 2)),
+                      (torch.empty(B, T, n, 3, D, dtype=dtype, device=DEV), lambda r: r[:, :, :, 1]),
+                      (torch.empty(n, T, B, D + 1, dtype=dtype, device=DEV), lambda r: r.permute(2, 1, 0, 3)[..., 1:])):
+        out = cut(room.fill_(9.0))
+        b.dp_qknorm_rope(x, None, out, None, None, None, 1e-6, freq)
+        within(out, want, 2.02 * (want.double().abs() * HALF[dtype] + size))
+        backward(out)
+        within(out, dwant, 2.02 * (dwant.double().abs() * HALF[dtype] + dsize))
+        out.fill_(9.0)
+        assert bool((room == 9).all())
+    for dim in (0, 1, 2):
+        bad = torch.empty_like(x).narrow(dim, 0, 1).expand_as(x)
+        with pytest.raises(b.DpError):
+            b.dp_qknorm_rope(x, None, bad, None, None, None, 1e-6, freq)
+        with pytest.raises(b.DpError):
+            backward(bad)
+        backward(dwant, dy.narrow(dim, 0, 1).expand_as(dy))            # an input may be broadcast
