@@ -415,6 +415,10 @@ def _native():
         if not os.path.exists(MODULE_PATH):
             raise ImportError(f"{MODULE_PATH} not found: run `python -m paper_2108_01624_b200.build` (needs nvcc and g++). "
                               "There is no fallback implementation.")
+        from . import build as builder
+        if not builder.module_fits(MODULE_PATH):          # before it is loaded: its view of a tensor may be another
+            raise ImportError(f"{MODULE_PATH} was built for another torch or Python than this one ({builder.module_key()}): "
+                              "run `python -m paper_2108_01624_b200.build`.")
         spec = importlib.util.spec_from_file_location("_dp_tensors", MODULE_PATH)
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)

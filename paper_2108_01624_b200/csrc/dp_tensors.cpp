@@ -455,4 +455,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dp_tensors", nullptr, -1, methods
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__dp_tensors(void) { return PyModule_Create(&module); }
+// DP_MODULE_KEY names the torch and the Python that this file was compiled against; build.py looks for it in the built file.
+PyMODINIT_FUNC PyInit__dp_tensors(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", DP_MODULE_KEY) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

@@ -101,3 +101,24 @@ def test_heads_that_would_overlap_themselves_are_refused(lib):
         wide = heads(4096, 0, 0, 0)
         assert call((T * H * D, H * D, D), x=wide) == ALIGN
     assert bwd((T * H * D, H * D, D), g=heads(4096, 0, H * D, 0)) == ALIGN
+
+
+# ---- what the module was built for --------------------------------------------------------------------------------
+def test_a_module_built_for_another_torch_is_rebuilt_and_never_loaded(lib, monkeypatch, tmp_path):
+    import torch
+    assert not builder.needs_module() and b._native().built_for == builder.module_key()
+    assert torch.__version__ in builder.module_key()
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "0.0.1+other")
+        assert builder.needs_module() and builder.needs_build() and not builder.needs_library()
+        m.setattr(b, "_module", None)
+        with pytest.raises(ImportError, match="another torch"):
+            b.dp_relpos_workspace_bytes(torch.empty(1, 1, 4, 4), 32)
+        assert b._module is None
+    # the commands that build count as sources
+    with monkeypatch.context() as m:
+        later = tmp_path / "build.py"
+        later.write_text("")
+        os.utime(later, (1 << 33, 1 << 33))
+        m.setattr(builder, "__file__", str(later))
+        assert builder.needs_library() and builder.needs_module()
