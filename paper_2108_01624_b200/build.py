@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -58,7 +59,11 @@ def build(force: bool = False, verbose: bool = False, defines=(), out: str = LIB
     if out != LIB or defines or force or needs_library():
         _build_library(verbose, defines, out)
     if out == LIB and (force or needs_module()):
-        build_module()
+        try:
+            build_module()
+        except RuntimeError as e:          # the C ABI and the calls bound by ctypes are complete without it
+            warnings.warn(f"_dp_tensors.so was not built, the calls on small tensors will raise ImportError: {e}",
+                          RuntimeWarning, stacklevel=2)
     return out
 
 
@@ -78,19 +83,25 @@ def _build_library(verbose: bool, defines, out: str) -> None:
 
 
 def build_module() -> str:
-    """The CPython module, host code only, against the installed torch's headers."""
+    """The CPython module, host code only, against the installed torch's headers.  Raises RuntimeError where a compiler or
+    headers are missing; no older module is left then."""
     import sysconfig
 
     import torch
     base = os.path.dirname(os.path.abspath(torch.__file__))
     cuda = os.path.dirname(os.path.dirname(os.path.abspath(_nvcc()))) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    if os.path.exists(MODULE):
+        os.remove(MODULE)
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DDP_MODULE_KEY="{module_key()}"',
            "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
            "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"),
            os.path.join(CSRC, "dp_tensors.cpp"), "-o", MODULE, "-L", os.path.join(base, "lib"),
            "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{os.path.join(base, 'lib')}"]
-    proc = subprocess.run(cmd, capture_output=True, text=True)
+    try:
+        proc = subprocess.run(cmd, capture_output=True, text=True)
+    except OSError as e:
+        raise RuntimeError(f"{cmd[0]}: {e}") from e
     if proc.returncode != 0:
         raise RuntimeError("g++ failed:\n" + proc.stdout + proc.stderr)
     return MODULE

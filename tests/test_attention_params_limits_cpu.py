@@ -122,3 +122,22 @@ def test_a_module_built_for_another_torch_is_rebuilt_and_never_loaded(lib, monke
         os.utime(later, (1 << 33, 1 << 33))
         m.setattr(builder, "__file__", str(later))
         assert builder.needs_library() and builder.needs_module()
+
+
+def test_the_library_is_built_where_the_module_cannot_be(lib, monkeypatch, tmp_path):
+    """The C ABI and the calls bound by ctypes need neither Python's headers nor torch's."""
+    import torch
+    module = tmp_path / "_dp_tensors.so"
+    module.write_bytes(b"left by an earlier build, of other sources")
+    monkeypatch.setattr(builder, "MODULE", str(module))
+    monkeypatch.setenv("CXX", str(tmp_path / "no compiler"))
+    with pytest.warns(RuntimeWarning, match="_dp_tensors"):
+        assert builder.build() == builder.LIB
+    assert not module.exists()                                        # nothing that does not fit the library is left
+    with pytest.raises(RuntimeError):                                 # asked for by itself it fails
+        builder.build_module()
+    monkeypatch.setattr(b, "MODULE_PATH", str(module))
+    monkeypatch.setattr(b, "_module", None)
+    with pytest.raises(ImportError):
+        b.dp_relpos_workspace_bytes(torch.empty(1, 1, 4, 4), 32)
+    assert b.dp_version() >= 100
