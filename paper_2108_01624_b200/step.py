@@ -260,6 +260,7 @@ class DPStep:
         norm of its tensors' elements in grad_sqsum."""
         if self.grad_sqsum is None:
             self.grad_sqsum = torch.zeros(1, dtype=torch.float64, device=self.device)
+        if self._norm_ws is None:       # after an end of a macro-batch with an empty shard there is a sum, but no workspace
             self._norm_ws = torch.empty(b.dp_global_norm_workspace_bytes(), dtype=torch.uint8, device=self.device)
         b.dp_add_noise_and_scale(acc, self.sigma, self.C, batch_size, self.seed, self.t, elem_offset, stream)
         b.dp_global_sqnorm(self.tensor_pieces(acc, elem_offset, elem_offset + acc.numel()), self.grad_sqsum, False,

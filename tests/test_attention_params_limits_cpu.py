@@ -141,3 +141,36 @@ def test_the_library_is_built_where_the_module_cannot_be(lib, monkeypatch, tmp_p
     with pytest.raises(ImportError):
         b.dp_relpos_workspace_bytes(torch.empty(1, 1, 4, 4), 32)
     assert b.dp_version() >= 100
+
+
+# ---- the clip of a macro-batch across ranks -------------------------------------------------------------------------
+class _OneRankOfMany:
+    """Collectives as a rank sees them whose peers add nothing."""
+    class ReduceOp:
+        MIN = "min"
+
+    def get_backend(self):
+        return "gloo"
+
+    def all_reduce(self, t, op=None):
+        pass
+
+    def all_gather(self, out, mine):
+        pass
+
+
+def test_a_rank_whose_shard_was_empty_can_finish_a_macro_batch_alone(monkeypatch):
+    from paper_2108_01624_b200.parallel import ShardedUpdate
+    from paper_2108_01624_b200.synth import LINEAR, LayerSpec
+
+    from .test_step_rows_cpu import make
+    st, fake = make(monkeypatch, [LayerSpec(LINEAR, 2, 2, False, "fc")], shard_world=3, max_grad_norm=0.5)
+    sharded = ShardedUpdate(st, _OneRankOfMany(), 3, 2, poll_fn=lambda: 0)
+    assert sharded.lo == sharded.hi
+    st.examples_seen = 8
+    sharded.finish_macro_batch()                                       # nothing of its own to sum or update
+    assert fake.calls == [] and float(st.grad_sqsum) == 0.0
+    st.examples_seen = 8
+    st.finish_macro_batch()                                            # the job goes on with one rank
+    norm = [a for name, a, _ in fake.calls if name == "dp_global_sqnorm"]
+    assert len(norm) == 1 and norm[0][1] is st.grad_sqsum and norm[0][3] is not None
