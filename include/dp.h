@@ -304,7 +304,7 @@ typedef struct dp_qknorm {
   int32_t B, T, n_q, n_k;      /* B * T <= 2^30; query and key heads: either may be 0, its tensors are then not looked at */
   int32_t dim, rot;            /* even, dim <= 512, 0 <= rot <= dim */
   int32_t interleaved;
-  double eps;                  /* >= 0 */
+  double eps;                  /* 0, or a normal fp32 number (at least 2^-126).  Squares are summed in fp32: |x| < 2^59 */
   const float* gain_q;         /* [dim] fp32, or NULL for ones */
   const float* gain_k;
   const int32_t* positions;    /* [B, T], or NULL for 0 .. T-1 */

@@ -12,6 +12,7 @@
 // The angle.  p * inv_freq loses its fractional turns in fp32 at far positions.  The host turns inv_freq[j] / (2 pi) into
 // a 64-bit binary fraction of a turn; p times that, modulo 2^64, is an ordinary wrapping integer product, and its upper
 // 32 bits are the angle in units of 2^-32 turns, at any 32-bit position, for the price of one multiplication.
+#include <cfloat>
 #include <type_traits>
 
 #include "dp_chain.cuh"
@@ -588,7 +589,8 @@ static int check_qk(const dp_qknorm* p) {
   if (!p || p->B <= 0 || p->T <= 0 || p->dim <= 0 || p->n_q < 0 || p->n_k < 0 || p->n_q + (int64_t)p->n_k <= 0) return DP_ERR_ARG;
   if (p->dtype != DP_F32 && p->dtype != DP_BF16) return DP_ERR_ARG;
   if ((p->dim & 1) || p->rot < 0 || (p->rot & 1) || p->rot > p->dim) return DP_ERR_ARG;
-  if (!(p->eps >= 0.0) || !std::isfinite(p->eps)) return DP_ERR_ARG;
+  // eps is added in fp32: 0, or a normal number there
+  if (!(p->eps == 0.0 || (p->eps >= FLT_MIN && p->eps <= FLT_MAX))) return DP_ERR_ARG;
   if (p->n_q > 65535 || p->n_k > 65535 || p->T > 1 << 24 || (int64_t)p->B * p->T > 1 << 30)
     return DP_ERR_UNSUPPORTED;
   if (p->dim > 2 * kMaxPairs) return DP_ERR_UNSUPPORTED;

@@ -174,3 +174,21 @@ def test_a_rank_whose_shard_was_empty_can_finish_a_macro_batch_alone(monkeypatch
     st.finish_macro_batch()                                            # the job goes on with one rank
     norm = [a for name, a, _ in fake.calls if name == "dp_global_sqnorm"]
     assert len(norm) == 1 and norm[0][1] is st.grad_sqsum and norm[0][3] is not None
+
+
+# ---- eps ----------------------------------------------------------------------------------------------------------
+def test_an_eps_that_fp32_cannot_hold_is_refused(lib):
+    """The kernels add eps in fp32: one that is lost there would turn a head of zeros into NaN, one beyond it any head into 0."""
+    h = C.byref(b.dp_heads(4096, 8 * 4 * 64, 4 * 64, 64))
+    off = C.byref(b.dp_heads(8193, 8 * 4 * 64, 4 * 64, 64))            # misaligned: the call ends before a launch
+
+    def call(eps):
+        p = C.byref(b.dp_qknorm(1, 2, 8, 4, 0, 64, 0, 0, eps, None, None, None, None, None))
+        a = lib.dp_qknorm_rope(p, h, None, off, None, None)
+        z = lib.dp_qknorm_rope_backward(p, h, None, h, None, off, None, None, None, 0, None, 0, None)
+        assert a == z
+        return a
+    for eps in (0.0, 1e-6, 1.0, 2.0 ** -126, 3e38):
+        assert call(eps) == ALIGN, eps
+    for eps in (1e-39, 1e-50, 5e-324, 1e39, float("inf"), -1e-6, float("nan")):
+        assert call(eps) == ARG, eps
