@@ -226,7 +226,8 @@ DP_API int dp_global_sqnorm(const void* const* tensors /*HOST*/, const int64_t* 
 
 /* outs[k] = tensors[k] * f, f = min(1, max_norm / sqrt(*sqsum)), 1 where *sqsum = 0.  outs[k] may be tensors[k] itself
  * (then nothing is written when f = 1); other overlaps are not allowed.  norm_and_factor (device float[2], or NULL)
- * receives sqrt(*sqsum) and f.  An infinite norm gives f = 0 and a NaN one f = NaN: both show in the result. */
+ * receives sqrt(*sqsum) and f.  f is an fp32 number and loses bits below 2^-126.  An infinite norm gives f = 0 and a NaN one
+ * f = NaN: both show in the result. */
 DP_API int dp_clip_by_global_norm(const void* const* tensors /*HOST*/, void* const* outs /*HOST*/,
                                   const int64_t* sizes /*HOST*/, int n_tensors, int dtype, const double* sqsum,
                                   double max_norm, float* norm_and_factor, void* cuda_stream);

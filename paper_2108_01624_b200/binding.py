@@ -503,7 +503,7 @@ def dp_relpos_bucket_starts(num_buckets: int, max_distance: int, bidirectional: 
 def dp_relpos_bias(table: torch.Tensor, out: torch.Tensor, max_distance: int = 128, bidirectional: bool = True,
                    offset: int = 0, stream=None) -> torch.Tensor:
     """out[h, q, k] = table[bucket(k - q - offset), h]; table [num_buckets, heads], out [heads, Tq, Tk] with unit stride
-    along the keys (fp32 or bf16 each)."""
+    along the keys and rows that do not overlap (fp32 or bf16 each)."""
     rc = (_module or _native()).relpos_bias(table, out, max_distance, bidirectional, offset,
                                             None if stream is None else stream.cuda_stream)
     if rc:
@@ -539,9 +539,9 @@ def dp_qknorm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], out_q: 
                    out_k: Optional[torch.Tensor], gain_q: Optional[torch.Tensor], gain_k: Optional[torch.Tensor],
                    eps: float, inv_freq: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
                    lengths: Optional[torch.Tensor] = None, interleaved: bool = False, stream=None) -> None:
-    """RMS norm per head with gain, then the position rotation.  q, k [B, T, heads, dim] (any strides, unit along dim),
-    either None; gains fp32 [dim] or None; inv_freq float64 on the host (rope_frequencies), its length is rot / 2, None
-    for no rotation; positions int32 [B, T], lengths int32 [B]."""
+    """RMS norm per head with gain, then the position rotation.  q, k [B, T, heads, dim] (any strides, unit along dim;
+    the outputs' heads do not overlap), either None; gains fp32 [dim] or None; inv_freq float64 on the host
+    (rope_frequencies), its length is rot / 2, None for no rotation; positions int32 [B, T], lengths int32 [B]."""
     rc = (_module or _native()).qknorm_rope(q, k, out_q, out_k, gain_q, gain_k, eps, inv_freq, positions, lengths,
                                             interleaved, None if stream is None else stream.cuda_stream)
     if rc:

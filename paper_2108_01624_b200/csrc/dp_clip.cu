@@ -291,7 +291,9 @@ static int fill_set(TensorSet<N>& S, const void* const* in, void* const* out, co
 
 // Up to this many chunks one block sums a list, in one launch: the host's second launch costs more than the time that more
 // blocks would save.  One block of 64 x 64 with its FFN and norms (13 chunks): 15.7 -> 12.9 us a pass; one layer of 64 x 64
-// (1 chunk) with its AdamW step: 12.3 -> 8.6.
+// (1 chunk) with its AdamW step: 12.3 -> 8.6.  Norm and scaling of one fp32 tensor in a bare loop of calls, many blocks against one: 1
+// chunk 6.5, 4.5 us; 8 6.4, 5.6; 12 6.4, 6.7; 16 6.4, 7.5; 24 6.4, 9.1 -- the fewer other calls the host makes, the lower they
+// cross.  Replayed from a graph, where the host does not count: 1 chunk 4.5, 3.9; 4 4.3, 4.4; 8 4.4, 5.3; 16 5.4, 7.1.
 constexpr unsigned long long kOneBlockChunks = 16;
 
 template <typename T, int N>

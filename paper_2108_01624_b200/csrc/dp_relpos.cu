@@ -7,7 +7,7 @@
 // every query reads at another place, and the gradient is a sum along diagonals first, over buckets last.  Both kernels
 // are bound by memory: the bias by writing [H][Tq][Tk] (16 x 4096 x 4096 in bf16: 75 us, 7.2 TB/s), the gradient by reading
 // G once (256 x 16 x 128 x 128 in bf16: 29 us, 4.6 TB/s; 64 x 16 x 512 x 512 padded at random: 45 us, 4.8 TB/s of what
-// counts; launches that short spend several microseconds on filling and draining the GPU).
+// counts; a block has no loads in flight while it adds its strands and sums its diagonals).
 #include <cstring>
 #include <type_traits>
 
@@ -243,7 +243,8 @@ __device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
 // Measured (256 x 16 scores of 128 x 128; 64 x 16 of 512 x 512 padded at random; bf16, whole chain of calls):
 //   (before the last steps)  rows per strand at most  16: 41 / 69 us, 32: 37 / 57, 64: 37 / 58
 //                            threads at most  64: 37 / 65 us, 128: 37 / 57, 256: 37 / 58
-//   blocks per SM  7: 38 / 56 us, 8: 37 / 53, 9: 37 / 53, 10: 47 / 91 (registers spill)
+//   blocks per SM  7: 38 / 56 us, 8: 37 / 53, 9: 37 / 53, 10: 47 / 91 (48 registers: up to 570 bytes of spills; at
+//   64 they are 12 to 40)
 constexpr int kGradThreads = 128, kGradMaxRows = 5;   // threads per block at most; log2 of the rows per strand at most
 constexpr int kGradBlocks = 8;
 constexpr int kGradRowBlock = 8;                 // rows whose loads are issued together
@@ -664,7 +665,9 @@ int dp_relpos_bias_grad(const dp_relpos* p, int B, int causal, const void* G, in
   else e = launch_grad<__nv_bfloat16>(G, bk, a, g, q_len, k_len, partial, rows, s);
   if (e != cudaSuccess) return DP_ERR_CUDA;
   if (partial) {
-    // enough strands that each has a handful of tiles, whose loads are all in flight
+    // enough strands that each has a handful of tiles, whose loads are all in flight.  The call in bf16 with one strand, this many,
+    // as many as fit: 64 x 16 x 512 x 512 (16 tiles a head) 83.9, 83.9, 86.2 us; 4 x 16 x 1024 x 1024 (64) 29.4, 27.6, 27.9;
+    // 1 x 16 x 2048 x 2048 (256) 32.7, 26.6, 27.5; 1 x 1 x 4096 x 4096 (2048) 94, 17.4, 17.4
     const int strands = per_bh <= 8 ? 1 : 1024 / nb < (per_bh + 7) / 8 ? 1024 / nb : (per_bh + 7) / 8;
     const int threads = (strands * nb + 31) / 32 * 32;
     e = launch_chained(k_relpos_units, B * p->n_heads, threads, 0, s, partial, p->n_heads, nb, per_bh, rows, a.accumulate);
