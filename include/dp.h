@@ -339,6 +339,87 @@ DP_API int dp_qknorm_rope_backward(const dp_qknorm* p /*HOST*/, const dp_heads* 
                                    float* rows_q, float* rows_k, int accumulate_into, void* workspace,
                                    size_t workspace_bytes, void* cuda_stream);
 
+/* ---- Cross entropy over a vocabulary, without the logits ---------------------------------------------------------------
+ * The masked-LM head of Section 4's model (and any softmax classifier over a table): tokens X [B, T, d], table W [V, d],
+ * z = X W^T + bias.  The logits are formed piece by piece and never kept; neither are their gradients
+ *   G[i][t][v] = weights[i][t] * (exp(z[i][t][v] - lse[i][t]) - [v = labels[i][t]]),
+ * of which a bounded piece of the vocabulary at a time lies in the workspace.  (The paper does not restate the loss.)
+ * One microbatch: dp_vocab_loss; dp_vocab_loss_backward, whose sqnorm joins those of the other layers
+ * (accumulate_into = 1) before dp_clip_factors; dp_vocab_loss_clipped_accumulate.  Where the table is the token
+ * embedding too, dp_vocab_loss_cross_sqnorms adds the inner product of the two parts of its gradient, and acc_w is the
+ * accumulator of the embedding layer.
+ * A token whose label is negative has no loss: its rows of X may hold anything, its loss, lse and dX are 0.  A label of V or
+ * more counts as none and is reported by dp_poll_status (DP_ERR_BAD_ID).
+ * bias and weights are fp32; entries of bias may be -inf (a word that cannot occur).  Infinite or NaN logits of a
+ * token with a label make what depends on it NaN.
+ * Sums are fp32, in an order that only the sizes and the device decide; the label's logit is formed in fp64.  With bf16 X
+ * and W the products are exact; G is rounded to 2^-17 of each element before it is summed over tokens, to 2^-9 where it
+ * forms a bf16 dX.  With fp32 X and W operands carry 24 bits in z and 17 in the products with G. */
+typedef struct dp_vocab_head {
+  int32_t dtype;               /* dp_dtype of X, W and dX */
+  int32_t B, T, d, V;          /* B * T and V at most 2^26, d at most 2^16 */
+  const void* X;               /* token n = i * T + t begins at X + n * ldx (elements) */
+  int64_t ldx;                 /* >= d */
+  const void* W;               /* entry v begins at W + v * ldw */
+  int64_t ldw;                 /* >= d */
+  const float* bias;           /* [V] or NULL */
+  const int32_t* labels;       /* [B, T] */
+  const float* weights;        /* [B, T] weight of each token's loss, or NULL for ones */
+} dp_vocab_head;
+/* bf16 rows that start on 16-byte boundaries (pointer and leading dimension) are read where they are; others, and fp32 ones,
+ * are copied into the workspace first. */
+
+/* Bytes of scratch for the calls below; 0 on invalid sizes.  It holds G for a piece of the vocabulary (256 MiB, more only
+ * where B * T * 2048 entries of G take more) and, where X or W are copied, their copies. */
+DP_API size_t dp_vocab_workspace_bytes(const dp_vocab_head* head /*HOST*/);
+
+/* loss[B, T] = weights * (lse - z[label]), lse[B, T] = log of the sum over v of exp z; fp32. */
+DP_API int dp_vocab_loss(const dp_vocab_head* head /*HOST*/, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                         void* cuda_stream);
+
+/* From the lse of dp_vocab_loss: dX = G W (rows of leading dimension ld_dx; of dtype; may not overlap X), and
+ *   sqnorm[i] = or += |G_i^T X_i|^2 + (with bias) |sum_t G_i|^2,
+ * the squared norm of example i's gradients of W and bias.  dX or sqnorm may be NULL. */
+DP_API int dp_vocab_loss_backward(const dp_vocab_head* head /*HOST*/, const float* lse, void* dX, int64_t ld_dx, float* sqnorm,
+                                  int accumulate_into, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* acc_w [V, d] += sum_i clip_i G_i^T X_i and, with a bias, acc_b [V] += sum_i clip_i sum_t G_i; fp32.  The order of the sums
+ * does not depend on the run. */
+DP_API int dp_vocab_loss_clipped_accumulate(const dp_vocab_head* head /*HOST*/, const float* lse, const float* clip, float* acc_w,
+                                            float* acc_b, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The cross term of a table that W shares with the token embedding (dp_shared_table_cross_sqnorms without dlogits):
+ *   sqnorm[i] += 2 * sum over inputs u < Tu, tokens t of G[i][t][ids[i][u]] * <X[i][t], G_emb[i][u]>,
+ * G as above.  ids int32 [B, Tu]; G_emb [B, Tu, d] of dtype, the gradient of the embedding's output, its rows ld_emb apart;
+ * call it before dp_clip_factors.  An id outside [0, V) is skipped and reported (DP_ERR_BAD_ID). */
+DP_API int dp_vocab_loss_cross_sqnorms(const dp_vocab_head* head /*HOST*/, const float* lse, const int32_t* ids,
+                                       const void* G_emb, int64_t ld_emb, int Tu, float* sqnorm, void* workspace,
+                                       size_t workspace_bytes, void* cuda_stream);
+
+/* ---- Distillation from a teacher's top logits -----------------------------------------------------------------------------
+ * The other loss such a head is trained with, on logits that the caller has: of every token the teacher gives its K
+ * largest logits and their words.  With q = softmax(top_logits / temperature) over the given words and
+ * p = softmax(logits / temperature) over all V,
+ *   loss[n] = weights[n] * temperature^2 * sum_k q_k (log q_k - log p[top_ids_k]),
+ *   dlogits[n][v] = weights[n] * temperature * (p_v - sum over k with top_ids_k = v of q_k),
+ * the output-gradient G that a DP_LINEAR layer (or a shared table's projection) takes.  A negative id is an empty place
+ * (fewer than K words given); a token without any, or whose teacher's logits are all -inf, has loss and gradient 0 and its
+ * logits are not looked at.  An id of V or more is an empty place and is reported by dp_poll_status (DP_ERR_BAD_ID).
+ * The same id may occur several times.  -inf logits are words that cannot occur. */
+typedef struct dp_distill {
+  int32_t dtype;               /* dp_dtype of logits and dlogits */
+  int32_t teacher_dtype;       /* of top_logits */
+  int32_t N, V, K;             /* tokens, vocabulary, words of the teacher per token (1 .. 1024) */
+  double temperature;          /* 1e-30 to 1e30 */
+  const void* logits;          /* row n begins at logits + n * ld (elements) */
+  int64_t ld;                  /* >= V; 0 allowed with N = 1 */
+  const int32_t* top_ids;      /* [N, K] */
+  const void* top_logits;      /* [N, K] */
+  const float* weights;        /* [N] or NULL for ones */
+} dp_distill;
+/* loss [N] fp32.  dlogits: rows ld_out apart, or NULL where only the loss is wanted; may be logits itself (ld_out = ld). */
+DP_API int dp_distill_loss(const dp_distill* p /*HOST*/, float* loss, void* dlogits, int64_t ld_out, void* cuda_stream);
+
 /* Test utility: out[k] = the raw Philox word of element elem_offset + k (lane (e & 3) of block e >> 2). */
 DP_API int dp_philox_u32(uint32_t* out, int64_t n_words, int64_t elem_offset, uint64_t seed, uint64_t step,
                   void* cuda_stream);

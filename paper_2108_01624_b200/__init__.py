@@ -13,4 +13,6 @@ from .binding import (RowList, dp_clip_adamw_step, dp_clip_by_global_norm, dp_gl
                       dp_global_sqnorm, dp_qknorm_rope, dp_qknorm_rope_backward, dp_qknorm_workspace_bytes,
                       dp_relpos_bias, dp_relpos_bias_grad, dp_relpos_bucket_starts, dp_relpos_workspace_bytes,
                       dp_rows_clipped_accumulate, dp_rows_sqnorms, rope_frequencies)
+from .binding import (VocabHead, dp_distill_loss, dp_vocab_loss, dp_vocab_loss_backward,  # noqa: F401
+                      dp_vocab_loss_clipped_accumulate, dp_vocab_loss_cross_sqnorms, dp_vocab_workspace_bytes)
 from .step import DeviceStatusError, DPStep  # noqa: F401

@@ -33,7 +33,9 @@ EXPORTS = ["dp_workspace_bytes", "dp_per_example_sqnorms", "dp_clip_factors", "d
            "dp_global_norm_workspace_bytes", "dp_global_sqnorm", "dp_clip_by_global_norm", "dp_clip_adamw_step",
            "dp_rows_sqnorms", "dp_rows_clipped_accumulate",
            "dp_relpos_bucket_starts", "dp_relpos_bias", "dp_relpos_workspace_bytes", "dp_relpos_bias_grad",
-           "dp_qknorm_rope", "dp_qknorm_workspace_bytes", "dp_qknorm_rope_backward"]
+           "dp_qknorm_rope", "dp_qknorm_workspace_bytes", "dp_qknorm_rope_backward",
+           "dp_vocab_workspace_bytes", "dp_vocab_loss", "dp_vocab_loss_backward", "dp_vocab_loss_clipped_accumulate",
+           "dp_vocab_loss_cross_sqnorms", "dp_distill_loss"]
 
 
 class dp_layer(C.Structure):
@@ -61,6 +63,18 @@ class dp_qknorm(C.Structure):
 
 class dp_heads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class dp_vocab_head(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("T", C.c_int32), ("d", C.c_int32), ("V", C.c_int32),
+                ("X", C.c_void_p), ("ldx", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+                ("labels", C.c_void_p), ("weights", C.c_void_p)]
+
+
+class dp_distill(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("teacher_dtype", C.c_int32), ("N", C.c_int32), ("V", C.c_int32), ("K", C.c_int32),
+                ("temperature", C.c_double), ("logits", C.c_void_p), ("ld", C.c_int64), ("top_ids", C.c_void_p),
+                ("top_logits", C.c_void_p), ("weights", C.c_void_p)]
 
 
 class DpError(RuntimeError):
@@ -117,6 +131,13 @@ def lib() -> C.CDLL:
         L.dp_qknorm_workspace_bytes.restype = sz
         L.dp_qknorm_workspace_bytes.argtypes = [vp]
         L.dp_qknorm_rope_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+        L.dp_vocab_workspace_bytes.restype = sz
+        L.dp_vocab_workspace_bytes.argtypes = [vp]
+        L.dp_vocab_loss.argtypes = [vp, vp, vp, vp, sz, vp]
+        L.dp_vocab_loss_backward.argtypes = [vp, vp, vp, i64, vp, i32, vp, sz, vp]
+        L.dp_vocab_loss_clipped_accumulate.argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
+        L.dp_vocab_loss_cross_sqnorms.argtypes = [vp, vp, vp, vp, i64, i32, vp, vp, sz, vp]
+        L.dp_distill_loss.argtypes = [vp, vp, vp, i64, vp]
         L.dp_poll_status.argtypes = [vp]
         L.dp_set_wait_limit_cycles.argtypes = [C.c_longlong]
         L.dp_selftest_wait_timeout.argtypes = [vp]
@@ -398,14 +419,16 @@ def dp_selftest_wait_timeout(stream=None) -> None:
 
 
 
-# ---- global norm over many tensors, rows, relative position bias, query/key norms -------------------------------------
+# ---- global norm over many tensors, rows, relative position bias, query/key norms, losses of a vocabulary head ---------
 # These calls serve small tensors too, where the host side of a call is most of its time: the CPython module _dp_tensors
 # (csrc/dp_tensors.cpp) checks the tensors, fills the descriptors and calls the library's entry points.  It takes what the
 # functions below take, in their order, and returns the status; a tensor that does not fit raises ValueError.
 MODULE_PATH = os.path.join(_HERE, "_dp_tensors.so")
 _BOUND = ["dp_global_sqnorm", "dp_clip_by_global_norm", "dp_clip_adamw_step", "dp_rows_sqnorms", "dp_rows_clipped_accumulate",
           "dp_relpos_bias", "dp_relpos_workspace_bytes", "dp_relpos_bias_grad", "dp_qknorm_rope",
-          "dp_qknorm_workspace_bytes", "dp_qknorm_rope_backward"]       # in the order of its bind()
+          "dp_qknorm_workspace_bytes", "dp_qknorm_rope_backward", "dp_vocab_workspace_bytes", "dp_vocab_loss",
+          "dp_vocab_loss_backward", "dp_vocab_loss_clipped_accumulate", "dp_vocab_loss_cross_sqnorms",
+          "dp_distill_loss"]       # in the order of its bind()
 _module = None
 
 
@@ -565,3 +588,75 @@ def dp_qknorm_rope_backward(q, k, dout_q, dout_k, dq, dk, gain_q: Optional[torch
                                                      None if stream is None else stream.cuda_stream)
     if rc:
         raise DpError("dp_qknorm_rope_backward", rc)
+
+
+class VocabHead:
+    """A softmax head over a vocabulary: tokens x [B, T, d] (evenly spaced rows), table weight [V, d] of the same dtype
+    (fp32 or bf16), labels int32 [B, T] (negative: no loss), bias fp32 [V] or None, token_weights fp32 [B, T] or None for
+    ones.  A HOST descriptor plus references that keep the tensors alive."""
+
+    def __init__(self, x: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                 token_weights: Optional[torch.Tensor] = None):
+        self.x, self.weight, self.labels, self.bias, self.token_weights = x, weight, labels, bias, token_weights
+        self.native = (_module or _native()).vocab_head(x, weight, labels, bias, token_weights)
+
+    @property
+    def B(self) -> int:
+        return self.x.shape[0]
+
+
+def dp_vocab_workspace_bytes(head: VocabHead) -> int:
+    """Scratch for the calls on this head (at least 256, so that it can be allocated)."""
+    return (_module or _native()).vocab_workspace_bytes(head.native)
+
+
+def dp_vocab_loss(head: VocabHead, loss: torch.Tensor, lse: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """loss, lse [B, T] fp32: weighted cross entropy of every token and the log-sum-exp of its logits, which are not kept."""
+    rc = (_module or _native()).vocab_loss(head.native, loss, lse, workspace, None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_vocab_loss", rc)
+    return loss
+
+
+def dp_vocab_loss_backward(head: VocabHead, lse: torch.Tensor, dx: Optional[torch.Tensor], sqnorm: Optional[torch.Tensor],
+                           accumulate_into: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx like x (may be a view with evenly spaced rows) and sqnorm [B] = or += every example's squared norm of the gradients
+    of table and bias; either may be None."""
+    rc = (_module or _native()).vocab_loss_backward(head.native, lse, dx, sqnorm, accumulate_into, workspace,
+                                                    None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_vocab_loss_backward", rc)
+
+
+def dp_vocab_loss_clipped_accumulate(head: VocabHead, lse: torch.Tensor, clip: torch.Tensor, acc_w: torch.Tensor,
+                                     acc_b: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                     stream=None) -> None:
+    """acc_w [V, d] and, with a bias, acc_b [V] += the clipped sum over the examples of their gradients."""
+    rc = (_module or _native()).vocab_loss_clipped_accumulate(head.native, lse, clip, acc_w, acc_b, workspace,
+                                                              None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_vocab_loss_clipped_accumulate", rc)
+
+
+def dp_vocab_loss_cross_sqnorms(head: VocabHead, lse: torch.Tensor, ids: torch.Tensor, g_emb: torch.Tensor,
+                                sqnorm: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """sqnorm[i] += twice the inner product of the two parts of example i's gradient of a table that the head shares with
+    the token embedding: ids int32 [B, inputs], g_emb [B, inputs, d] the gradient of the embedding's output."""
+    rc = (_module or _native()).vocab_loss_cross_sqnorms(head.native, lse, ids, g_emb, sqnorm, workspace,
+                                                         None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_vocab_loss_cross_sqnorms", rc)
+    return sqnorm
+
+
+def dp_distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.Tensor, temperature: float,
+                    loss: torch.Tensor, dlogits: Optional[torch.Tensor], token_weights: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Distillation of logits [B, T, V] from the teacher's K top logits (top_ids int32, top_logits fp32 or bf16, [B, T, K];
+    negative ids are empty places): loss [B, T] fp32 and, unless None, dlogits like logits (which may be logits itself)."""
+    rc = (_module or _native()).distill_loss(logits, top_ids, top_logits, temperature, loss, dlogits, token_weights,
+                                             None if stream is None else stream.cuda_stream)
+    if rc:
+        raise DpError("dp_distill_loss", rc)
+    return loss

@@ -12,7 +12,8 @@ LIB = os.path.join(HERE, "libdp_b200.so")
 HEADER = os.path.join(HERE, "..", "include", "dp.h")
 MODULE = os.path.join(HERE, "_dp_tensors.so")          # CPython module: torch tensors into the C ABI
 SOURCES = ["dp_api.cu", "dp_stream.cu", "dp_generic.cu", "dp_umma.cu", "dp_noalloc.cu",
-           "dp_clip.cu", "dp_rows.cu", "dp_relpos.cu", "dp_qknorm.cu"]
+           "dp_clip.cu", "dp_rows.cu", "dp_relpos.cu", "dp_qknorm.cu", "dp_vocab.cu",
+           "dp_distill.cu", "dp_vocab_cross.cu"]
 
 
 def _nvcc() -> str:

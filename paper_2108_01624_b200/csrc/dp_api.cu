@@ -14,7 +14,7 @@ static std::atomic<long long> g_launches{0};
 void note_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 
 // Device address of the status word for the current device (looked up once per device).
-static int* status_ptr() {
+int* status_ptr() {
   static int* cache[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
@@ -27,7 +27,6 @@ static int* status_ptr() {
 }
 
 static size_t elem_size(int dtype) { return dtype == DP_F32 ? 4 : 2; }
-static bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 // Shape/pointer checks shared by the two layer-list entry points.
 static int validate_layers(const dp_layer* layers, int n_layers, bool need_acc) {
@@ -67,7 +66,7 @@ static int validate_layers(const dp_layer* layers, int n_layers, bool need_acc) 
 // multiply-accumulates per block pair of the upper triangle and came out ahead whenever that count stayed under
 // about 1.75 times the tile kernel's T x d_in x d_out (whose tiles re-read A and G through L2 for every tile row
 // and column): T from 256 to 4096, widths from 256 to 4096, one mispick of 13 % among fifteen shapes.
-static bool use_gram(const dp_layer& L) {
+bool use_gram(const dp_layer& L) {
   if (L.path == DP_PATH_GRAM) return true;
   if (L.path == DP_PATH_MATERIALIZED) return false;
   if (L.kind == DP_LINEAR && umma_supported(L)) {

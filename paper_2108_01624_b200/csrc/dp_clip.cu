@@ -330,7 +330,6 @@ static int list_scale(const void* const* in, void* const* out, const int64_t* si
   return DP_OK;
 }
 
-static bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 static int check_list(const void* const* in, void* const* out, bool want_out, const int64_t* sizes, int n, int dtype) {
   if (n < 0 || (n > 0 && (!in || !sizes || (want_out && !out)))) return DP_ERR_ARG;

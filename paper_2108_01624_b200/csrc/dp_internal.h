@@ -116,8 +116,24 @@ long long umma_accumulate_schedule(const dp_layer* layers, const int* idx, int n
 int launch_umma_accumulate(const dp_layer* layers, const int* idx, int n, const float* clip, int* status,
                            unsigned int* wave_sync, cudaStream_t s);
 
+// Per-device facts, looked up once for each device a process drives (one process may drive several GPUs).
+constexpr int kMaxDevices = 64;
+int current_device();        // -1 where it cannot be told
+int sm_count();
+// Device address of the sticky status word (nullptr where it cannot be told).
+int* status_ptr();
+// Whether a layer's norm goes through the token Gram (dp_path AUTO: the cheaper way).
+bool use_gram(const dp_layer& L);
+static inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+// The cross term of a shared table (dp_vocab_cross.cu); partial: B * kCrossChunks floats.
+constexpr int kCrossChunks = 64;
+int launch_vocab_cross(const dp_vocab_head& h, const float* lse, const int32_t* ids, const void* G_emb, long long ld_emb, int Tu,
+                       float* sqnorm, float* partial, int* status, cudaStream_t s);
+
 // Limit of every bounded device-side wait on the current device, in SM cycles (<= 0 restores the default).
 int set_wait_limit_cycles(long long cycles);
+int set_vocab_wait_limit(long long cycles);     // the part of it that dp_vocab.cu's kernels read
 // One CTA that waits, bounded, on a barrier nobody arrives on: records a timeout (site tag 98 or 99) and returns.
 int launch_selftest_wait(int* status, cudaStream_t s);
 

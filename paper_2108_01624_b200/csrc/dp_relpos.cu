@@ -515,7 +515,6 @@ static int make_buckets(int num_buckets, int max_distance, int both, Buckets* bk
   return DP_OK;
 }
 
-static bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 static int check_relpos(const dp_relpos* p, Buckets* bk) {
   if (!p || p->n_heads <= 0 || p->Tq <= 0 || p->Tk <= 0) return DP_ERR_ARG;

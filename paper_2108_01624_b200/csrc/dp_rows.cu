@@ -77,7 +77,6 @@ k_rows_accum(const __grid_constant__ RowSet R, int B, const float* clip) {
   }
 }
 
-static bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 static int check_rows(const dp_rows* rows, int n, int B, bool need_acc) {
   if (!rows || n <= 0 || B <= 0) return DP_ERR_ARG;

@@ -1,5 +1,5 @@
 // CPython module _dp_tensors: torch tensors into the C ABI of include/dp.h for the calls on small tensors (global norm,
-// rows, relative position bias, query/key norms), where reading a tensor's address, sizes and strides from Python takes
+// rows, relative position bias, query/key norms, losses of a vocabulary head), where reading a tensor's address, sizes and strides from Python takes
 // several times as long as the launch.  Argument marshalling only: every function checks its tensors, fills the
 // descriptors and calls the entry point whose address bind() was given, on the current stream of the tensors' device (or
 // the stream it is handed).  A tensor that does not fit raises ValueError before anything is launched; the entry point's
@@ -12,6 +12,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <string>
 #include <vector>
 
@@ -36,6 +37,12 @@ struct Api {
   decltype(&dp_qknorm_rope) qknorm_rope;
   decltype(&dp_qknorm_workspace_bytes) qknorm_workspace_bytes;
   decltype(&dp_qknorm_rope_backward) qknorm_rope_backward;
+  decltype(&dp_vocab_workspace_bytes) vocab_workspace_bytes;
+  decltype(&dp_vocab_loss) vocab_loss;
+  decltype(&dp_vocab_loss_backward) vocab_loss_backward;
+  decltype(&dp_vocab_loss_clipped_accumulate) vocab_loss_clipped_accumulate;
+  decltype(&dp_vocab_loss_cross_sqnorms) vocab_loss_cross_sqnorms;
+  decltype(&dp_distill_loss) distill_loss;
 };
 Api api = {};
 
@@ -402,6 +409,157 @@ int qknorm_rope_backward(Args a) {  // q, k, dout_q, dout_k, dq, dk, gain_q, gai
   return api.qknorm_rope_backward(&H.p, q, k, gq, gk, dq, dk, rq, rk, truth(a[15]), w.p, w.n, on.stream);
 }
 
+// Rows [n, width] of a tensor whose leading dimensions are evenly spaced: the distance between neighbouring rows.
+int64_t row_stride(const at::Tensor& t, const char* what) {
+  const int64_t last = t.dim() - 1;
+  if (t.size(last) > 1 && t.stride(last) != 1) throw Refused{std::string(what) + ": unit stride along the width expected"};
+  int64_t ld = -1, rows = 1;       // rows of one step of the dimension at hand
+  for (int64_t k = last - 1; k >= 0; --k) {
+    if (t.size(k) == 1) continue;
+    if (ld < 0) ld = t.stride(k);
+    else if (t.stride(k) != rows * ld) throw Refused{std::string(what) + ": evenly spaced rows expected"};
+    rows *= t.size(k);
+  }
+  return ld < 0 ? std::max<int64_t>(t.size(last), 1) : ld;
+}
+
+// Head descriptors live in a bytes object: (device, descriptor).
+PyObject* vocab_head(Args a) {    // x, weight, labels, bias, token_weights
+  const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "weight");
+  const int device = device_of(x, "x");
+  on_device(w, device, "weight");
+  if (x.dim() != 3) throw Refused{"x: [B, T, d] expected"};
+  if (w.dim() != 2 || w.size(1) != x.size(2)) throw Refused{"weight: [V, " + std::to_string(x.size(2)) + "] expected, got " + shape_text(w.sizes())};
+  dp_vocab_head h = {};
+  h.dtype = dp_dtype_of(x, "x");
+  if (dp_dtype_of(w, "weight") != h.dtype) throw Refused{"x and weight share one dtype"};
+  h.B = extent(x.size(0));
+  h.T = extent(x.size(1));
+  h.d = extent(x.size(2));
+  h.V = extent(w.size(0));
+  const int64_t tokens[2] = {x.size(0), x.size(1)}, words[1] = {w.size(0)};
+  h.X = x.data_ptr();
+  h.ldx = row_stride(x, "x");
+  h.W = w.data_ptr();
+  h.ldw = row_stride(w, "weight");
+  if (a[2] == Py_None) throw Refused{"labels expected"};
+  h.labels = static_cast<const int32_t*>(dense(a[2], device, at::kInt, "labels", -1, tokens));
+  h.bias = static_cast<const float*>(dense(a[3], device, at::kFloat, "bias", -1, words));
+  h.weights = static_cast<const float*>(dense(a[4], device, at::kFloat, "token_weights", -1, tokens));
+  PyObject* out = Py_BuildValue("(iy#)", device, reinterpret_cast<const char*>(&h), (Py_ssize_t)sizeof(h));
+  if (!out) throw Raised{};
+  return out;
+}
+struct Head {
+  int device;
+  dp_vocab_head h;
+  Head(PyObject* o) {              // what vocab_head returned
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2 || !PyBytes_Check(PyTuple_GET_ITEM(o, 1)) ||
+        PyBytes_GET_SIZE(PyTuple_GET_ITEM(o, 1)) != (Py_ssize_t)sizeof(h))
+      throw Refused{"vocabulary head expected"};
+    device = (int)integer(PyTuple_GET_ITEM(o, 0));
+    memcpy(&h, PyBytes_AS_STRING(PyTuple_GET_ITEM(o, 1)), sizeof(h));
+  }
+  float* tokens(PyObject* o, const char* what) const {
+    if (o == Py_None) throw Refused{std::string(what) + " expected"};
+    const int64_t shape[2] = {h.B, h.T};
+    return static_cast<float*>(dense(o, device, at::kFloat, what, -1, shape));
+  }
+  float* examples(PyObject* o, const char* what) const {
+    return static_cast<float*>(dense(o, device, at::kFloat, what, h.B));
+  }
+};
+PyObject* vocab_workspace_bytes(Args a) {    // head
+  const Head H(a[0]);
+  const size_t n = api.vocab_workspace_bytes(&H.h);
+  return PyLong_FromSize_t(n < 256 ? 256 : n);
+}
+int vocab_loss(Args a) {          // head, loss, lse, workspace, stream
+  const Head H(a[0]);
+  float *loss = H.tokens(a[1], "loss"), *lse = H.tokens(a[2], "lse");
+  const Workspace w = workspace_of(a[3], H.device);
+  const On on(H.device, a[4]);
+  return api.vocab_loss(&H.h, loss, lse, w.p, w.n, on.stream);
+}
+int vocab_loss_backward(Args a) { // head, lse, dx, sqnorm, accumulate_into, workspace, stream
+  const Head H(a[0]);
+  const float* lse = H.tokens(a[1], "lse");
+  void* dx = nullptr;
+  int64_t ld = 0;
+  if (a[2] != Py_None) {
+    const at::Tensor& t = tensor(a[2], "dx");
+    on_device(t, H.device, "dx");
+    const int64_t shape[3] = {H.h.B, H.h.T, H.h.d};
+    if (dp_dtype_of(t, "dx") != H.h.dtype) throw Refused{"dx: the dtype of x expected"};
+    if (t.sizes() != c10::IntArrayRef(shape, 3)) throw Refused{"dx: shape " + shape_text({shape, 3}) + " expected, got " + shape_text(t.sizes())};
+    dx = t.data_ptr();
+    ld = row_stride(t, "dx");
+  }
+  float* sqnorm = H.examples(a[3], "sqnorm");
+  const Workspace w = workspace_of(a[5], H.device);
+  const On on(H.device, a[6]);
+  return api.vocab_loss_backward(&H.h, lse, dx, ld, sqnorm, truth(a[4]), w.p, w.n, on.stream);
+}
+int vocab_loss_clipped_accumulate(Args a) {  // head, lse, clip, acc_w, acc_b, workspace, stream
+  const Head H(a[0]);
+  const float *lse = H.tokens(a[1], "lse"), *clip = H.examples(a[2], "clip");
+  const int64_t table[2] = {H.h.V, H.h.d}, words[1] = {H.h.V};
+  auto* acc_w = static_cast<float*>(dense(a[3], H.device, at::kFloat, "acc_w", -1, table));
+  auto* acc_b = static_cast<float*>(dense(a[4], H.device, at::kFloat, "acc_b", -1, words));
+  const Workspace w = workspace_of(a[5], H.device);
+  const On on(H.device, a[6]);
+  return api.vocab_loss_clipped_accumulate(&H.h, lse, clip, acc_w, acc_b, w.p, w.n, on.stream);
+}
+int vocab_loss_cross_sqnorms(Args a) {       // head, lse, ids, g_emb, sqnorm, workspace, stream
+  const Head H(a[0]);
+  const float* lse = H.tokens(a[1], "lse");
+  const at::Tensor &ids = tensor(a[2], "ids"), &g = tensor(a[3], "g_emb");
+  if (ids.dim() != 2 || ids.size(0) != H.h.B) throw Refused{"ids: [" + std::to_string(H.h.B) + ", T] expected, got " + shape_text(ids.sizes())};
+  const int64_t shape[3] = {H.h.B, ids.size(1), H.h.d};
+  on_device(g, H.device, "g_emb");
+  if (dp_dtype_of(g, "g_emb") != H.h.dtype) throw Refused{"g_emb: the dtype of x expected"};
+  if (g.sizes() != c10::IntArrayRef(shape, 3)) throw Refused{"g_emb: shape " + shape_text({shape, 3}) + " expected, got " + shape_text(g.sizes())};
+  auto* at_ids = static_cast<const int32_t*>(dense(a[2], H.device, at::kInt, "ids"));
+  float* sqnorm = H.examples(a[4], "sqnorm");
+  const Workspace w = workspace_of(a[5], H.device);
+  const On on(H.device, a[6]);
+  return api.vocab_loss_cross_sqnorms(&H.h, lse, at_ids, g.data_ptr(), row_stride(g, "g_emb"), extent(ids.size(1)), sqnorm, w.p,
+                                      w.n, on.stream);
+}
+
+int distill_loss(Args a) {        // logits, top_ids, top_logits, temperature, loss, dlogits, token_weights, stream
+  const at::Tensor &z = tensor(a[0], "logits"), &ids = tensor(a[1], "top_ids"), &top = tensor(a[2], "top_logits");
+  const int device = device_of(z, "logits");
+  if (z.dim() != 3) throw Refused{"logits: [B, T, V] expected"};
+  if (ids.dim() != 3 || ids.size(0) != z.size(0) || ids.size(1) != z.size(1))
+    throw Refused{"top_ids: [" + std::to_string(z.size(0)) + ", " + std::to_string(z.size(1)) + ", K] expected, got " + shape_text(ids.sizes())};
+  dp_distill p = {};
+  p.dtype = dp_dtype_of(z, "logits");
+  p.teacher_dtype = dp_dtype_of(top, "top_logits");
+  const int64_t n = z.size(0) * z.size(1), tokens[2] = {z.size(0), z.size(1)};
+  p.N = extent(n);
+  p.V = extent(z.size(2));
+  p.K = extent(ids.size(2));
+  p.temperature = number(a[3]);
+  p.logits = z.data_ptr();
+  p.ld = row_stride(z, "logits");
+  p.top_ids = static_cast<const int32_t*>(dense(a[1], device, at::kInt, "top_ids"));
+  p.top_logits = dense(a[2], device, top.scalar_type(), "top_logits", -1, ids.sizes());
+  p.weights = static_cast<const float*>(dense(a[6], device, at::kFloat, "token_weights", -1, tokens));
+  auto* loss = static_cast<float*>(dense(a[4], device, at::kFloat, "loss", -1, tokens));
+  void* dz = nullptr;
+  int64_t ld = 0;
+  if (a[5] != Py_None) {
+    const at::Tensor& t = tensor(a[5], "dlogits");
+    on_device(t, device, "dlogits");
+    if (dp_dtype_of(t, "dlogits") != p.dtype || t.sizes() != z.sizes()) throw Refused{"dlogits: the shape and dtype of logits expected"};
+    dz = t.data_ptr();
+    ld = row_stride(t, "dlogits");
+  }
+  const On on(device, a[7]);
+  return api.distill_loss(&p, loss, dz, ld, on.stream);
+}
+
 // ---- module -------------------------------------------------------------------------------------------------------------
 PyObject* as_object(int rc) { return PyLong_FromLong(rc); }
 PyObject* as_object(PyObject* o) { return o; }
@@ -450,6 +608,8 @@ PyMethodDef methods[] = {
     ENTRY(rows_list, 1), ENTRY(rows_sqnorms, 4), ENTRY(rows_clipped_accumulate, 3),
     ENTRY(relpos_bias, 6), ENTRY(relpos_workspace_bytes, 2), ENTRY(relpos_bias_grad, 11),
     ENTRY(qknorm_rope, 12), ENTRY(qknorm_workspace_bytes, 2), ENTRY(qknorm_rope_backward, 18),
+    ENTRY(vocab_head, 5), ENTRY(vocab_workspace_bytes, 1), ENTRY(vocab_loss, 5), ENTRY(vocab_loss_backward, 7),
+    ENTRY(vocab_loss_clipped_accumulate, 7), ENTRY(vocab_loss_cross_sqnorms, 7), ENTRY(distill_loss, 8),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dp_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

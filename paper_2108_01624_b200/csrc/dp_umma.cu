@@ -26,6 +26,7 @@
 
 #include "dp_internal.h"
 #include "dp_ptx.cuh"
+#include "dp_tma.h"
 
 namespace dpk {
 using namespace ptx;
@@ -1205,23 +1206,6 @@ k_accum_pair(const __grid_constant__ UmmaParams P) {
 // =================================================================================================
 // Host side: tensor maps, work lists, launches
 // =================================================================================================
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver entry point is resolved at run time so that the library loads on machines without a driver.
-static EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
-  return fn;
-}
-
 // bf16 tensor [B, T, d] viewed as (x = 64 features, y = token, a = 64-feature group, z = example);
 // box = 64 x box_rows x groups x 1, 128-byte swizzle, out-of-range elements read as zero.
 static bool encode_map4(CUtensorMap* map, const void* base, int B, int T, int d, int box_rows, int groups) {
@@ -1285,14 +1269,12 @@ size_t umma_sqnorm_partials_per_example(const dp_layer* layers, const int* idx, 
   return c;
 }
 
-// Per-device facts, looked up once for each device a process drives (one process may drive several GPUs).
-constexpr int kMaxDevices = 64;
-static int current_device() {
+int current_device() {
   int dev = 0;
   return (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices) ? dev : -1;
 }
 
-static int sm_count() {
+int sm_count() {
   static int sms[kMaxDevices] = {};
   const int dev = current_device();
   if (dev < 0) return 148;
@@ -1586,7 +1568,8 @@ int launch_umma_accumulate(const dp_layer* layers, const int* idx, int n, const 
 // ---------------------------------------------------------------------------------------------
 int set_wait_limit_cycles(long long cycles) {
   if (cycles <= 0) cycles = kDefaultWaitLimitCycles;
-  return cudaMemcpyToSymbol(g_wait_limit_cycles, &cycles, sizeof(cycles)) == cudaSuccess ? DP_OK : DP_ERR_CUDA;
+  return cudaMemcpyToSymbol(g_wait_limit_cycles, &cycles, sizeof(cycles)) == cudaSuccess ? set_vocab_wait_limit(cycles)
+                                                                                         : DP_ERR_CUDA;
 }
 
 // One CTA whose two waiters poll a barrier that nobody ever arrives on, through the same bounded wait as the

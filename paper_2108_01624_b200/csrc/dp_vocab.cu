@@ -1,0 +1,1164 @@
+// Softmax cross entropy of tokens X [N, d] against a vocabulary table W [V, d] and a bias, without keeping the logits:
+//   z = X W^T + bias,  lse_n = log sum_v exp z_nv,  loss_n = w_n (lse_n - z_n,label)
+//   G_nv = w_n (exp(z_nv - lse_n) - [v = label_n])
+//   dX = G W,   |G_i^T X_i|^2 (+ |sum_t G_i|^2) of every example i,   acc += sum_i clip_i G_i^T X_i.
+//
+// k_vocab_gemm is one tensor-core kernel in four forms:
+//   LSE    z tile by tile; the epilogue keeps a row's maximum and its sum of exponentials over the tile's columns
+//   GRAD   z again; the epilogue turns it into G and stores it, for a piece of the vocabulary at a time
+//   DX     dX = G W over the piece
+//   DW     acc += G^T X over the piece
+// All are bound by the tensor cores where there are enough tokens (256 x 20 tokens of width 1024 and 30522 words are 0.32
+// TFLOP a product), and by reading the table where there are few.
+//
+// Exactness.  A product of bf16 numbers is exact in fp32 and the tensor cores sum in fp32, but drop low bits at every
+// step of 16: a sum of 64 steps comes out 7e-7 too small.  So
+//   - a sum longer than `seg` blocks is taken over by the epilogue, which adds its parts in registers;
+//   - the label's own logit is formed by itself, in fp64: loss = w log1p(exp(lse of the others - z_label)) and
+//     G_label = w expm1(z_label - lse) keep their relative error where the model is sure of the label;
+//   - G is held as two bf16 numbers, hi + lo, 2^-17 of it: rows (token, plane) of G meet rows (token, plane) of X in the
+//     sums over tokens, whose results are fp32.  dX in bf16 reads hi alone: its own rounding is as large.
+//   - fp32 X and W are split into three bf16 numbers each for the logits (24 bits; six products, the smallest first) and
+//     into two for the products with G (2^-17 again, four products).
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "dp_chain.cuh"
+#include "dp_internal.h"
+#include "dp_ptx.cuh"
+#include "dp_tma.h"
+
+namespace dpk {
+using namespace ptx;
+
+enum : int { V_LSE = 0, V_GRAD = 1, V_DX = 2, V_DW = 3 };
+
+constexpr int V_THREADS = 320;                  // warp 0 TMA, warp 1 UMMA issue (or forwarding), warps 2..9 epilogue
+constexpr int V_TILE = 256;                     // rows and columns of a pair's tile; a CTA holds 128 rows of it
+constexpr int V_BOX_BYTES = 128 * 128;          // one copy: 64 bf16 columns of 128 rows, 128-byte swizzle
+constexpr int V_STAGE_COLS = 32;                // GRAD: columns that a warp hands over at a time
+constexpr int V_WARP_STAGE = 32 * 2 * V_STAGE_COLS * 2;   // 32 tokens x 2 planes, 64-byte rows
+constexpr int V_BIAS_BYTES = 8 * 128 * 4;       // every epilogue warp's 128 bias values
+constexpr float kLog2e = 1.4426950408889634f;
+
+// K columns (or rows) of a stage and stages in flight.
+template <int MODE> struct VForm {
+  static constexpr bool KMAJOR_A = MODE != V_DW;               // rows of A are tokens with K contiguous
+  static constexpr bool KMAJOR_B = MODE == V_LSE || MODE == V_GRAD;
+  static constexpr int BK = KMAJOR_B ? 64 : 128;
+  static constexpr int STAGES = MODE == V_LSE ? 6 : MODE == V_GRAD ? 5 : 3;
+  static constexpr int HALF_BYTES = BK / 64 * V_BOX_BYTES;     // 128 rows (columns) of one operand
+  static constexpr int STAGE_BYTES = 2 * HALF_BYTES;
+};
+
+struct VCtl {
+  uint64_t full[6], empty[6], ready[6], tmem_full[2], tmem_empty[2], drain;
+  uint32_t tmem_base;
+  int abort;
+};
+
+template <int MODE> constexpr int v_smem() {
+  return 1024 + VForm<MODE>::STAGES * VForm<MODE>::STAGE_BYTES + V_BIAS_BYTES + (MODE == V_GRAD ? 8 * V_WARP_STAGE : 0) +
+         (int)sizeof(VCtl);
+}
+static_assert(v_smem<V_LSE>() <= 232448 && v_smem<V_GRAD>() <= 232448 && v_smem<V_DX>() <= 232448, "over a CTA's shared memory");
+
+struct alignas(64) VParams {
+  CUtensorMap a[3], b[3];        // operand planes
+  CUtensorMap st;                // GRAD: G
+  int n_pairs;
+  unsigned char pa[8], pb[8];    // planes of each product, smallest product first
+  int kb;                        // K blocks of one product
+  int seg;                       // K blocks that are summed before the epilogue takes over
+  int tiles_m, tiles_n, nt;      // nt: columns of a tile, 256 or 128
+  int units;                     // CTA pairs that share the work
+  int M, N;                      // rows and columns that exist
+  int sub;                       // columns of one block of G (GRAD, DX, DW)
+  int v0, V;                     // first vocabulary entry of the piece, entries in all
+  int planes2;                   // GRAD: store rows 2, 3 of a token too (fp32 X: two planes)
+  int stride_c;                  // leading dimension of the output is stride_c (DX, DW)
+  const float* bias;             // LSE, GRAD: [V] or null
+  const int32_t* labels;         // LSE
+  const float4* meta;            // GRAD: lse, scale, G at the label, label (bits) of every token
+  float2* part;                  // LSE: [2 tiles_n][M] maximum and sum
+  float* bias_part;              // GRAD: [rows of 32 tokens][columns of the piece] column sums, or null
+  float* slots;                  // DX, DW: tiles that several pairs share, [2 units][256][256]
+  float* sum;                    // DX: fp32 sums over the pieces [M, N]; DW: the accumulator
+  void* out;                     // DX: the result
+  int out_bf16, first, last, vec;
+  int* status;
+};
+
+struct VWork { int tile, j0, j1; };
+
+// What the pair does next: whole tiles in turn (LSE, GRAD), or its share of the line of all tiles' K blocks (DX, DW).
+template <int MODE>
+__device__ __forceinline__ bool next_work(const VParams& P, long long& pos, long long hi, VWork& w) {
+  const int nkb = P.n_pairs * P.kb;
+  if (pos >= hi) return false;
+  if (MODE == V_LSE || MODE == V_GRAD) {
+    w = {(int)pos, 0, nkb};
+    pos += P.units;
+    return true;
+  }
+  w.tile = (int)(pos / nkb);
+  w.j0 = (int)(pos - (long long)w.tile * nkb);
+  const long long end = (long long)(w.tile + 1) * nkb < hi ? (long long)(w.tile + 1) * nkb : hi;
+  w.j1 = w.j0 + (int)(end - pos);
+  pos = end;
+  return true;
+}
+__host__ __device__ __forceinline__ long long share_begin(long long total, int units, int u) { return total * u / units; }
+
+template <int MODE>
+__device__ __forceinline__ void tile_origin(const VParams& P, int tile, int& m0, int& n0) {
+  if (MODE == V_LSE || MODE == V_GRAD) {        // the tiles of a column block of W follow one another
+    n0 = tile / P.tiles_m;
+    m0 = tile - n0 * P.tiles_m;
+  } else {                                      // the tiles of a row block of G follow one another
+    m0 = tile / P.tiles_n;
+    n0 = tile - m0 * P.tiles_n;
+  }
+  m0 *= V_TILE;
+  n0 *= P.nt;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void load2(uint8_t* dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void store4(const CUtensorMap* map, const void* src, int x, int y, int z, int w) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// Copies of K block j of a tile into a stage: this CTA's 128 rows of A and its half of the columns of B.
+template <int MODE>
+__device__ __forceinline__ void load_block(const VParams& P, uint8_t* st, uint64_t* bar, int j, int m0, int n0, int rank) {
+  using F = VForm<MODE>;
+  const int pair = j / P.kb, k = (j - pair * P.kb) * F::BK;
+  const CUtensorMap *a = &P.a[P.pa[pair]], *b = &P.b[P.pb[pair]];
+  const int m = m0 + 128 * rank, n = n0 + (P.nt >> 1) * rank;
+  uint8_t* sb = st + F::HALF_BYTES;
+  if (MODE == V_LSE || MODE == V_GRAD) {
+    load2(st, a, bar, k, m);
+    load2(sb, b, bar, k, n);
+  } else if (MODE == V_DX) {                    // A: columns of G, block by block; B: rows of W
+    const int z = k / P.sub, x = k - z * P.sub;
+    tma_load_3d(st, a, bar, x, m, z);
+    tma_load_3d(st + V_BOX_BYTES, a, bar, x + 64, m, z);
+    load2(sb, b, bar, n, P.v0 + k);
+    if (P.nt == 256) load2(sb + V_BOX_BYTES, b, bar, n + 64, P.v0 + k);
+  } else {                                      // A: rows of G; B: rows of X
+    const int z = m / P.sub, x = m - z * P.sub;
+    tma_load_3d(st, a, bar, x, k, z);
+    tma_load_3d(st + V_BOX_BYTES, a, bar, x + 64, k, z);
+    load2(sb, b, bar, n, k);
+    if (P.nt == 256) load2(sb + V_BOX_BYTES, b, bar, n + 64, k);
+  }
+}
+
+// Row maximum and sum of exponentials over this thread's 128 columns of logits, the label's left out.
+__device__ __forceinline__ void finish_lse(const VParams& P, float (&z)[128], const float* bias, int m, int n0, int col, int label) {
+  const int rel = label - (n0 + col);
+  const bool here = (unsigned)rel < 128u;
+#pragma unroll
+  for (int j = 0; j < 128; j += 4) {
+    const float4 b = *reinterpret_cast<const float4*>(bias + j);
+    z[j] += b.x;
+    z[j + 1] += b.y;
+    z[j + 2] += b.z;
+    z[j + 3] += b.w;
+  }
+  if (__any_sync(0xffffffffu, here)) {
+#pragma unroll
+    for (int j = 0; j < 128; ++j) z[j] = rel == j ? -INFINITY : z[j];
+  }
+  float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+  for (int j = 4; j < 128; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
+  const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  const float base = most == -INFINITY ? 0.0f : most;       // a row of -inf keeps exponentials of -inf: 0
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 128; ++j) s[j & 3] += ex2((z[j] - base) * kLog2e);
+  if (m < P.M) P.part[(size_t)((n0 + col) >> 7) * P.M + m] = make_float2(most, (s[0] + s[1]) + (s[2] + s[3]));
+}
+
+// G of this thread's 128 columns: two planes through shared memory, 32 columns at a time, and the warp's column sums.
+__device__ __forceinline__ void finish_grad(const VParams& P, float (&z)[128], const float* bias, uint8_t* stage, float4 meta,
+                                            int m0w, int n0, int col, int lane) {
+  const int label = __float_as_int(meta.w), rel = label - (P.v0 + n0 + col);
+  const bool live = label >= 0;
+  const int at = n0 + col, z4 = at / P.sub, x4 = at - z4 * P.sub;
+#pragma unroll
+  for (int ch = 0; ch < 4; ++ch) {
+    float g[32];
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 b = *reinterpret_cast<const float4*>(bias + ch * 32 + j);
+      const float bb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float p = meta.y * ex2((z[ch * 32 + j + u] + bb[u] - meta.x) * kLog2e);
+        g[j + u] = live ? p : 0.0f;
+      }
+    }
+    if (__any_sync(0xffffffffu, live && (unsigned)(rel - ch * 32) < 32u)) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) g[j] = live && rel == ch * 32 + j ? meta.z : g[j];
+    }
+    if (lane == 0) store_wait_read();           // the copy of the chunk before has left the staging rows
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {               // 16 bytes = 8 columns
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float x = g[c * 8 + 2 * u], y = g[c * 8 + 2 * u + 1];
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        hi[u] = *reinterpret_cast<const uint32_t*>(&h);
+        const __nv_bfloat162 l = __floats2bfloat162_rn(x - __uint_as_float(hi[u] << 16), y - __uint_as_float(hi[u] & 0xffff0000u));
+        lo[u] = *reinterpret_cast<const uint32_t*>(&l);
+      }
+      uint8_t* p = stage + lane * 128 + ((c ^ (lane & 3)) << 4);       // 64-byte swizzle: rows 2 lane and 2 lane + 1
+      *reinterpret_cast<uint4*>(p) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(p + 64) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0 && m0w < P.M) {
+      store4(&P.st, stage, x4 + ch * 32, 0, m0w, z4);
+      if (P.planes2) store4(&P.st, stage, x4 + ch * 32, 2, m0w, z4);
+    }
+    if (lane == 0) store_commit();
+    if (P.bias_part) {
+      // sum over the warp's 32 tokens: at every step a lane keeps half of its columns and hands the others over, so
+      // that lane l ends with column l
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int j = 0; j < o; ++j) {
+          const float keep = up ? g[j + o] : g[j], give = up ? g[j] : g[j + o];
+          g[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+      P.bias_part[(size_t)(m0w >> 5) * P.N + at + ch * 32 + lane] = g[0];
+    }
+  }
+}
+
+// One row's `n` (32) columns from column c on of dX: summed over the pieces so far, rounded after the last.
+__device__ __forceinline__ void put_dx(const VParams& P, int m, int c, const float* v) {
+  if (m >= P.M || c >= P.N) return;
+  const size_t at = (size_t)m * P.N + c;
+  const int n = P.N - c < 32 ? P.N - c : 32;
+  float x[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) x[j] = v[j];
+  if (!P.first) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j < n) x[j] += P.sum[at + j];
+  }
+  if (!P.last) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j < n) P.sum[at + j] = x[j];
+    return;
+  }
+  const size_t to = (size_t)m * P.stride_c + c;
+  if (P.out_bf16) {
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(P.out) + to;
+    if (P.vec && n == 32) {
+#pragma unroll
+      for (int j = 0; j < 32; j += 8) {
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) h[u] = __floats2bfloat162_rn(x[j + 2 * u], x[j + 2 * u + 1]);
+        *reinterpret_cast<uint4*>(o + j) = *reinterpret_cast<const uint4*>(h);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j < n) o[j] = __float2bfloat16_rn(x[j]);
+    }
+  } else {
+    float* o = static_cast<float*>(P.out) + to;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j < n) o[j] = x[j];
+  }
+}
+
+// acc += for one row's 32 columns from column c on.  An element has one writer per launch.
+__device__ __forceinline__ void put_dw(const VParams& P, int m, int c, const float* v) {
+  const int row = P.v0 + m;
+  if (row >= P.V || c >= P.N) return;
+  float* o = P.sum + (size_t)row * P.stride_c + c;
+  if (P.vec && c + 32 <= P.N) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 4)
+      asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(o + j), "f"(v[j]), "f"(v[j + 1]), "f"(v[j + 2]), "f"(v[j + 3]) : "memory");
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (c + j < P.N) atomicAdd(o + j, v[j]);
+  }
+}
+
+template <int MODE>
+__global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_constant__ VParams P) {
+  extern __shared__ uint8_t smem_raw[];
+  wait_for_predecessor();
+  let_successor_in();
+  using F = VForm<MODE>;
+  constexpr int STAGES = F::STAGES;
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* staging = tiles + STAGES * F::STAGE_BYTES;                      // GRAD only
+  float* bias_s = reinterpret_cast<float*>(staging + (MODE == V_GRAD ? 8 * V_WARP_STAGE : 0));
+  VCtl* S = reinterpret_cast<VCtl*>(reinterpret_cast<uint8_t*>(bias_s) + V_BIAS_BYTES);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abort_flag = &S->abort;
+  const int rank = (int)cluster_ctarank(), unit = (int)cluster_id_x();
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(&S->full[s], 1); mbar_init(&S->empty[s], 1); mbar_init(&S->ready[s], 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&S->tmem_full[b], 1); mbar_init(&S->tmem_empty[b], 16); }
+    mbar_init(&S->drain, 1);
+    S->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) { tmem_alloc_pair(&S->tmem_base, 512); tmem_relinquish_pair(); }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();           // the peer's barriers are initialised before anyone signals them
+  tc_fence_after();
+  const uint32_t tmem_base = S->tmem_base;
+  const long long tiles_all = (long long)P.tiles_m * P.tiles_n;
+  const bool whole = MODE == V_LSE || MODE == V_GRAD;
+  const long long line = whole ? tiles_all : tiles_all * P.n_pairs * P.kb;
+  const long long lo = whole ? unit : share_begin(line, P.units, unit);
+  const long long hi = whole ? line : share_begin(line, P.units, unit + 1);
+  long long pos = lo;
+  VWork w;
+
+  if (warp == 0) {
+    if (lane == 0) {   // ---------------- TMA producer (each CTA, its own halves) ----------------
+      uint32_t it = 0;
+      bool alive = true;
+      const uint32_t tx = (uint32_t)(F::HALF_BYTES + (!F::KMAJOR_B && P.nt == 128 ? V_BOX_BYTES : F::HALF_BYTES));
+      while (alive && next_work<MODE>(P, pos, hi, w)) {
+        int m0, n0;
+        tile_origin<MODE>(P, w.tile, m0, n0);
+        for (int j = w.j0; j < w.j1; ++j, ++it) {
+          const uint32_t slot = it % STAGES, ph = (it / STAGES) & 1u;
+          if (!mbar_wait(&S->empty[slot], ph ^ 1u, abort_flag, P.status, 61, (int)it)) { alive = false; break; }
+          mbar_arrive_expect_tx(&S->full[slot], tx);
+          load_block<MODE>(P, tiles + slot * F::STAGE_BYTES, &S->full[slot], j, m0, n0, rank);
+        }
+      }
+      const uint32_t pending = it < (uint32_t)STAGES ? it : (uint32_t)STAGES;
+      for (uint32_t k = 0; k < pending; ++k) {
+        const uint32_t j = it - 1 - k;
+        mbar_wait_drain(&S->full[j % STAGES], (j / STAGES) & 1u, P.status);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 1) {   // ---------------- odd CTA: forward "stage landed" to the issuer ----------------
+      uint32_t it = 0;
+      bool alive = true;
+      while (alive && next_work<MODE>(P, pos, hi, w)) {
+        for (int j = w.j0; j < w.j1; ++j, ++it) {
+          const uint32_t slot = it % STAGES, ph = (it / STAGES) & 1u;
+          if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 62, (int)it)) { alive = false; break; }
+          mbar_arrive_cluster(&S->ready[slot], 0u);
+        }
+      }
+    } else if (lane == 0) {   // ---------------- even CTA: UMMA issuer ----------------
+      const uint32_t idesc = idesc_bf16_f32(256, P.nt, !F::KMAJOR_A, !F::KMAJOR_B);
+      uint32_t it = 0, part = 0;
+      bool alive = true;
+      while (alive && next_work<MODE>(P, pos, hi, w)) {
+        for (int j0 = w.j0; j0 < w.j1 && alive; j0 += P.seg, ++part) {
+          const int j1 = j0 + P.seg < w.j1 ? j0 + P.seg : w.j1;
+          const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
+          if (!mbar_wait(&S->tmem_empty[buf], tph ^ 1u, abort_flag, P.status, 63, (int)part)) { alive = false; break; }
+          tc_fence_after();
+          const uint32_t d_tmem = tmem_base + buf * 256u;
+          for (int j = j0; j < j1; ++j, ++it) {
+            const uint32_t slot = it % STAGES, ph = (it / STAGES) & 1u;
+            if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 64, (int)it) ||
+                !mbar_wait(&S->ready[slot], ph, abort_flag, P.status, 65, (int)it)) {
+              alive = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t am = smem_u32(tiles + slot * F::STAGE_BYTES), an = am + F::HALF_BYTES;
+#pragma unroll
+            for (int k = 0; k < F::BK / 16; ++k) {
+              const uint64_t ad = F::KMAJOR_A ? smem_desc_sw128(am + (k >> 2) * V_BOX_BYTES + (k & 3) * 32, 16, 1024)
+                                              : smem_desc_sw128(am + k * 2048, V_BOX_BYTES, 1024);
+              const uint64_t bd = F::KMAJOR_B ? smem_desc_sw128(an + k * 32, 16, 1024)
+                                              : smem_desc_sw128(an + k * 2048, V_BOX_BYTES, 1024);
+              umma_bf16_pair(d_tmem, ad, bd, idesc, (j > j0 || k > 0) ? 1u : 0u);
+            }
+            umma_commit_pair(&S->empty[slot], (uint16_t)3);
+          }
+          if (alive) umma_commit_pair(&S->tmem_full[buf], (uint16_t)3);
+        }
+      }
+      umma_commit_pair(&S->drain, (uint16_t)1);
+      mbar_wait_drain(&S->drain, 0u, P.status);
+    }
+  } else {   // ---------------- epilogue warps 2..9: lanes [32 q, +32), columns [h nt/2, +nt/2) ----------------
+    const int q = warp & 3, h = warp >= 6 ? 1 : 0;
+    const int half = P.nt >> 1;
+    float* bias_w = bias_s + (warp - 2) * 128;
+    uint8_t* stage = staging + (warp - 2) * V_WARP_STAGE;
+    uint32_t part = 0;
+    bool alive = true;
+    while (next_work<MODE>(P, pos, hi, w)) {
+      int m0, n0;
+      tile_origin<MODE>(P, w.tile, m0, n0);
+      const int m0w = m0 + 128 * rank + 32 * q, m = m0w + lane, col = h * half;
+      float4 meta = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+      int label = -1;
+      if (MODE == V_LSE && m < P.M) label = P.labels[m];
+      if (MODE == V_GRAD && m < P.M) meta = P.meta[m];
+      if (whole) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {           // -inf beyond the vocabulary: no weight in a sum, zero in G
+          const int v = P.v0 + n0 + col + 32 * k + lane;
+          bias_w[32 * k + lane] = v >= P.V ? -INFINITY : P.bias ? P.bias[v] : 0.0f;
+        }
+        __syncwarp();
+      }
+      float acc[128];
+#pragma unroll
+      for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+      for (int j0 = w.j0; j0 < w.j1; j0 += P.seg, ++part) {
+        const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
+        if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[buf], tph, abort_flag, P.status, 66, (int)part));
+        if (!alive) continue;
+        tc_fence_after();
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          if (whole || ch * 32 < half) {
+            uint32_t v[32];
+            tmem_ld_32x32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * 256u + (uint32_t)(col + ch * 32), v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[ch * 32 + j] += __uint_as_float(v[j]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(&S->tmem_empty[buf], 0u);
+      }
+      if (!alive) continue;
+      if constexpr (MODE == V_LSE) {
+        finish_lse(P, acc, bias_w, m, n0, col, label);
+      } else if constexpr (MODE == V_GRAD) {
+        finish_grad(P, acc, bias_w, stage, meta, m0w, n0, col, lane);
+      } else {
+        const bool shared_tile = w.j0 != 0 || w.j1 != P.n_pairs * P.kb;
+        const int slot = 2 * unit + ((long long)w.tile * (P.n_pairs * P.kb) > lo ? 1 : 0);
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          if (ch * 32 >= half) continue;
+          const int c = n0 + col + ch * 32;
+          if (shared_tile) {
+            float* to = P.slots + ((size_t)slot * V_TILE + (m - m0)) * V_TILE + col + ch * 32;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              *reinterpret_cast<float4*>(to + j) = make_float4(acc[ch * 32 + j], acc[ch * 32 + j + 1], acc[ch * 32 + j + 2], acc[ch * 32 + j + 3]);
+          } else if constexpr (MODE == V_DX) {
+            put_dx(P, m, c, acc + ch * 32);
+          } else {
+            put_dw(P, m, c, acc + ch * 32);
+          }
+        }
+      }
+      if (whole) __syncwarp();                  // everyone has read the bias values
+    }
+    if (MODE == V_GRAD && lane == 0) store_wait_all();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();           // neither CTA leaves while the other may still read its memory or signal it
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// The tiles of a DX or DW launch that several pairs shared: their parts are added in the pairs' order.  Block (u, r): the
+// tile that begins inside or before unit u's share and goes on into it, rows [16 r, +16); a tile is handled by the
+// first unit that continues it.
+template <int MODE>
+__global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VParams P) {
+  wait_for_predecessor();
+  let_successor_in();
+  const int nkb = P.n_pairs * P.kb;
+  const long long line = (long long)P.tiles_m * P.tiles_n * nkb;
+  const int u0 = blockIdx.x + 1;
+  const long long lo = share_begin(line, P.units, u0);
+  const long long tile = lo / nkb;
+  if (lo == tile * nkb || lo >= line) return;                       // a unit that begins with a tile of its own
+  if (share_begin(line, P.units, u0 - 1) > tile * nkb) return;      // an earlier unit continues this tile already
+  int m0, n0;
+  tile_origin<MODE>(P, (int)tile, m0, n0);
+  const int r = blockIdx.y * 16 + (threadIdx.x >> 4), c = (threadIdx.x & 15) * 16;   // 16 columns a thread
+  if (c >= P.nt) return;
+  float v[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+  for (int u = u0 - 1; u < P.units; ++u) {
+    const long long b = share_begin(line, P.units, u);
+    if (b >= (tile + 1) * nkb) break;
+    const int slot = 2 * u + (tile * nkb > b ? 1 : 0);
+    const float* from = P.slots + ((size_t)slot * V_TILE + r) * V_TILE + c;
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(from + j);
+      v[j] += x.x;
+      v[j + 1] += x.y;
+      v[j + 2] += x.z;
+      v[j + 3] += x.w;
+    }
+  }
+  const int m = m0 + r;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const int cc = n0 + c + j;
+    if (MODE == V_DX) {
+      if (m >= P.M || cc >= P.N) break;
+      const size_t at = (size_t)m * P.N + cc;
+      const float x = P.first ? v[j] : v[j] + P.sum[at];
+      if (!P.last) P.sum[at] = x;
+      else if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[(size_t)m * P.stride_c + cc] = __float2bfloat16_rn(x);
+      else static_cast<float*>(P.out)[(size_t)m * P.stride_c + cc] = x;
+    } else {
+      if (P.v0 + m >= P.V || cc >= P.N) break;
+      P.sum[(size_t)(P.v0 + m) * P.stride_c + cc] += v[j];
+    }
+  }
+}
+
+// ---- what surrounds the products ------------------------------------------------------------------------------------
+struct VHead {                   // dp_vocab_head with its sizes worked out
+  const void* x;
+  const void* w;
+  const float* bias;
+  const int32_t* labels;
+  const float* weights;
+  long long ldx, ldw;
+  int N, T, d, V, f32;
+};
+
+__device__ __forceinline__ float element(const VHead& H, const void* p, long long i) {
+  return H.f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+// A label that takes part: -1 for none, and for one beyond the vocabulary, which is reported.
+__device__ __forceinline__ int label_of(const VHead& H, int n, int* status) {
+  const int y = H.labels[n];
+  if (y >= H.V) {
+    atomicCAS(status, 0, (int)STATUS_BAD_ID);
+    return -1;
+  }
+  return y < 0 ? -1 : y;
+}
+// <x_n, W_y> + bias_y in fp64, by one warp; every lane gets it.
+__device__ __forceinline__ double label_logit(const VHead& H, int n, int y, int lane) {
+  double s = 0.0;
+  const long long xr = (long long)n * H.ldx, wr = (long long)y * H.ldw;
+  for (int k = lane; k < H.d; k += 32) s = fma((double)element(H, H.x, xr + k), (double)element(H, H.w, wr + k), s);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return H.bias ? s + (double)H.bias[y] : s;
+}
+
+// A bf16 number and what it leaves of x.
+__device__ __forceinline__ __nv_bfloat16 split_off(float& x) {
+  const __nv_bfloat16 h = __float2bfloat16_rn(x);
+  x -= __bfloat162float(h);
+  return h;
+}
+
+// Planes of a matrix [rows, d]: out[plane][row][dp], zeros beyond d.  (fp32: three, bf16: one, where the tensor's own
+// rows cannot be copied by TMA.)
+__global__ void __launch_bounds__(256)
+k_vocab_planes(const void* src, long long ld, int rows, int d, int dp, int f32, int planes, __nv_bfloat16* out) {
+  wait_for_predecessor();
+  let_successor_in();
+  const long long total = (long long)rows * dp, plane = total;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const long long r = i / dp;
+    const int c = (int)(i - r * dp);
+    float x = 0.0f;
+    if (c < d) x = f32 ? static_cast<const float*>(src)[r * ld + c] : __bfloat162float(static_cast<const __nv_bfloat16*>(src)[r * ld + c]);
+    for (int p = 0; p < planes; ++p) out[p * plane + i] = split_off(x);
+  }
+}
+
+// A warp per token: its row of X as R rows of planes (zeros where it has no label: what such a row holds may be
+// anything), the third plane of fp32 apart, and lse, scale, G at the label, label.  Column `one` (-1: none) beyond X's is a
+// one: with it as X's last column the norm of G^T X holds the bias' part (as that of W, whose column d is zero, it leaves
+// the logits alone).
+__global__ void __launch_bounds__(256)
+k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* clip, int R, int dp, int one, __nv_bfloat16* xe,
+               __nv_bfloat16* x2, float4* meta, int* status) {
+  wait_for_predecessor();
+  let_successor_in();
+  const int n = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (n >= H.N) return;
+  const int y = label_of(H, n, status);
+  for (int c = lane; c < dp; c += 32) {
+    float x = y >= 0 && c < H.d ? element(H, H.x, (long long)n * H.ldx + c) : c == one ? 1.0f : 0.0f;
+    const __nv_bfloat16 p0 = split_off(x);
+    __nv_bfloat16* row = xe + (size_t)n * R * dp + c;
+    row[0] = row[dp] = p0;
+    if (R == 4) {
+      row[2 * dp] = row[3 * dp] = split_off(x);
+      x2[(size_t)n * dp + c] = split_off(x);
+    }
+  }
+  float4 m = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+  if (y >= 0) {
+    const double z = label_logit(H, n, y, lane);
+    float scale = H.weights ? H.weights[n] : 1.0f;
+    if (clip) scale *= clip[n / H.T];
+    m = make_float4(lse[n], scale, scale * expm1f((float)(z - (double)lse[n])), __int_as_float(y));
+  }
+  if (lane == 0) meta[n] = m;
+}
+
+// lse and loss of a token from the parts over the column blocks, which leave the label out.  32 tokens a block: eight
+// strands of threads take every eighth part each; then a warp per token forms the label's logit.
+__global__ void __launch_bounds__(256)
+k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, float* loss, float* lse, int* status) {
+  __shared__ float2 s[8][33];
+  wait_for_predecessor();
+  let_successor_in();
+  const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
+  const int n0 = blockIdx.x * 32;
+  float most = -INFINITY, sum = 0.0f;
+  if (n0 + lane < H.N) {
+#pragma unroll 4
+    for (int p = strand; p < parts; p += 8) {
+      const float2 v = part[(size_t)p * H.N + n0 + lane];
+      const float top = fmaxf(most, v.x);
+      if (top != -INFINITY) {
+        sum = sum * ex2((most - top) * kLog2e) + v.y * ex2((v.x - top) * kLog2e);
+        most = top;
+      } else {
+        sum += v.y;                             // 0, or NaN
+      }
+    }
+  }
+  s[strand][lane] = make_float2(most, sum);
+  __syncthreads();
+  for (int k = strand; k < 32; k += 8) {        // token n0 + k
+    const int n = n0 + k;
+    if (n >= H.N) break;
+    const int y = label_of(H, n, status);
+    if (y < 0) {
+      if (lane == 0) loss[n] = lse[n] = 0.0f;
+      continue;
+    }
+    const float2 v = lane < 8 ? s[lane][k] : make_float2(-INFINITY, 0.0f);
+    float top = v.x;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float all = top == -INFINITY ? v.y : v.y * ex2((v.x - top) * kLog2e);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    const double z = label_logit(H, n, y, lane);
+    if (lane == 0) {
+      const double others = (double)top + (double)logf(all);           // -inf where there are none
+      const float gap = (float)(others - z);
+      float l = gap > 0.0f ? gap + log1pf(expf(-gap)) : log1pf(expf(gap));
+      if (z == INFINITY) l = NAN;               // as any other infinite logit
+      loss[n] = (H.weights ? H.weights[n] : 1.0f) * l;
+      lse[n] = (float)(z == -INFINITY ? others : z + (double)l);
+    }
+  }
+}
+
+// acc_b[v] += the sum over rows of part[row][v]: 32 columns a block, eight strands of rows, added in order.
+__global__ void __launch_bounds__(256) k_vocab_bias(const float* part, int rows, int cols, int n, float* acc_b) {
+  __shared__ float s[8][33];
+  wait_for_predecessor();
+  let_successor_in();
+  const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  float sum = 0.0f;
+#pragma unroll 8
+  for (int r = strand; r < rows; r += 8) sum += part[(size_t)r * cols + c];
+  s[strand][lane] = sum;
+  __syncthreads();
+  if (strand == 0 && c < n) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) sum += s[k][lane];
+    acc_b[c] += sum;
+  }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------------
+int set_vocab_wait_limit(long long cycles) {
+  return cudaMemcpyToSymbol(g_wait_limit_cycles, &cycles, sizeof(cycles)) == cudaSuccess ? DP_OK : DP_ERR_CUDA;
+}
+
+static bool vocab_kernels_ready() {
+  static signed char state[kMaxDevices] = {};     // 0 unknown, 1 ready, -1 failed
+  const int dev = current_device();
+  if (dev < 0) return false;
+  if (!state[dev]) {
+    const auto opt = [](const void* k, int bytes) {
+      return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+    };
+    state[dev] = (opt((const void*)k_vocab_gemm<V_LSE>, v_smem<V_LSE>()) && opt((const void*)k_vocab_gemm<V_GRAD>, v_smem<V_GRAD>()) &&
+                  opt((const void*)k_vocab_gemm<V_DX>, v_smem<V_DX>()) && opt((const void*)k_vocab_gemm<V_DW>, v_smem<V_DW>())) ? 1 : -1;
+  }
+  return state[dev] > 0;
+}
+
+// A bf16 tensor of up to four dimensions, innermost first; strides (bytes) of dimensions 1.. .
+static bool encode(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                   const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn fn = encode_fn();
+  const cuuint32_t ones[4] = {1u, 1u, 1u, 1u};
+  return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Boxes of 64 columns x 128 rows of [rows, cols] with a row stride in elements.
+static bool encode_rows(CUtensorMap* map, const void* base, long long rows, int cols, long long ld) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {64u, 128u};
+  return encode(map, base, 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// The same of every block of G [blocks][rows, ld][sub].
+static bool encode_blocks(CUtensorMap* map, const void* base, long long rows, int sub, long long ld, int blocks, long long block) {
+  const cuuint64_t dims[3] = {(cuuint64_t)sub, (cuuint64_t)rows, (cuuint64_t)blocks};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)block * 2};
+  const cuuint32_t box[3] = {64u, 128u, 1u};
+  return encode(map, base, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+constexpr int kSubColumns = 2048;               // columns of one block of G, at most
+constexpr size_t kPieceBytes = (size_t)256 << 20;   // G of one piece, unless one block alone is larger
+
+// Sizes and the workspace of a call.
+struct VPlan {
+  int R;                         // rows of X and G per token: 2, or 4 for fp32
+  int dp;                        // width of packed rows
+  bool direct;                   // X and W can be copied by TMA as they are
+  int sub, n_sub, piece_subs, pieces;
+  int mt;                        // 256-token tiles
+  size_t part, xe, x2, xp, wp, meta, G, slots, dx, gram, cols, bias, total;
+  int gram_count;                // partial sums per example of one piece
+  bool gram_way;
+};
+
+static bool direct_rows(const void* p, long long ld) { return !misaligned(p, 16) && ld % 8 == 0; }
+
+static dp_layer piece_layer(const dp_vocab_head& h, const VPlan& p, const void* xe, const void* G) {
+  dp_layer L = {};
+  L.kind = DP_LINEAR;
+  L.dtype = DP_BF16;
+  L.path = DP_PATH_AUTO;
+  L.has_bias = h.bias && p.R == 2;     // a column of ones stands for it where tokens have rows of several planes of X
+  L.B = h.B;
+  L.T = h.T * p.R;
+  L.d_in = p.dp;
+  L.d_out = p.sub;
+  L.A = xe;
+  L.G = G;
+  return L;
+}
+
+// op: 0 loss, 1 backward, 2 clipped sum
+static VPlan plan_vocab(const dp_vocab_head& h, int op) {
+  VPlan p = {};
+  const long long N = (long long)h.B * h.T;
+  const bool f32 = h.dtype == DP_F32;
+  p.R = f32 ? 4 : 2;
+  p.dp = (h.d + (f32 && h.bias && op == 1 ? 1 : 0) + 63) / 64 * 64;
+  p.direct = !f32 && direct_rows(h.W, h.ldw) && (op != 0 || direct_rows(h.X, h.ldx));
+  p.n_sub = ceil_div(h.V, kSubColumns);
+  p.sub = (ceil_div(h.V, p.n_sub) + 255) / 256 * 256;
+  p.n_sub = ceil_div(h.V, p.sub);
+  p.mt = (int)((N + V_TILE - 1) / V_TILE);
+  size_t at = 0;
+  const auto take = [&](size_t& off, size_t bytes) {
+    off = at;
+    at = align_up(at + bytes, 256);
+  };
+  const int planes = f32 ? 3 : 1;
+  if (!p.direct) take(p.wp, (size_t)planes * h.V * p.dp * 2);
+  if (op == 0) {
+    if (!p.direct) take(p.xp, (size_t)planes * N * p.dp * 2);
+    take(p.part, (size_t)2 * ceil_div(h.V, V_TILE) * N * sizeof(float2));
+    p.total = at;
+    return p;
+  }
+  const size_t block = (size_t)N * p.R * p.sub * 2;
+  int subs = (int)std::min<size_t>(std::max<size_t>(kPieceBytes / block, 1), (size_t)p.n_sub);
+  p.pieces = ceil_div(p.n_sub, subs);
+  p.piece_subs = ceil_div(p.n_sub, p.pieces);
+  p.pieces = ceil_div(p.n_sub, p.piece_subs);
+  take(p.xe, (size_t)N * p.R * p.dp * 2);
+  if (f32) take(p.x2, (size_t)N * p.dp * 2);
+  take(p.meta, (size_t)N * sizeof(float4));
+  take(p.G, block * p.piece_subs);
+  take(p.slots, (size_t)2 * (sm_count() / 2) * V_TILE * V_TILE * sizeof(float));
+  if (op == 1) {
+    if (p.pieces > 1) take(p.dx, (size_t)N * h.d * sizeof(float));
+    const dp_layer L = piece_layer(h, p, nullptr, nullptr);
+    p.gram_way = use_gram(L);
+    std::vector<dp_layer> layers(p.piece_subs, L);
+    std::vector<int> idx(p.piece_subs), way(p.piece_subs, p.gram_way ? 1 : 0);
+    for (int k = 0; k < p.piece_subs; ++k) idx[k] = k;
+    p.gram_count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), p.piece_subs, way.data());
+    take(p.gram, (size_t)h.B * p.gram_count * sizeof(float));
+    if (!p.gram_way && h.bias && p.R == 2) take(p.cols, (size_t)p.piece_subs * h.B * p.sub * sizeof(float));
+  } else if (h.bias) {
+    take(p.bias, (size_t)p.mt * 8 * p.piece_subs * p.sub * sizeof(float));
+  }
+  p.total = at;
+  return p;
+}
+
+static int check_head(const dp_vocab_head* h) {
+  if (!h || !h->X || !h->W || !h->labels) return DP_ERR_ARG;
+  if (h->dtype != DP_F32 && h->dtype != DP_BF16) return DP_ERR_ARG;
+  if (h->B <= 0 || h->T <= 0 || h->d <= 0 || h->V <= 0) return DP_ERR_ARG;
+  if (h->ldx < h->d || h->ldw < h->d) return DP_ERR_ARG;
+  if ((long long)h->B * h->T > (1 << 26) || h->V > (1 << 26) || h->d > (1 << 16) || h->ldx > (1ll << 36) || h->ldw > (1ll << 36))
+    return DP_ERR_UNSUPPORTED;
+  const size_t e = h->dtype == DP_F32 ? 4 : 2;
+  if (misaligned(h->X, e) || misaligned(h->W, e) || misaligned(h->labels, 4) || misaligned(h->bias, 4) || misaligned(h->weights, 4))
+    return DP_ERR_ALIGN;
+  return DP_OK;
+}
+
+static VHead head_of(const dp_vocab_head& h) {
+  return {h.X, h.W, h.bias, h.labels, h.weights, h.ldx, h.ldw, h.B * h.T, h.T, h.d, h.V, h.dtype == DP_F32};
+}
+
+struct VRun {                    // a call under way
+  const dp_vocab_head& h;
+  const VPlan& p;
+  char* ws;
+  cudaStream_t s;
+  int* status;
+  template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+};
+
+#define VOCAB_CUDA(expr) do { note_launch(1); if ((expr) != cudaSuccess) return DP_ERR_CUDA; } while (0)
+
+static int pack_rows(const VRun& r, const void* src, long long ld, long long rows, size_t off) {
+  const long long n = rows * r.p.dp;
+  const unsigned grid = (unsigned)std::min<long long>((n + 255) / 256, 148 * 16);
+  const int f32 = r.h.dtype == DP_F32;
+  VOCAB_CUDA(launch_chained(k_vocab_planes, grid, 256, 0, r.s, src, ld, (int)rows, r.h.d, r.p.dp, f32, f32 ? 3 : 1, r.at<__nv_bfloat16>(off)));
+  return DP_OK;
+}
+
+// The planes of W, and the products of a logit.
+static int logits_operands(const VRun& r, VParams& P) {
+  const dp_vocab_head& h = r.h;
+  const bool f32 = h.dtype == DP_F32;
+  for (int k = 0; k < (f32 ? 3 : 1); ++k) {
+    const bool ok = r.p.direct ? encode_rows(&P.b[k], h.W, h.V, h.d, h.ldw)
+                               : encode_rows(&P.b[k], r.at<__nv_bfloat16>(r.p.wp) + (size_t)k * h.V * r.p.dp, h.V, r.p.dp, r.p.dp);
+    if (!ok) return DP_ERR_CUDA;
+  }
+  static const unsigned char pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+  P.n_pairs = f32 ? 6 : 1;
+  for (int k = 0; k < P.n_pairs; ++k) {
+    P.pa[k] = f32 ? pa[k] : 0;
+    P.pb[k] = f32 ? pb[k] : 0;
+  }
+  P.kb = ceil_div(h.d, 64);
+  P.seg = f32 ? 8 : 32;
+  P.nt = V_TILE;
+  P.bias = h.bias;
+  P.V = h.V;
+  P.status = r.status;
+  return DP_OK;
+}
+
+// Units of a DX or DW launch: every pair, or fewer where a share would be shorter than four K blocks.
+static int share_units(long long line) {
+  const long long most = sm_count() / 2;
+  return (int)std::max<long long>(1, std::min<long long>(most, line / 4));
+}
+
+template <int MODE>
+static int launch_product(const VRun& r, VParams& P) {
+  const long long tiles = (long long)P.tiles_m * P.tiles_n, line = tiles * P.n_pairs * P.kb;
+  if (tiles > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
+  if (MODE == V_LSE || MODE == V_GRAD) P.units = (int)std::min<long long>(tiles, sm_count() / 2);
+  else P.units = share_units(line);
+  VOCAB_CUDA(launch_chained(k_vocab_gemm<MODE>, Pairs{(unsigned)P.units}, V_THREADS, v_smem<MODE>(), r.s, P));
+  if constexpr (MODE == V_DX || MODE == V_DW) {
+    if (P.units > 1)
+      VOCAB_CUDA(launch_chained(k_vocab_join<MODE>, dim3((unsigned)P.units - 1, V_TILE / 16), 256, 0, r.s, P));
+  }
+  return DP_OK;
+}
+
+// Tokens, planes of W, then G piece by piece; each piece is handed to `use`.
+template <typename Use>
+static int over_pieces(const VRun& r, const float* lse, const float* clip, float* bias_part, Use use) {
+  const dp_vocab_head& h = r.h;
+  const VPlan& p = r.p;
+  const int N = h.B * h.T;
+  const bool f32 = h.dtype == DP_F32;
+  int rc;
+  if (!p.direct && (rc = pack_rows(r, h.W, h.ldw, h.V, p.wp)) != DP_OK) return rc;
+  __nv_bfloat16 *xe = r.at<__nv_bfloat16>(p.xe), *x2 = r.at<__nv_bfloat16>(p.x2), *G = r.at<__nv_bfloat16>(p.G);
+  VOCAB_CUDA(launch_chained(k_vocab_tokens, (unsigned)ceil_div(N, 8), 256, 0, r.s, head_of(h), lse, clip, p.R, p.dp, p.dp > h.d && f32 && h.bias && !clip ? h.d : -1, xe, x2,
+                            r.at<float4>(p.meta), r.status));
+  for (int s0 = 0; s0 < p.n_sub; s0 += p.piece_subs) {
+    const int subs = std::min(p.piece_subs, p.n_sub - s0);
+    VParams P = {};
+    if ((rc = logits_operands(r, P)) != DP_OK) return rc;
+    if (!encode_rows(&P.a[0], xe, N, p.dp, (long long)p.R * p.dp)) return DP_ERR_CUDA;
+    if (f32 && (!encode_rows(&P.a[1], xe + 2 * p.dp, N, p.dp, (long long)p.R * p.dp) || !encode_rows(&P.a[2], x2, N, p.dp, p.dp)))
+      return DP_ERR_CUDA;
+    const long long block = (long long)N * p.R * p.sub;
+    const cuuint64_t dims[4] = {(cuuint64_t)p.sub, (cuuint64_t)p.R, (cuuint64_t)N, (cuuint64_t)subs};
+    const cuuint64_t strides[3] = {(cuuint64_t)p.sub * 2, (cuuint64_t)p.R * p.sub * 2, (cuuint64_t)block * 2};
+    const cuuint32_t box[4] = {(cuuint32_t)V_STAGE_COLS, 2u, 32u, 1u};
+    if (!encode(&P.st, G, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B)) return DP_ERR_CUDA;
+    P.tiles_m = p.mt;
+    P.tiles_n = subs * p.sub / V_TILE;
+    P.M = N;
+    P.N = subs * p.sub;
+    P.sub = p.sub;
+    P.v0 = s0 * p.sub;
+    P.planes2 = f32;
+    P.meta = r.at<float4>(p.meta);
+    P.bias_part = bias_part;
+    // the rows of W of this piece
+    for (int k = 0; k < (f32 ? 3 : 1); ++k) {
+      const long long rows = std::min<long long>((long long)subs * p.sub, h.V - P.v0);
+      const bool ok = p.direct ? encode_rows(&P.b[k], static_cast<const __nv_bfloat16*>(h.W) + P.v0 * h.ldw, rows, h.d, h.ldw)
+                               : encode_rows(&P.b[k], r.at<__nv_bfloat16>(p.wp) + ((size_t)k * h.V + P.v0) * p.dp, rows, p.dp, p.dp);
+      if (!ok) return DP_ERR_CUDA;
+    }
+    if ((rc = launch_product<V_GRAD>(r, P)) != DP_OK) return rc;
+    if ((rc = use(s0, subs, block)) != DP_OK) return rc;
+  }
+  return DP_OK;
+}
+
+static int check_call(const dp_vocab_head* h, int op, void* workspace, size_t bytes, VPlan* p) {
+  *p = plan_vocab(*h, op);
+  if (p->total > ((size_t)1 << 40)) return DP_ERR_UNSUPPORTED;
+  if (!workspace || misaligned(workspace, 256) || bytes < p->total) return DP_ERR_WORKSPACE;
+  return DP_OK;
+}
+
+}  // namespace dpk
+
+using namespace dpk;
+
+extern "C" {
+
+size_t dp_vocab_workspace_bytes(const dp_vocab_head* head) {
+  if (check_head(head) != DP_OK) return 0;
+  size_t most = (size_t)head->B * kCrossChunks * sizeof(float);
+  for (int op = 0; op < 3; ++op) most = std::max(most, plan_vocab(*head, op).total);
+  return most;
+}
+
+int dp_vocab_loss(const dp_vocab_head* head, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                  void* cuda_stream) {
+  int rc = check_head(head);
+  if (rc != DP_OK) return rc;
+  if (!loss || !lse) return DP_ERR_ARG;
+  if (misaligned(loss, 4) || misaligned(lse, 4)) return DP_ERR_ALIGN;
+  VPlan p;
+  if ((rc = check_call(head, 0, workspace, workspace_bytes, &p)) != DP_OK) return rc;
+  const dp_vocab_head& h = *head;
+  int* status = status_ptr();
+  if (!status || !vocab_kernels_ready()) return DP_ERR_CUDA;
+  const VRun r = {h, p, static_cast<char*>(workspace), static_cast<cudaStream_t>(cuda_stream), status};
+  const int N = h.B * h.T;
+  if (!p.direct && ((rc = pack_rows(r, h.W, h.ldw, h.V, p.wp)) != DP_OK || (rc = pack_rows(r, h.X, h.ldx, N, p.xp)) != DP_OK)) return rc;
+  VParams P = {};
+  if ((rc = logits_operands(r, P)) != DP_OK) return rc;
+  for (int k = 0; k < (h.dtype == DP_F32 ? 3 : 1); ++k) {
+    const bool ok = p.direct ? encode_rows(&P.a[k], h.X, N, h.d, h.ldx)
+                             : encode_rows(&P.a[k], r.at<__nv_bfloat16>(p.xp) + (size_t)k * N * p.dp, N, p.dp, p.dp);
+    if (!ok) return DP_ERR_CUDA;
+  }
+  P.tiles_m = p.mt;
+  P.tiles_n = ceil_div(h.V, V_TILE);
+  P.M = N;
+  P.N = h.V;
+  P.labels = h.labels;
+  P.part = r.at<float2>(p.part);
+  if ((rc = launch_product<V_LSE>(r, P)) != DP_OK) return rc;
+  VOCAB_CUDA(launch_chained(k_vocab_loss, (unsigned)ceil_div(N, 32), 256, 0, r.s, head_of(h), r.at<float2>(p.part), 2 * P.tiles_n,
+                            loss, lse, status));
+  return DP_OK;
+}
+
+int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx, int64_t ld_dx, float* sqnorm,
+                           int accumulate_into, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_head(head);
+  if (rc != DP_OK) return rc;
+  if (!lse || (!dx && !sqnorm)) return DP_ERR_ARG;
+  const dp_vocab_head& h = *head;
+  if (dx && (ld_dx < h.d || ld_dx > 0x7fffffffll)) return DP_ERR_ARG;
+  if (misaligned(lse, 4) || misaligned(sqnorm, 4) || misaligned(dx, h.dtype == DP_F32 ? 4 : 2)) return DP_ERR_ALIGN;
+  VPlan p;
+  if ((rc = check_call(head, 1, workspace, workspace_bytes, &p)) != DP_OK) return rc;
+  int* status = status_ptr();
+  if (!status || !vocab_kernels_ready()) return DP_ERR_CUDA;
+  const VRun r = {h, p, static_cast<char*>(workspace), static_cast<cudaStream_t>(cuda_stream), status};
+  const int N = h.B * h.T;
+  const bool f32 = h.dtype == DP_F32;
+  if (sqnorm && !accumulate_into && launch_fill_zero(sqnorm, h.B, r.s) != cudaSuccess) return DP_ERR_CUDA;
+  __nv_bfloat16* G = r.at<__nv_bfloat16>(p.G);
+  return over_pieces(r, lse, nullptr, nullptr, [&](int s0, int subs, long long block) -> int {
+    int rc = DP_OK;
+    if (dx) {
+      VParams P = {};
+      const int v0 = s0 * p.sub, cols = std::min(subs * p.sub, h.V - v0);
+      for (int k = 0; k < (f32 ? 2 : 1); ++k) {
+        if (!encode_blocks(&P.a[k], G + (size_t)k * p.sub, N, p.sub, (long long)p.R * p.sub, subs, block)) return DP_ERR_CUDA;
+        const bool ok = p.direct ? encode_rows(&P.b[k], h.W, h.V, h.d, h.ldw)
+                                 : encode_rows(&P.b[k], r.at<__nv_bfloat16>(p.wp) + (size_t)k * h.V * p.dp, h.V, h.d, p.dp);
+        if (!ok) return DP_ERR_CUDA;
+      }
+      static const unsigned char pa[4] = {1, 1, 0, 0}, pb[4] = {1, 0, 1, 0};
+      P.n_pairs = f32 ? 4 : 1;
+      for (int k = 0; k < P.n_pairs; ++k) {
+        P.pa[k] = f32 ? pa[k] : 0;
+        P.pb[k] = f32 ? pb[k] : 0;
+      }
+      P.kb = ceil_div(cols, 128);
+      P.seg = 16;
+      P.nt = h.d <= 128 ? 128 : V_TILE;
+      P.tiles_m = p.mt;
+      P.tiles_n = ceil_div(h.d, P.nt);
+      P.M = N;
+      P.N = h.d;
+      P.sub = p.sub;
+      P.v0 = v0;
+      P.V = h.V;
+      P.stride_c = (int)ld_dx;
+      P.slots = r.at<float>(p.slots);
+      P.sum = p.pieces > 1 ? r.at<float>(p.dx) : nullptr;
+      P.out = dx;
+      P.out_bf16 = !f32;
+      P.first = s0 == 0;
+      P.last = s0 + subs >= p.n_sub;
+      P.vec = !misaligned(dx, 16) && ld_dx % 8 == 0;
+      P.status = status;
+      if ((rc = launch_product<V_DX>(r, P)) != DP_OK) return rc;
+    }
+    if (sqnorm) {
+      std::vector<dp_layer> layers(subs);
+      std::vector<int> idx(subs), way(subs, p.gram_way ? 1 : 0);
+      std::vector<ColTaskHost> cols;
+      for (int k = 0; k < subs; ++k) {
+        layers[k] = piece_layer(h, p, r.at<__nv_bfloat16>(p.xe), G + (size_t)k * block);
+        idx[k] = k;
+      }
+      float* partial = r.at<float>(p.gram);
+      const int count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), subs, way.data());
+      if ((rc = launch_umma_sqnorms(layers.data(), idx.data(), subs, way.data(), partial, count, 0, status, r.s)) != DP_OK) return rc;
+      if (launch_reduce_partials(partial, h.B, count, sqnorm, r.s) != cudaSuccess) return DP_ERR_CUDA;
+      if (!p.gram_way && h.bias && p.R == 2) {
+        for (int k = 0; k < subs; ++k) cols.push_back({&layers[k], false, r.at<float>(p.cols) + (size_t)k * h.B * p.sub});
+        if (launch_colsums_batched(cols.data(), (int)cols.size(), r.s) != cudaSuccess ||
+            launch_rows_sqsum_batched(cols.data(), (int)cols.size(), sqnorm, r.s) != cudaSuccess) return DP_ERR_CUDA;
+      }
+    }
+    return rc;
+  });
+}
+
+int dp_vocab_loss_clipped_accumulate(const dp_vocab_head* head, const float* lse, const float* clip, float* acc_w, float* acc_b,
+                                     void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_head(head);
+  if (rc != DP_OK) return rc;
+  const dp_vocab_head& h = *head;
+  if (!lse || !clip || !acc_w || (h.bias && !acc_b)) return DP_ERR_ARG;
+  if (misaligned(lse, 4) || misaligned(clip, 4) || misaligned(acc_w, 4) || misaligned(acc_b, 4)) return DP_ERR_ALIGN;
+  VPlan p;
+  if ((rc = check_call(head, 2, workspace, workspace_bytes, &p)) != DP_OK) return rc;
+  int* status = status_ptr();
+  if (!status || !vocab_kernels_ready()) return DP_ERR_CUDA;
+  const VRun r = {h, p, static_cast<char*>(workspace), static_cast<cudaStream_t>(cuda_stream), status};
+  const int N = h.B * h.T;
+  __nv_bfloat16* G = r.at<__nv_bfloat16>(p.G);
+  float* bias_part = h.bias ? r.at<float>(p.bias) : nullptr;
+  return over_pieces(r, lse, clip, bias_part, [&](int s0, int subs, long long block) -> int {
+    int rc = DP_OK;
+    VParams P = {};
+    const int v0 = s0 * p.sub, cols = std::min(subs * p.sub, h.V - v0);
+    const long long rows = (long long)N * p.R;
+    if (!encode_blocks(&P.a[0], G, rows, p.sub, p.sub, subs, block) ||
+        !encode_rows(&P.b[0], r.at<__nv_bfloat16>(p.xe), rows, p.dp, p.dp)) return DP_ERR_CUDA;
+    P.n_pairs = 1;
+    P.kb = (int)((rows + 127) / 128);
+    P.seg = 16;
+    P.nt = h.d <= 128 ? 128 : V_TILE;
+    P.tiles_m = ceil_div(cols, V_TILE);
+    P.tiles_n = ceil_div(h.d, P.nt);
+    P.M = subs * p.sub;
+    P.N = h.d;
+    P.sub = p.sub;
+    P.v0 = v0;
+    P.V = h.V;
+    P.stride_c = h.d;
+    P.slots = r.at<float>(p.slots);
+    P.sum = acc_w;
+    P.vec = !misaligned(acc_w, 16) && h.d % 4 == 0;
+    P.status = status;
+    if ((rc = launch_product<V_DW>(r, P)) != DP_OK) return rc;
+    if (bias_part)
+      VOCAB_CUDA(launch_chained(k_vocab_bias, (unsigned)ceil_div(cols, 32), 256, 0, r.s, bias_part, p.mt * 8, subs * p.sub, cols, acc_b + v0));
+    return rc;
+  });
+}
+
+int dp_vocab_loss_cross_sqnorms(const dp_vocab_head* head, const float* lse, const int32_t* ids, const void* G_emb, int64_t ld_emb,
+                                int Tu, float* sqnorm, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const int rc = check_head(head);
+  if (rc != DP_OK) return rc;
+  if (!lse || !ids || !G_emb || !sqnorm || Tu <= 0 || ld_emb < head->d) return DP_ERR_ARG;
+  if (Tu > (1 << 26) || ld_emb > (1ll << 36)) return DP_ERR_UNSUPPORTED;
+  if (misaligned(lse, 4) || misaligned(ids, 4) || misaligned(sqnorm, 4) || misaligned(G_emb, head->dtype == DP_F32 ? 4 : 2))
+    return DP_ERR_ALIGN;
+  if (!workspace || misaligned(workspace, 256) || workspace_bytes < (size_t)head->B * kCrossChunks * sizeof(float))
+    return DP_ERR_WORKSPACE;
+  int* status = status_ptr();
+  if (!status) return DP_ERR_CUDA;
+  return launch_vocab_cross(*head, lse, ids, G_emb, ld_emb, Tu, sqnorm, static_cast<float*>(workspace), status,
+                            static_cast<cudaStream_t>(cuda_stream));
+}
+
+}  // extern "C"

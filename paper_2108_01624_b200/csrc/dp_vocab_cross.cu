@@ -1,0 +1,225 @@
+// The cross term of a table that a vocabulary head shares with the token embedding: example i's gradient of the table is
+// sum_u e_u at row ids_u (the embedding's part) plus G_i^T X_i (the head's), and the norm of the sum needs
+//   2 sum over inputs u, tokens t of G[t][ids_u] <x_t, e_u>,   G[t][v] = w_t (exp(<x_t, W_v> + bias_v - lse_t) - [v = label_t]).
+// Only the columns of G that the ids name are formed: two products of [inputs, d] x [d, tokens] an example, of the named
+// rows of W and of e.
+//
+// Bound by memory (e and the named rows of W are read once): a warp takes 16 inputs against up to 64 tokens, rows straight
+// from memory into the operands of m16n8k16 products.  A dot product does not mind the order of its terms, so a lane
+// gives 8 neighbouring elements of a row (16 bytes) to the places that two products ask of it, the same for both operands.
+// fp32 rows are split into three bf16 numbers in registers: six products, the smallest first.
+// fp32 sums of 32 elements a step; G is not rounded.
+#include <algorithm>
+
+#include "dp_chain.cuh"
+#include "dp_internal.h"
+
+namespace dpk {
+
+struct CrossArgs {
+  const void* x;
+  const void* w;
+  const void* e;
+  const float* bias;
+  const int32_t* labels;
+  const float* weights;
+  const float* lse;
+  const int32_t* ids;
+  float* out;                    // sqnorm, or partial sums [B][chunks]
+  long long ldx, ldw, lde;
+  int T, Tu, d, V, chunks, t_chunks, all;   // all: (128-input x 64-token) tasks of an example, shared by `chunks` blocks
+  int vec;
+  int* status;
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Elements [k, k + 8) of a row as PLANES times four words of two bf16 numbers, zeros beyond d.
+template <typename T> struct CrossRow;
+template <> struct CrossRow<__nv_bfloat16> {
+  static constexpr int PLANES = 1;
+  uint32_t r[1][4];
+  __device__ __forceinline__ void load(const void* base, long long row, int k, int d, bool vec) {
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(base) + row + k;
+    if (vec && k + 8 <= d) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p);
+      r[0][0] = v.x, r[0][1] = v.y, r[0][2] = v.z, r[0][3] = v.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = k + 2 * j < d ? __bfloat16_as_ushort(p[2 * j]) : 0u, hi = k + 2 * j + 1 < d ? __bfloat16_as_ushort(p[2 * j + 1]) : 0u;
+        r[0][j] = lo | hi << 16;
+      }
+    }
+  }
+};
+template <> struct CrossRow<float> {
+  static constexpr int PLANES = 3;
+  uint32_t r[3][4];
+  __device__ __forceinline__ void load(const void* base, long long row, int k, int d, bool vec) {
+    const float* p = static_cast<const float*>(base) + row + k;
+    float x[8];
+    if (vec && k + 8 <= d) {
+      const float4 u = *reinterpret_cast<const float4*>(p), v = *reinterpret_cast<const float4*>(p + 4);
+      x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = k + j < d ? p[j] : 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+        r[q][j] = *reinterpret_cast<const uint32_t*>(&h);
+        x[2 * j] -= __uint_as_float(r[q][j] << 16);
+        x[2 * j + 1] -= __uint_as_float(r[q][j] & 0xffff0000u);
+      }
+    }
+  }
+};
+
+// c += rows (a of lane/4, b of lane/4 + 8) x tokens over 32 elements.
+template <typename R>
+__device__ __forceinline__ void cross_step(float (&c)[4], const R& a, const R& b, const R& x) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if constexpr (R::PLANES == 1) {
+      mma_bf16(c, a.r[0][2 * s], b.r[0][2 * s], a.r[0][2 * s + 1], b.r[0][2 * s + 1], x.r[0][2 * s], x.r[0][2 * s + 1]);
+    } else {
+      constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+      for (int q = 0; q < 6; ++q)
+        mma_bf16(c, a.r[pa[q]][2 * s], b.r[pa[q]][2 * s], a.r[pa[q]][2 * s + 1], b.r[pa[q]][2 * s + 1], x.r[pb[q]][2 * s], x.r[pb[q]][2 * s + 1]);
+    }
+  }
+}
+
+// Block (chunk, example): eight warps, 16 inputs each, against NT groups of 8 tokens.
+template <typename T, int NT>
+__global__ void __launch_bounds__(256) k_vocab_cross(const __grid_constant__ CrossArgs a) {
+  __shared__ float red[8];
+  wait_for_predecessor();
+  let_successor_in();
+  using R = CrossRow<T>;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const long long i = blockIdx.y;
+  float sum = 0.0f;
+  for (int task = blockIdx.x; task < a.all; task += a.chunks) {
+    const int u0 = (task / a.t_chunks) * 128 + warp * 16, t0 = (task % a.t_chunks) * (NT * 8);
+    if (u0 >= a.Tu) continue;
+    int id[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int u = u0 + g + 8 * h;
+      id[h] = u < a.Tu ? a.ids[i * a.Tu + u] : -1;
+      if (u < a.Tu && (id[h] < 0 || id[h] >= a.V)) {
+        atomicCAS(a.status, 0, (int)STATUS_BAD_ID);
+        id[h] = -1;
+      }
+    }
+    // rows that do not count are read from a place that exists; their columns or rows of the products are left out below
+    const long long w0 = (long long)max(id[0], 0) * a.ldw, w1 = (long long)max(id[1], 0) * a.ldw;
+    const long long e0 = (i * a.Tu + min(u0 + g, a.Tu - 1)) * a.lde, e1 = (i * a.Tu + min(u0 + g + 8, a.Tu - 1)) * a.lde;
+    float cz[NT][4], ck[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) cz[j][k] = ck[j][k] = 0.0f;
+#pragma unroll 2
+    for (int k = 8 * q; k < (a.d + 31) / 32 * 32; k += 32) {
+      R wa, wb, ea, eb;
+      wa.load(a.w, w0, k, a.d, a.vec);
+      wb.load(a.w, w1, k, a.d, a.vec);
+      ea.load(a.e, e0, k, a.d, a.vec);
+      eb.load(a.e, e1, k, a.d, a.vec);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        R x;
+        x.load(a.x, (i * a.T + min(t0 + 8 * j + g, a.T - 1)) * a.ldx, k, a.d, a.vec);
+        cross_step(cz[j], wa, wb, x);
+        cross_step(ck[j], ea, eb, x);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {              // row g + 8 (k / 2), token 2 q + k % 2 of the group
+        const int t = t0 + 8 * j + 2 * q + (k & 1), v = id[k >> 1];
+        if (t >= a.T || v < 0) continue;
+        const long long n = i * a.T + t;
+        const int y = a.labels[n];
+        if (y < 0 || y >= a.V) continue;
+        const float z = cz[j][k] + (a.bias ? a.bias[v] : 0.0f) - a.lse[n];
+        const float G = v == y ? expm1f(z) : expf(z);
+        sum = fmaf((a.weights ? a.weights[n] : 1.0f) * G, ck[j][k], sum);
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+  if (lane == 0) red[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += red[w];
+    if (a.chunks > 1) a.out[i * a.chunks + blockIdx.x] = 2.0f * s;
+    else a.out[i] += 2.0f * s;
+  }
+}
+
+// sqnorm[i] += the partial sums of example i, in order.
+__global__ void __launch_bounds__(256) k_vocab_cross_sum(const float* part, int B, int chunks, float* sqnorm) {
+  wait_for_predecessor();
+  let_successor_in();
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= B) return;
+  float s = 0.0f;
+  for (int k = 0; k < chunks; ++k) s += part[(long long)i * chunks + k];
+  sqnorm[i] += s;
+}
+
+// Blocks of an example: enough that the device is full, as long as each has a task.
+static int cross_chunks(int B, long long all) {
+  const long long want = (4ll * sm_count() + B - 1) / B;
+  return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(all, want), kCrossChunks));
+}
+
+template <typename T>
+static cudaError_t launch_cross(CrossArgs a, int B, int nt, cudaStream_t s) {
+  const dim3 grid((unsigned)a.chunks, (unsigned)B);
+  return nt == 1 ? launch_chained(k_vocab_cross<T, 1>, grid, 256, 0, s, a)
+       : nt == 2 ? launch_chained(k_vocab_cross<T, 2>, grid, 256, 0, s, a)
+       : nt == 3 ? launch_chained(k_vocab_cross<T, 3>, grid, 256, 0, s, a)
+                 : launch_chained(k_vocab_cross<T, 4>, grid, 256, 0, s, a);
+}
+
+int launch_vocab_cross(const dp_vocab_head& h, const float* lse, const int32_t* ids, const void* G_emb, long long ld_emb, int Tu,
+                       float* sqnorm, float* partial, int* status, cudaStream_t s) {
+  const bool f32 = h.dtype == DP_F32;
+  const int nt = std::min(4, ceil_div(h.T, 8));
+  CrossArgs a = {h.X, h.W, G_emb, h.bias, h.labels, h.weights, lse, ids, sqnorm, h.ldx, h.ldw, ld_emb, h.T, Tu, h.d, h.V};
+  a.t_chunks = ceil_div(h.T, 8 * nt);
+  const long long all = (long long)ceil_div(Tu, 128) * a.t_chunks;
+  if (h.B > 65535 || all > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
+  a.all = (int)all;
+  a.chunks = cross_chunks(h.B, all);
+  if (a.chunks > 1) a.out = partial;
+  const int e = f32 ? 4 : 8;
+  a.vec = !misaligned(h.X, 16) && !misaligned(h.W, 16) && !misaligned(G_emb, 16) && h.ldx % e == 0 && h.ldw % e == 0 && ld_emb % e == 0;
+  a.status = status;
+  note_launch(1);
+  if ((f32 ? launch_cross<float>(a, h.B, nt, s) : launch_cross<__nv_bfloat16>(a, h.B, nt, s)) != cudaSuccess) return DP_ERR_CUDA;
+  if (a.chunks > 1) {
+    note_launch(1);
+    if (launch_chained(k_vocab_cross_sum, (unsigned)ceil_div(h.B, 256), 256, 0, s, partial, h.B, a.chunks, sqnorm) != cudaSuccess)
+      return DP_ERR_CUDA;
+  }
+  return DP_OK;
+}
+
+}  // namespace dpk
