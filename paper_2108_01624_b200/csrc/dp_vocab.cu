@@ -83,7 +83,7 @@ struct alignas(64) VParams {
   const float4* meta;            // GRAD: lse, scale, G at the label, label (bits) of every token
   float2* part;                  // LSE: [2 tiles_n][M] maximum and sum
   float* bias_part;              // GRAD: [rows of 32 tokens][columns of the piece] column sums, or null
-  float* slots;                  // DX, DW: tiles that several pairs share, [2 units][256][256]
+  float4* slots;                 // DX, DW: tiles that several pairs share, [2 units][64 groups of four columns][256 rows]
   float* sum;                    // DX: fp32 sums over the pieces [M, N]; DW: the accumulator
   void* out;                     // DX: the result
   int out_bf16, first, last, vec;
@@ -262,62 +262,48 @@ __device__ __forceinline__ void finish_grad(const VParams& P, float (&z)[128], c
   }
 }
 
-// One row's `n` (32) columns from column c on of dX: summed over the pieces so far, rounded after the last.
-__device__ __forceinline__ void put_dx(const VParams& P, int m, int c, const float* v) {
+// Four neighbouring columns from c on of a row of dX: summed over the pieces so far, rounded after the last.
+__device__ __forceinline__ void put_dx(const VParams& P, int m, int c, float4 v) {
   if (m >= P.M || c >= P.N) return;
-  const size_t at = (size_t)m * P.N + c;
-  const int n = P.N - c < 32 ? P.N - c : 32;
-  float x[32];
-#pragma unroll
-  for (int j = 0; j < 32; ++j) x[j] = v[j];
-  if (!P.first) {
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < n) x[j] += P.sum[at + j];
-  }
-  if (!P.last) {
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < n) P.sum[at + j] = x[j];
+  const size_t at = (size_t)m * P.N + c, to = (size_t)m * P.stride_c + c;
+  if (P.vec && c + 4 <= P.N) {                  // rows of dX and of the sums start on 16-byte boundaries
+    if (!P.first) {
+      const float4 s = *reinterpret_cast<const float4*>(P.sum + at);
+      v = make_float4(v.x + s.x, v.y + s.y, v.z + s.z, v.w + s.w);
+    }
+    if (!P.last) {
+      *reinterpret_cast<float4*>(P.sum + at) = v;
+    } else if (P.out_bf16) {
+      const __nv_bfloat162 h[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.out) + to) = *reinterpret_cast<const uint2*>(h);
+    } else {
+      *reinterpret_cast<float4*>(static_cast<float*>(P.out) + to) = v;
+    }
     return;
   }
-  const size_t to = (size_t)m * P.stride_c + c;
-  if (P.out_bf16) {
-    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(P.out) + to;
-    if (P.vec && n == 32) {
+  const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int j = 0; j < 32; j += 8) {
-        __nv_bfloat162 h[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) h[u] = __floats2bfloat162_rn(x[j + 2 * u], x[j + 2 * u + 1]);
-        *reinterpret_cast<uint4*>(o + j) = *reinterpret_cast<const uint4*>(h);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (j < n) o[j] = __float2bfloat16_rn(x[j]);
-    }
-  } else {
-    float* o = static_cast<float*>(P.out) + to;
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < n) o[j] = x[j];
+  for (int j = 0; j < 4; ++j) {
+    if (c + j >= P.N) break;
+    const float y = P.first ? x[j] : x[j] + P.sum[at + j];
+    if (!P.last) P.sum[at + j] = y;
+    else if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[to + j] = __float2bfloat16_rn(y);
+    else static_cast<float*>(P.out)[to + j] = y;
   }
 }
 
-// acc += for one row's 32 columns from column c on.  An element has one writer per launch.
-__device__ __forceinline__ void put_dw(const VParams& P, int m, int c, const float* v) {
+// acc += for four neighbouring columns from c on of a row.  An element has one writer per launch.
+__device__ __forceinline__ void put_dw(const VParams& P, int m, int c, float4 v) {
   const int row = P.v0 + m;
   if (row >= P.V || c >= P.N) return;
   float* o = P.sum + (size_t)row * P.stride_c + c;
-  if (P.vec && c + 32 <= P.N) {
-#pragma unroll
-    for (int j = 0; j < 32; j += 4)
-      asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(o + j), "f"(v[j]), "f"(v[j + 1]), "f"(v[j + 2]), "f"(v[j + 3]) : "memory");
+  if (P.vec && c + 4 <= P.N) {
+    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(o), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
   } else {
+    const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (c + j < P.N) atomicAdd(o + j, v[j]);
+    for (int j = 0; j < 4; ++j)
+      if (c + j < P.N) atomicAdd(o + j, x[j]);
   }
 }
 
@@ -483,14 +469,17 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
           if (ch * 32 >= half) continue;
           const int c = n0 + col + ch * 32;
           if (shared_tile) {
-            float* to = P.slots + ((size_t)slot * V_TILE + (m - m0)) * V_TILE + col + ch * 32;
+            float4* to = P.slots + ((size_t)slot * (V_TILE / 4) + (col + ch * 32) / 4) * V_TILE + (m - m0);
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<float4*>(to + j) = make_float4(acc[ch * 32 + j], acc[ch * 32 + j + 1], acc[ch * 32 + j + 2], acc[ch * 32 + j + 3]);
-          } else if constexpr (MODE == V_DX) {
-            put_dx(P, m, c, acc + ch * 32);
+              to[(j / 4) * V_TILE] = make_float4(acc[ch * 32 + j], acc[ch * 32 + j + 1], acc[ch * 32 + j + 2], acc[ch * 32 + j + 3]);
           } else {
-            put_dw(P, m, c, acc + ch * 32);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              const float4 v = make_float4(acc[ch * 32 + j], acc[ch * 32 + j + 1], acc[ch * 32 + j + 2], acc[ch * 32 + j + 3]);
+              if constexpr (MODE == V_DX) put_dx(P, m, c + j, v);
+              else put_dw(P, m, c + j, v);
+            }
           }
         }
       }
@@ -509,7 +498,7 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
 
 // The tiles of a DX or DW launch that several pairs shared: their parts are added in the pairs' order.  Block (u, r): the
 // tile that begins inside or before unit u's share and goes on into it, rows [16 r, +16); a tile is handled by the
-// first unit that continues it.
+// first unit that continues it.  A warp: 4 rows, 8 groups of four columns (64 bytes of a slot, 128 of a result at a time).
 template <int MODE>
 __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VParams P) {
   wait_for_predecessor();
@@ -518,45 +507,211 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
   const long long line = (long long)P.tiles_m * P.tiles_n * nkb;
   const int u0 = blockIdx.x + 1;
   const long long lo = share_begin(line, P.units, u0);
-  const long long tile = lo / nkb;
-  if (lo == tile * nkb || lo >= line) return;                       // a unit that begins with a tile of its own
-  if (share_begin(line, P.units, u0 - 1) > tile * nkb) return;      // an earlier unit continues this tile already
+  const long long tile = lo / nkb, begin = tile * nkb;
+  if (lo == begin || lo >= line) return;                          // a unit that begins with a tile of its own
+  if (share_begin(line, P.units, u0 - 1) > begin) return;         // an earlier unit continues this tile already
   int m0, n0;
   tile_origin<MODE>(P, (int)tile, m0, n0);
-  const int r = blockIdx.y * 16 + (threadIdx.x >> 4), c = (threadIdx.x & 15) * 16;   // 16 columns a thread
-  if (c >= P.nt) return;
-  float v[32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = blockIdx.y * 16 + (warp & 3) * 4 + (lane & 3);
+  int last = u0;                                                  // units u0 - 1 .. last have a part
+  while (last + 1 < P.units && share_begin(line, P.units, last + 1) < begin + nkb) ++last;
+  const int first_slot = 2 * (u0 - 1) + (begin > share_begin(line, P.units, u0 - 1) ? 1 : 0);
+  for (int g = (warp >> 2) * 8 + (lane >> 2); g < P.nt / 4; g += 16) {
+    const size_t at = (size_t)g * V_TILE + r;
+    float4 v = P.slots[(size_t)first_slot * (V_TILE / 4) * V_TILE + at];
+#pragma unroll 4
+    for (int u = u0; u <= last; ++u) {                            // the tile is the first of these units' shares
+      const float4 x = P.slots[(size_t)(2 * u) * (V_TILE / 4) * V_TILE + at];
+      v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+    }
+    if constexpr (MODE == V_DX) put_dx(P, m0 + r, n0 + 4 * g, v);
+    else put_dw(P, m0 + r, n0 + 4 * g, v);
+  }
+}
+
+// =================================================================================================
+// Squared norms of short examples (at most 128 rows of planes): |G_i^T X_i|^2 = sum over rows r, s of the example of
+// (<x_r, x_s> + bias) <g_r, g_s>.  A CTA takes as many whole examples as 128 rows hold and some blocks of G; both Grams are
+// 128 x 128 x 16 UMMAs of a tile with itself, of which the epilogue uses each row's own example.  The Gram of G is taken
+// over by the epilogue every kNormSeg columns and added in registers: its squares are one large (the label's) and a
+// vocabulary of small ones, which a longer sum on the tensor core would lose.  Bound by reading G.
+// =================================================================================================
+constexpr int N_STAGES = 6, N_STAGE_BYTES = 2 * V_BOX_BYTES;    // 128 rows x 128 columns
+constexpr int N_THREADS = 192;                                  // warp 0 TMA, warp 1 UMMA, warps 2..5 epilogue
+constexpr int kNormSeg = 8;                                     // stages
+struct NCtl {
+  uint64_t full[N_STAGES], empty[N_STAGES], tmem_full[3], tmem_empty[2], drain;
+  uint32_t tmem_base;
+  int abort;
+  float row[128];
+};
+constexpr int N_SMEM = 1024 + N_STAGES * N_STAGE_BYTES + (int)sizeof(NCtl);
+struct alignas(64) NParams {
+  CUtensorMap x, g;
+  int rows;                      // of an example
+  int examples;                  // of a CTA's 128 rows
+  int B, groups, splits, subs, sub, dp, bias;
+  float* partial;                // [B][splits]
+  int* status;
+};
+
+__global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_constant__ NParams P) {
+  extern __shared__ uint8_t smem_raw[];
+  wait_for_predecessor();
+  let_successor_in();
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  NCtl* S = reinterpret_cast<NCtl*>(tiles + N_STAGES * N_STAGE_BYTES);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abort_flag = &S->abort;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < N_STAGES; ++s) { mbar_init(&S->full[s], 1); mbar_init(&S->empty[s], 1); }
+    for (int b = 0; b < 3; ++b) mbar_init(&S->tmem_full[b], 1);
+    for (int b = 0; b < 2; ++b) mbar_init(&S->tmem_empty[b], 4);
+    mbar_init(&S->drain, 1);
+    S->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) { tmem_alloc(&S->tmem_base, 512); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = S->tmem_base;        // columns 0, 128: G, in turn; 256: X
+  const int px = (P.dp + 127) / 128;              // stages of X
+  const int items = P.groups * P.splits;
+
+  if (warp == 0) {
+    if (lane == 0) {   // ---------------- TMA producer ----------------
+      uint32_t it = 0;
+      bool alive = true;
+      for (int item = blockIdx.x; item < items && alive; item += gridDim.x) {
+        const int grp = item % P.groups, split = item / P.groups;
+        const int y = grp * P.examples * P.rows;
+        const int s0 = (int)((long long)P.subs * split / P.splits), s1 = (int)((long long)P.subs * (split + 1) / P.splits);
+        const int pg = P.sub / 128, all = px + (s1 - s0) * pg;
+        for (int j = 0; j < all; ++j, ++it) {
+          const uint32_t slot = it % N_STAGES, ph = (it / N_STAGES) & 1u;
+          if (!mbar_wait(&S->empty[slot], ph ^ 1u, abort_flag, P.status, 71, (int)it)) { alive = false; break; }
+          uint8_t* st = tiles + slot * N_STAGE_BYTES;
+          mbar_arrive_expect_tx(&S->full[slot], (uint32_t)N_STAGE_BYTES);
+          if (j < px) {                           // columns beyond X's arrive as zeros
+            load2(st, &P.x, &S->full[slot], 128 * j, y);
+            load2(st + V_BOX_BYTES, &P.x, &S->full[slot], 128 * j + 64, y);
+          } else {
+            const int z = s0 + (j - px) / pg, x = (j - px) % pg * 128;
+            tma_load_3d(st, &P.g, &S->full[slot], x, y, z);
+            tma_load_3d(st + V_BOX_BYTES, &P.g, &S->full[slot], x + 64, y, z);
+          }
+        }
+      }
+      const uint32_t pending = it < (uint32_t)N_STAGES ? it : (uint32_t)N_STAGES;
+      for (uint32_t k = 0; k < pending; ++k) {
+        const uint32_t j = it - 1 - k;
+        mbar_wait_drain(&S->full[j % N_STAGES], (j / N_STAGES) & 1u, P.status);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {   // ---------------- UMMA issuer ----------------
+      const int n = (P.examples * P.rows + 15) / 16 * 16;
+      const uint32_t idesc = idesc_bf16_f32(128, n, false, false);
+      uint32_t it = 0, part = 0;
+      bool alive = true;
+      for (int item = blockIdx.x; item < items && alive; item += gridDim.x) {
+        const int split = item / P.groups;
+        const int s0 = (int)((long long)P.subs * split / P.splits), s1 = (int)((long long)P.subs * (split + 1) / P.splits);
+        const int all = px + (s1 - s0) * (P.sub / 128);
+        // X first (the epilogue has read the X of the item before: it gave back that item's last part of G after it)
+        for (int j0 = 0; j0 < all && alive;) {
+          const bool isx = j0 == 0;
+          const int j1 = isx ? px : j0 + kNormSeg < all ? j0 + kNormSeg : all;
+          const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
+          if (!mbar_wait(&S->tmem_empty[buf], tph ^ 1u, abort_flag, P.status, 72, (int)part)) { alive = false; break; }
+          if (isx && part > 0 && !mbar_wait(&S->tmem_empty[buf ^ 1u], ((part - 1) >> 1) & 1u, abort_flag, P.status, 73, (int)part)) { alive = false; break; }
+          tc_fence_after();
+          const uint32_t d_tmem = tmem_base + (isx ? 256u : buf * 128u);
+          for (int j = j0; j < j1; ++j, ++it) {
+            const uint32_t slot = it % N_STAGES, ph = (it / N_STAGES) & 1u;
+            if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 74, (int)it)) { alive = false; break; }
+            tc_fence_after();
+            const uint32_t a = smem_u32(tiles + slot * N_STAGE_BYTES);
 #pragma unroll
-  for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-  for (int u = u0 - 1; u < P.units; ++u) {
-    const long long b = share_begin(line, P.units, u);
-    if (b >= (tile + 1) * nkb) break;
-    const int slot = 2 * u + (tile * nkb > b ? 1 : 0);
-    const float* from = P.slots + ((size_t)slot * V_TILE + r) * V_TILE + c;
+            for (int k = 0; k < 8; ++k) {
+              const uint64_t desc = smem_desc_sw128(a + (k >> 2) * V_BOX_BYTES + (k & 3) * 32, 16, 1024);
+              umma_bf16(d_tmem, desc, desc, idesc, (j > j0 || k > 0) ? 1u : 0u);
+            }
+            umma_commit(&S->empty[slot]);
+          }
+          if (alive) umma_commit(&S->tmem_full[isx ? 2 : buf]);
+          if (!isx) ++part;
+          j0 = j1;
+        }
+      }
+      umma_commit(&S->drain);
+      mbar_wait_drain(&S->drain, 0u, P.status);
+    }
+  } else {   // ---------------- epilogue warps 2..5: a row each ----------------
+    const int q = warp & 3, r = q * 32 + lane;
+    const uint32_t lane_base = tmem_base + ((uint32_t)(q * 32) << 16);
+    uint32_t part = 0, xs = 0;
+    bool alive = true;
+    for (int item = blockIdx.x; item < items; item += gridDim.x, ++xs) {
+      const int grp = item % P.groups, split = item / P.groups;
+      const int s0 = (int)((long long)P.subs * split / P.splits), s1 = (int)((long long)P.subs * (split + 1) / P.splits);
+      const int parts = ((s1 - s0) * (P.sub / 128) + kNormSeg - 1) / kNormSeg;
+      if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[2], xs & 1u, abort_flag, P.status, 75, (int)xs));
+      float acc[128];
 #pragma unroll
-    for (int j = 0; j < 16; j += 4) {
-      const float4 x = *reinterpret_cast<const float4*>(from + j);
-      v[j] += x.x;
-      v[j + 1] += x.y;
-      v[j + 2] += x.z;
-      v[j + 3] += x.w;
+      for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+      float sum = 0.0f;
+      const int c0 = r / P.rows * P.rows, c1 = c0 + P.rows;       // this row's example
+      for (int k = 0; k < parts; ++k, ++part) {
+        const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
+        if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[buf], tph, abort_flag, P.status, 76, (int)part));
+        if (!alive) continue;
+        tc_fence_after();
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t v[32];
+          tmem_ld_32x32(lane_base + buf * 128u + (uint32_t)ch * 32u, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) acc[ch * 32 + j] += __uint_as_float(v[j]);
+        }
+        if (k == parts - 1) {                     // before this part's columns are given back, so is X's Gram
+          const float one = P.bias ? 1.0f : 0.0f;
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) {
+            uint32_t v[32];
+            tmem_ld_32x32(lane_base + 256u + (uint32_t)ch * 32u, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const bool own = ch * 32 + j >= c0 && ch * 32 + j < c1;
+              sum += own ? (__uint_as_float(v[j]) + one) * acc[ch * 32 + j] : 0.0f;
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S->tmem_empty[buf]);
+      }
+      S->row[r] = sum;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      const int e = threadIdx.x - 64, i = grp * P.examples + e;
+      if (alive && e < P.examples && i < P.B) {
+        float s = 0.0f;
+        for (int k = 0; k < P.rows; ++k) s += S->row[e * P.rows + k];
+        P.partial[(size_t)i * P.splits + split] = s;
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
     }
   }
-  const int m = m0 + r;
-#pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const int cc = n0 + c + j;
-    if (MODE == V_DX) {
-      if (m >= P.M || cc >= P.N) break;
-      const size_t at = (size_t)m * P.N + cc;
-      const float x = P.first ? v[j] : v[j] + P.sum[at];
-      if (!P.last) P.sum[at] = x;
-      else if (P.out_bf16) static_cast<__nv_bfloat16*>(P.out)[(size_t)m * P.stride_c + cc] = __float2bfloat16_rn(x);
-      else static_cast<float*>(P.out)[(size_t)m * P.stride_c + cc] = x;
-    } else {
-      if (P.v0 + m >= P.V || cc >= P.N) break;
-      P.sum[(size_t)(P.v0 + m) * P.stride_c + cc] += v[j];
-    }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
   }
 }
 
@@ -568,12 +723,9 @@ struct VHead {                   // dp_vocab_head with its sizes worked out
   const int32_t* labels;
   const float* weights;
   long long ldx, ldw;
-  int N, T, d, V, f32;
+  int N, T, d, V, f32, vec;      // vec: rows of X and W start on 16-byte boundaries
 };
 
-__device__ __forceinline__ float element(const VHead& H, const void* p, long long i) {
-  return H.f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-}
 // A label that takes part: -1 for none, and for one beyond the vocabulary, which is reported.
 __device__ __forceinline__ int label_of(const VHead& H, int n, int* status) {
   const int y = H.labels[n];
@@ -583,14 +735,32 @@ __device__ __forceinline__ int label_of(const VHead& H, int n, int* status) {
   }
   return y < 0 ? -1 : y;
 }
-// <x_n, W_y> + bias_y in fp64, by one warp; every lane gets it.
-__device__ __forceinline__ double label_logit(const VHead& H, int n, int y, int lane) {
-  double s = 0.0;
-  const long long xr = (long long)n * H.ldx, wr = (long long)y * H.ldw;
-  for (int k = lane; k < H.d; k += 32) s = fma((double)element(H, H.x, xr + k), (double)element(H, H.w, wr + k), s);
+// Elements [c, c + 8) of a row, zeros beyond d.
+__device__ __forceinline__ void eight(const VHead& H, const void* p, long long row, int c, float (&x)[8]) {
+  if (H.vec && c + 8 <= H.d) {
+    if (H.f32) {
+      const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + row + c);
+      const float4 u = q[0], v = q[1];
+      x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+    } else {
+      const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + row + c);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] = __uint_as_float(w[j] << 16);
+        x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      x[j] = c + j >= H.d ? 0.0f : H.f32 ? static_cast<const float*>(p)[row + c + j] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[row + c + j]);
+  }
+}
+__device__ __forceinline__ double warp_sum(double s) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return H.bias ? s + (double)H.bias[y] : s;
+  return s;
 }
 
 // A bf16 number and what it leaves of x.
@@ -598,6 +768,17 @@ __device__ __forceinline__ __nv_bfloat16 split_off(float& x) {
   const __nv_bfloat16 h = __float2bfloat16_rn(x);
   x -= __bfloat162float(h);
   return h;
+}
+
+// The bf16 parts of eight numbers, which keep what is left.
+__device__ __forceinline__ uint4 split_eight(float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t lo = __bfloat16_as_ushort(split_off(x[2 * j])), hi = __bfloat16_as_ushort(split_off(x[2 * j + 1]));
+    w[j] = lo | hi << 16;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Planes of a matrix [rows, d]: out[plane][row][dp], zeros beyond d.  (fp32: three, bf16: one, where the tensor's own
@@ -628,19 +809,31 @@ k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* c
   const int n = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (n >= H.N) return;
   const int y = label_of(H, n, status);
-  for (int c = lane; c < dp; c += 32) {
-    float x = y >= 0 && c < H.d ? element(H, H.x, (long long)n * H.ldx + c) : c == one ? 1.0f : 0.0f;
-    const __nv_bfloat16 p0 = split_off(x);
-    __nv_bfloat16* row = xe + (size_t)n * R * dp + c;
-    row[0] = row[dp] = p0;
+  double s = 0.0;
+#pragma unroll 4
+  for (int c = 8 * lane; c < dp; c += 256) {
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (y >= 0) {
+      float w[8];
+      eight(H, H.x, (long long)n * H.ldx, c, x);
+      eight(H, H.w, (long long)y * H.ldw, c, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fma((double)x[j], (double)w[j], s);
+    }
+    if ((unsigned)(one - c) < 8u) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = c + j == one ? 1.0f : x[j];
+    }
+    uint4* row = reinterpret_cast<uint4*>(xe + (size_t)n * R * dp + c);
+    row[0] = row[dp / 8] = split_eight(x);
     if (R == 4) {
-      row[2 * dp] = row[3 * dp] = split_off(x);
-      x2[(size_t)n * dp + c] = split_off(x);
+      row[2 * (dp / 8)] = row[3 * (dp / 8)] = split_eight(x);
+      *reinterpret_cast<uint4*>(x2 + (size_t)n * dp + c) = split_eight(x);
     }
   }
   float4 m = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
   if (y >= 0) {
-    const double z = label_logit(H, n, y, lane);
+    const double z = warp_sum(s) + (H.bias ? (double)H.bias[y] : 0.0);
     float scale = H.weights ? H.weights[n] : 1.0f;
     if (clip) scale *= clip[n / H.T];
     m = make_float4(lse[n], scale, scale * expm1f((float)(z - (double)lse[n])), __int_as_float(y));
@@ -648,55 +841,54 @@ k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* c
   if (lane == 0) meta[n] = m;
 }
 
-// lse and loss of a token from the parts over the column blocks, which leave the label out.  32 tokens a block: eight
-// strands of threads take every eighth part each; then a warp per token forms the label's logit.
+// lse and loss of a token from the parts over the column blocks, which leave the label out: a warp per token (eight
+// neighbours a block, whose parts share sectors), its label's logit in fp64.
 __global__ void __launch_bounds__(256)
 k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, float* loss, float* lse, int* status) {
-  __shared__ float2 s[8][33];
   wait_for_predecessor();
   let_successor_in();
-  const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
-  const int n0 = blockIdx.x * 32;
-  float most = -INFINITY, sum = 0.0f;
-  if (n0 + lane < H.N) {
+  const int lane = threadIdx.x & 31, n = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (n >= H.N) return;
+  const int y = label_of(H, n, status);
+  if (y < 0) {
+    if (lane == 0) loss[n] = lse[n] = 0.0f;
+    return;
+  }
+  double s = 0.0;
 #pragma unroll 4
-    for (int p = strand; p < parts; p += 8) {
-      const float2 v = part[(size_t)p * H.N + n0 + lane];
-      const float top = fmaxf(most, v.x);
-      if (top != -INFINITY) {
-        sum = sum * ex2((most - top) * kLog2e) + v.y * ex2((v.x - top) * kLog2e);
-        most = top;
-      } else {
-        sum += v.y;                             // 0, or NaN
-      }
+  for (int c = 8 * lane; c < H.d; c += 256) {
+    float x[8], w[8];
+    eight(H, H.x, (long long)n * H.ldx, c, x);
+    eight(H, H.w, (long long)y * H.ldw, c, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fma((double)x[j], (double)w[j], s);
+  }
+  float most = -INFINITY, sum = 0.0f;
+#pragma unroll 4
+  for (int p = lane; p < parts; p += 32) {
+    const float2 v = part[(size_t)p * H.N + n];
+    const float top = fmaxf(most, v.x);
+    if (top != -INFINITY) {
+      sum = sum * ex2((most - top) * kLog2e) + v.y * ex2((v.x - top) * kLog2e);
+      most = top;
+    } else {
+      sum += v.y;                               // 0, or NaN
     }
   }
-  s[strand][lane] = make_float2(most, sum);
-  __syncthreads();
-  for (int k = strand; k < 32; k += 8) {        // token n0 + k
-    const int n = n0 + k;
-    if (n >= H.N) break;
-    const int y = label_of(H, n, status);
-    if (y < 0) {
-      if (lane == 0) loss[n] = lse[n] = 0.0f;
-      continue;
-    }
-    const float2 v = lane < 8 ? s[lane][k] : make_float2(-INFINITY, 0.0f);
-    float top = v.x;
+  float top = most;
 #pragma unroll
-    for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float all = top == -INFINITY ? v.y : v.y * ex2((v.x - top) * kLog2e);
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float all = top == -INFINITY ? sum : sum * ex2((most - top) * kLog2e);
 #pragma unroll
-    for (int o = 4; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-    const double z = label_logit(H, n, y, lane);
-    if (lane == 0) {
-      const double others = (double)top + (double)logf(all);           // -inf where there are none
-      const float gap = (float)(others - z);
-      float l = gap > 0.0f ? gap + log1pf(expf(-gap)) : log1pf(expf(gap));
-      if (z == INFINITY) l = NAN;               // as any other infinite logit
-      loss[n] = (H.weights ? H.weights[n] : 1.0f) * l;
-      lse[n] = (float)(z == -INFINITY ? others : z + (double)l);
-    }
+  for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  const double z = warp_sum(s) + (H.bias ? (double)H.bias[y] : 0.0);
+  if (lane == 0) {
+    const double others = (double)top + (double)logf(all);             // -inf where there are none
+    const float gap = (float)(others - z);
+    float l = gap > 0.0f ? gap + log1pf(expf(-gap)) : log1pf(expf(gap));
+    if (z == INFINITY) l = NAN;                 // as any other infinite logit
+    loss[n] = (H.weights ? H.weights[n] : 1.0f) * l;
+    lse[n] = (float)(z == -INFINITY ? others : z + (double)l);
   }
 }
 
@@ -732,7 +924,7 @@ static bool vocab_kernels_ready() {
       return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
     };
     state[dev] = (opt((const void*)k_vocab_gemm<V_LSE>, v_smem<V_LSE>()) && opt((const void*)k_vocab_gemm<V_GRAD>, v_smem<V_GRAD>()) &&
-                  opt((const void*)k_vocab_gemm<V_DX>, v_smem<V_DX>()) && opt((const void*)k_vocab_gemm<V_DW>, v_smem<V_DW>())) ? 1 : -1;
+                  opt((const void*)k_vocab_gemm<V_DX>, v_smem<V_DX>()) && opt((const void*)k_vocab_gemm<V_DW>, v_smem<V_DW>()) && opt((const void*)k_vocab_norms, N_SMEM)) ? 1 : -1;
   }
   return state[dev] > 0;
 }
@@ -763,6 +955,18 @@ static bool encode_blocks(CUtensorMap* map, const void* base, long long rows, in
 constexpr int kSubColumns = 2048;               // columns of one block of G, at most
 constexpr size_t kPieceBytes = (size_t)256 << 20;   // G of one piece, unless one block alone is larger
 
+// How many CTAs share a group's blocks of G: each forms the Gram of X again, so as few as fill the device well, by the
+// columns that the longest-working CTA sums.
+static int norm_splits(int groups, int subs, int sub, int dp) {
+  int best = 1;
+  long long least = 0;
+  for (int s = 1; s <= subs; ++s) {
+    const long long rounds = ((long long)groups * s + sm_count() - 1) / sm_count(), cost = rounds * (dp + (long long)ceil_div(subs, s) * sub);
+    if (s == 1 || cost < least) best = s, least = cost;
+  }
+  return best;
+}
+
 // Sizes and the workspace of a call.
 struct VPlan {
   int R;                         // rows of X and G per token: 2, or 4 for fp32
@@ -773,6 +977,7 @@ struct VPlan {
   size_t part, xe, x2, xp, wp, meta, G, slots, dx, gram, cols, bias, total;
   int gram_count;                // partial sums per example of one piece
   bool gram_way;
+  int short_examples;            // examples that 128 rows of planes hold; 0: longer ones, for the layers' norm kernels
 };
 
 static bool direct_rows(const void* p, long long ld) { return !misaligned(p, 16) && ld % 8 == 0; }
@@ -829,12 +1034,14 @@ static VPlan plan_vocab(const dp_vocab_head& h, int op) {
   take(p.slots, (size_t)2 * (sm_count() / 2) * V_TILE * V_TILE * sizeof(float));
   if (op == 1) {
     if (p.pieces > 1) take(p.dx, (size_t)N * h.d * sizeof(float));
+    p.short_examples = 128 / (p.R * h.T);
     const dp_layer L = piece_layer(h, p, nullptr, nullptr);
     p.gram_way = use_gram(L);
     std::vector<dp_layer> layers(p.piece_subs, L);
     std::vector<int> idx(p.piece_subs), way(p.piece_subs, p.gram_way ? 1 : 0);
     for (int k = 0; k < p.piece_subs; ++k) idx[k] = k;
-    p.gram_count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), p.piece_subs, way.data());
+    if (p.short_examples) p.gram_count = p.piece_subs;
+    else p.gram_count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), p.piece_subs, way.data());
     take(p.gram, (size_t)h.B * p.gram_count * sizeof(float));
     if (!p.gram_way && h.bias && p.R == 2) take(p.cols, (size_t)p.piece_subs * h.B * p.sub * sizeof(float));
   } else if (h.bias) {
@@ -858,7 +1065,9 @@ static int check_head(const dp_vocab_head* h) {
 }
 
 static VHead head_of(const dp_vocab_head& h) {
-  return {h.X, h.W, h.bias, h.labels, h.weights, h.ldx, h.ldw, h.B * h.T, h.T, h.d, h.V, h.dtype == DP_F32};
+  const int f32 = h.dtype == DP_F32, e = f32 ? 4 : 8;
+  const int vec = !misaligned(h.X, 16) && !misaligned(h.W, 16) && h.ldx % e == 0 && h.ldw % e == 0;
+  return {h.X, h.W, h.bias, h.labels, h.weights, h.ldx, h.ldw, h.B * h.T, h.T, h.d, h.V, f32, vec};
 }
 
 struct VRun {                    // a call under way
@@ -1018,7 +1227,7 @@ int dp_vocab_loss(const dp_vocab_head* head, float* loss, float* lse, void* work
   P.labels = h.labels;
   P.part = r.at<float2>(p.part);
   if ((rc = launch_product<V_LSE>(r, P)) != DP_OK) return rc;
-  VOCAB_CUDA(launch_chained(k_vocab_loss, (unsigned)ceil_div(N, 32), 256, 0, r.s, head_of(h), r.at<float2>(p.part), 2 * P.tiles_n,
+  VOCAB_CUDA(launch_chained(k_vocab_loss, (unsigned)ceil_div(N, 8), 256, 0, r.s, head_of(h), r.at<float2>(p.part), 2 * P.tiles_n,
                             loss, lse, status));
   return DP_OK;
 }
@@ -1068,17 +1277,37 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
       P.v0 = v0;
       P.V = h.V;
       P.stride_c = (int)ld_dx;
-      P.slots = r.at<float>(p.slots);
+      P.slots = r.at<float4>(p.slots);
       P.sum = p.pieces > 1 ? r.at<float>(p.dx) : nullptr;
       P.out = dx;
       P.out_bf16 = !f32;
       P.first = s0 == 0;
       P.last = s0 + subs >= p.n_sub;
-      P.vec = !misaligned(dx, 16) && ld_dx % 8 == 0;
+      P.vec = !misaligned(dx, 16) && ld_dx % (f32 ? 4 : 8) == 0 && h.d % 4 == 0;
       P.status = status;
       if ((rc = launch_product<V_DX>(r, P)) != DP_OK) return rc;
     }
-    if (sqnorm) {
+    if (sqnorm && p.short_examples) {
+      NParams Q = {};
+      const long long rows = (long long)N * p.R;
+      if (!encode_rows(&Q.x, r.at<__nv_bfloat16>(p.xe), rows, p.dp, p.dp) || !encode_blocks(&Q.g, G, rows, p.sub, p.sub, subs, block))
+        return DP_ERR_CUDA;
+      Q.rows = p.R * h.T;
+      Q.examples = p.short_examples;
+      Q.B = h.B;
+      Q.groups = ceil_div(h.B, Q.examples);
+      Q.subs = subs;
+      Q.sub = p.sub;
+      Q.dp = p.dp;
+      Q.splits = norm_splits(Q.groups, subs, p.sub, p.dp);
+      Q.bias = h.bias && p.R == 2;
+      Q.partial = r.at<float>(p.gram);
+      Q.status = status;
+      const long long items = (long long)Q.groups * Q.splits;
+      if (items > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
+      VOCAB_CUDA(launch_chained(k_vocab_norms, (unsigned)std::min<long long>(items, sm_count()), N_THREADS, N_SMEM, r.s, Q));
+      if (launch_reduce_partials(Q.partial, h.B, Q.splits, sqnorm, r.s) != cudaSuccess) return DP_ERR_CUDA;
+    } else if (sqnorm) {
       std::vector<dp_layer> layers(subs);
       std::vector<int> idx(subs), way(subs, p.gram_way ? 1 : 0);
       std::vector<ColTaskHost> cols;
@@ -1134,7 +1363,7 @@ int dp_vocab_loss_clipped_accumulate(const dp_vocab_head* head, const float* lse
     P.v0 = v0;
     P.V = h.V;
     P.stride_c = h.d;
-    P.slots = r.at<float>(p.slots);
+    P.slots = r.at<float4>(p.slots);
     P.sum = acc_w;
     P.vec = !misaligned(acc_w, 16) && h.d % 4 == 0;
     P.status = status;

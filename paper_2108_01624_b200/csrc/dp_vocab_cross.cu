@@ -8,13 +8,15 @@
 // from memory into the operands of m16n8k16 products.  A dot product does not mind the order of its terms, so a lane
 // gives 8 neighbouring elements of a row (16 bytes) to the places that two products ask of it, the same for both operands.
 // fp32 rows are split into three bf16 numbers in registers: six products, the smallest first.
-// fp32 sums of 32 elements a step; G is not rounded.
+// fp32 sums; the products drop low bits at every step, so each run of kCrossSeg elements is summed apart.  G is not rounded.
 #include <algorithm>
 
 #include "dp_chain.cuh"
 #include "dp_internal.h"
 
 namespace dpk {
+
+constexpr int kCrossSeg = 256;
 
 struct CrossArgs {
   const void* x;
@@ -129,20 +131,31 @@ __global__ void __launch_bounds__(256) k_vocab_cross(const __grid_constant__ Cro
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int k = 0; k < 4; ++k) cz[j][k] = ck[j][k] = 0.0f;
+    for (int k0 = 0; k0 < a.d; k0 += kCrossSeg) {
+      float sz[NT][4] = {}, sk[NT][4] = {};
+      const int k1 = min(k0 + kCrossSeg, (a.d + 31) / 32 * 32);
 #pragma unroll 2
-    for (int k = 8 * q; k < (a.d + 31) / 32 * 32; k += 32) {
-      R wa, wb, ea, eb;
-      wa.load(a.w, w0, k, a.d, a.vec);
-      wb.load(a.w, w1, k, a.d, a.vec);
-      ea.load(a.e, e0, k, a.d, a.vec);
-      eb.load(a.e, e1, k, a.d, a.vec);
+      for (int k = k0 + 8 * q; k < k1; k += 32) {
+        R wa, wb, ea, eb;
+        wa.load(a.w, w0, k, a.d, a.vec);
+        wb.load(a.w, w1, k, a.d, a.vec);
+        ea.load(a.e, e0, k, a.d, a.vec);
+        eb.load(a.e, e1, k, a.d, a.vec);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        R x;
-        x.load(a.x, (i * a.T + min(t0 + 8 * j + g, a.T - 1)) * a.ldx, k, a.d, a.vec);
-        cross_step(cz[j], wa, wb, x);
-        cross_step(ck[j], ea, eb, x);
+        for (int j = 0; j < NT; ++j) {
+          R x;
+          x.load(a.x, (i * a.T + min(t0 + 8 * j + g, a.T - 1)) * a.ldx, k, a.d, a.vec);
+          cross_step(sz[j], wa, wb, x);
+          cross_step(sk[j], ea, eb, x);
+        }
       }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          cz[j][k] += sz[j][k];
+          ck[j][k] += sk[j][k];
+        }
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
