@@ -38,7 +38,7 @@ constexpr int V_THREADS = 320;                  // warp 0 TMA, warp 1 UMMA issue
 constexpr int V_TILE = 256;                     // rows and columns of a pair's tile; a CTA holds 128 rows of it
 constexpr int V_BOX_BYTES = 128 * 128;          // one copy: 64 bf16 columns of 128 rows, 128-byte swizzle
 constexpr int V_STAGE_COLS = 32;                // GRAD: columns that a warp hands over at a time
-constexpr int V_WARP_STAGE = 32 * 2 * V_STAGE_COLS * 2;   // 32 tokens x 2 planes, 64-byte rows
+constexpr int V_WARP_STAGE = 32 * 2 * V_STAGE_COLS * 2;   // 32 tokens x 2 planes, 64-byte rows; DX, DW: 32 x 32 fp32
 constexpr int V_BIAS_BYTES = 8 * 128 * 4;       // every epilogue warp's 128 bias values
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -59,8 +59,8 @@ struct VCtl {
 };
 
 template <int MODE> constexpr int v_smem() {
-  return 1024 + VForm<MODE>::STAGES * VForm<MODE>::STAGE_BYTES + V_BIAS_BYTES + (MODE == V_GRAD ? 8 * V_WARP_STAGE : 0) +
-         (int)sizeof(VCtl);
+  return 1024 + VForm<MODE>::STAGES * VForm<MODE>::STAGE_BYTES + (MODE == V_LSE ? 0 : 8 * V_WARP_STAGE) +
+         (VForm<MODE>::KMAJOR_B ? V_BIAS_BYTES : 0) + (int)sizeof(VCtl);
 }
 static_assert(v_smem<V_LSE>() <= 232448 && v_smem<V_GRAD>() <= 232448 && v_smem<V_DX>() <= 232448, "over a CTA's shared memory");
 
@@ -92,24 +92,43 @@ struct alignas(64) VParams {
 
 struct VWork { int tile, j0, j1; };
 
-// What the pair does next: whole tiles in turn (LSE, GRAD), or its share of the line of all tiles' K blocks (DX, DW).
+// What the pair does next.  LSE, GRAD: whole tiles in turn.  DX, DW: whole tiles in turn while there is one for every pair;
+// the K blocks of the tiles that are left, laid end to end, are shared evenly.
+struct VShare {
+  long long lo, hi, pos;         // this pair's part of that line
+  int tile, whole;               // next whole tile, and how many of them there are
+};
+__host__ __device__ __forceinline__ long long share_begin(long long total, int units, int u) { return total * u / units; }
+__host__ __device__ __forceinline__ int whole_tiles(int mode, int tiles, int units) {
+  return mode == V_LSE || mode == V_GRAD ? tiles : tiles / units * units;
+}
 template <int MODE>
-__device__ __forceinline__ bool next_work(const VParams& P, long long& pos, long long hi, VWork& w) {
+__device__ __forceinline__ VShare share_of(const VParams& P, int unit) {
+  const int tiles = P.tiles_m * P.tiles_n;
+  VShare s;
+  s.whole = whole_tiles(MODE, tiles, P.units);
+  s.tile = unit;
+  const long long line = (long long)(tiles - s.whole) * P.n_pairs * P.kb;
+  s.lo = s.pos = share_begin(line, P.units, unit);
+  s.hi = share_begin(line, P.units, unit + 1);
+  return s;
+}
+template <int MODE>
+__device__ __forceinline__ bool next_work(const VParams& P, VShare& s, VWork& w) {
   const int nkb = P.n_pairs * P.kb;
-  if (pos >= hi) return false;
-  if (MODE == V_LSE || MODE == V_GRAD) {
-    w = {(int)pos, 0, nkb};
-    pos += P.units;
+  if (s.tile < s.whole) {
+    w = {s.tile, 0, nkb};
+    s.tile += P.units;
     return true;
   }
-  w.tile = (int)(pos / nkb);
-  w.j0 = (int)(pos - (long long)w.tile * nkb);
-  const long long end = (long long)(w.tile + 1) * nkb < hi ? (long long)(w.tile + 1) * nkb : hi;
-  w.j1 = w.j0 + (int)(end - pos);
-  pos = end;
+  if (MODE == V_LSE || MODE == V_GRAD || s.pos >= s.hi) return false;
+  const long long t = s.pos / nkb, end = (t + 1) * nkb < s.hi ? (t + 1) * nkb : s.hi;
+  w.tile = s.whole + (int)t;
+  w.j0 = (int)(s.pos - t * nkb);
+  w.j1 = w.j0 + (int)(end - s.pos);
+  s.pos = end;
   return true;
 }
-__host__ __device__ __forceinline__ long long share_begin(long long total, int units, int u) { return total * u / units; }
 
 template <int MODE>
 __device__ __forceinline__ void tile_origin(const VParams& P, int tile, int& m0, int& n0) {
@@ -315,9 +334,9 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
   using F = VForm<MODE>;
   constexpr int STAGES = F::STAGES;
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* staging = tiles + STAGES * F::STAGE_BYTES;                      // GRAD only
-  float* bias_s = reinterpret_cast<float*>(staging + (MODE == V_GRAD ? 8 * V_WARP_STAGE : 0));
-  VCtl* S = reinterpret_cast<VCtl*>(reinterpret_cast<uint8_t*>(bias_s) + V_BIAS_BYTES);
+  uint8_t* staging = tiles + STAGES * F::STAGE_BYTES;                      // not LSE
+  float* bias_s = reinterpret_cast<float*>(staging + (MODE == V_LSE ? 0 : 8 * V_WARP_STAGE));      // LSE, GRAD
+  VCtl* S = reinterpret_cast<VCtl*>(reinterpret_cast<uint8_t*>(bias_s) + (F::KMAJOR_B ? V_BIAS_BYTES : 0));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &S->abort;
   const int rank = (int)cluster_ctarank(), unit = (int)cluster_id_x();
@@ -335,12 +354,8 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
   cluster_sync_all();           // the peer's barriers are initialised before anyone signals them
   tc_fence_after();
   const uint32_t tmem_base = S->tmem_base;
-  const long long tiles_all = (long long)P.tiles_m * P.tiles_n;
-  const bool whole = MODE == V_LSE || MODE == V_GRAD;
-  const long long line = whole ? tiles_all : tiles_all * P.n_pairs * P.kb;
-  const long long lo = whole ? unit : share_begin(line, P.units, unit);
-  const long long hi = whole ? line : share_begin(line, P.units, unit + 1);
-  long long pos = lo;
+  constexpr bool whole = MODE == V_LSE || MODE == V_GRAD;
+  VShare share = share_of<MODE>(P, unit);
   VWork w;
 
   if (warp == 0) {
@@ -348,7 +363,7 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
       uint32_t it = 0;
       bool alive = true;
       const uint32_t tx = (uint32_t)(F::HALF_BYTES + (!F::KMAJOR_B && P.nt == 128 ? V_BOX_BYTES : F::HALF_BYTES));
-      while (alive && next_work<MODE>(P, pos, hi, w)) {
+      while (alive && next_work<MODE>(P, share, w)) {
         int m0, n0;
         tile_origin<MODE>(P, w.tile, m0, n0);
         for (int j = w.j0; j < w.j1; ++j, ++it) {
@@ -368,7 +383,7 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
     if (lane == 0 && rank == 1) {   // ---------------- odd CTA: forward "stage landed" to the issuer ----------------
       uint32_t it = 0;
       bool alive = true;
-      while (alive && next_work<MODE>(P, pos, hi, w)) {
+      while (alive && next_work<MODE>(P, share, w)) {
         for (int j = w.j0; j < w.j1; ++j, ++it) {
           const uint32_t slot = it % STAGES, ph = (it / STAGES) & 1u;
           if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 62, (int)it)) { alive = false; break; }
@@ -379,7 +394,7 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
       const uint32_t idesc = idesc_bf16_f32(256, P.nt, !F::KMAJOR_A, !F::KMAJOR_B);
       uint32_t it = 0, part = 0;
       bool alive = true;
-      while (alive && next_work<MODE>(P, pos, hi, w)) {
+      while (alive && next_work<MODE>(P, share, w)) {
         for (int j0 = w.j0; j0 < w.j1 && alive; j0 += P.seg, ++part) {
           const int j1 = j0 + P.seg < w.j1 ? j0 + P.seg : w.j1;
           const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
@@ -418,7 +433,7 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
     uint8_t* stage = staging + (warp - 2) * V_WARP_STAGE;
     uint32_t part = 0;
     bool alive = true;
-    while (next_work<MODE>(P, pos, hi, w)) {
+    while (next_work<MODE>(P, share, w)) {
       int m0, n0;
       tile_origin<MODE>(P, w.tile, m0, n0);
       const int m0w = m0 + 128 * rank + 32 * q, m = m0w + lane, col = h * half;
@@ -463,7 +478,7 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
         finish_grad(P, acc, bias_w, stage, meta, m0w, n0, col, lane);
       } else {
         const bool shared_tile = w.j0 != 0 || w.j1 != P.n_pairs * P.kb;
-        const int slot = 2 * unit + ((long long)w.tile * (P.n_pairs * P.kb) > lo ? 1 : 0);
+        const int slot = 2 * unit + ((long long)(w.tile - share.whole) * (P.n_pairs * P.kb) > share.lo ? 1 : 0);
 #pragma unroll
         for (int ch = 0; ch < 4; ++ch) {
           if (ch * 32 >= half) continue;
@@ -473,13 +488,20 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
               to[(j / 4) * V_TILE] = make_float4(acc[ch * 32 + j], acc[ch * 32 + j + 1], acc[ch * 32 + j + 2], acc[ch * 32 + j + 3]);
-          } else {
+          } else {                              // turned in shared memory: a warp writes 128 bytes of 4 rows at a time
+            float4* mine = reinterpret_cast<float4*>(stage + lane * 128);
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              const float4 v = make_float4(acc[ch * 32 + j], acc[ch * 32 + j + 1], acc[ch * 32 + j + 2], acc[ch * 32 + j + 3]);
-              if constexpr (MODE == V_DX) put_dx(P, m, c + j, v);
-              else put_dw(P, m, c + j, v);
+            for (int j = 0; j < 8; ++j)
+              mine[j ^ (lane & 7)] = make_float4(acc[ch * 32 + 4 * j], acc[ch * 32 + 4 * j + 1], acc[ch * 32 + 4 * j + 2], acc[ch * 32 + 4 * j + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int r = 4 * j + (lane >> 3), g = lane & 7;
+              const float4 v = reinterpret_cast<const float4*>(stage + r * 128)[g ^ (r & 7)];
+              if constexpr (MODE == V_DX) put_dx(P, m0w + r, c + 4 * g, v);
+              else put_dw(P, m0w + r, c + 4 * g, v);
             }
+            __syncwarp();
           }
         }
       }
@@ -496,38 +518,33 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
   }
 }
 
-// The tiles of a DX or DW launch that several pairs shared: their parts are added in the pairs' order.  Block (u, r): the
-// tile that begins inside or before unit u's share and goes on into it, rows [16 r, +16); a tile is handled by the
-// first unit that continues it.  A warp: 4 rows, 8 groups of four columns (64 bytes of a slot, 128 of a result at a time).
+// The tiles of a DX or DW launch that several pairs shared: their parts are added in the pairs' order.  Block (t, r): tile t
+// of those that were shared, rows [16 (r / 4), +16), columns [64 (r % 4), +64).  A warp: 4 rows, 8 groups of four columns
+// (64 bytes of a slot, 128 of a result at a time).
 template <int MODE>
 __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VParams P) {
   wait_for_predecessor();
   let_successor_in();
-  const int nkb = P.n_pairs * P.kb;
-  const long long line = (long long)P.tiles_m * P.tiles_n * nkb;
-  const int u0 = blockIdx.x + 1;
-  const long long lo = share_begin(line, P.units, u0);
-  const long long tile = lo / nkb, begin = tile * nkb;
-  if (lo == begin || lo >= line) return;                          // a unit that begins with a tile of its own
-  if (share_begin(line, P.units, u0 - 1) > begin) return;         // an earlier unit continues this tile already
+  const int nkb = P.n_pairs * P.kb, tiles = P.tiles_m * P.tiles_n, whole = whole_tiles(MODE, tiles, P.units);
+  const long long line = (long long)(tiles - whole) * nkb, begin = (long long)blockIdx.x * nkb;
+  // block x of the line is in the share of unit ((x + 1) * units - 1) / line: units u0 .. last have a part of the tile
+  const int u0 = (int)(((begin + 1) * P.units - 1) / line), last = (int)(((begin + nkb) * P.units - 1) / line);
+  if (last == u0) return;                                         // one unit had it all, and has written it
   int m0, n0;
-  tile_origin<MODE>(P, (int)tile, m0, n0);
+  tile_origin<MODE>(P, whole + (int)blockIdx.x, m0, n0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = blockIdx.y * 16 + (warp & 3) * 4 + (lane & 3);
-  int last = u0;                                                  // units u0 - 1 .. last have a part
-  while (last + 1 < P.units && share_begin(line, P.units, last + 1) < begin + nkb) ++last;
-  const int first_slot = 2 * (u0 - 1) + (begin > share_begin(line, P.units, u0 - 1) ? 1 : 0);
-  for (int g = (warp >> 2) * 8 + (lane >> 2); g < P.nt / 4; g += 16) {
-    const size_t at = (size_t)g * V_TILE + r;
-    float4 v = P.slots[(size_t)first_slot * (V_TILE / 4) * V_TILE + at];
-#pragma unroll 4
-    for (int u = u0; u <= last; ++u) {                            // the tile is the first of these units' shares
-      const float4 x = P.slots[(size_t)(2 * u) * (V_TILE / 4) * V_TILE + at];
-      v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
-    }
-    if constexpr (MODE == V_DX) put_dx(P, m0 + r, n0 + 4 * g, v);
-    else put_dw(P, m0 + r, n0 + 4 * g, v);
+  const int r = (blockIdx.y >> 2) * 16 + (warp & 3) * 4 + (lane & 3), g = (blockIdx.y & 3) * 16 + (warp >> 2) * 8 + (lane >> 2);
+  if (g >= P.nt / 4) return;
+  const int first_slot = 2 * u0 + (begin > share_begin(line, P.units, u0) ? 1 : 0);
+  const size_t at = (size_t)g * V_TILE + r;
+  float4 v = P.slots[(size_t)first_slot * (V_TILE / 4) * V_TILE + at];
+#pragma unroll 8
+  for (int u = u0 + 1; u <= last; ++u) {                          // the tile is the first of these units' shares
+    const float4 x = P.slots[(size_t)(2 * u) * (V_TILE / 4) * V_TILE + at];
+    v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
   }
+  if constexpr (MODE == V_DX) put_dx(P, m0 + r, n0 + 4 * g, v);
+  else put_dw(P, m0 + r, n0 + 4 * g, v);
 }
 
 // =================================================================================================
@@ -953,7 +970,10 @@ static bool encode_blocks(CUtensorMap* map, const void* base, long long rows, in
 }
 
 constexpr int kSubColumns = 2048;               // columns of one block of G, at most
-constexpr size_t kPieceBytes = (size_t)256 << 20;   // G of one piece, unless one block alone is larger
+#ifndef DP_VOCAB_PIECE_MB
+#define DP_VOCAB_PIECE_MB 1024
+#endif
+constexpr size_t kPieceBytes = (size_t)DP_VOCAB_PIECE_MB << 20;   // G of one piece, unless one block alone is larger
 
 // How many CTAs share a group's blocks of G: each forms the Gram of X again, so as few as fill the device well, by the
 // columns that the longest-working CTA sums.
@@ -1127,8 +1147,9 @@ static int launch_product(const VRun& r, VParams& P) {
   else P.units = share_units(line);
   VOCAB_CUDA(launch_chained(k_vocab_gemm<MODE>, Pairs{(unsigned)P.units}, V_THREADS, v_smem<MODE>(), r.s, P));
   if constexpr (MODE == V_DX || MODE == V_DW) {
-    if (P.units > 1)
-      VOCAB_CUDA(launch_chained(k_vocab_join<MODE>, dim3((unsigned)P.units - 1, V_TILE / 16), 256, 0, r.s, P));
+    const int shared = (int)tiles - whole_tiles(MODE, (int)tiles, P.units);
+    if (P.units > 1 && shared)
+      VOCAB_CUDA(launch_chained(k_vocab_join<MODE>, dim3((unsigned)shared, V_TILE / 16 * 4), 256, 0, r.s, P));
   }
   return DP_OK;
 }
