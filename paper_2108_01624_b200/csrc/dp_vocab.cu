@@ -34,33 +34,33 @@ using namespace ptx;
 
 enum : int { V_LSE = 0, V_GRAD = 1, V_DX = 2, V_DW = 3 };
 
-constexpr int V_THREADS = 320;                  // warp 0 TMA, warp 1 UMMA issue (or forwarding), warps 2..9 epilogue
+constexpr int V_THREADS = 320;                  // warp 0 TMA, warp 1 UMMA issue (even CTA), warps 2..9 epilogue
 constexpr int V_TILE = 256;                     // rows and columns of a pair's tile; a CTA holds 128 rows of it
 constexpr int V_BOX_BYTES = 128 * 128;          // one copy: 64 bf16 columns of 128 rows, 128-byte swizzle
 constexpr int V_STAGE_COLS = 32;                // GRAD: columns that a warp hands over at a time
 constexpr int V_WARP_STAGE = 32 * 2 * V_STAGE_COLS * 2;   // 32 tokens x 2 planes, 64-byte rows; DX, DW: 32 x 32 fp32
-constexpr int V_BIAS_BYTES = 8 * 128 * 4;       // every epilogue warp's 128 bias values
 constexpr float kLog2e = 1.4426950408889634f;
 
 // K columns (or rows) of a stage and stages in flight.
 template <int MODE> struct VForm {
   static constexpr bool KMAJOR_A = MODE != V_DW;               // rows of A are tokens with K contiguous
   static constexpr bool KMAJOR_B = MODE == V_LSE || MODE == V_GRAD;
-  static constexpr int BK = KMAJOR_B ? 64 : 128;
-  static constexpr int STAGES = MODE == V_LSE ? 6 : MODE == V_GRAD ? 5 : 3;
+  static constexpr int BK = 128;
+  static constexpr int STAGES = 3;
   static constexpr int HALF_BYTES = BK / 64 * V_BOX_BYTES;     // 128 rows (columns) of one operand
   static constexpr int STAGE_BYTES = 2 * HALF_BYTES;
+  // an epilogue warp's own: 128 bias values; 32 columns of G; 32 x 32 results
+  static constexpr int WARP_BYTES = MODE == V_LSE ? 128 * 4 : V_WARP_STAGE;
 };
 
 struct VCtl {
-  uint64_t full[6], empty[6], ready[6], tmem_full[2], tmem_empty[2], drain;
+  uint64_t full[3], empty[3], tmem_full[2], tmem_empty[2], drain;   // full, tmem_empty: the even CTA's count for the pair
   uint32_t tmem_base;
   int abort;
 };
 
 template <int MODE> constexpr int v_smem() {
-  return 1024 + VForm<MODE>::STAGES * VForm<MODE>::STAGE_BYTES + (MODE == V_LSE ? 0 : 8 * V_WARP_STAGE) +
-         (VForm<MODE>::KMAJOR_B ? V_BIAS_BYTES : 0) + (int)sizeof(VCtl);
+  return 1024 + VForm<MODE>::STAGES * VForm<MODE>::STAGE_BYTES + 8 * VForm<MODE>::WARP_BYTES + (int)sizeof(VCtl);
 }
 static_assert(v_smem<V_LSE>() <= 232448 && v_smem<V_GRAD>() <= 232448 && v_smem<V_DX>() <= 232448, "over a CTA's shared memory");
 
@@ -78,10 +78,10 @@ struct alignas(64) VParams {
   int v0, V;                     // first vocabulary entry of the piece, entries in all
   int planes2;                   // GRAD: store rows 2, 3 of a token too (fp32 X: two planes)
   int stride_c;                  // leading dimension of the output is stride_c (DX, DW)
-  const float* bias;             // LSE, GRAD: [V] or null
+  const float* bias;             // LSE: [V] or null; GRAD: [columns of all blocks], -inf beyond V
   const int32_t* labels;         // LSE
-  const float4* meta;            // GRAD: lse, scale, G at the label, label (bits) of every token
-  float2* part;                  // LSE: [2 tiles_n][M] maximum and sum
+  const float4* meta;            // GRAD: of every token lse log2e, rounded, and scale over what it was rounded by; G at the label; label (bits)
+  float2* part;                  // LSE: [2 tiles_n][M] maximum times log2e, and sum
   float* bias_part;              // GRAD: [rows of 32 tokens][columns of the piece] column sums, or null
   float4* slots;                 // DX, DW: tiles that several pairs share, [2 units][64 groups of four columns][256 rows]
   float* sum;                    // DX: fp32 sums over the pieces [M, N]; DW: the accumulator
@@ -143,12 +143,62 @@ __device__ __forceinline__ void tile_origin(const VParams& P, int tile, int& m0,
   n0 *= P.nt;
 }
 
+// What a token without a loss has for `meta`: powers 2^-inf.
+#define kNoToken make_float4(INFINITY, 0.0f, 0.0f, __int_as_float(-1))
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
+// Two fp32 numbers in one instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float x, float y) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(f32x2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// Copies of a CTA pair: the data go to this CTA's shared memory, the completion to a barrier of the even CTA (its address in
+// the cluster's window).
+__device__ __forceinline__ uint32_t in_even_cta(uint64_t* bar) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(bar)));
+  return a;
+}
+__device__ __forceinline__ void pair_load2(uint8_t* dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void pair_load3(uint8_t* dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
 __device__ __forceinline__ void load2(uint8_t* dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
@@ -166,79 +216,86 @@ __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.w
 
 // Copies of K block j of a tile into a stage: this CTA's 128 rows of A and its half of the columns of B.
 template <int MODE>
-__device__ __forceinline__ void load_block(const VParams& P, uint8_t* st, uint64_t* bar, int j, int m0, int n0, int rank) {
+__device__ __forceinline__ void load_block(const VParams& P, uint8_t* st, uint32_t bar, int j, int m0, int n0, int rank) {
   using F = VForm<MODE>;
   const int pair = j / P.kb, k = (j - pair * P.kb) * F::BK;
   const CUtensorMap *a = &P.a[P.pa[pair]], *b = &P.b[P.pb[pair]];
   const int m = m0 + 128 * rank, n = n0 + (P.nt >> 1) * rank;
   uint8_t* sb = st + F::HALF_BYTES;
   if (MODE == V_LSE || MODE == V_GRAD) {
-    load2(st, a, bar, k, m);
-    load2(sb, b, bar, k, n);
+    pair_load2(st, a, bar, k, m);
+    pair_load2(st + V_BOX_BYTES, a, bar, k + 64, m);
+    pair_load2(sb, b, bar, k, n);
+    pair_load2(sb + V_BOX_BYTES, b, bar, k + 64, n);
   } else if (MODE == V_DX) {                    // A: columns of G, block by block; B: rows of W
     const int z = k / P.sub, x = k - z * P.sub;
-    tma_load_3d(st, a, bar, x, m, z);
-    tma_load_3d(st + V_BOX_BYTES, a, bar, x + 64, m, z);
-    load2(sb, b, bar, n, P.v0 + k);
-    if (P.nt == 256) load2(sb + V_BOX_BYTES, b, bar, n + 64, P.v0 + k);
+    pair_load3(st, a, bar, x, m, z);
+    pair_load3(st + V_BOX_BYTES, a, bar, x + 64, m, z);
+    pair_load2(sb, b, bar, n, P.v0 + k);
+    if (P.nt == 256) pair_load2(sb + V_BOX_BYTES, b, bar, n + 64, P.v0 + k);
   } else {                                      // A: rows of G; B: rows of X
     const int z = m / P.sub, x = m - z * P.sub;
-    tma_load_3d(st, a, bar, x, k, z);
-    tma_load_3d(st + V_BOX_BYTES, a, bar, x + 64, k, z);
-    load2(sb, b, bar, n, k);
-    if (P.nt == 256) load2(sb + V_BOX_BYTES, b, bar, n + 64, k);
+    pair_load3(st, a, bar, x, k, z);
+    pair_load3(st + V_BOX_BYTES, a, bar, x + 64, k, z);
+    pair_load2(sb, b, bar, n, k);
+    if (P.nt == 256) pair_load2(sb + V_BOX_BYTES, b, bar, n + 64, k);
   }
 }
 
-// Row maximum and sum of exponentials over this thread's 128 columns of logits, the label's left out.
-__device__ __forceinline__ void finish_lse(const VParams& P, float (&z)[128], const float* bias, int m, int n0, int col, int label) {
+// Exponentials are powers of two: exp(z - m) = 2^(z log2e - top) with top = m log2e rounded to fp32, one fma and one
+// rounding an element, and what top was rounded by in a factor of the row.
+
+// Maximum (as `top`) and sum of powers over this thread's 128 columns of logits, the label's left out.
+__device__ __forceinline__ void finish_lse(const VParams& P, f32x2 (&z)[64], int m, int n0, int col, int label) {
   const int rel = label - (n0 + col);
-  const bool here = (unsigned)rel < 128u;
+  if (__any_sync(0xffffffffu, (unsigned)rel < 128u)) {
 #pragma unroll
-  for (int j = 0; j < 128; j += 4) {
-    const float4 b = *reinterpret_cast<const float4*>(bias + j);
-    z[j] += b.x;
-    z[j + 1] += b.y;
-    z[j + 2] += b.z;
-    z[j + 3] += b.w;
+    for (int j = 0; j < 64; ++j) {
+      const float2 v = unpack2(z[j]);
+      z[j] = pack2(rel == 2 * j ? -INFINITY : v.x, rel == 2 * j + 1 ? -INFINITY : v.y);
+    }
   }
-  if (__any_sync(0xffffffffu, here)) {
+  float high[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int j = 0; j < 128; ++j) z[j] = rel == j ? -INFINITY : z[j];
+  for (int j = 0; j < 64; ++j) {
+    const float2 v = unpack2(z[j]);
+    high[j & 3] = fmaxf(high[j & 3], fmaxf(v.x, v.y));
   }
-  float top[4] = {z[0], z[1], z[2], z[3]};
+  const float top = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])) * kLog2e;
+  const float base = top == -INFINITY ? 0.0f : -top;        // a row of -inf keeps powers of -inf: 0
+  const f32x2 k2 = pack2(kLog2e, kLog2e), base2 = pack2(base, base);
+  f32x2 s[2] = {0ull, 0ull};
 #pragma unroll
-  for (int j = 4; j < 128; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
-  const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-  const float base = most == -INFINITY ? 0.0f : most;       // a row of -inf keeps exponentials of -inf: 0
-  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int j = 0; j < 128; ++j) s[j & 3] += ex2((z[j] - base) * kLog2e);
-  if (m < P.M) P.part[(size_t)((n0 + col) >> 7) * P.M + m] = make_float2(most, (s[0] + s[1]) + (s[2] + s[3]));
+  for (int j = 0; j < 64; ++j) {
+    const float2 e = unpack2(fma2(z[j], k2, base2));
+    s[j & 1] = add2(s[j & 1], pack2(ex2(e.x), ex2(e.y)));
+  }
+  const float2 sum = unpack2(add2(s[0], s[1]));
+  if (m < P.M) P.part[(size_t)((n0 + col) >> 7) * P.M + m] = make_float2(top, sum.x + sum.y);
 }
 
 // G of this thread's 128 columns: two planes through shared memory, 32 columns at a time, and the warp's column sums.
-__device__ __forceinline__ void finish_grad(const VParams& P, float (&z)[128], const float* bias, uint8_t* stage, float4 meta,
-                                            int m0w, int n0, int col, int lane) {
-  const int label = __float_as_int(meta.w), rel = label - (P.v0 + n0 + col);
-  const bool live = label >= 0;
+__device__ __forceinline__ void finish_grad(const VParams& P, f32x2 (&z)[64], uint8_t* stage, float4 meta, int m0w, int n0, int col,
+                                            int lane) {
+  const int rel = __float_as_int(meta.w) - (P.v0 + n0 + col);     // no label: -1, never in range
+  const bool labelled = __float_as_int(meta.w) >= 0;
   const int at = n0 + col, z4 = at / P.sub, x4 = at - z4 * P.sub;
+  const f32x2 k2 = pack2(kLog2e, kLog2e), base2 = pack2(-meta.x, -meta.x), scale2 = pack2(meta.y, meta.y), minus2 = pack2(-1.0f, -1.0f);
 #pragma unroll
   for (int ch = 0; ch < 4; ++ch) {
-    float g[32];
+    f32x2 g[16];
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      const float4 b = *reinterpret_cast<const float4*>(bias + ch * 32 + j);
-      const float bb[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float p = meta.y * ex2((z[ch * 32 + j + u] + bb[u] - meta.x) * kLog2e);
-        g[j + u] = live ? p : 0.0f;
-      }
+    for (int j = 0; j < 16; ++j) {
+      const float2 e = unpack2(fma2(z[ch * 16 + j], k2, base2));
+      g[j] = mul2(pack2(ex2(e.x), ex2(e.y)), scale2);
     }
-    if (__any_sync(0xffffffffu, live && (unsigned)(rel - ch * 32) < 32u)) {
+    if (__any_sync(0xffffffffu, labelled && (unsigned)(rel - ch * 32) < 32u)) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) g[j] = live && rel == ch * 32 + j ? meta.z : g[j];
+      for (int j = 0; j < 16; ++j) {
+        const float2 v = unpack2(g[j]);
+        const int r = labelled ? rel - ch * 32 - 2 * j : -1;
+        g[j] = pack2(r == 0 ? meta.z : v.x, r == 1 ? meta.z : v.y);
+      }
     }
     if (lane == 0) store_wait_read();           // the copy of the chunk before has left the staging rows
     __syncwarp();
@@ -247,10 +304,12 @@ __device__ __forceinline__ void finish_grad(const VParams& P, float (&z)[128], c
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const float x = g[c * 8 + 2 * u], y = g[c * 8 + 2 * u + 1];
-        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        const float2 v = unpack2(g[c * 4 + u]);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
         hi[u] = *reinterpret_cast<const uint32_t*>(&h);
-        const __nv_bfloat162 l = __floats2bfloat162_rn(x - __uint_as_float(hi[u] << 16), y - __uint_as_float(hi[u] & 0xffff0000u));
+        const f32x2 back = pack2(__uint_as_float(hi[u] << 16), __uint_as_float(hi[u] & 0xffff0000u));
+        const float2 left = unpack2(fma2(back, minus2, g[c * 4 + u]));
+        const __nv_bfloat162 l = __floats2bfloat162_rn(left.x, left.y);
         lo[u] = *reinterpret_cast<const uint32_t*>(&l);
       }
       uint8_t* p = stage + lane * 128 + ((c ^ (lane & 3)) << 4);       // 64-byte swizzle: rows 2 lane and 2 lane + 1
@@ -267,16 +326,23 @@ __device__ __forceinline__ void finish_grad(const VParams& P, float (&z)[128], c
     if (P.bias_part) {
       // sum over the warp's 32 tokens: at every step a lane keeps half of its columns and hands the others over, so
       // that lane l ends with column l
+      float s[32];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float2 v = unpack2(g[j]);
+        s[2 * j] = v.x;
+        s[2 * j + 1] = v.y;
+      }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
         const bool up = lane & o;
 #pragma unroll
         for (int j = 0; j < o; ++j) {
-          const float keep = up ? g[j + o] : g[j], give = up ? g[j] : g[j + o];
-          g[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+          const float keep = up ? s[j + o] : s[j], give = up ? s[j] : s[j + o];
+          s[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
         }
       }
-      P.bias_part[(size_t)(m0w >> 5) * P.N + at + ch * 32 + lane] = g[0];
+      P.bias_part[(size_t)(m0w >> 5) * P.N + at + ch * 32 + lane] = s[0];
     }
   }
 }
@@ -334,15 +400,14 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
   using F = VForm<MODE>;
   constexpr int STAGES = F::STAGES;
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* staging = tiles + STAGES * F::STAGE_BYTES;                      // not LSE
-  float* bias_s = reinterpret_cast<float*>(staging + (MODE == V_LSE ? 0 : 8 * V_WARP_STAGE));      // LSE, GRAD
-  VCtl* S = reinterpret_cast<VCtl*>(reinterpret_cast<uint8_t*>(bias_s) + (F::KMAJOR_B ? V_BIAS_BYTES : 0));
+  uint8_t* staging = tiles + STAGES * F::STAGE_BYTES;
+  VCtl* S = reinterpret_cast<VCtl*>(staging + 8 * F::WARP_BYTES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &S->abort;
   const int rank = (int)cluster_ctarank(), unit = (int)cluster_id_x();
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(&S->full[s], 1); mbar_init(&S->empty[s], 1); mbar_init(&S->ready[s], 1); }
+    for (int s = 0; s < STAGES; ++s) { mbar_init(&S->full[s], 1); mbar_init(&S->empty[s], 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(&S->tmem_full[b], 1); mbar_init(&S->tmem_empty[b], 16); }
     mbar_init(&S->drain, 1);
     S->abort = 0;
@@ -362,35 +427,27 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
     if (lane == 0) {   // ---------------- TMA producer (each CTA, its own halves) ----------------
       uint32_t it = 0;
       bool alive = true;
-      const uint32_t tx = (uint32_t)(F::HALF_BYTES + (!F::KMAJOR_B && P.nt == 128 ? V_BOX_BYTES : F::HALF_BYTES));
+      const uint32_t tx = 2u * (uint32_t)(F::HALF_BYTES + (!F::KMAJOR_B && P.nt == 128 ? V_BOX_BYTES : F::HALF_BYTES));   // of both CTAs
       while (alive && next_work<MODE>(P, share, w)) {
         int m0, n0;
         tile_origin<MODE>(P, w.tile, m0, n0);
         for (int j = w.j0; j < w.j1; ++j, ++it) {
           const uint32_t slot = it % STAGES, ph = (it / STAGES) & 1u;
           if (!mbar_wait(&S->empty[slot], ph ^ 1u, abort_flag, P.status, 61, (int)it)) { alive = false; break; }
-          mbar_arrive_expect_tx(&S->full[slot], tx);
-          load_block<MODE>(P, tiles + slot * F::STAGE_BYTES, &S->full[slot], j, m0, n0, rank);
+          if (rank == 0) mbar_arrive_expect_tx(&S->full[slot], tx);
+          load_block<MODE>(P, tiles + slot * F::STAGE_BYTES, in_even_cta(&S->full[slot]), j, m0, n0, rank);
         }
       }
+      // Every copy of the pair has landed before either CTA's shared memory is released (the odd CTA waits for the even one
+      // at the end).
       const uint32_t pending = it < (uint32_t)STAGES ? it : (uint32_t)STAGES;
-      for (uint32_t k = 0; k < pending; ++k) {
+      for (uint32_t k = 0; rank == 0 && k < pending; ++k) {
         const uint32_t j = it - 1 - k;
         mbar_wait_drain(&S->full[j % STAGES], (j / STAGES) & 1u, P.status);
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 1) {   // ---------------- odd CTA: forward "stage landed" to the issuer ----------------
-      uint32_t it = 0;
-      bool alive = true;
-      while (alive && next_work<MODE>(P, share, w)) {
-        for (int j = w.j0; j < w.j1; ++j, ++it) {
-          const uint32_t slot = it % STAGES, ph = (it / STAGES) & 1u;
-          if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 62, (int)it)) { alive = false; break; }
-          mbar_arrive_cluster(&S->ready[slot], 0u);
-        }
-      }
-    } else if (lane == 0) {   // ---------------- even CTA: UMMA issuer ----------------
+    if (lane == 0 && rank == 0) {   // ---------------- UMMA issuer (even CTA only) ----------------
       const uint32_t idesc = idesc_bf16_f32(256, P.nt, !F::KMAJOR_A, !F::KMAJOR_B);
       uint32_t it = 0, part = 0;
       bool alive = true;
@@ -403,18 +460,14 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
           const uint32_t d_tmem = tmem_base + buf * 256u;
           for (int j = j0; j < j1; ++j, ++it) {
             const uint32_t slot = it % STAGES, ph = (it / STAGES) & 1u;
-            if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 64, (int)it) ||
-                !mbar_wait(&S->ready[slot], ph, abort_flag, P.status, 65, (int)it)) {
-              alive = false;
-              break;
-            }
+            if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 64, (int)it)) { alive = false; break; }
             tc_fence_after();
             const uint32_t am = smem_u32(tiles + slot * F::STAGE_BYTES), an = am + F::HALF_BYTES;
 #pragma unroll
             for (int k = 0; k < F::BK / 16; ++k) {
               const uint64_t ad = F::KMAJOR_A ? smem_desc_sw128(am + (k >> 2) * V_BOX_BYTES + (k & 3) * 32, 16, 1024)
                                               : smem_desc_sw128(am + k * 2048, V_BOX_BYTES, 1024);
-              const uint64_t bd = F::KMAJOR_B ? smem_desc_sw128(an + k * 32, 16, 1024)
+              const uint64_t bd = F::KMAJOR_B ? smem_desc_sw128(an + (k >> 2) * V_BOX_BYTES + (k & 3) * 32, 16, 1024)
                                               : smem_desc_sw128(an + k * 2048, V_BOX_BYTES, 1024);
               umma_bf16_pair(d_tmem, ad, bd, idesc, (j > j0 || k > 0) ? 1u : 0u);
             }
@@ -429,29 +482,43 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
   } else {   // ---------------- epilogue warps 2..9: lanes [32 q, +32), columns [h nt/2, +nt/2) ----------------
     const int q = warp & 3, h = warp >= 6 ? 1 : 0;
     const int half = P.nt >> 1;
-    float* bias_w = bias_s + (warp - 2) * 128;
-    uint8_t* stage = staging + (warp - 2) * V_WARP_STAGE;
+    uint8_t* stage = staging + (warp - 2) * F::WARP_BYTES;
     uint32_t part = 0;
     bool alive = true;
     while (next_work<MODE>(P, share, w)) {
       int m0, n0;
       tile_origin<MODE>(P, w.tile, m0, n0);
       const int m0w = m0 + 128 * rank + 32 * q, m = m0w + lane, col = h * half;
-      float4 meta = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+      float4 meta = kNoToken;
       int label = -1;
       if (MODE == V_LSE && m < P.M) label = P.labels[m];
       if (MODE == V_GRAD && m < P.M) meta = P.meta[m];
-      if (whole) {
+      // The sums start from the bias: -inf beyond the vocabulary, which has no weight in a sum and is zero in G.
+      const float* bias_w = nullptr;
+      if (MODE == V_LSE) {
+        float* own = reinterpret_cast<float*>(stage);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {           // -inf beyond the vocabulary: no weight in a sum, zero in G
-          const int v = P.v0 + n0 + col + 32 * k + lane;
-          bias_w[32 * k + lane] = v >= P.V ? -INFINITY : P.bias ? P.bias[v] : 0.0f;
+        for (int k = 0; k < 4; ++k) {
+          const int v = n0 + col + 32 * k + lane;
+          own[32 * k + lane] = v >= P.V ? -INFINITY : P.bias ? P.bias[v] : 0.0f;
         }
         __syncwarp();
+        bias_w = own;
+      } else if (MODE == V_GRAD) {
+        bias_w = P.bias + P.v0 + n0 + col;      // padded
       }
-      float acc[128];
+      f32x2 acc[64];
 #pragma unroll
-      for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+      for (int j = 0; j < 64; j += 2) {
+        if constexpr (whole) {
+          const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(bias_w + 2 * j);
+          acc[j] = b.x;
+          acc[j + 1] = b.y;
+        } else {
+          acc[j] = acc[j + 1] = 0ull;
+        }
+      }
+      if (MODE == V_LSE) __syncwarp();          // everyone has read the bias values
       for (int j0 = w.j0; j0 < w.j1; j0 += P.seg, ++part) {
         const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
         if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[buf], tph, abort_flag, P.status, 66, (int)part));
@@ -464,7 +531,8 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
             tmem_ld_32x32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * 256u + (uint32_t)(col + ch * 32), v);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) acc[ch * 32 + j] += __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j)
+              acc[ch * 16 + j] = add2(acc[ch * 16 + j], pack2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
           }
         }
         tc_fence_before();
@@ -473,9 +541,9 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
       }
       if (!alive) continue;
       if constexpr (MODE == V_LSE) {
-        finish_lse(P, acc, bias_w, m, n0, col, label);
+        finish_lse(P, acc, m, n0, col, label);
       } else if constexpr (MODE == V_GRAD) {
-        finish_grad(P, acc, bias_w, stage, meta, m0w, n0, col, lane);
+        finish_grad(P, acc, stage, meta, m0w, n0, col, lane);
       } else {
         const bool shared_tile = w.j0 != 0 || w.j1 != P.n_pairs * P.kb;
         const int slot = 2 * unit + ((long long)(w.tile - share.whole) * (P.n_pairs * P.kb) > share.lo ? 1 : 0);
@@ -486,13 +554,12 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
           if (shared_tile) {
             float4* to = P.slots + ((size_t)slot * (V_TILE / 4) + (col + ch * 32) / 4) * V_TILE + (m - m0);
 #pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              to[(j / 4) * V_TILE] = make_float4(acc[ch * 32 + j], acc[ch * 32 + j + 1], acc[ch * 32 + j + 2], acc[ch * 32 + j + 3]);
-          } else {                              // turned in shared memory: a warp writes 128 bytes of 4 rows at a time
-            float4* mine = reinterpret_cast<float4*>(stage + lane * 128);
-#pragma unroll
             for (int j = 0; j < 8; ++j)
-              mine[j ^ (lane & 7)] = make_float4(acc[ch * 32 + 4 * j], acc[ch * 32 + 4 * j + 1], acc[ch * 32 + 4 * j + 2], acc[ch * 32 + 4 * j + 3]);
+              *reinterpret_cast<ulonglong2*>(to + j * V_TILE) = make_ulonglong2(acc[ch * 16 + 2 * j], acc[ch * 16 + 2 * j + 1]);
+          } else {                              // turned in shared memory: a warp writes 128 bytes of 4 rows at a time
+            ulonglong2* mine = reinterpret_cast<ulonglong2*>(stage + lane * 128);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mine[j ^ (lane & 7)] = make_ulonglong2(acc[ch * 16 + 2 * j], acc[ch * 16 + 2 * j + 1]);
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -505,7 +572,6 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
           }
         }
       }
-      if (whole) __syncwarp();                  // everyone has read the bias values
     }
     if (MODE == V_GRAD && lane == 0) store_wait_all();
   }
@@ -815,15 +881,17 @@ k_vocab_planes(const void* src, long long ld, int rows, int d, int dp, int f32, 
 }
 
 // A warp per token: its row of X as R rows of planes (zeros where it has no label: what such a row holds may be
-// anything), the third plane of fp32 apart, and lse, scale, G at the label, label.  Column `one` (-1: none) beyond X's is a
+// anything), the third plane of fp32 apart, and its `meta`; all threads: the bias, padded.  Column `one` (-1: none) beyond X's is a
 // one: with it as X's last column the norm of G^T X holds the bias' part (as that of W, whose column d is zero, it leaves
 // the logits alone).
 __global__ void __launch_bounds__(256)
 k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* clip, int R, int dp, int one, __nv_bfloat16* xe,
-               __nv_bfloat16* x2, float4* meta, int* status) {
+               __nv_bfloat16* x2, float4* meta, float* bias, int columns, int* status) {
   wait_for_predecessor();
   let_successor_in();
   const int n = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  for (int v = blockIdx.x * 256 + threadIdx.x; v < columns; v += gridDim.x * 256)
+    bias[v] = v >= H.V ? -INFINITY : H.bias ? H.bias[v] : 0.0f;
   if (n >= H.N) return;
   const int y = label_of(H, n, status);
   double s = 0.0;
@@ -848,12 +916,13 @@ k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* c
       *reinterpret_cast<uint4*>(x2 + (size_t)n * dp + c) = split_eight(x);
     }
   }
-  float4 m = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+  float4 m = kNoToken;
   if (y >= 0) {
     const double z = warp_sum(s) + (H.bias ? (double)H.bias[y] : 0.0);
     float scale = H.weights ? H.weights[n] : 1.0f;
     if (clip) scale *= clip[n / H.T];
-    m = make_float4(lse[n], scale, scale * expm1f((float)(z - (double)lse[n])), __int_as_float(y));
+    const float top = lse[n] * kLog2e, left = fmaf(lse[n], kLog2e, -top);
+    m = make_float4(top, scale * ex2(-left), scale * expm1f((float)(z - (double)lse[n])), __int_as_float(y));
   }
   if (lane == 0) meta[n] = m;
 }
@@ -886,7 +955,7 @@ k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, flo
     const float2 v = part[(size_t)p * H.N + n];
     const float top = fmaxf(most, v.x);
     if (top != -INFINITY) {
-      sum = sum * ex2((most - top) * kLog2e) + v.y * ex2((v.x - top) * kLog2e);
+      sum = sum * ex2(most - top) + v.y * ex2(v.x - top);
       most = top;
     } else {
       sum += v.y;                               // 0, or NaN
@@ -895,12 +964,12 @@ k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, flo
   float top = most;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  float all = top == -INFINITY ? sum : sum * ex2((most - top) * kLog2e);
+  float all = top == -INFINITY ? sum : sum * ex2(most - top);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
   const double z = warp_sum(s) + (H.bias ? (double)H.bias[y] : 0.0);
   if (lane == 0) {
-    const double others = (double)top + (double)logf(all);             // -inf where there are none
+    const double others = ((double)top + (double)log2f(all)) * 0.69314718055994530942;   // -inf where there are none
     const float gap = (float)(others - z);
     float l = gap > 0.0f ? gap + log1pf(expf(-gap)) : log1pf(expf(gap));
     if (z == INFINITY) l = NAN;                 // as any other infinite logit
@@ -994,7 +1063,7 @@ struct VPlan {
   bool direct;                   // X and W can be copied by TMA as they are
   int sub, n_sub, piece_subs, pieces;
   int mt;                        // 256-token tiles
-  size_t part, xe, x2, xp, wp, meta, G, slots, dx, gram, cols, bias, total;
+  size_t part, xe, x2, xp, wp, meta, padded, G, slots, dx, gram, cols, bias, total;
   int gram_count;                // partial sums per example of one piece
   bool gram_way;
   int short_examples;            // examples that 128 rows of planes hold; 0: longer ones, for the layers' norm kernels
@@ -1050,6 +1119,7 @@ static VPlan plan_vocab(const dp_vocab_head& h, int op) {
   take(p.xe, (size_t)N * p.R * p.dp * 2);
   if (f32) take(p.x2, (size_t)N * p.dp * 2);
   take(p.meta, (size_t)N * sizeof(float4));
+  take(p.padded, (size_t)p.n_sub * p.sub * sizeof(float));
   take(p.G, block * p.piece_subs);
   take(p.slots, (size_t)2 * (sm_count() / 2) * V_TILE * V_TILE * sizeof(float));
   if (op == 1) {
@@ -1124,8 +1194,8 @@ static int logits_operands(const VRun& r, VParams& P) {
     P.pa[k] = f32 ? pa[k] : 0;
     P.pb[k] = f32 ? pb[k] : 0;
   }
-  P.kb = ceil_div(h.d, 64);
-  P.seg = f32 ? 8 : 32;
+  P.kb = ceil_div(h.d, 128);
+  P.seg = f32 ? 4 : 16;
   P.nt = V_TILE;
   P.bias = h.bias;
   P.V = h.V;
@@ -1164,8 +1234,9 @@ static int over_pieces(const VRun& r, const float* lse, const float* clip, float
   int rc;
   if (!p.direct && (rc = pack_rows(r, h.W, h.ldw, h.V, p.wp)) != DP_OK) return rc;
   __nv_bfloat16 *xe = r.at<__nv_bfloat16>(p.xe), *x2 = r.at<__nv_bfloat16>(p.x2), *G = r.at<__nv_bfloat16>(p.G);
-  VOCAB_CUDA(launch_chained(k_vocab_tokens, (unsigned)ceil_div(N, 8), 256, 0, r.s, head_of(h), lse, clip, p.R, p.dp, p.dp > h.d && f32 && h.bias && !clip ? h.d : -1, xe, x2,
-                            r.at<float4>(p.meta), r.status));
+  const int columns = p.n_sub * p.sub;
+  VOCAB_CUDA(launch_chained(k_vocab_tokens, (unsigned)ceil_div(std::max(N, columns / 64), 8), 256, 0, r.s, head_of(h), lse, clip, p.R, p.dp, p.dp > h.d && f32 && h.bias && !clip ? h.d : -1, xe, x2,
+                            r.at<float4>(p.meta), r.at<float>(p.padded), columns, r.status));
   for (int s0 = 0; s0 < p.n_sub; s0 += p.piece_subs) {
     const int subs = std::min(p.piece_subs, p.n_sub - s0);
     VParams P = {};
@@ -1184,6 +1255,7 @@ static int over_pieces(const VRun& r, const float* lse, const float* clip, float
     P.N = subs * p.sub;
     P.sub = p.sub;
     P.v0 = s0 * p.sub;
+    P.bias = r.at<float>(p.padded);
     P.planes2 = f32;
     P.meta = r.at<float4>(p.meta);
     P.bias_part = bias_part;
