@@ -2,12 +2,15 @@
 //   q = softmax(t / tau) over the K words,  p = softmax(z / tau) over the vocabulary,
 //   loss = w tau^2 sum_k q_k (log q_k - log p_ids_k),   dz = w tau (p - q at its words).
 //
-// Bound by memory: a row is read once and its gradient written once.  It stays in registers between the three things that
-// need it (its maximum, the sum of its exponentials, the gradient): up to 8 vectors of 16 bytes a thread, 512 threads a
-// row, so 32768 bf16 or 16384 fp32 words; longer rows are read again, from L2.  Rows of at most 8 vectors a lane have a
-// warp of their own.  Rows start anywhere: vectors lie on 16-byte boundaries of memory, and the two that reach beyond
-// the row are moved element by element.
+// Bound by memory: a row is read once and its gradient written once.  A block of up to 512 threads walks over its rows; a row
+// lies in shared memory while it is needed three times (maximum, sum of exponentials, gradient), every thread fetching and
+// reading its own vectors, so that the next row's are on their way as soon as this row's have been read for the last
+// time; several blocks an SM (three at 30522 bf16 words) fill one another's pauses.  Short rows have a warp of their own and stay in
+// registers; rows beyond shared memory are read three times, from L2.
+// Rows start anywhere: vectors of 16 bytes lie on 16-byte boundaries of memory, the two that reach beyond the row are masked,
+// and those that reach beyond the first or last row are read element by element.
 // Sums and statistics are fp32; a gradient is rounded once.
+#include <algorithm>
 #include <cmath>
 
 #include "dp_chain.cuh"
@@ -16,6 +19,7 @@
 namespace dpk {
 
 constexpr int kDistillThreads = 512;
+constexpr size_t kRowsMost = 225 * 1024;         // dynamic shared memory of a block of k_distill_rows, at most
 constexpr int kDistillWords = 1024;              // most words of a teacher
 constexpr float kLog2ePerE = 1.4426950408889634f;
 
@@ -93,7 +97,7 @@ __device__ __forceinline__ void over_row(float (&x)[N], float (*red)[N], F f) {
 
 // NV: vectors a thread keeps; 0: rows of any length, read three times.  WARP: a warp per row, several rows a block.
 template <typename T, int NV, bool WARP>
-__global__ void __launch_bounds__(kDistillThreads, NV == 8 && !WARP ? 2 : 1) k_distill(const __grid_constant__ DistillArgs a) {
+__global__ void __launch_bounds__(kDistillThreads) k_distill(const __grid_constant__ DistillArgs a) {
   constexpr int E = 16 / sizeof(T);              // elements of a vector
   constexpr int KEEP = NV ? NV : 1;
   extern __shared__ float smem[];
@@ -224,7 +228,213 @@ __global__ void __launch_bounds__(kDistillThreads, NV == 8 && !WARP ? 2 : 1) k_d
   }
 }
 
-// The form for rows of `nv` vectors at most: a warp a row up to 8 vectors a lane, then blocks of up to 512 threads.
+// Two fp32 numbers in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{.reg .b64 w, x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float warp_max(float x) {       // NaN are passed over
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The larger of the elements of a vector so far.
+template <typename T> __device__ __forceinline__ float vector_max(const uint4& d) {
+  if constexpr (sizeof(T) == 4) {
+    return fmaxf(fmaxf(__uint_as_float(d.x), __uint_as_float(d.y)), fmaxf(__uint_as_float(d.z), __uint_as_float(d.w)));
+  } else {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&d);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+}
+
+// Rows in shared memory.  Dynamic shared memory: a row, then the teacher's words, those of two rows.
+// Three barriers a row: the maximum (the row and its words are complete in shared memory), the sums (what the words need of the
+// row has been read), the gradient (the words' own values come last).
+template <typename T>
+__global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __grid_constant__ DistillArgs a, int row_bytes) {
+  constexpr int E = 16 / sizeof(T);              // elements of a vector
+  extern __shared__ uint8_t rows[];
+  __shared__ float red_max[16][2];
+  __shared__ float red_sum[16][4];
+  wait_for_predecessor();
+  let_successor_in();
+  const int threads = (int)blockDim.x, tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
+  float* words = reinterpret_cast<float*>(rows + row_bytes);
+  const uintptr_t begin = reinterpret_cast<uintptr_t>(a.z), end = begin + ((a.N - 1) * a.ld + a.V) * sizeof(T);
+  const auto row_at = [&](long long n) { return begin + (uintptr_t)(n * a.ld) * sizeof(T); };
+  const auto vectors = [&](uintptr_t row) { return (int)(((row & 15) + (uintptr_t)a.V * sizeof(T) + 15) >> 4); };
+  const auto fetch = [&](uintptr_t row, int v) {             // vector v of a row
+    const uintptr_t at = (row & ~(uintptr_t)15) + (uintptr_t)v * 16;
+    uint8_t* to = rows + v * 16;
+    if (at >= begin && at + 16 <= end) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(at) : "memory");
+    } else {
+#pragma unroll
+      for (int u = 0; u < E; ++u)
+        if (at + u * sizeof(T) >= begin && at + (u + 1) * sizeof(T) <= end)
+          reinterpret_cast<T*>(to)[u] = *reinterpret_cast<const T*>(at + u * sizeof(T));
+    }
+  };
+  // vector v as it counts: -inf outside the row
+  const auto masked = [&](int v, int off) {
+    uint4 d = *reinterpret_cast<const uint4*>(rows + v * 16);
+    const int e0 = v * E - off;
+    if (e0 < 0 || e0 + E > a.V) {
+      float x[E];
+#pragma unroll
+      for (int u = 0; u < E; ++u) x[u] = e0 + u < 0 || e0 + u >= a.V ? -INFINITY : lane_of<T>(d, u);
+      d = packed<T>(x);
+    }
+    return d;
+  };
+  struct Word { int id; float t; };
+  const auto word = [&](long long n, int k) -> Word {        // of the teacher; id -1: an empty place
+    Word w = {-1, -INFINITY};
+    if (n < a.N && k < a.K) {
+      w.id = a.ids[n * a.K + k];
+      w.t = a.t_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(a.t)[n * a.K + k]) : static_cast<const float*>(a.t)[n * a.K + k];
+      if (w.id >= a.V) {
+        atomicCAS(a.status, 0, (int)STATUS_BAD_ID);
+        w.id = -1;
+      }
+      if (w.id < 0 || w.t == -INFINITY) w = {-1, -INFINITY};
+    }
+    return w;
+  };
+  long long n = blockIdx.x;
+  for (int v = tid, nv = vectors(row_at(n)); v < nv; v += threads) fetch(row_at(n), v);
+  Word next = word(n, tid);
+  for (int i = 0; n < a.N; n += gridDim.x, ++i) {
+    float* s_t = words + (size_t)(i & 1) * 3 * a.K;          // the teacher's logits, the student's exponents, the words
+    float* s_y = s_t + a.K;
+    int* s_id = reinterpret_cast<int*>(s_y + a.K);
+    const uintptr_t row = row_at(n);
+    const T* z = reinterpret_cast<const T*>(rows + (row & 15));
+    const int off = (int)(row & 15) / (int)sizeof(T), nv = vectors(row);
+    float top_t = -INFINITY, top = -INFINITY;
+    for (int k = tid; k < a.K; k += threads) {
+      const Word w = k == tid ? next : word(n, k);
+      s_id[k] = w.id;
+      s_t[k] = w.t;
+      top_t = fmaxf(top_t, w.t == w.t ? w.t : INFINITY);     // a NaN makes the differences to the maximum NaN
+    }
+    next = word(n + gridDim.x, tid);
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+#pragma unroll 4
+    for (int v = tid; v < nv; v += threads) top = fmaxf(top, vector_max<T>(masked(v, off)));
+    top = warp_max(top);
+    if (32 * warp < a.K) top_t = warp_max(top_t);
+    if (lane == 0) red_max[warp][0] = top, red_max[warp][1] = top_t;
+    __syncthreads();
+    top = warp_max(lane < warps ? red_max[lane][0] : -INFINITY);
+    top_t = warp_max(lane < warps ? red_max[lane][1] : -INFINITY);
+    const bool live = top_t != -INFINITY;
+    // powers of two of x log2(e) / tau, less the maximum's, rounded: what it was rounded by is common to a row and falls out
+    const float sub = top == -INFINITY ? 0.0f : -top * a.scale2, sub_t = -top_t * a.scale2;
+    const float w = live ? (a.weights ? a.weights[n] : 1.0f) : 0.0f;
+    // sums: of the student's powers, the teacher's, and the teacher's weight times the gap of the two exponents
+    float sum_t = 0.0f, gap = 0.0f;
+    for (int k = tid; k < a.K; k += threads) {
+      if (s_id[k] < 0) continue;
+      const float y = fmaf(to_float(z[s_id[k]]), a.scale2, sub), t = fmaf(s_t[k], a.scale2, sub_t), e = exp2_fast(t);
+      s_y[k] = y;
+      sum_t += e;
+      if (e != 0.0f) gap += e * (t - y);
+    }
+    const float2 k2 = make_float2(a.scale2, a.scale2), sub2 = make_float2(sub, sub), one2 = make_float2(1.0f, 1.0f);
+    float2 part = make_float2(0.0f, 0.0f);
+#pragma unroll 4
+    for (int v = tid; v < nv; v += threads) {
+      const uint4 d = masked(v, off);
+#pragma unroll
+      for (int u = 0; u < E; u += 2) {
+        const float2 y = fma2(make_float2(lane_of<T>(d, u), lane_of<T>(d, u + 1)), k2, sub2);
+        part = fma2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), one2, part);
+      }
+    }
+    float sum = part.x + part.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (32 * warp < a.K) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        sum_t += __shfl_xor_sync(0xffffffffu, sum_t, o);
+        gap += __shfl_xor_sync(0xffffffffu, gap, o);
+      }
+    }
+    if (lane == 0) *reinterpret_cast<float4*>(red_sum[warp]) = make_float4(sum, sum_t, gap, 0.0f);
+    __syncthreads();
+    const float4 r = lane < warps ? *reinterpret_cast<const float4*>(red_sum[lane]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    sum = r.x, sum_t = r.y, gap = r.z;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {            // at most 16 warps
+      sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      sum_t += __shfl_xor_sync(0xffffffffu, sum_t, o);
+    }
+    if (warp == 0) {
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) gap += __shfl_xor_sync(0xffffffffu, gap, o);
+      if (lane == 0) a.loss[n] = live ? w * a.tau * a.tau * 0.693147181f * (gap / sum_t + (log2f(sum) - log2f(sum_t))) : 0.0f;
+    }
+    const uintptr_t row2 = row_at(n + gridDim.x);
+    const int nv2 = n + gridDim.x < a.N ? vectors(row2) : 0;
+    T* out = a.dz ? static_cast<T*>(a.dz) + n * a.ld_out : nullptr;
+    sum = __shfl_sync(0xffffffffu, sum, 0);      // lanes 16 and up have summed nothing
+    sum_t = __shfl_sync(0xffffffffu, sum_t, 0);
+    const float c = w * a.tau, cp = __fdividef(c, sum), cq = __fdividef(c, sum_t);
+    const bool same = out && (reinterpret_cast<uintptr_t>(out) & 15) == (row & 15);
+    const float2 cp2 = make_float2(cp, cp), zero2 = make_float2(0.0f, 0.0f);
+#pragma unroll 2
+    for (int v = tid; v < nv || v < nv2; v += threads) {
+      const int e0 = v * E - off;
+      const uint4 d = *reinterpret_cast<const uint4*>(rows + v * 16);
+      if (v < nv2) fetch(row2, v);               // its place is free: the words have been read, and this was its last time
+      if (!out || v >= nv) continue;
+      float g[E];
+#pragma unroll
+      for (int u = 0; u < E; u += 2) {
+        const float2 y = fma2(make_float2(lane_of<T>(d, u), lane_of<T>(d, u + 1)), k2, sub2);
+        const float2 p = live ? fma2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), cp2, zero2) : zero2;   // a dead row may hold anything
+        g[u] = p.x;
+        g[u + 1] = p.y;
+      }
+      if (same && e0 >= 0 && e0 + E <= a.V) {
+        *reinterpret_cast<uint4*>(out + e0) = packed<T>(g);
+      } else {
+#pragma unroll
+        for (int u = 0; u < E; ++u)
+          if (e0 + u >= 0 && e0 + u < a.V) out[e0 + u] = from_float<T>(g[u]);
+      }
+    }
+    __syncthreads();
+    if (out) {
+      // a warp a word, its lanes looking for the word among all: the same word again adds to its first place
+      for (int k = live ? warp : a.K; k < a.K; k += warps) {
+        const int id = s_id[k];
+        if (id < 0) continue;
+        float q = 0.0f;
+        bool before = false;
+        for (int o = lane; o < a.K; o += 32) {
+          if (s_id[o] != id) continue;
+          before = before || o < k;
+          q += exp2_fast(fmaf(s_t[o], a.scale2, sub_t));
+        }
+        if (__any_sync(0xffffffffu, before)) continue;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+        if (lane == 0) out[id] = from_float<T>(cp * exp2_fast(s_y[k]) - cq * q);
+      }
+    }
+  }
+}
+
+// The form for rows of `nv` vectors at most: a warp a row up to 8 vectors a lane, then a block a row.
 template <typename T>
 static cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s) {
   const long long nv = (a.V + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T)) + 1;
@@ -235,10 +445,19 @@ static cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s) {
     const unsigned grid = (unsigned)((a.N + rows - 1) / rows);
     return launch_chained(nv <= 2 * 32 ? k_distill<T, 2, true> : k_distill<T, 8, true>, grid, 32 * rows, rows * words, s, a);
   }
-  const int per = nv <= 4 * kDistillThreads ? 4 : 8;
-  const int threads = nv > 8 * kDistillThreads ? kDistillThreads : (int)((nv + 32 * per - 1) / (32 * per)) * 32;
-  return launch_chained(nv > 8 * kDistillThreads ? k_distill<T, 0, false> : per == 4 ? k_distill<T, 4, false> : k_distill<T, 8, false>,
-                        (unsigned)a.N, threads, words, s, a);
+  const size_t row_bytes = (size_t)nv * 16, list = (size_t)6 * a.K * sizeof(float), smem = row_bytes + list;
+  if (smem > kRowsMost) return launch_chained(k_distill<T, 0, false>, (unsigned)a.N, kDistillThreads, words, s, a);
+  // four vectors a thread, as far as there are threads, and as many blocks an SM as registers, threads and shared memory allow
+  const int threads = (int)std::min<long long>(kDistillThreads, (nv + 127) / 128 * 32);
+  const int resident = std::max(1, std::min(3 * kDistillThreads / threads, (int)(kRowsMost / (smem + 1536))));
+  const unsigned grid = (unsigned)std::min<long long>(a.N, (long long)resident * sm_count());
+  static signed char ready[kMaxDevices] = {};    // 0 unknown, 1 ready, -1 failed (one flag per form and device)
+  const int dev = current_device();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  if (!ready[dev])
+    ready[dev] = cudaFuncSetAttribute(k_distill_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowsMost) == cudaSuccess ? 1 : -1;
+  if (ready[dev] < 0) return cudaErrorInvalidValue;
+  return launch_chained(k_distill_rows<T>, grid, threads, smem, s, a, (int)row_bytes);
 }
 
 }  // namespace dpk
