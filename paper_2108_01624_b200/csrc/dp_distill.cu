@@ -228,14 +228,6 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(const __grid_consta
   }
 }
 
-// Two fp32 numbers in one instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("{.reg .b64 w, x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;}"
-      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return r;
-}
 __device__ __forceinline__ float warp_max(float x) {       // NaN are passed over
   float y;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
@@ -267,31 +259,34 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
   const int threads = (int)blockDim.x, tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
   float* words = reinterpret_cast<float*>(rows + row_bytes);
   const uintptr_t begin = reinterpret_cast<uintptr_t>(a.z), end = begin + ((a.N - 1) * a.ld + a.V) * sizeof(T);
-  const auto row_at = [&](long long n) { return begin + (uintptr_t)(n * a.ld) * sizeof(T); };
-  const auto vectors = [&](uintptr_t row) { return (int)(((row & 15) + (uintptr_t)a.V * sizeof(T) + 15) >> 4); };
-  const auto fetch = [&](uintptr_t row, int v) {             // vector v of a row
-    const uintptr_t at = (row & ~(uintptr_t)15) + (uintptr_t)v * 16;
-    uint8_t* to = rows + v * 16;
-    if (at >= begin && at + 16 <= end) {
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(at) : "memory");
-    } else {
-#pragma unroll
-      for (int u = 0; u < E; ++u)
-        if (at + u * sizeof(T) >= begin && at + (u + 1) * sizeof(T) <= end)
-          reinterpret_cast<T*>(to)[u] = *reinterpret_cast<const T*>(at + u * sizeof(T));
-    }
+  const uint32_t rows32 = (uint32_t)__cvta_generic_to_shared(rows);
+  // A row: its first byte, its vectors, whether they all lie inside the tensor (of those of the first and the last row one may
+  // reach beyond it: they are then read element by element).
+  struct Row { uintptr_t at; int nv; bool inside; };
+  const auto row_of = [&](long long n) -> Row {
+    Row r;
+    r.at = begin + (uintptr_t)(n * a.ld) * sizeof(T);
+    r.nv = n < a.N ? (int)(((r.at & 15) + (uintptr_t)a.V * sizeof(T) + 15) >> 4) : 0;
+    const uintptr_t first = r.at & ~(uintptr_t)15;
+    r.inside = first >= begin && first + (uintptr_t)r.nv * 16 <= end;
+    return r;
   };
-  // vector v as it counts: -inf outside the row
-  const auto masked = [&](int v, int off) {
-    uint4 d = *reinterpret_cast<const uint4*>(rows + v * 16);
-    const int e0 = v * E - off;
-    if (e0 < 0 || e0 + E > a.V) {
-      float x[E];
+  const auto copy = [&](int v, const uint8_t* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(rows32 + v * 16), "l"(from) : "memory");
+  };
+  const auto fetch = [&](const Row& r, int v) {              // this thread's vectors from v on
+    const uintptr_t first = r.at & ~(uintptr_t)15;
+    for (; v < r.nv; v += threads) {
+      const uintptr_t at = first + (uintptr_t)v * 16;
+      if (r.inside || (at >= begin && at + 16 <= end)) {
+        copy(v, reinterpret_cast<const uint8_t*>(at));
+      } else {
 #pragma unroll
-      for (int u = 0; u < E; ++u) x[u] = e0 + u < 0 || e0 + u >= a.V ? -INFINITY : lane_of<T>(d, u);
-      d = packed<T>(x);
+        for (int u = 0; u < E; ++u)
+          if (at + u * sizeof(T) >= begin && at + (u + 1) * sizeof(T) <= end)
+            reinterpret_cast<T*>(rows + v * 16)[u] = *reinterpret_cast<const T*>(at + u * sizeof(T));
+      }
     }
-    return d;
   };
   struct Word { int id; float t; };
   const auto word = [&](long long n, int k) -> Word {        // of the teacher; id -1: an empty place
@@ -308,15 +303,15 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
     return w;
   };
   long long n = blockIdx.x;
-  for (int v = tid, nv = vectors(row_at(n)); v < nv; v += threads) fetch(row_at(n), v);
+  Row row = row_of(n);
+  fetch(row, tid);
   Word next = word(n, tid);
   for (int i = 0; n < a.N; n += gridDim.x, ++i) {
-    float* s_t = words + (size_t)(i & 1) * 3 * a.K;          // the teacher's logits, the student's exponents, the words
-    float* s_y = s_t + a.K;
-    int* s_id = reinterpret_cast<int*>(s_y + a.K);
-    const uintptr_t row = row_at(n);
-    const T* z = reinterpret_cast<const T*>(rows + (row & 15));
-    const int off = (int)(row & 15) / (int)sizeof(T), nv = vectors(row);
+    float* s_t = words + (size_t)(i & 1) * 4 * a.K;          // the teacher's logits, the student's exponents, the teacher's powers
+    float *s_y = s_t + a.K, *s_q = s_y + a.K;
+    int* s_id = reinterpret_cast<int*>(s_q + a.K);           // the words
+    const T* z = reinterpret_cast<const T*>(rows + (row.at & 15));
+    const int off = (int)(row.at & 15) / (int)sizeof(T), nv = row.nv, last = nv - 1;
     float top_t = -INFINITY, top = -INFINITY;
     for (int k = tid; k < a.K; k += threads) {
       const Word w = k == tid ? next : word(n, k);
@@ -326,8 +321,15 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
     }
     next = word(n + gridDim.x, tid);
     asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    const auto trim = [&](int v) {               // the elements beside the row become -inf
+#pragma unroll
+      for (int u = 0; u < E; ++u)
+        if (v * E - off + u < 0 || v * E - off + u >= a.V) reinterpret_cast<T*>(rows + v * 16)[u] = from_float<T>(-INFINITY);
+    };
+    if (tid == 0) trim(0);
+    if (tid == (last & (threads - 1))) trim(last);      // threads: a power of two
 #pragma unroll 4
-    for (int v = tid; v < nv; v += threads) top = fmaxf(top, vector_max<T>(masked(v, off)));
+    for (int v = tid; v < nv; v += threads) top = fmaxf(top, vector_max<T>(*reinterpret_cast<const uint4*>(rows + v * 16)));
     top = warp_max(top);
     if (32 * warp < a.K) top_t = warp_max(top_t);
     if (lane == 0) red_max[warp][0] = top, red_max[warp][1] = top_t;
@@ -341,24 +343,37 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
     // sums: of the student's powers, the teacher's, and the teacher's weight times the gap of the two exponents
     float sum_t = 0.0f, gap = 0.0f;
     for (int k = tid; k < a.K; k += threads) {
-      if (s_id[k] < 0) continue;
-      const float y = fmaf(to_float(z[s_id[k]]), a.scale2, sub), t = fmaf(s_t[k], a.scale2, sub_t), e = exp2_fast(t);
-      s_y[k] = y;
+      const int id = s_id[k];
+      if (id < 0) continue;
+      const float y = fmaf(to_float(z[id]), a.scale2, sub), t = fmaf(s_t[k], a.scale2, sub_t), e = exp2_fast(t);
       sum_t += e;
       if (e != 0.0f) gap += e * (t - y);
-    }
-    const float2 k2 = make_float2(a.scale2, a.scale2), sub2 = make_float2(sub, sub), one2 = make_float2(1.0f, 1.0f);
-    float2 part = make_float2(0.0f, 0.0f);
+      // the same word again adds to its first place (s_q < 0: not the first)
+      int again = 0;
 #pragma unroll 4
-    for (int v = tid; v < nv; v += threads) {
-      const uint4 d = masked(v, off);
-#pragma unroll
-      for (int u = 0; u < E; u += 2) {
-        const float2 y = fma2(make_float2(lane_of<T>(d, u), lane_of<T>(d, u + 1)), k2, sub2);
-        part = fma2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), one2, part);
+      for (int o = 0; o < a.K; ++o) again += s_id[o] == id;
+      float q = e;
+      if (again > 1) {
+        q = 0.0f;
+        bool first = true;
+        for (int o = 0; o < a.K; ++o) {
+          if (s_id[o] != id) continue;
+          first = first && o >= k;
+          q += exp2_fast(fmaf(s_t[o], a.scale2, sub_t));
+        }
+        if (!first) q = -1.0f;
       }
+      s_y[k] = y;
+      s_q[k] = q;
     }
-    float sum = part.x + part.y;
+    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+    for (int v = tid; v < nv; v += threads) {
+      const uint4 d = *reinterpret_cast<const uint4*>(rows + v * 16);
+#pragma unroll
+      for (int u = 0; u < E; ++u) part[u & 3] += exp2_fast(fmaf(lane_of<T>(d, u), a.scale2, sub));
+    }
+    float sum = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (32 * warp < a.K) {
@@ -382,53 +397,60 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
       for (int o = 8; o > 0; o >>= 1) gap += __shfl_xor_sync(0xffffffffu, gap, o);
       if (lane == 0) a.loss[n] = live ? w * a.tau * a.tau * 0.693147181f * (gap / sum_t + (log2f(sum) - log2f(sum_t))) : 0.0f;
     }
-    const uintptr_t row2 = row_at(n + gridDim.x);
-    const int nv2 = n + gridDim.x < a.N ? vectors(row2) : 0;
+    const Row after = row_of(n + gridDim.x);
+    const int nv2 = after.inside ? after.nv : 0;
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(after.at & ~(uintptr_t)15);
     T* out = a.dz ? static_cast<T*>(a.dz) + n * a.ld_out : nullptr;
     sum = __shfl_sync(0xffffffffu, sum, 0);      // lanes 16 and up have summed nothing
     sum_t = __shfl_sync(0xffffffffu, sum_t, 0);
     const float c = w * a.tau, cp = __fdividef(c, sum), cq = __fdividef(c, sum_t);
-    const bool same = out && (reinterpret_cast<uintptr_t>(out) & 15) == (row & 15);
-    const float2 cp2 = make_float2(cp, cp), zero2 = make_float2(0.0f, 0.0f);
-#pragma unroll 2
-    for (int v = tid; v < nv || v < nv2; v += threads) {
-      const int e0 = v * E - off;
-      const uint4 d = *reinterpret_cast<const uint4*>(rows + v * 16);
-      if (v < nv2) fetch(row2, v);               // its place is free: the words have been read, and this was its last time
-      if (!out || v >= nv) continue;
-      float g[E];
+    const bool same = (reinterpret_cast<uintptr_t>(out) & 15) == (row.at & 15);
+    // whole vectors of the result: [lo, hi)
+    const int lo = off ? 1 : 0, hi = out && same ? (off + a.V) / E : lo;
+    if (out) {
+      const auto single = [&](int v) {           // element by element
 #pragma unroll
-      for (int u = 0; u < E; u += 2) {
-        const float2 y = fma2(make_float2(lane_of<T>(d, u), lane_of<T>(d, u + 1)), k2, sub2);
-        const float2 p = live ? fma2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), cp2, zero2) : zero2;   // a dead row may hold anything
-        g[u] = p.x;
-        g[u + 1] = p.y;
-      }
-      if (same && e0 >= 0 && e0 + E <= a.V) {
-        *reinterpret_cast<uint4*>(out + e0) = packed<T>(g);
+        for (int u = 0; u < E; ++u) {
+          const int e = v * E - off + u;
+          if (e >= 0 && e < a.V) out[e] = from_float<T>(live ? cp * exp2_fast(fmaf(to_float(reinterpret_cast<const T*>(rows + v * 16)[u]), a.scale2, sub)) : 0.0f);
+        }
+      };
+      if (!same) {
+        for (int v = tid; v < nv; v += threads) single(v);
       } else {
-#pragma unroll
-        for (int u = 0; u < E; ++u)
-          if (e0 + u >= 0 && e0 + u < a.V) out[e0 + u] = from_float<T>(g[u]);
+        if (tid == 0 && lo) single(0);
+        if (tid == (last & (threads - 1)) && last >= hi && last >= lo) single(last);
       }
     }
-    __syncthreads();
-    if (out) {
-      // a warp a word, its lanes looking for the word among all: the same word again adds to its first place
-      for (int k = live ? warp : a.K; k < a.K; k += warps) {
-        const int id = s_id[k];
-        if (id < 0) continue;
-        float q = 0.0f;
-        bool before = false;
-        for (int o = lane; o < a.K; o += 32) {
-          if (s_id[o] != id) continue;
-          before = before || o < k;
-          q += exp2_fast(fmaf(s_t[o], a.scale2, sub_t));
-        }
-        if (__any_sync(0xffffffffu, before)) continue;
+    const uint8_t* there = rows;
+    int v = tid;
+    if (live) {
+      uint4* to = reinterpret_cast<uint4*>(out - off);
+#pragma unroll 2
+      for (; v < nv; v += threads) {
+        const uint4 d = *reinterpret_cast<const uint4*>(there + v * 16);
+        if (v < nv2) copy(v, from + (size_t)v * 16);   // its place is free: the words have been read, and this was its last time
+        if (v >= lo && v < hi) {
+          float g[E];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-        if (lane == 0) out[id] = from_float<T>(cp * exp2_fast(s_y[k]) - cq * q);
+          for (int u = 0; u < E; ++u) g[u] = cp * exp2_fast(fmaf(lane_of<T>(d, u), a.scale2, sub));
+          to[v] = packed<T>(g);
+        }
+      }
+    } else {                                     // a row without a teacher may hold anything
+      uint4* to = reinterpret_cast<uint4*>(out - off);
+      for (; v < nv; v += threads) {
+        if (v < nv2) copy(v, from + (size_t)v * 16);
+        if (v >= lo && v < hi) to[v] = make_uint4(0, 0, 0, 0);
+      }
+    }
+    fetch(after, after.inside ? v : tid);        // a row may begin one vector further on
+    row = after;
+    __syncthreads();
+    if (out && live) {
+      for (int k = tid; k < a.K; k += threads) {
+        const float q = s_q[k];
+        if (s_id[k] >= 0 && !(q < 0.0f)) out[s_id[k]] = from_float<T>(cp * exp2_fast(s_y[k]) - cq * q);
       }
     }
   }
@@ -445,11 +467,14 @@ static cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s) {
     const unsigned grid = (unsigned)((a.N + rows - 1) / rows);
     return launch_chained(nv <= 2 * 32 ? k_distill<T, 2, true> : k_distill<T, 8, true>, grid, 32 * rows, rows * words, s, a);
   }
-  const size_t row_bytes = (size_t)nv * 16, list = (size_t)6 * a.K * sizeof(float), smem = row_bytes + list;
+  const size_t row_bytes = (size_t)nv * 16, list = (size_t)8 * a.K * sizeof(float), smem = row_bytes + list;
   if (smem > kRowsMost) return launch_chained(k_distill<T, 0, false>, (unsigned)a.N, kDistillThreads, words, s, a);
-  // four vectors a thread, as far as there are threads, and as many blocks an SM as registers, threads and shared memory allow
-  const int threads = (int)std::min<long long>(kDistillThreads, (nv + 127) / 128 * 32);
-  const int resident = std::max(1, std::min(3 * kDistillThreads / threads, (int)(kRowsMost / (smem + 1536))));
+  // A power of two of threads, at least four vectors each, and as many blocks an SM as threads and shared memory allow.  256 threads
+  // where three rows fit (30522 bf16 words: 182 us for 6144 rows; 384 threads 188, 512 197), more where fewer do.
+  const int rows = std::max(1, (int)(kRowsMost / (smem + 1536)));
+  int threads = 64;
+  while (threads < (rows >= 3 ? 256 : kDistillThreads) && threads * 8 <= nv) threads *= 2;
+  const int resident = std::min(rows, 3 * kDistillThreads / threads);
   const unsigned grid = (unsigned)std::min<long long>(a.N, (long long)resident * sm_count());
   static signed char ready[kMaxDevices] = {};    // 0 unknown, 1 ready, -1 failed (one flag per form and device)
   const int dev = current_device();
