@@ -353,8 +353,8 @@ DP_API int dp_qknorm_rope_backward(const dp_qknorm* p /*HOST*/, const dp_heads* 
  * bias and weights are fp32; entries of bias may be -inf (a word that cannot occur).  Infinite or NaN logits of a
  * token with a label make what depends on it NaN.
  * Sums are fp32, in an order that only the sizes and the device decide; the label's logit is formed in fp64.  With bf16 X
- * and W the products are exact; G is rounded to 2^-17 of each element before it is summed over tokens, to 2^-9 where it
- * forms a bf16 dX.  With fp32 X and W operands carry 24 bits in z and 17 in the products with G. */
+ * and W the products are exact; G is rounded to 2^-16 of each element before it is summed over tokens, to 2^-8 where it
+ * forms a bf16 dX.  With fp32 X and W operands carry 24 bits in z and 16 in the products with G. */
 typedef struct dp_vocab_head {
   int32_t dtype;               /* dp_dtype of X, W and dX */
   int32_t B, T, d, V;          /* B * T and V at most 2^26, d at most 2^16 */
@@ -369,7 +369,7 @@ typedef struct dp_vocab_head {
 /* bf16 rows that start on 16-byte boundaries (pointer and leading dimension) are read where they are; others, and fp32 ones,
  * are copied into the workspace first. */
 
-/* Bytes of scratch for the calls below; 0 on invalid sizes.  It holds G for a piece of the vocabulary (256 MiB, more only
+/* Bytes of scratch for the calls below; 0 on invalid sizes.  It holds G for a piece of the vocabulary (1 GiB at most, more only
  * where B * T * 2048 entries of G take more) and, where X or W are copied, their copies. */
 DP_API size_t dp_vocab_workspace_bytes(const dp_vocab_head* head /*HOST*/);
 

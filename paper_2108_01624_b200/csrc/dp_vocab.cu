@@ -16,10 +16,10 @@
 //   - a sum longer than `seg` blocks is taken over by the epilogue, which adds its parts in registers;
 //   - the label's own logit is formed by itself, in fp64: loss = w log1p(exp(lse of the others - z_label)) and
 //     G_label = w expm1(z_label - lse) keep their relative error where the model is sure of the label;
-//   - G is held as two bf16 numbers, hi + lo, 2^-17 of it: rows (token, plane) of G meet rows (token, plane) of X in the
+//   - G is held as two bf16 numbers, hi + lo, to 2^-16 of it: rows (token, plane) of G meet rows (token, plane) of X in the
 //     sums over tokens, whose results are fp32.  dX in bf16 reads hi alone: its own rounding is as large.
 //   - fp32 X and W are split into three bf16 numbers each for the logits (24 bits; six products, the smallest first) and
-//     into two for the products with G (2^-17 again, four products).
+//     into two for the products with G (2^-16 again, four products).
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -247,7 +247,7 @@ __device__ __forceinline__ void load_block(const VParams& P, uint8_t* st, uint32
 
 // Maximum (as `top`) and sum of powers over this thread's 128 columns of logits, the label's left out.
 __device__ __forceinline__ void finish_lse(const VParams& P, f32x2 (&z)[64], int m, int n0, int col, int label) {
-  const int rel = label - (n0 + col);
+  const int rel = label - (P.v0 + n0 + col);
   if (__any_sync(0xffffffffu, (unsigned)rel < 128u)) {
 #pragma unroll
     for (int j = 0; j < 64; ++j) {
@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
         float* own = reinterpret_cast<float*>(stage);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int v = n0 + col + 32 * k + lane;
+          const int v = P.v0 + n0 + col + 32 * k + lane;
           own[32 * k + lane] = v >= P.V ? -INFINITY : P.bias ? P.bias[v] : 0.0f;
         }
         __syncwarp();
@@ -928,21 +928,22 @@ k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* c
 }
 
 // lse and loss of a token from the parts over the column blocks, which leave the label out: a warp per token (eight
-// neighbours a block, whose parts share sectors), its label's logit in fp64.
+// neighbours a block, whose parts share sectors), its label's logit in fp64.  With `carry`, more columns are to come: the
+// parts become one, kept there.
 __global__ void __launch_bounds__(256)
-k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, float* loss, float* lse, int* status) {
+k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, float2* carry, float* loss, float* lse, int* status) {
   wait_for_predecessor();
   let_successor_in();
   const int lane = threadIdx.x & 31, n = blockIdx.x * 8 + (threadIdx.x >> 5);
   if (n >= H.N) return;
   const int y = label_of(H, n, status);
   if (y < 0) {
-    if (lane == 0) loss[n] = lse[n] = 0.0f;
+    if (lane == 0 && !carry) loss[n] = lse[n] = 0.0f;
     return;
   }
   double s = 0.0;
 #pragma unroll 4
-  for (int c = 8 * lane; c < H.d; c += 256) {
+  for (int c = 8 * lane; c < H.d && !carry; c += 256) {
     float x[8], w[8];
     eight(H, H.x, (long long)n * H.ldx, c, x);
     eight(H, H.w, (long long)y * H.ldw, c, w);
@@ -968,7 +969,9 @@ k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, flo
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
   const double z = warp_sum(s) + (H.bias ? (double)H.bias[y] : 0.0);
-  if (lane == 0) {
+  if (carry) {
+    if (lane == 0) carry[n] = make_float2(top, all);
+  } else if (lane == 0) {
     const double others = ((double)top + (double)log2f(all)) * 0.69314718055994530942;   // -inf where there are none
     const float gap = (float)(others - z);
     float l = gap > 0.0f ? gap + log1pf(expf(-gap)) : log1pf(expf(gap));
@@ -1038,6 +1041,7 @@ static bool encode_blocks(CUtensorMap* map, const void* base, long long rows, in
   return encode(map, base, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
+constexpr size_t kPartBytes = (size_t)256 << 20;    // maxima and sums of the column blocks that are joined at a time
 constexpr int kSubColumns = 2048;               // columns of one block of G, at most
 #ifndef DP_VOCAB_PIECE_MB
 #define DP_VOCAB_PIECE_MB 1024
@@ -1063,6 +1067,7 @@ struct VPlan {
   bool direct;                   // X and W can be copied by TMA as they are
   int sub, n_sub, piece_subs, pieces;
   int mt;                        // 256-token tiles
+  int loss_columns;              // vocabulary entries whose parts are joined at a time
   size_t part, xe, x2, xp, wp, meta, padded, G, slots, dx, gram, cols, bias, total;
   int gram_count;                // partial sums per example of one piece
   bool gram_way;
@@ -1107,7 +1112,9 @@ static VPlan plan_vocab(const dp_vocab_head& h, int op) {
   if (!p.direct) take(p.wp, (size_t)planes * h.V * p.dp * 2);
   if (op == 0) {
     if (!p.direct) take(p.xp, (size_t)planes * N * p.dp * 2);
-    take(p.part, (size_t)2 * ceil_div(h.V, V_TILE) * N * sizeof(float2));
+    const long long tiles = std::max<long long>(1, (long long)(kPartBytes / (2 * N * sizeof(float2))));
+    p.loss_columns = (int)std::min<long long>(ceil_div(h.V, V_TILE), tiles) * V_TILE;
+    take(p.part, (size_t)(1 + 2 * (p.loss_columns / V_TILE)) * N * sizeof(float2));
     p.total = at;
     return p;
   }
@@ -1179,13 +1186,13 @@ static int pack_rows(const VRun& r, const void* src, long long ld, long long row
   return DP_OK;
 }
 
-// The planes of W, and the products of a logit.
-static int logits_operands(const VRun& r, VParams& P) {
+// Rows [v0, v0 + rows) of W in planes, and the products of a logit.
+static int logits_operands(const VRun& r, VParams& P, int v0, int rows) {
   const dp_vocab_head& h = r.h;
   const bool f32 = h.dtype == DP_F32;
   for (int k = 0; k < (f32 ? 3 : 1); ++k) {
-    const bool ok = r.p.direct ? encode_rows(&P.b[k], h.W, h.V, h.d, h.ldw)
-                               : encode_rows(&P.b[k], r.at<__nv_bfloat16>(r.p.wp) + (size_t)k * h.V * r.p.dp, h.V, r.p.dp, r.p.dp);
+    const bool ok = r.p.direct ? encode_rows(&P.b[k], static_cast<const __nv_bfloat16*>(h.W) + v0 * h.ldw, rows, h.d, h.ldw)
+                               : encode_rows(&P.b[k], r.at<__nv_bfloat16>(r.p.wp) + ((size_t)k * h.V + v0) * r.p.dp, rows, r.p.dp, r.p.dp);
     if (!ok) return DP_ERR_CUDA;
   }
   static const unsigned char pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
@@ -1197,7 +1204,7 @@ static int logits_operands(const VRun& r, VParams& P) {
   P.kb = ceil_div(h.d, 128);
   P.seg = f32 ? 4 : 16;
   P.nt = V_TILE;
-  P.bias = h.bias;
+  P.v0 = v0;
   P.V = h.V;
   P.status = r.status;
   return DP_OK;
@@ -1240,7 +1247,8 @@ static int over_pieces(const VRun& r, const float* lse, const float* clip, float
   for (int s0 = 0; s0 < p.n_sub; s0 += p.piece_subs) {
     const int subs = std::min(p.piece_subs, p.n_sub - s0);
     VParams P = {};
-    if ((rc = logits_operands(r, P)) != DP_OK) return rc;
+    const int v0 = s0 * p.sub;
+    if ((rc = logits_operands(r, P, v0, std::min(subs * p.sub, h.V - v0))) != DP_OK) return rc;
     if (!encode_rows(&P.a[0], xe, N, p.dp, (long long)p.R * p.dp)) return DP_ERR_CUDA;
     if (f32 && (!encode_rows(&P.a[1], xe + 2 * p.dp, N, p.dp, (long long)p.R * p.dp) || !encode_rows(&P.a[2], x2, N, p.dp, p.dp)))
       return DP_ERR_CUDA;
@@ -1254,18 +1262,10 @@ static int over_pieces(const VRun& r, const float* lse, const float* clip, float
     P.M = N;
     P.N = subs * p.sub;
     P.sub = p.sub;
-    P.v0 = s0 * p.sub;
     P.bias = r.at<float>(p.padded);
     P.planes2 = f32;
     P.meta = r.at<float4>(p.meta);
     P.bias_part = bias_part;
-    // the rows of W of this piece
-    for (int k = 0; k < (f32 ? 3 : 1); ++k) {
-      const long long rows = std::min<long long>((long long)subs * p.sub, h.V - P.v0);
-      const bool ok = p.direct ? encode_rows(&P.b[k], static_cast<const __nv_bfloat16*>(h.W) + P.v0 * h.ldw, rows, h.d, h.ldw)
-                               : encode_rows(&P.b[k], r.at<__nv_bfloat16>(p.wp) + ((size_t)k * h.V + P.v0) * p.dp, rows, p.dp, p.dp);
-      if (!ok) return DP_ERR_CUDA;
-    }
     if ((rc = launch_product<V_GRAD>(r, P)) != DP_OK) return rc;
     if ((rc = use(s0, subs, block)) != DP_OK) return rc;
   }
@@ -1306,22 +1306,28 @@ int dp_vocab_loss(const dp_vocab_head* head, float* loss, float* lse, void* work
   const VRun r = {h, p, static_cast<char*>(workspace), static_cast<cudaStream_t>(cuda_stream), status};
   const int N = h.B * h.T;
   if (!p.direct && ((rc = pack_rows(r, h.W, h.ldw, h.V, p.wp)) != DP_OK || (rc = pack_rows(r, h.X, h.ldx, N, p.xp)) != DP_OK)) return rc;
-  VParams P = {};
-  if ((rc = logits_operands(r, P)) != DP_OK) return rc;
-  for (int k = 0; k < (h.dtype == DP_F32 ? 3 : 1); ++k) {
-    const bool ok = p.direct ? encode_rows(&P.a[k], h.X, N, h.d, h.ldx)
-                             : encode_rows(&P.a[k], r.at<__nv_bfloat16>(p.xp) + (size_t)k * N * p.dp, N, p.dp, p.dp);
-    if (!ok) return DP_ERR_CUDA;
+  float2* part = r.at<float2>(p.part);          // [what went before][column blocks], a value a token each
+  for (int v0 = 0; v0 < h.V; v0 += p.loss_columns) {
+    VParams P = {};
+    if ((rc = logits_operands(r, P, v0, h.V - v0)) != DP_OK) return rc;
+    for (int k = 0; k < (h.dtype == DP_F32 ? 3 : 1); ++k) {
+      const bool ok = p.direct ? encode_rows(&P.a[k], h.X, N, h.d, h.ldx)
+                               : encode_rows(&P.a[k], r.at<__nv_bfloat16>(p.xp) + (size_t)k * N * p.dp, N, p.dp, p.dp);
+      if (!ok) return DP_ERR_CUDA;
+    }
+    const int columns = std::min(p.loss_columns, h.V - v0);
+    const bool last = v0 + columns >= h.V;
+    P.bias = h.bias;
+    P.tiles_m = p.mt;
+    P.tiles_n = ceil_div(columns, V_TILE);
+    P.M = N;
+    P.N = columns;
+    P.labels = h.labels;
+    P.part = part + N;
+    if ((rc = launch_product<V_LSE>(r, P)) != DP_OK) return rc;
+    VOCAB_CUDA(launch_chained(k_vocab_loss, (unsigned)ceil_div(N, 8), 256, 0, r.s, head_of(h), part + (v0 ? 0 : N),
+                              2 * P.tiles_n + (v0 ? 1 : 0), last ? nullptr : part, loss, lse, status));
   }
-  P.tiles_m = p.mt;
-  P.tiles_n = ceil_div(h.V, V_TILE);
-  P.M = N;
-  P.N = h.V;
-  P.labels = h.labels;
-  P.part = r.at<float2>(p.part);
-  if ((rc = launch_product<V_LSE>(r, P)) != DP_OK) return rc;
-  VOCAB_CUDA(launch_chained(k_vocab_loss, (unsigned)ceil_div(N, 8), 256, 0, r.s, head_of(h), r.at<float2>(p.part), 2 * P.tiles_n,
-                            loss, lse, status));
   return DP_OK;
 }
 

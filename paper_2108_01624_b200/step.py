@@ -12,7 +12,7 @@ from typing import List, Optional, Sequence
 import torch
 
 from . import binding as b
-from .synth import EMBEDDING, LAYERNORM, LINEAR, ROWS, LayerData, LayerSpec
+from .synth import EMBEDDING, HEAD, LAYERNORM, LINEAR, ROWS, LayerData, LayerSpec
 
 
 class DeviceStatusError(RuntimeError):
@@ -50,6 +50,10 @@ class DPStep:
         also trains (BERT's masked-LM decoder): the projection gets no storage of its own, both layers accumulate into
         the table, and the per-example norm includes the inner product of their two contributions.
 
+        A HEAD spec [V, d] is a softmax head whose logits and their gradients are not kept (binding.VocabHead).  Its turn in a
+        microbatch: head_backward(li, head, lse, dx) in the backward pass, accumulate_microbatch after it.  It may share the table
+        of an EMBEDDING spec through shared_tables too, with a bias of its own.
+
         max_grad_norm clips the noised mean gradient of a macro-batch to this global L2 norm, over all tensors, before
         the AdamW update (post-processing of Algorithm 1's g_t, so it changes nothing about the privacy of a step).
 
@@ -67,9 +71,11 @@ class DPStep:
         self.shared_tables = dict(shared_tables or {})
         for p_li, e_li in self.shared_tables.items():
             sp, se = self.specs[p_li], self.specs[e_li]
-            if not (e_li < p_li and se.kind == EMBEDDING and sp.kind == LINEAR and not sp.has_bias
+            if not (e_li < p_li and se.kind == EMBEDDING and (sp.kind == HEAD or sp.kind == LINEAR and not sp.has_bias)
                     and sp.d_in == se.d_in and sp.d_out == se.d_out):
-                raise ValueError("a shared table needs an EMBEDDING [V, d] listed before a bias-free LINEAR V -> d")
+                raise ValueError("a shared table needs an EMBEDDING [V, d] listed before a bias-free LINEAR V -> d or a HEAD")
+            if sp.kind == HEAD and list(self.shared_tables.values()).count(e_li) > 1:
+                raise ValueError("a HEAD that shares a table is the only one that does")
         self.device = torch.device(device)
         self.C, self.sigma, self.lr, self.beta1, self.beta2 = C, sigma, lr, beta1, beta2
         self.xi, self.weight_decay, self.seed = xi, weight_decay, seed
@@ -77,19 +83,19 @@ class DPStep:
         self.shapes: List[List[tuple]] = []
         pos = 0
         for li, sp in enumerate(self.specs):
-            if li in self.shared_tables:              # alias of the embedding's table
-                e_li = self.shared_tables[li]
-                self.offsets.append(list(self.offsets[e_li]))
-                self.shapes.append(list(self.shapes[e_li]))
-                continue
             if sp.kind == LINEAR:
                 shp = [(sp.d_in, sp.d_out)] + ([(sp.d_out,)] if sp.has_bias else [])
             elif sp.kind == LAYERNORM:
                 shp = [(sp.d_out,), (sp.d_out,)]
+            elif sp.kind == HEAD:
+                shp = [(sp.d_in, sp.d_out)] + ([(sp.d_in,)] if sp.has_bias else [])
             else:
                 shp = [(sp.d_in, sp.d_out)]
             offs = []
-            for s in shp:
+            for k, s in enumerate(shp):
+                if k == 0 and li in self.shared_tables:              # alias of the embedding's table
+                    offs.append(self.offsets[self.shared_tables[li]][0])
+                    continue
                 offs.append(pos)
                 n = 1
                 for x in s:
@@ -113,6 +119,8 @@ class DPStep:
         self._ws = None
         self._sqnorm = None
         self._clip = None
+        self._heads: dict = {}          # heads of the microbatch under way: spec index -> (head, lse)
+        self._head_ws = None
 
     def view(self, flat: torch.Tensor, li: int, k: int) -> torch.Tensor:
         shp = self.shapes[li][k]
@@ -123,10 +131,13 @@ class DPStep:
         return flat[off:off + n].view(*shp)
 
     def layer_list(self, data: Sequence[LayerData], paths: Optional[Sequence[int]] = None) -> b.LayerList:
-        """Descriptors for one microbatch; data[k] must correspond to specs[k].  ROWS entries are left to row_list."""
+        """Descriptors for one microbatch; data[k] must correspond to specs[k].  ROWS entries are left to row_list, HEAD
+        entries (None) to head_backward."""
         out = []
         for li, ld in enumerate(data):
             sp = self.specs[li]
+            if sp.kind == HEAD:
+                continue
             assert ld.spec.kind == sp.kind and ld.spec.d_out == sp.d_out
             if sp.kind == ROWS:
                 continue
@@ -149,9 +160,8 @@ class DPStep:
         hi = self.n_flat if hi is None else hi
         out = []
         for li in range(len(self.specs)):
-            if li in self.shared_tables:
-                continue
-            for off, shp in zip(self.offsets[li], self.shapes[li]):
+            own = slice(1 if li in self.shared_tables else 0, None)
+            for off, shp in zip(self.offsets[li][own], self.shapes[li][own]):
                 a, z = max(off, lo), min(off + math.prod(shp), hi)
                 if a < z:
                     out.append(flat[a - lo:z - lo])
@@ -167,6 +177,34 @@ class DPStep:
             groups.setdefault(int(L.G.shape[1]), []).append(L)
         return [b.LayerList(ls) for ls in groups.values()]
 
+    def _batch(self, B: int) -> None:
+        """Norms and factors of a microbatch of B examples."""
+        if self._sqnorm is None or self._sqnorm.numel() != B:
+            self._sqnorm = torch.empty(B, dtype=torch.float32, device=self.device)
+            self._clip = torch.empty(B, dtype=torch.float32, device=self.device)
+
+    def _head_workspace(self, head: b.VocabHead) -> torch.Tensor:
+        need = b.dp_vocab_workspace_bytes(head)
+        if self._head_ws is None or self._head_ws.numel() < need:
+            self._head_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self._head_ws
+
+    def head_backward(self, li: int, head: b.VocabHead, lse: torch.Tensor, dx: Optional[torch.Tensor], stream=None) -> None:
+        """Backward pass of the HEAD spec `li` for the microbatch under way, from dp_vocab_loss's lse: dx, and the norms of its
+        gradients for the clip.  accumulate_microbatch, which wants every HEAD spec's call before it, adds its clipped sum, so
+        the head's tensors and lse stay as they are until then.  Again for the same spec, or with another number of examples: the
+        microbatch begins anew."""
+        sp = self.specs[li]
+        if sp.kind != HEAD:
+            raise ValueError(f"spec {li} is no HEAD")
+        if tuple(head.weight.shape) != (sp.d_in, sp.d_out) or (head.bias is not None) != sp.has_bias:
+            raise ValueError(f"spec {li}: a head [{sp.d_in}, {sp.d_out}] {'with' if sp.has_bias else 'without'} bias expected")
+        if li in self._heads or any(h.B != head.B for h, _ in self._heads.values()):
+            self._heads = {}
+        self._batch(head.B)
+        b.dp_vocab_loss_backward(head, lse, dx, self._sqnorm, bool(self._heads), self._head_workspace(head), stream)
+        self._heads[li] = (head, lse)
+
     def accumulate_microbatch(self, layers, stream=None, rows=None):
         """norms -> clip factors -> clipped accumulate for one microbatch (all enqueued, no sync).
         `layers` is a LayerList, or a list of them (layer_lists) when token counts differ between layers; `rows` is the
@@ -174,24 +212,27 @@ class DPStep:
         tensors: one left out would break the bound that the noise is calibrated to)."""
         lists = [layers] if isinstance(layers, b.LayerList) else list(layers)
         lists = [ll for ll in lists if len(ll)]
+        heads = dict(sorted(self._heads.items()))
+        if len(heads) != sum(sp.kind == HEAD for sp in self.specs):
+            raise ValueError("every HEAD spec needs its head_backward before accumulate_microbatch")
         n_rows = sum(sp.kind == ROWS for sp in self.specs)
         if (0 if rows is None else len(rows)) != n_rows:
             raise ValueError(f"the model has {n_rows} ROWS tensors: pass row_list(data) of this microbatch as rows")
-        if not lists and rows is None:
+        if not lists and rows is None and not heads:
             raise ValueError("no layers")
-        B = lists[0].B if lists else rows.B
+        B = lists[0].B if lists else rows.B if rows is not None else next(iter(heads.values()))[0].B
+        if any(h.B != B for h, _ in heads.values()):
+            raise ValueError(f"heads of other numbers of examples than {B}")
         if rows is not None and rows.B != B:
             raise ValueError(f"rows of {rows.B} examples, layers of {B}")
-        if self._sqnorm is None or self._sqnorm.numel() != B:
-            self._sqnorm = torch.empty(B, dtype=torch.float32, device=self.device)
-            self._clip = torch.empty(B, dtype=torch.float32, device=self.device)
+        self._batch(B)
         if self._ws is None or len(self._ws) != len(lists):
             self._ws = [None] * len(lists)
         for k, ll in enumerate(lists):
             need = b.dp_workspace_bytes(ll)
             if self._ws[k] is None or self._ws[k].numel() < need:
                 self._ws[k] = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-            b.dp_per_example_sqnorms(ll, self._sqnorm, k > 0, self._ws[k], stream)
+            b.dp_per_example_sqnorms(ll, self._sqnorm, k > 0 or bool(heads), self._ws[k], stream)
         if self.shared_tables:
             by_acc = {}
             for ll in lists:
@@ -201,11 +242,22 @@ class DPStep:
                 if len(pair) == 2:
                     emb, proj = (pair[0], pair[1]) if pair[0].kind == EMBEDDING else (pair[1], pair[0])
                     b.dp_shared_table_cross_sqnorms(emb, proj, self._sqnorm, stream)
+            for li, (head, lse) in heads.items():
+                if li in self.shared_tables:
+                    emb = by_acc.get(self.view(self.acc, li, 0).data_ptr(), [])
+                    if len(emb) != 1:
+                        raise ValueError(f"the embedding that shares its table with head {li} is missing")
+                    b.dp_vocab_loss_cross_sqnorms(head, lse, emb[0].ids, emb[0].G, self._sqnorm, self._head_workspace(head), stream)
         if rows is not None:
-            b.dp_rows_sqnorms(rows, self._sqnorm, bool(lists), stream)
+            b.dp_rows_sqnorms(rows, self._sqnorm, bool(lists) or bool(heads), stream)
         b.dp_clip_factors(self._sqnorm, self.C, self._clip, stream)
         for k, ll in enumerate(lists):
             b.dp_clipped_accumulate_after_sqnorms(ll, self._clip, self._ws[k], stream)
+        for li, (head, lse) in heads.items():
+            b.dp_vocab_loss_clipped_accumulate(head, lse, self._clip, self.view(self.acc, li, 0),
+                                               self.view(self.acc, li, 1) if head.bias is not None else None,
+                                               self._head_workspace(head), stream)
+        self._heads = {}
         if rows is not None:
             b.dp_rows_clipped_accumulate(rows, self._clip, stream)
         self.examples_seen += B
@@ -214,6 +266,7 @@ class DPStep:
     def discard_macro_batch(self) -> None:
         """Drops the partly accumulated macro-batch: the accumulator is cleared, theta, m, v and t stay as they are."""
         self.acc.zero_()
+        self._heads = {}
         self.examples_seen = 0
 
     def check_device_status(self, stream=None) -> None:

@@ -26,12 +26,13 @@ import torch
 
 LINEAR, LAYERNORM, EMBEDDING = "linear", "layernorm", "embedding"
 ROWS = "rows"           # a small tensor [d_in, d_out] whose per-example gradient is given
+HEAD = "head"           # a softmax head [V, d] over a vocabulary whose logits are not kept (binding.VocabHead)
 
 
 @dataclass
 class LayerSpec:
     kind: str
-    d_in: int           # LINEAR: input width; LAYERNORM: d; EMBEDDING: vocab V; ROWS: rows of the tensor
+    d_in: int           # LINEAR: input width; LAYERNORM: d; EMBEDDING, HEAD: vocab V; ROWS: rows of the tensor
     d_out: int
     has_bias: bool = False
     name: str = ""
@@ -40,6 +41,8 @@ class LayerSpec:
     def n_params(self) -> int:
         if self.kind == LINEAR:
             return self.d_in * self.d_out + (self.d_out if self.has_bias else 0)
+        if self.kind == HEAD:
+            return self.d_in * self.d_out + (self.d_in if self.has_bias else 0)
         if self.kind == LAYERNORM:
             return 2 * self.d_out
         return self.d_in * self.d_out
@@ -128,6 +131,8 @@ def kappa(specs: List[LayerSpec], T: int) -> float:
     are unit Gaussians (embedding rows counted as if ids were distinct)."""
     s = 0.0
     for sp in specs:
+        if sp.kind == HEAD:          # its gradients follow from states and labels, not from a drawn G
+            continue
         if sp.kind == LINEAR:
             s += T * sp.d_out * (sp.d_in + (1 if sp.has_bias else 0))
         elif sp.kind == LAYERNORM:
@@ -185,6 +190,8 @@ def generate(wl: Workload, seed: int = 0, device="cpu", microbatch: int = 0,
     for li, sp in enumerate(wl.specs):
         if specs is not None and not any(sp is q for q in specs):
             continue
+        if sp.kind == HEAD:
+            raise ValueError("a head's gradients are not drawn: they follow from states and labels (binding.VocabHead)")
         gG = _gen(device, seed, microbatch, li, 1)
         if sp.kind == ROWS:
             G = torch.randn(B, sp.d_in, sp.d_out, generator=gG, device=device, dtype=torch.float32)
