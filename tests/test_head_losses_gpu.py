@@ -153,6 +153,7 @@ def test_loss_gradient_sum_and_cross_term(shape, dtype):
     c.check_backward()
     c.check_sum()
     c.check_cross(9)
+    c.check_cross(150, seed=4)
     assert dp.dp_poll_status() == 0
 
 
