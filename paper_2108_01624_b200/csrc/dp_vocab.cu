@@ -584,11 +584,15 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
   }
 }
 
-// The tiles of a DX or DW launch that several pairs shared: their parts are added in the pairs' order.  Block (t, r): tile t
-// of those that were shared, rows [16 (r / 4), +16), columns [64 (r % 4), +64).  A warp: 4 rows, 8 groups of four columns
-// (64 bytes of a slot, 128 of a result at a time).
-template <int MODE>
+// The tiles of a DX or DW launch that several pairs shared: their parts are added, in an order that the sizes decide.  Block (t, r):
+// tile t of those that were shared, 16 / STRANDS rows from (r / 4) of them on, columns [64 (r % 4), +64).  Strands of threads take a run
+// of the parts each; a warp reads 4 rows, 8 groups of four columns (64 bytes of a slot, 128 of a result at a time).  One strand where
+// a tile has few parts (360 tiles on 74 pairs: four strands, four times the blocks, take 70 us more), four where many (37: 9.9 us, one
+// strand 11.8).
+template <int MODE, int STRANDS>
 __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VParams P) {
+  constexpr int OUTPUTS = 256 / STRANDS, ROWS = 16 / STRANDS;
+  __shared__ float4 strands[STRANDS][OUTPUTS];
   wait_for_predecessor();
   let_successor_in();
   const int nkb = P.n_pairs * P.kb, tiles = P.tiles_m * P.tiles_n, whole = whole_tiles(MODE, tiles, P.units);
@@ -598,16 +602,27 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
   if (last == u0) return;                                         // one unit had it all, and has written it
   int m0, n0;
   tile_origin<MODE>(P, whole + (int)blockIdx.x, m0, n0);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = (blockIdx.y >> 2) * 16 + (warp & 3) * 4 + (lane & 3), g = (blockIdx.y & 3) * 16 + (warp >> 2) * 8 + (lane >> 2);
-  if (g >= P.nt / 4) return;
-  const int first_slot = 2 * u0 + (begin > share_begin(line, P.units, u0) ? 1 : 0);
-  const size_t at = (size_t)g * V_TILE + r;
-  float4 v = P.slots[(size_t)first_slot * (V_TILE / 4) * V_TILE + at];
+  const int strand = threadIdx.x / OUTPUTS, one = threadIdx.x % OUTPUTS, lane = one & 31, warp = one >> 5;
+  const int r0 = (blockIdx.y >> 2) * ROWS, r = r0 + (warp >> 1) * 4 + (lane & 3), g = (blockIdx.y & 3) * 16 + (warp & 1) * 8 + (lane >> 2);
+  if ((blockIdx.y & 3) * 64 >= P.nt || m0 + r0 >= P.M) return;
+  const int parts = last - u0 + 1, k0 = parts * strand / STRANDS, k1 = parts * (strand + 1) / STRANDS;
+  const size_t slot_size = (size_t)(V_TILE / 4) * V_TILE;
+  const float4* from = P.slots + (size_t)g * V_TILE + r;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
-  for (int u = u0 + 1; u <= last; ++u) {                          // the tile is the first of these units' shares
-    const float4 x = P.slots[(size_t)(2 * u) * (V_TILE / 4) * V_TILE + at];
+  for (int k = k0; k < k1; ++k) {                                 // the tile is the first of a unit's share but, perhaps, unit u0's
+    const float4 x = from[(2 * (u0 + k) + (k == 0 && begin > share_begin(line, P.units, u0) ? 1 : 0)) * slot_size];
     v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+  }
+  if constexpr (STRANDS > 1) {
+    strands[strand][one] = v;
+    __syncthreads();
+    if (strand) return;
+#pragma unroll
+    for (int k = 1; k < STRANDS; ++k) {
+      const float4 x = strands[k][one];
+      v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+    }
   }
   if constexpr (MODE == V_DX) put_dx(P, m0 + r, n0 + 4 * g, v);
   else put_dw(P, m0 + r, n0 + 4 * g, v);
@@ -864,19 +879,22 @@ __device__ __forceinline__ uint4 split_eight(float (&x)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Planes of a matrix [rows, d]: out[plane][row][dp], zeros beyond d.  (fp32: three, bf16: one, where the tensor's own
-// rows cannot be copied by TMA.)
+// Planes of W and (from row H.V on) X: out[plane][row][dp], zeros beyond d; a warp a row.  (fp32: three, bf16: one, where the
+// tensors' own rows cannot be copied by TMA.)
 __global__ void __launch_bounds__(256)
-k_vocab_planes(const void* src, long long ld, int rows, int d, int dp, int f32, int planes, __nv_bfloat16* out) {
+k_vocab_planes(const __grid_constant__ VHead H, int rows_x, int dp, int planes, __nv_bfloat16* out_w, __nv_bfloat16* out_x) {
   wait_for_predecessor();
   let_successor_in();
-  const long long total = (long long)rows * dp, plane = total;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-    const long long r = i / dp;
-    const int c = (int)(i - r * dp);
-    float x = 0.0f;
-    if (c < d) x = f32 ? static_cast<const float*>(src)[r * ld + c] : __bfloat162float(static_cast<const __nv_bfloat16*>(src)[r * ld + c]);
-    for (int p = 0; p < planes; ++p) out[p * plane + i] = split_off(x);
+  const int lane = threadIdx.x & 31;
+  for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < (long long)H.V + rows_x; r += (long long)gridDim.x * 8) {
+    const bool isx = r >= H.V;
+    const long long row = isx ? r - H.V : r, rows = isx ? rows_x : H.V;
+    __nv_bfloat16* out = (isx ? out_x : out_w) + row * dp;
+    for (int c = 8 * lane; c < dp; c += 256) {
+      float x[8];
+      eight(H, isx ? H.x : H.w, row * (isx ? H.ldx : H.ldw), c, x);
+      for (int p = 0; p < planes; ++p) *reinterpret_cast<uint4*>(out + p * rows * dp + c) = split_eight(x);
+    }
   }
 }
 
@@ -997,6 +1015,19 @@ __global__ void __launch_bounds__(256) k_vocab_bias(const float* part, int rows,
     for (int k = 1; k < 8; ++k) sum += s[k][lane];
     acc_b[c] += sum;
   }
+}
+
+// sqnorm[i] = or += the parts of example i, in order: a warp an example, its lanes every 32nd part each, then a fixed tree.
+__global__ void __launch_bounds__(256) k_vocab_norm_sum(const float* part, int B, int parts, float* sqnorm, int add) {
+  wait_for_predecessor();
+  let_successor_in();
+  const int i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (i >= B) return;
+  float s = 0.0f;
+  for (int k = lane; k < parts; k += 32) s += part[(long long)i * parts + k];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
+  if (lane == 0) sqnorm[i] = add ? sqnorm[i] + s : s;
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------------
@@ -1178,11 +1209,11 @@ struct VRun {                    // a call under way
 
 #define VOCAB_CUDA(expr) do { note_launch(1); if ((expr) != cudaSuccess) return DP_ERR_CUDA; } while (0)
 
-static int pack_rows(const VRun& r, const void* src, long long ld, long long rows, size_t off) {
-  const long long n = rows * r.p.dp;
-  const unsigned grid = (unsigned)std::min<long long>((n + 255) / 256, 148 * 16);
-  const int f32 = r.h.dtype == DP_F32;
-  VOCAB_CUDA(launch_chained(k_vocab_planes, grid, 256, 0, r.s, src, ld, (int)rows, r.h.d, r.p.dp, f32, f32 ? 3 : 1, r.at<__nv_bfloat16>(off)));
+static int pack_rows(const VRun& r, int rows_x, size_t off_x) {
+  const bool f32 = r.h.dtype == DP_F32;
+  const unsigned grid = (unsigned)std::min<long long>(((long long)r.h.V + rows_x + 7) / 8, (long long)sm_count() * 8);
+  VOCAB_CUDA(launch_chained(k_vocab_planes, grid, 256, 0, r.s, head_of(r.h), rows_x, r.p.dp, f32 ? 3 : 1, r.at<__nv_bfloat16>(r.p.wp),
+                            r.at<__nv_bfloat16>(off_x)));
   return DP_OK;
 }
 
@@ -1226,7 +1257,8 @@ static int launch_product(const VRun& r, VParams& P) {
   if constexpr (MODE == V_DX || MODE == V_DW) {
     const int shared = (int)tiles - whole_tiles(MODE, (int)tiles, P.units);
     if (P.units > 1 && shared)
-      VOCAB_CUDA(launch_chained(k_vocab_join<MODE>, dim3((unsigned)shared, V_TILE / 16 * 4), 256, 0, r.s, P));
+      VOCAB_CUDA(P.units <= 8 * shared ? launch_chained(k_vocab_join<MODE, 1>, dim3((unsigned)shared, V_TILE / 4), 256, 0, r.s, P)
+                                       : launch_chained(k_vocab_join<MODE, 4>, dim3((unsigned)shared, V_TILE), 256, 0, r.s, P));
   }
   return DP_OK;
 }
@@ -1239,7 +1271,7 @@ static int over_pieces(const VRun& r, const float* lse, const float* clip, float
   const int N = h.B * h.T;
   const bool f32 = h.dtype == DP_F32;
   int rc;
-  if (!p.direct && (rc = pack_rows(r, h.W, h.ldw, h.V, p.wp)) != DP_OK) return rc;
+  if (!p.direct && (rc = pack_rows(r, 0, 0)) != DP_OK) return rc;
   __nv_bfloat16 *xe = r.at<__nv_bfloat16>(p.xe), *x2 = r.at<__nv_bfloat16>(p.x2), *G = r.at<__nv_bfloat16>(p.G);
   const int columns = p.n_sub * p.sub;
   VOCAB_CUDA(launch_chained(k_vocab_tokens, (unsigned)ceil_div(std::max(N, columns / 64), 8), 256, 0, r.s, head_of(h), lse, clip, p.R, p.dp, p.dp > h.d && f32 && h.bias && !clip ? h.d : -1, xe, x2,
@@ -1305,7 +1337,7 @@ int dp_vocab_loss(const dp_vocab_head* head, float* loss, float* lse, void* work
   if (!status || !vocab_kernels_ready()) return DP_ERR_CUDA;
   const VRun r = {h, p, static_cast<char*>(workspace), static_cast<cudaStream_t>(cuda_stream), status};
   const int N = h.B * h.T;
-  if (!p.direct && ((rc = pack_rows(r, h.W, h.ldw, h.V, p.wp)) != DP_OK || (rc = pack_rows(r, h.X, h.ldx, N, p.xp)) != DP_OK)) return rc;
+  if (!p.direct && (rc = pack_rows(r, N, p.xp)) != DP_OK) return rc;
   float2* part = r.at<float2>(p.part);          // [what went before][column blocks], a value a token each
   for (int v0 = 0; v0 < h.V; v0 += p.loss_columns) {
     VParams P = {};
@@ -1346,7 +1378,6 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
   const VRun r = {h, p, static_cast<char*>(workspace), static_cast<cudaStream_t>(cuda_stream), status};
   const int N = h.B * h.T;
   const bool f32 = h.dtype == DP_F32;
-  if (sqnorm && !accumulate_into && launch_fill_zero(sqnorm, h.B, r.s) != cudaSuccess) return DP_ERR_CUDA;
   __nv_bfloat16* G = r.at<__nv_bfloat16>(p.G);
   return over_pieces(r, lse, nullptr, nullptr, [&](int s0, int subs, long long block) -> int {
     int rc = DP_OK;
@@ -1386,6 +1417,7 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
       P.status = status;
       if ((rc = launch_product<V_DX>(r, P)) != DP_OK) return rc;
     }
+    const int add = accumulate_into || s0 > 0;
     if (sqnorm && p.short_examples) {
       NParams Q = {};
       const long long rows = (long long)N * p.R;
@@ -1405,7 +1437,7 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
       const long long items = (long long)Q.groups * Q.splits;
       if (items > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
       VOCAB_CUDA(launch_chained(k_vocab_norms, (unsigned)std::min<long long>(items, sm_count()), N_THREADS, N_SMEM, r.s, Q));
-      if (launch_reduce_partials(Q.partial, h.B, Q.splits, sqnorm, r.s) != cudaSuccess) return DP_ERR_CUDA;
+      VOCAB_CUDA(launch_chained(k_vocab_norm_sum, (unsigned)ceil_div(h.B, 8), 256, 0, r.s, Q.partial, h.B, Q.splits, sqnorm, add));
     } else if (sqnorm) {
       std::vector<dp_layer> layers(subs);
       std::vector<int> idx(subs), way(subs, p.gram_way ? 1 : 0);
@@ -1417,7 +1449,7 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
       float* partial = r.at<float>(p.gram);
       const int count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), subs, way.data());
       if ((rc = launch_umma_sqnorms(layers.data(), idx.data(), subs, way.data(), partial, count, 0, status, r.s)) != DP_OK) return rc;
-      if (launch_reduce_partials(partial, h.B, count, sqnorm, r.s) != cudaSuccess) return DP_ERR_CUDA;
+      VOCAB_CUDA(launch_chained(k_vocab_norm_sum, (unsigned)ceil_div(h.B, 8), 256, 0, r.s, partial, h.B, count, sqnorm, add));
       if (!p.gram_way && h.bias && p.R == 2) {
         for (int k = 0; k < subs; ++k) cols.push_back({&layers[k], false, r.at<float>(p.cols) + (size_t)k * h.B * p.sub});
         if (launch_colsums_batched(cols.data(), (int)cols.size(), r.s) != cudaSuccess ||
