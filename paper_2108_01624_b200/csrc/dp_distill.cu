@@ -473,7 +473,7 @@ static cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s) {
   // where three rows fit (30522 bf16 words: 182 us for 6144 rows; 384 threads 188, 512 197), more where fewer do.
   const int rows = std::max(1, (int)(kRowsMost / (smem + 1536)));
   int threads = 64;
-  while (threads < (rows >= 3 ? 256 : kDistillThreads) && threads * 8 <= nv) threads *= 2;
+  while (threads < (rows >= 3 && a.N > sm_count() ? 256 : kDistillThreads) && threads * 8 <= nv) threads *= 2;
   const int resident = std::min(rows, 3 * kDistillThreads / threads);
   const unsigned grid = (unsigned)std::min<long long>(a.N, (long long)resident * sm_count());
   static signed char ready[kMaxDevices] = {};    // 0 unknown, 1 ready, -1 failed (one flag per form and device)
