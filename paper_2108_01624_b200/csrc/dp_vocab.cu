@@ -9,7 +9,10 @@
 //   DX     dX = G W over the piece
 //   DW     acc += G^T X over the piece
 // All are bound by the tensor cores where there are enough tokens (256 x 20 tokens of width 1024 and 30522 words are 0.32
-// TFLOP a product), and by reading the table where there are few.
+// TFLOP a product), and by reading the table where there are few.  There, alone: LSE 204 us (1.57 PFLOP/s, tensor pipe 86 % of the
+// time), GRAD 272 (it writes 625 MB of G besides: without its stores 221), DX 210 (1.52 PFLOP/s), DW 417 (both planes of G: 1.53), the norms
+// 110 (6.2 TB/s); back to back under the power cap 10 to 25 % longer.  Copies of 128 columns: stages of 64 with twice as many in
+// flight took 230 us in LSE, and a forwarding warp in the odd CTA instead of one barrier for the pair's copies 10 more.
 //
 // Exactness.  A product of bf16 numbers is exact in fp32 and the tensor cores sum in fp32, but drop low bits at every
 // step of 16: a sum of 64 steps comes out 7e-7 too small.  So
@@ -22,6 +25,7 @@
 //     into two for the products with G (2^-16 again, four products).
 #include <algorithm>
 #include <cmath>
+#include <new>
 #include <vector>
 
 #include "dp_chain.cuh"
@@ -37,7 +41,7 @@ enum : int { V_LSE = 0, V_GRAD = 1, V_DX = 2, V_DW = 3 };
 constexpr int V_THREADS = 320;                  // warp 0 TMA, warp 1 UMMA issue (even CTA), warps 2..9 epilogue
 constexpr int V_TILE = 256;                     // rows and columns of a pair's tile; a CTA holds 128 rows of it
 constexpr int V_BOX_BYTES = 128 * 128;          // one copy: 64 bf16 columns of 128 rows, 128-byte swizzle
-constexpr int V_STAGE_COLS = 32;                // GRAD: columns that a warp hands over at a time
+constexpr int V_STAGE_COLS = 32;                // GRAD: columns that a warp turns at a time
 constexpr int V_WARP_STAGE = 32 * 2 * V_STAGE_COLS * 2;   // 32 tokens x 2 planes, 64-byte rows; DX, DW: 32 x 32 fp32
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -49,7 +53,7 @@ template <int MODE> struct VForm {
   static constexpr int STAGES = 3;
   static constexpr int HALF_BYTES = BK / 64 * V_BOX_BYTES;     // 128 rows (columns) of one operand
   static constexpr int STAGE_BYTES = 2 * HALF_BYTES;
-  // an epilogue warp's own: 128 bias values; 32 columns of G; 32 x 32 results
+  // an epilogue warp's own: 128 bias values, or what it turns
   static constexpr int WARP_BYTES = MODE == V_LSE ? 128 * 4 : V_WARP_STAGE;
 };
 
@@ -274,7 +278,9 @@ __device__ __forceinline__ void finish_lse(const VParams& P, f32x2 (&z)[64], int
   if (m < P.M) P.part[(size_t)((n0 + col) >> 7) * P.M + m] = make_float2(top, sum.x + sum.y);
 }
 
-// G of this thread's 128 columns: two planes through shared memory, 32 columns at a time, and the warp's column sums.
+// G of this thread's 128 columns: two planes through shared memory, 32 columns at a time, and the warp's column sums.  (Measured
+// instead, GRAD at 272 us: plain stores of the turned chunk 327; 64 columns of half the tokens at a time 336; column sums by
+// m16n8k16 products of the staged rows, at 297 with shuffles then, 378.)
 __device__ __forceinline__ void finish_grad(const VParams& P, f32x2 (&z)[64], uint8_t* stage, float4 meta, int m0w, int n0, int col,
                                             int lane) {
   const int rel = __float_as_int(meta.w) - (P.v0 + n0 + col);     // no label: -1, never in range
@@ -587,8 +593,8 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
 // The tiles of a DX or DW launch that several pairs shared: their parts are added, in an order that the sizes decide.  Block (t, r):
 // tile t of those that were shared, 16 / STRANDS rows from (r / 4) of them on, columns [64 (r % 4), +64).  Strands of threads take a run
 // of the parts each; a warp reads 4 rows, 8 groups of four columns (64 bytes of a slot, 128 of a result at a time).  One strand where
-// a tile has few parts (360 tiles on 74 pairs: four strands, four times the blocks, take 70 us more), four where many (37: 9.9 us, one
-// strand 11.8).
+// a tile has few parts (two or three each: four strands are four times the blocks, most of whose threads idle), four where many (37:
+// 9.9 us, one strand 11.8).
 template <int MODE, int STRANDS>
 __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VParams P) {
   constexpr int OUTPUTS = 256 / STRANDS, ROWS = 16 / STRANDS;
@@ -633,7 +639,8 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
 // (<x_r, x_s> + bias) <g_r, g_s>.  A CTA takes as many whole examples as 128 rows hold and some blocks of G; both Grams are
 // 128 x 128 x 16 UMMAs of a tile with itself, of which the epilogue uses each row's own example.  The Gram of G is taken
 // over by the epilogue every kNormSeg columns and added in registers: its squares are one large (the label's) and a
-// vocabulary of small ones, which a longer sum on the tensor core would lose.  Bound by reading G.
+// vocabulary of small ones, which a longer sum on the tensor core would lose.  Bound by reading G: 110 us for 625 MB, where the
+// layers' kernel with one example at a time took 318.
 // =================================================================================================
 constexpr int N_STAGES = 6, N_STAGE_BYTES = 2 * V_BOX_BYTES;    // 128 rows x 128 columns
 constexpr int N_THREADS = 192;                                  // warp 0 TMA, warp 1 UMMA, warps 2..5 epilogue
@@ -1074,10 +1081,10 @@ static bool encode_blocks(CUtensorMap* map, const void* base, long long rows, in
 
 constexpr size_t kPartBytes = (size_t)256 << 20;    // maxima and sums of the column blocks that are joined at a time
 constexpr int kSubColumns = 2048;               // columns of one block of G, at most
-#ifndef DP_VOCAB_PIECE_MB
-#define DP_VOCAB_PIECE_MB 1024
-#endif
-constexpr size_t kPieceBytes = (size_t)DP_VOCAB_PIECE_MB << 20;   // G of one piece, unless one block alone is larger
+// G of one piece, unless one block alone is larger.  Every piece costs the start and the end of three kernels and another pass
+// over the sums of dX: 256 x 20 tokens of width 1024, 30522 words, gradient / clipped sum with pieces of 128 MiB 1048 / 987 us, 256 MiB
+// 875 / 932, 384 MiB 781 / 908, all of G (640 MiB) 686 / 863.
+constexpr size_t kPieceBytes = (size_t)1 << 30;
 
 // How many CTAs share a group's blocks of G: each forms the Gram of X again, so as few as fill the device well, by the
 // columns that the longest-working CTA sums.
@@ -1165,11 +1172,8 @@ static VPlan plan_vocab(const dp_vocab_head& h, int op) {
     p.short_examples = 128 / (p.R * h.T);
     const dp_layer L = piece_layer(h, p, nullptr, nullptr);
     p.gram_way = use_gram(L);
-    std::vector<dp_layer> layers(p.piece_subs, L);
-    std::vector<int> idx(p.piece_subs), way(p.piece_subs, p.gram_way ? 1 : 0);
-    for (int k = 0; k < p.piece_subs; ++k) idx[k] = k;
-    if (p.short_examples) p.gram_count = p.piece_subs;
-    else p.gram_count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), p.piece_subs, way.data());
+    const int first = 0, way = p.gram_way ? 1 : 0;
+    p.gram_count = p.piece_subs * (p.short_examples ? 1 : (int)umma_sqnorm_partials_per_example(&L, &first, 1, &way));
     take(p.gram, (size_t)h.B * p.gram_count * sizeof(float));
     if (!p.gram_way && h.bias && p.R == 2) take(p.cols, (size_t)p.piece_subs * h.B * p.sub * sizeof(float));
   } else if (h.bias) {
@@ -1379,85 +1383,89 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
   const int N = h.B * h.T;
   const bool f32 = h.dtype == DP_F32;
   __nv_bfloat16* G = r.at<__nv_bfloat16>(p.G);
-  return over_pieces(r, lse, nullptr, nullptr, [&](int s0, int subs, long long block) -> int {
-    int rc = DP_OK;
-    if (dx) {
-      VParams P = {};
-      const int v0 = s0 * p.sub, cols = std::min(subs * p.sub, h.V - v0);
-      for (int k = 0; k < (f32 ? 2 : 1); ++k) {
-        if (!encode_blocks(&P.a[k], G + (size_t)k * p.sub, N, p.sub, (long long)p.R * p.sub, subs, block)) return DP_ERR_CUDA;
-        const bool ok = p.direct ? encode_rows(&P.b[k], h.W, h.V, h.d, h.ldw)
-                                 : encode_rows(&P.b[k], r.at<__nv_bfloat16>(p.wp) + (size_t)k * h.V * p.dp, h.V, h.d, p.dp);
-        if (!ok) return DP_ERR_CUDA;
+  try {                          // the layers' norm kernels keep lists of a piece's blocks
+    return over_pieces(r, lse, nullptr, nullptr, [&](int s0, int subs, long long block) -> int {
+      int rc = DP_OK;
+      if (dx) {
+        VParams P = {};
+        const int v0 = s0 * p.sub, cols = std::min(subs * p.sub, h.V - v0);
+        for (int k = 0; k < (f32 ? 2 : 1); ++k) {
+          if (!encode_blocks(&P.a[k], G + (size_t)k * p.sub, N, p.sub, (long long)p.R * p.sub, subs, block)) return DP_ERR_CUDA;
+          const bool ok = p.direct ? encode_rows(&P.b[k], h.W, h.V, h.d, h.ldw)
+                                   : encode_rows(&P.b[k], r.at<__nv_bfloat16>(p.wp) + (size_t)k * h.V * p.dp, h.V, h.d, p.dp);
+          if (!ok) return DP_ERR_CUDA;
+        }
+        static const unsigned char pa[4] = {1, 1, 0, 0}, pb[4] = {1, 0, 1, 0};
+        P.n_pairs = f32 ? 4 : 1;
+        for (int k = 0; k < P.n_pairs; ++k) {
+          P.pa[k] = f32 ? pa[k] : 0;
+          P.pb[k] = f32 ? pb[k] : 0;
+        }
+        P.kb = ceil_div(cols, 128);
+        P.seg = 16;
+        P.nt = h.d <= 128 ? 128 : V_TILE;
+        P.tiles_m = p.mt;
+        P.tiles_n = ceil_div(h.d, P.nt);
+        P.M = N;
+        P.N = h.d;
+        P.sub = p.sub;
+        P.v0 = v0;
+        P.V = h.V;
+        P.stride_c = (int)ld_dx;
+        P.slots = r.at<float4>(p.slots);
+        P.sum = p.pieces > 1 ? r.at<float>(p.dx) : nullptr;
+        P.out = dx;
+        P.out_bf16 = !f32;
+        P.first = s0 == 0;
+        P.last = s0 + subs >= p.n_sub;
+        P.vec = !misaligned(dx, 16) && ld_dx % (f32 ? 4 : 8) == 0 && h.d % 4 == 0;
+        P.status = status;
+        if ((rc = launch_product<V_DX>(r, P)) != DP_OK) return rc;
       }
-      static const unsigned char pa[4] = {1, 1, 0, 0}, pb[4] = {1, 0, 1, 0};
-      P.n_pairs = f32 ? 4 : 1;
-      for (int k = 0; k < P.n_pairs; ++k) {
-        P.pa[k] = f32 ? pa[k] : 0;
-        P.pb[k] = f32 ? pb[k] : 0;
+      const int add = accumulate_into || s0 > 0;
+      if (sqnorm && p.short_examples) {
+        NParams Q = {};
+        const long long rows = (long long)N * p.R;
+        if (!encode_rows(&Q.x, r.at<__nv_bfloat16>(p.xe), rows, p.dp, p.dp) || !encode_blocks(&Q.g, G, rows, p.sub, p.sub, subs, block))
+          return DP_ERR_CUDA;
+        Q.rows = p.R * h.T;
+        Q.examples = p.short_examples;
+        Q.B = h.B;
+        Q.groups = ceil_div(h.B, Q.examples);
+        Q.subs = subs;
+        Q.sub = p.sub;
+        Q.dp = p.dp;
+        Q.splits = norm_splits(Q.groups, subs, p.sub, p.dp);
+        Q.bias = h.bias && p.R == 2;
+        Q.partial = r.at<float>(p.gram);
+        Q.status = status;
+        const long long items = (long long)Q.groups * Q.splits;
+        if (items > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
+        VOCAB_CUDA(launch_chained(k_vocab_norms, (unsigned)std::min<long long>(items, sm_count()), N_THREADS, N_SMEM, r.s, Q));
+        VOCAB_CUDA(launch_chained(k_vocab_norm_sum, (unsigned)ceil_div(h.B, 8), 256, 0, r.s, Q.partial, h.B, Q.splits, sqnorm, add));
+      } else if (sqnorm) {
+        std::vector<dp_layer> layers(subs);
+        std::vector<int> idx(subs), way(subs, p.gram_way ? 1 : 0);
+        std::vector<ColTaskHost> cols;
+        for (int k = 0; k < subs; ++k) {
+          layers[k] = piece_layer(h, p, r.at<__nv_bfloat16>(p.xe), G + (size_t)k * block);
+          idx[k] = k;
+        }
+        float* partial = r.at<float>(p.gram);
+        const int count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), subs, way.data());
+        if ((rc = launch_umma_sqnorms(layers.data(), idx.data(), subs, way.data(), partial, count, 0, status, r.s)) != DP_OK) return rc;
+        VOCAB_CUDA(launch_chained(k_vocab_norm_sum, (unsigned)ceil_div(h.B, 8), 256, 0, r.s, partial, h.B, count, sqnorm, add));
+        if (!p.gram_way && h.bias && p.R == 2) {
+          for (int k = 0; k < subs; ++k) cols.push_back({&layers[k], false, r.at<float>(p.cols) + (size_t)k * h.B * p.sub});
+          if (launch_colsums_batched(cols.data(), (int)cols.size(), r.s) != cudaSuccess ||
+              launch_rows_sqsum_batched(cols.data(), (int)cols.size(), sqnorm, r.s) != cudaSuccess) return DP_ERR_CUDA;
+        }
       }
-      P.kb = ceil_div(cols, 128);
-      P.seg = 16;
-      P.nt = h.d <= 128 ? 128 : V_TILE;
-      P.tiles_m = p.mt;
-      P.tiles_n = ceil_div(h.d, P.nt);
-      P.M = N;
-      P.N = h.d;
-      P.sub = p.sub;
-      P.v0 = v0;
-      P.V = h.V;
-      P.stride_c = (int)ld_dx;
-      P.slots = r.at<float4>(p.slots);
-      P.sum = p.pieces > 1 ? r.at<float>(p.dx) : nullptr;
-      P.out = dx;
-      P.out_bf16 = !f32;
-      P.first = s0 == 0;
-      P.last = s0 + subs >= p.n_sub;
-      P.vec = !misaligned(dx, 16) && ld_dx % (f32 ? 4 : 8) == 0 && h.d % 4 == 0;
-      P.status = status;
-      if ((rc = launch_product<V_DX>(r, P)) != DP_OK) return rc;
-    }
-    const int add = accumulate_into || s0 > 0;
-    if (sqnorm && p.short_examples) {
-      NParams Q = {};
-      const long long rows = (long long)N * p.R;
-      if (!encode_rows(&Q.x, r.at<__nv_bfloat16>(p.xe), rows, p.dp, p.dp) || !encode_blocks(&Q.g, G, rows, p.sub, p.sub, subs, block))
-        return DP_ERR_CUDA;
-      Q.rows = p.R * h.T;
-      Q.examples = p.short_examples;
-      Q.B = h.B;
-      Q.groups = ceil_div(h.B, Q.examples);
-      Q.subs = subs;
-      Q.sub = p.sub;
-      Q.dp = p.dp;
-      Q.splits = norm_splits(Q.groups, subs, p.sub, p.dp);
-      Q.bias = h.bias && p.R == 2;
-      Q.partial = r.at<float>(p.gram);
-      Q.status = status;
-      const long long items = (long long)Q.groups * Q.splits;
-      if (items > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
-      VOCAB_CUDA(launch_chained(k_vocab_norms, (unsigned)std::min<long long>(items, sm_count()), N_THREADS, N_SMEM, r.s, Q));
-      VOCAB_CUDA(launch_chained(k_vocab_norm_sum, (unsigned)ceil_div(h.B, 8), 256, 0, r.s, Q.partial, h.B, Q.splits, sqnorm, add));
-    } else if (sqnorm) {
-      std::vector<dp_layer> layers(subs);
-      std::vector<int> idx(subs), way(subs, p.gram_way ? 1 : 0);
-      std::vector<ColTaskHost> cols;
-      for (int k = 0; k < subs; ++k) {
-        layers[k] = piece_layer(h, p, r.at<__nv_bfloat16>(p.xe), G + (size_t)k * block);
-        idx[k] = k;
-      }
-      float* partial = r.at<float>(p.gram);
-      const int count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), subs, way.data());
-      if ((rc = launch_umma_sqnorms(layers.data(), idx.data(), subs, way.data(), partial, count, 0, status, r.s)) != DP_OK) return rc;
-      VOCAB_CUDA(launch_chained(k_vocab_norm_sum, (unsigned)ceil_div(h.B, 8), 256, 0, r.s, partial, h.B, count, sqnorm, add));
-      if (!p.gram_way && h.bias && p.R == 2) {
-        for (int k = 0; k < subs; ++k) cols.push_back({&layers[k], false, r.at<float>(p.cols) + (size_t)k * h.B * p.sub});
-        if (launch_colsums_batched(cols.data(), (int)cols.size(), r.s) != cudaSuccess ||
-            launch_rows_sqsum_batched(cols.data(), (int)cols.size(), sqnorm, r.s) != cudaSuccess) return DP_ERR_CUDA;
-      }
-    }
-    return rc;
-  });
+      return rc;
+    });
+  } catch (const std::bad_alloc&) {
+    return DP_ERR_UNSUPPORTED;
+  }
 }
 
 int dp_vocab_loss_clipped_accumulate(const dp_vocab_head* head, const float* lse, const float* clip, float* acc_w, float* acc_b,

@@ -31,7 +31,7 @@ struct CrossArgs {
   const int32_t* ids;
   float* out;                    // sqnorm, or partial sums [B][chunks]
   long long ldx, ldw, lde;
-  int T, Tu, d, V, chunks, t_chunks, all;   // all: (128-input x 8 NT-token) tasks of an example, shared by `chunks` blocks
+  int B, T, Tu, d, V, chunks, t_chunks, all;   // all: (128-input x 8 NT-token) tasks of an example, shared by `chunks` blocks
   int vec;
   int* status;
 };
@@ -150,9 +150,10 @@ __device__ __forceinline__ void cross_store(const CrossArgs& a, long long i, flo
     if (a.chunks > 1) a.out[i * a.chunks + blockIdx.x] = 2.0f * s;
     else a.out[i] += 2.0f * s;
   }
+  __syncthreads();
 }
 
-// Block (chunk, example): eight warps, 16 inputs each, against NT groups of 8 tokens.
+// Block (chunk, example, and every 65535th after it): eight warps, 16 inputs each, against NT groups of 8 tokens.
 template <typename T, int NT>
 __global__ void __launch_bounds__(256) k_vocab_cross(const __grid_constant__ CrossArgs a) {
   __shared__ float red[8];
@@ -160,45 +161,46 @@ __global__ void __launch_bounds__(256) k_vocab_cross(const __grid_constant__ Cro
   let_successor_in();
   using R = CrossRow<T>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const long long i = blockIdx.y;
-  float sum = 0.0f;
-  for (int task = blockIdx.x; task < a.all; task += a.chunks) {
-    const int u0 = (task / a.t_chunks) * 128 + warp * 16, t0 = (task % a.t_chunks) * (NT * 8);
-    if (u0 >= a.Tu) continue;
-    const int2 id = cross_words(a, i, u0 + g);
-    // rows that do not count are read from a place that exists; their columns or rows of the products are left out below
-    const long long w0 = (long long)max(id.x, 0) * a.ldw, w1 = (long long)max(id.y, 0) * a.ldw;
-    const long long e0 = (i * a.Tu + min(u0 + g, a.Tu - 1)) * a.lde, e1 = (i * a.Tu + min(u0 + g + 8, a.Tu - 1)) * a.lde;
-    float cz[NT][4] = {}, ck[NT][4] = {};
-    for (int k0 = 0; k0 < a.d; k0 += kCrossSeg) {
-      float sz[NT][4] = {}, sk[NT][4] = {};
-      const int k1 = min(k0 + kCrossSeg, (a.d + 31) / 32 * 32);
+  for (long long i = blockIdx.y; i < a.B; i += gridDim.y) {
+    float sum = 0.0f;
+    for (int task = blockIdx.x; task < a.all; task += a.chunks) {
+      const int u0 = (task / a.t_chunks) * 128 + warp * 16, t0 = (task % a.t_chunks) * (NT * 8);
+      if (u0 >= a.Tu) continue;
+      const int2 id = cross_words(a, i, u0 + g);
+      // rows that do not count are read from a place that exists; their columns or rows of the products are left out below
+      const long long w0 = (long long)max(id.x, 0) * a.ldw, w1 = (long long)max(id.y, 0) * a.ldw;
+      const long long e0 = (i * a.Tu + min(u0 + g, a.Tu - 1)) * a.lde, e1 = (i * a.Tu + min(u0 + g + 8, a.Tu - 1)) * a.lde;
+      float cz[NT][4] = {}, ck[NT][4] = {};
+      for (int k0 = 0; k0 < a.d; k0 += kCrossSeg) {
+        float sz[NT][4] = {}, sk[NT][4] = {};
+        const int k1 = min(k0 + kCrossSeg, (a.d + 31) / 32 * 32);
 #pragma unroll 2
-      for (int k = k0 + 8 * q; k < k1; k += 32) {
-        R wa, wb, ea, eb;
-        wa.load(a.w, w0, k, a.d, a.vec);
-        wb.load(a.w, w1, k, a.d, a.vec);
-        ea.load(a.e, e0, k, a.d, a.vec);
-        eb.load(a.e, e1, k, a.d, a.vec);
+        for (int k = k0 + 8 * q; k < k1; k += 32) {
+          R wa, wb, ea, eb;
+          wa.load(a.w, w0, k, a.d, a.vec);
+          wb.load(a.w, w1, k, a.d, a.vec);
+          ea.load(a.e, e0, k, a.d, a.vec);
+          eb.load(a.e, e1, k, a.d, a.vec);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          R x;
-          x.load(a.x, (i * a.T + min(t0 + 8 * j + g, a.T - 1)) * a.ldx, k, a.d, a.vec);
-          cross_step(sz[j], wa, wb, x);
-          cross_step(sk[j], ea, eb, x);
+          for (int j = 0; j < NT; ++j) {
+            R x;
+            x.load(a.x, (i * a.T + min(t0 + 8 * j + g, a.T - 1)) * a.ldx, k, a.d, a.vec);
+            cross_step(sz[j], wa, wb, x);
+            cross_step(sk[j], ea, eb, x);
+          }
         }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            cz[j][k] += sz[j][k];
+            ck[j][k] += sk[j][k];
+          }
       }
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          cz[j][k] += sz[j][k];
-          ck[j][k] += sk[j][k];
-        }
-    }
-    sum += cross_finish<NT>(a, i, id, t0, q, cz, ck);
+      sum += cross_finish<NT>(a, i, id, t0, q, cz, ck);
   }
   cross_store(a, i, sum, red);
+  }
 }
 
 // The same for bf16 rows of whole 128-byte lines (64 elements).  Shared memory: the tokens' rows [8 NT][d], and of every warp
@@ -219,7 +221,6 @@ __global__ void __launch_bounds__(256) k_vocab_cross_lines(const __grid_constant
   using R = CrossRow<__nv_bfloat16>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int lines = a.d / 64, row_bytes = a.d * 2;
-  const long long i = blockIdx.y;
   uint8_t* mine = smem + (size_t)8 * NT * row_bytes + (size_t)warp * (kCrossStages * kCrossStageBytes);
   const uint32_t smem32 = (uint32_t)__cvta_generic_to_shared(smem), mine32 = (uint32_t)__cvta_generic_to_shared(mine);
   const auto place = [](int row, int chunk) { return (uint32_t)((chunk ^ ((row & 1) << 2)) << 4); };
@@ -227,79 +228,81 @@ __global__ void __launch_bounds__(256) k_vocab_cross_lines(const __grid_constant
     const uint4 v = *reinterpret_cast<const uint4*>(rows + row * stride + line * 128 + place(row, chunk));
     r.r[0][0] = v.x, r.r[0][1] = v.y, r.r[0][2] = v.z, r.r[0][3] = v.w;
   };
-  float sum = 0.0f;
-  for (int task = blockIdx.x; task < a.all; task += a.chunks) {
-    const int u0 = (task / a.t_chunks) * 128 + warp * 16, t0 = (task % a.t_chunks) * (NT * 8);
-    const bool busy = u0 < a.Tu;
-    __syncthreads();                             // the tokens' rows of the task before have been read
-    for (int c = threadIdx.x; c < 8 * NT * lines * 8; c += 256) {
-      const int row = c / (lines * 8), chunk = c - row * (lines * 8);
-      copy16(smem32 + row * row_bytes + (chunk >> 3) * 128 + place(row, chunk & 7),
-             static_cast<const __nv_bfloat16*>(a.x) + (i * a.T + min(t0 + row, a.T - 1)) * a.ldx + chunk * 8);
-    }
-    const int2 id = busy ? cross_words(a, i, u0 + g) : make_int2(-1, -1);
-    // copies: 4 rows of a line a time, 8 lanes each; rows that do not count from a place that exists
-    const __nv_bfloat16 *from_w[4], *from_e[4];
-    uint32_t to[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int row = 4 * k + (lane >> 3);       // k < 2: rows 0 .. 7, whose words are id.x of lanes 4 row
-      const int word = __shfl_sync(0xffffffffu, k < 2 ? id.x : id.y, (row & 7) * 4);
-      from_w[k] = static_cast<const __nv_bfloat16*>(a.w) + (long long)max(word, 0) * a.ldw + (lane & 7) * 8;
-      from_e[k] = static_cast<const __nv_bfloat16*>(a.e) + (i * a.Tu + min(u0 + row, a.Tu - 1)) * a.lde + (lane & 7) * 8;
-      to[k] = mine32 + row * 128 + place(row, lane & 7);
-    }
-    const auto fetch = [&](int line) {
-      if (busy && line < lines) {
-        const uint32_t st = (line % kCrossStages) * kCrossStageBytes;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          copy16(to[k] + st, from_w[k] + line * 64);
-          copy16(to[k] + st + 2048, from_e[k] + line * 64);
-        }
+  for (long long i = blockIdx.y; i < a.B; i += gridDim.y) {
+    float sum = 0.0f;
+    for (int task = blockIdx.x; task < a.all; task += a.chunks) {
+      const int u0 = (task / a.t_chunks) * 128 + warp * 16, t0 = (task % a.t_chunks) * (NT * 8);
+      const bool busy = u0 < a.Tu;
+      __syncthreads();                             // the tokens' rows of the task before have been read
+      for (int c = threadIdx.x; c < 8 * NT * lines * 8; c += 256) {
+        const int row = c / (lines * 8), chunk = c - row * (lines * 8);
+        copy16(smem32 + row * row_bytes + (chunk >> 3) * 128 + place(row, chunk & 7),
+               static_cast<const __nv_bfloat16*>(a.x) + (i * a.T + min(t0 + row, a.T - 1)) * a.ldx + chunk * 8);
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
+      const int2 id = busy ? cross_words(a, i, u0 + g) : make_int2(-1, -1);
+      // copies: 4 rows of a line a time, 8 lanes each; rows that do not count from a place that exists
+      const __nv_bfloat16 *from_w[4], *from_e[4];
+      uint32_t to[4];
 #pragma unroll
-    for (int s = 0; s < kCrossStages - 1; ++s) fetch(s);
-    asm volatile("cp.async.wait_group %0;" ::"n"(kCrossStages - 2) : "memory");   // the tokens' rows came with the first line
-    __syncthreads();
-    if (!busy) continue;
-    float cz[NT][4] = {}, ck[NT][4] = {};
-    for (int l0 = 0; l0 < lines; l0 += kCrossSeg / 64) {
-      float sz[NT][4] = {}, sk[NT][4] = {};
-      for (int line = l0; line < lines && line < l0 + kCrossSeg / 64; ++line) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kCrossStages - 2) : "memory");
-        __syncwarp();
-        fetch(line + kCrossStages - 1);          // into the stage that was read last time round
-        const uint8_t* st = mine + (line % kCrossStages) * kCrossStageBytes;
+      for (int k = 0; k < 4; ++k) {
+        const int row = 4 * k + (lane >> 3);       // k < 2: rows 0 .. 7, whose words are id.x of lanes 4 row
+        const int word = __shfl_sync(0xffffffffu, k < 2 ? id.x : id.y, (row & 7) * 4);
+        from_w[k] = static_cast<const __nv_bfloat16*>(a.w) + (long long)max(word, 0) * a.ldw + (lane & 7) * 8;
+        from_e[k] = static_cast<const __nv_bfloat16*>(a.e) + (i * a.Tu + min(u0 + row, a.Tu - 1)) * a.lde + (lane & 7) * 8;
+        to[k] = mine32 + row * 128 + place(row, lane & 7);
+      }
+      const auto fetch = [&](int line) {
+        if (busy && line < lines) {
+          const uint32_t st = (line % kCrossStages) * kCrossStageBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          R wa, wb, ea, eb;
-          chunk_of(st, 128, g, 0, 4 * h + q, wa);
-          chunk_of(st, 128, g + 8, 0, 4 * h + q, wb);
-          chunk_of(st + 2048, 128, g, 0, 4 * h + q, ea);
-          chunk_of(st + 2048, 128, g + 8, 0, 4 * h + q, eb);
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            R x;
-            chunk_of(smem, row_bytes, 8 * j + g, line, 4 * h + q, x);
-            cross_step(sz[j], wa, wb, x);
-            cross_step(sk[j], ea, eb, x);
+          for (int k = 0; k < 4; ++k) {
+            copy16(to[k] + st, from_w[k] + line * 64);
+            copy16(to[k] + st + 2048, from_e[k] + line * 64);
           }
         }
-      }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+      for (int s = 0; s < kCrossStages - 1; ++s) fetch(s);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kCrossStages - 2) : "memory");   // the tokens' rows came with the first line
+      __syncthreads();
+      if (!busy) continue;
+      float cz[NT][4] = {}, ck[NT][4] = {};
+      for (int l0 = 0; l0 < lines; l0 += kCrossSeg / 64) {
+        float sz[NT][4] = {}, sk[NT][4] = {};
+        for (int line = l0; line < lines && line < l0 + kCrossSeg / 64; ++line) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kCrossStages - 2) : "memory");
+          __syncwarp();
+          fetch(line + kCrossStages - 1);          // into the stage that was read last time round
+          const uint8_t* st = mine + (line % kCrossStages) * kCrossStageBytes;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          cz[j][k] += sz[j][k];
-          ck[j][k] += sk[j][k];
+          for (int h = 0; h < 2; ++h) {
+            R wa, wb, ea, eb;
+            chunk_of(st, 128, g, 0, 4 * h + q, wa);
+            chunk_of(st, 128, g + 8, 0, 4 * h + q, wb);
+            chunk_of(st + 2048, 128, g, 0, 4 * h + q, ea);
+            chunk_of(st + 2048, 128, g + 8, 0, 4 * h + q, eb);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              R x;
+              chunk_of(smem, row_bytes, 8 * j + g, line, 4 * h + q, x);
+              cross_step(sz[j], wa, wb, x);
+              cross_step(sk[j], ea, eb, x);
+            }
+          }
         }
-    }
-    sum += cross_finish<NT>(a, i, id, t0, q, cz, ck);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            cz[j][k] += sz[j][k];
+            ck[j][k] += sk[j][k];
+          }
+      }
+      sum += cross_finish<NT>(a, i, id, t0, q, cz, ck);
   }
   cross_store(a, i, sum, red);
+  }
 }
 
 // sqnorm[i] += the partial sums of example i, in order.
@@ -320,8 +323,8 @@ static int cross_chunks(int B, long long all) {
 }
 
 template <typename T>
-static cudaError_t launch_cross(const CrossArgs& a, int B, int nt, cudaStream_t s) {
-  const dim3 grid((unsigned)a.chunks, (unsigned)B);
+static cudaError_t launch_cross(const CrossArgs& a, int nt, cudaStream_t s) {
+  const dim3 grid((unsigned)a.chunks, (unsigned)std::min(a.B, 65535));
   return nt == 1 ? launch_chained(k_vocab_cross<T, 1>, grid, 256, 0, s, a)
        : nt == 3 ? launch_chained(k_vocab_cross<T, 3>, grid, 256, 0, s, a)
                  : launch_chained(k_vocab_cross<T, 4>, grid, 256, 0, s, a);
@@ -329,7 +332,7 @@ static cudaError_t launch_cross(const CrossArgs& a, int B, int nt, cudaStream_t 
 
 constexpr int kCrossLinesMost = 225 * 1024;      // shared memory of a block of k_vocab_cross_lines, at most
 static size_t lines_smem(int nt, int d) { return (size_t)8 * nt * d * 2 + 8 * kCrossStages * kCrossStageBytes; }
-static cudaError_t launch_lines(const CrossArgs& a, int B, int nt, cudaStream_t s) {
+static cudaError_t launch_lines(const CrossArgs& a, int nt, cudaStream_t s) {
   static signed char ready[kMaxDevices] = {};    // 0 unknown, 1 ready, -1 failed
   const int dev = current_device();
   if (dev < 0) return cudaErrorInvalidDevice;
@@ -340,7 +343,7 @@ static cudaError_t launch_lines(const CrossArgs& a, int B, int nt, cudaStream_t 
     ready[dev] = ok ? 1 : -1;
   }
   if (ready[dev] < 0) return cudaErrorInvalidValue;
-  const dim3 grid((unsigned)a.chunks, (unsigned)B);
+  const dim3 grid((unsigned)a.chunks, (unsigned)std::min(a.B, 65535));
   const size_t smem = lines_smem(nt, a.d);
   return nt == 1 ? launch_chained(k_vocab_cross_lines<1>, grid, 256, smem, s, a)
        : nt == 3 ? launch_chained(k_vocab_cross_lines<3>, grid, 256, smem, s, a)
@@ -351,10 +354,10 @@ int launch_vocab_cross(const dp_vocab_head& h, const float* lse, const int32_t* 
                        float* sqnorm, float* partial, int* status, cudaStream_t s) {
   const bool f32 = h.dtype == DP_F32;
   const int nt = h.T <= 8 ? 1 : h.T <= 24 ? 3 : 4;        // 8, 24 or 32 tokens a pass over the inputs' rows
-  CrossArgs a = {h.X, h.W, G_emb, h.bias, h.labels, h.weights, lse, ids, sqnorm, h.ldx, h.ldw, ld_emb, h.T, Tu, h.d, h.V};
+  CrossArgs a = {h.X, h.W, G_emb, h.bias, h.labels, h.weights, lse, ids, sqnorm, h.ldx, h.ldw, ld_emb, h.B, h.T, Tu, h.d, h.V};
   a.t_chunks = ceil_div(h.T, 8 * nt);
   const long long all = (long long)ceil_div(Tu, 128) * a.t_chunks;
-  if (h.B > 65535 || all > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
+  if (all > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
   a.all = (int)all;
   a.chunks = cross_chunks(h.B, all);
   if (a.chunks > 1) a.out = partial;
@@ -363,7 +366,7 @@ int launch_vocab_cross(const dp_vocab_head& h, const float* lse, const int32_t* 
   a.status = status;
   note_launch(1);
   const bool whole = !f32 && a.vec && h.d % 64 == 0 && lines_smem(nt, h.d) <= kCrossLinesMost;
-  const cudaError_t rc = f32 ? launch_cross<float>(a, h.B, nt, s) : whole ? launch_lines(a, h.B, nt, s) : launch_cross<__nv_bfloat16>(a, h.B, nt, s);
+  const cudaError_t rc = f32 ? launch_cross<float>(a, nt, s) : whole ? launch_lines(a, nt, s) : launch_cross<__nv_bfloat16>(a, nt, s);
   if (rc != cudaSuccess) return DP_ERR_CUDA;
   if (a.chunks > 1) {
     note_launch(1);

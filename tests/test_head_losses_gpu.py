@@ -325,6 +325,11 @@ def test_several_pieces_of_the_vocabulary():
     c.check_sum()
 
 
+@pytest.mark.parametrize("d", [64, 24])
+def test_cross_term_of_many_examples(d):
+    Case(70001, 1, d, 50, BF16, dead=0.2).check_cross(2)
+
+
 def test_parts_of_the_log_sum_exp_are_joined_in_pieces():
     B, T, d, V = 700, 100, 8, 70000
     g = torch.Generator(device=DEV).manual_seed(0)
