@@ -76,7 +76,8 @@ struct alignas(64) VParams {
   int kb;                        // K blocks of one product
   int seg;                       // K blocks that are summed before the epilogue takes over
   int tiles_m, tiles_n, nt;      // nt: columns of a tile, 256 or 128
-  int units;                     // CTA pairs that share the work
+  int units;                     // CTA pairs
+  int sharers;                   // DX, DW: the pairs that share what whole tiles leave over, at least one K block each
   int M, N;                      // rows and columns that exist
   int sub;                       // columns of one block of G (GRAD, DX, DW)
   int v0, V;                     // first vocabulary entry of the piece, entries in all
@@ -113,8 +114,8 @@ __device__ __forceinline__ VShare share_of(const VParams& P, int unit) {
   s.whole = whole_tiles(MODE, tiles, P.units);
   s.tile = unit;
   const long long line = (long long)(tiles - s.whole) * P.n_pairs * P.kb;
-  s.lo = s.pos = share_begin(line, P.units, unit);
-  s.hi = share_begin(line, P.units, unit + 1);
+  s.lo = s.pos = unit < P.sharers ? share_begin(line, P.sharers, unit) : line;
+  s.hi = unit < P.sharers ? share_begin(line, P.sharers, unit + 1) : line;
   return s;
 }
 template <int MODE>
@@ -603,8 +604,8 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
   let_successor_in();
   const int nkb = P.n_pairs * P.kb, tiles = P.tiles_m * P.tiles_n, whole = whole_tiles(MODE, tiles, P.units);
   const long long line = (long long)(tiles - whole) * nkb, begin = (long long)blockIdx.x * nkb;
-  // block x of the line is in the share of unit ((x + 1) * units - 1) / line: units u0 .. last have a part of the tile
-  const int u0 = (int)(((begin + 1) * P.units - 1) / line), last = (int)(((begin + nkb) * P.units - 1) / line);
+  // block x of the line is in the share of unit ((x + 1) * sharers - 1) / line: units u0 .. last have a part of the tile
+  const int u0 = (int)(((begin + 1) * P.sharers - 1) / line), last = (int)(((begin + nkb) * P.sharers - 1) / line);
   if (last == u0) return;                                         // one unit had it all, and has written it
   int m0, n0;
   tile_origin<MODE>(P, whole + (int)blockIdx.x, m0, n0);
@@ -617,7 +618,7 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
   for (int k = k0; k < k1; ++k) {                                 // the tile is the first of a unit's share but, perhaps, unit u0's
-    const float4 x = from[(2 * (u0 + k) + (k == 0 && begin > share_begin(line, P.units, u0) ? 1 : 0)) * slot_size];
+    const float4 x = from[(2 * (u0 + k) + (k == 0 && begin > share_begin(line, P.sharers, u0) ? 1 : 0)) * slot_size];
     v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
   }
   if constexpr (STRANDS > 1) {
@@ -1245,7 +1246,7 @@ static int logits_operands(const VRun& r, VParams& P, int v0, int rows) {
   return DP_OK;
 }
 
-// Units of a DX or DW launch: every pair, or fewer where a share would be shorter than four K blocks.
+// Pairs that share a line of K blocks: all, or fewer where a share would be shorter than four (one pair for fewer).
 static int share_units(long long line) {
   const long long most = sm_count() / 2;
   return (int)std::max<long long>(1, std::min<long long>(most, line / 4));
@@ -1257,11 +1258,12 @@ static int launch_product(const VRun& r, VParams& P) {
   if (tiles > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
   if (MODE == V_LSE || MODE == V_GRAD) P.units = (int)std::min<long long>(tiles, sm_count() / 2);
   else P.units = share_units(line);
+  const int shared = (int)tiles - whole_tiles(MODE, (int)tiles, P.units);
+  P.sharers = std::min(P.units, share_units((long long)shared * P.n_pairs * P.kb));
   VOCAB_CUDA(launch_chained(k_vocab_gemm<MODE>, Pairs{(unsigned)P.units}, V_THREADS, v_smem<MODE>(), r.s, P));
   if constexpr (MODE == V_DX || MODE == V_DW) {
-    const int shared = (int)tiles - whole_tiles(MODE, (int)tiles, P.units);
-    if (P.units > 1 && shared)
-      VOCAB_CUDA(P.units <= 8 * shared ? launch_chained(k_vocab_join<MODE, 1>, dim3((unsigned)shared, V_TILE / 4), 256, 0, r.s, P)
+    if (P.sharers > 1 && shared)
+      VOCAB_CUDA(P.sharers <= 8 * shared ? launch_chained(k_vocab_join<MODE, 1>, dim3((unsigned)shared, V_TILE / 4), 256, 0, r.s, P)
                                        : launch_chained(k_vocab_join<MODE, 4>, dim3((unsigned)shared, V_TILE), 256, 0, r.s, P));
   }
   return DP_OK;

@@ -17,7 +17,8 @@ F32, BF16 = torch.float32, torch.bfloat16
 
 
 def workspace(head):
-    return torch.empty(dp.dp_vocab_workspace_bytes(head), dtype=torch.uint8, device=DEV)
+    """All bytes 255: what is read before it is written shows as NaN."""
+    return torch.full((dp.dp_vocab_workspace_bytes(head),), 255, dtype=torch.uint8, device=DEV)
 
 
 class Case:
@@ -140,9 +141,10 @@ class Case:
 
 
 # one word, one token; words that do not fill a tile; rows that do not fill 16 bytes; 3 blocks of G; examples of 41 tokens (82 rows of
-# planes: one a CTA), 70 (140 rows: the layers' kernels), a long one (their tiles, and column sums for the bias); many tiles
+# planes: one a CTA), 70 (140 rows: the layers' kernels), a long one (their tiles, and column sums for the bias); many tiles;
+# one tile of two K blocks left over for eleven pairs
 SHAPES = [(1, 1, 8, 1), (1, 1, 64, 1000), (2, 3, 17, 5), (3, 20, 64, 257), (7, 20, 128, 511), (4, 5, 200, 7), (5, 41, 72, 4500),
-          (2, 70, 40, 300), (2, 700, 64, 300), (40, 20, 264, 2050), (3, 2, 1024, 777)]
+          (2, 70, 40, 300), (2, 700, 64, 300), (40, 20, 264, 2050), (3, 2, 1024, 777), (6, 20, 16, 5821)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
