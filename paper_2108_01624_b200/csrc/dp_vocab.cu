@@ -956,7 +956,7 @@ k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* c
 // lse and loss of a token from the parts over the column blocks, which leave the label out: a warp per token (eight
 // neighbours a block, whose parts share sectors), its label's logit in fp64.  With `carry`, more columns are to come: the
 // parts become one, kept there.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 5)
 k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, float2* carry, float* loss, float* lse, int* status) {
   wait_for_predecessor();
   let_successor_in();
@@ -967,6 +967,9 @@ k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, flo
     if (lane == 0 && !carry) loss[n] = lse[n] = 0.0f;
     return;
   }
+  float2 ahead[4];                              // the first 128 parts are on their way while the logit is formed
+#pragma unroll
+  for (int j = 0; j < 4; ++j) ahead[j] = lane + 32 * j < parts ? part[(size_t)(lane + 32 * j) * H.N + n] : make_float2(-INFINITY, 0.0f);
   double s = 0.0;
 #pragma unroll 4
   for (int c = 8 * lane; c < H.d && !carry; c += 256) {
@@ -977,9 +980,7 @@ k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, flo
     for (int j = 0; j < 8; ++j) s = fma((double)x[j], (double)w[j], s);
   }
   float most = -INFINITY, sum = 0.0f;
-#pragma unroll 4
-  for (int p = lane; p < parts; p += 32) {
-    const float2 v = part[(size_t)p * H.N + n];
+  const auto join = [&](float2 v) {
     const float top = fmaxf(most, v.x);
     if (top != -INFINITY) {
       sum = sum * ex2(most - top) + v.y * ex2(v.x - top);
@@ -987,7 +988,11 @@ k_vocab_loss(const __grid_constant__ VHead H, const float2* part, int parts, flo
     } else {
       sum += v.y;                               // 0, or NaN
     }
-  }
+  };
+#pragma unroll
+  for (int j = 0; j < 4; ++j) join(ahead[j]);
+#pragma unroll 4
+  for (int p = lane + 128; p < parts; p += 32) join(part[(size_t)p * H.N + n]);
   float top = most;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
