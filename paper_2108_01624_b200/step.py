@@ -183,9 +183,11 @@ class DPStep:
             self._sqnorm = torch.empty(B, dtype=torch.float32, device=self.device)
             self._clip = torch.empty(B, dtype=torch.float32, device=self.device)
 
-    def _head_workspace(self, head: b.VocabHead) -> torch.Tensor:
+    def _head_workspace(self, head: b.VocabHead, stream=None) -> torch.Tensor:
         need = b.dp_vocab_workspace_bytes(head)
         if self._head_ws is None or self._head_ws.numel() < need:
+            if self._head_ws is not None and stream is not None:
+                self._head_ws.record_stream(stream)      # calls on it may still be at work there
             self._head_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self._head_ws
 
@@ -202,7 +204,7 @@ class DPStep:
         if li in self._heads or any(h.B != head.B for h, _ in self._heads.values()):
             self._heads = {}
         self._batch(head.B)
-        b.dp_vocab_loss_backward(head, lse, dx, self._sqnorm, bool(self._heads), self._head_workspace(head), stream)
+        b.dp_vocab_loss_backward(head, lse, dx, self._sqnorm, bool(self._heads), self._head_workspace(head, stream), stream)
         self._heads[li] = (head, lse)
 
     def accumulate_microbatch(self, layers, stream=None, rows=None):
@@ -247,7 +249,7 @@ class DPStep:
                     emb = by_acc.get(self.view(self.acc, li, 0).data_ptr(), [])
                     if len(emb) != 1:
                         raise ValueError(f"the embedding that shares its table with head {li} is missing")
-                    b.dp_vocab_loss_cross_sqnorms(head, lse, emb[0].ids, emb[0].G, self._sqnorm, self._head_workspace(head), stream)
+                    b.dp_vocab_loss_cross_sqnorms(head, lse, emb[0].ids, emb[0].G, self._sqnorm, self._head_workspace(head, stream), stream)
         if rows is not None:
             b.dp_rows_sqnorms(rows, self._sqnorm, bool(lists) or bool(heads), stream)
         b.dp_clip_factors(self._sqnorm, self.C, self._clip, stream)
@@ -256,7 +258,7 @@ class DPStep:
         for li, (head, lse) in heads.items():
             b.dp_vocab_loss_clipped_accumulate(head, lse, self._clip, self.view(self.acc, li, 0),
                                                self.view(self.acc, li, 1) if head.bias is not None else None,
-                                               self._head_workspace(head), stream)
+                                               self._head_workspace(head, stream), stream)
         self._heads = {}
         if rows is not None:
             b.dp_rows_clipped_accumulate(rows, self._clip, stream)

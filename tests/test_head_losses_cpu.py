@@ -188,3 +188,24 @@ def test_a_microbatch_wants_every_head(monkeypatch):
     assert step.examples_seen == 0
     with pytest.raises(ValueError, match="every HEAD"):
         step.accumulate_microbatch([])
+
+
+def test_a_heads_outgrown_workspace_outlives_the_stream_that_uses_it(monkeypatch):
+    """Calls on a stream of the caller's may still be at work in a workspace when a larger microbatch replaces it."""
+    step = dp_step([LayerSpec(HEAD, 20, 8, False, "mlm")])
+    recorded = []
+
+    class Buffer:
+        def numel(self):
+            return 256
+
+        def record_stream(self, stream):
+            recorded.append(stream)
+
+    step._head_ws = Buffer()
+    monkeypatch.setattr(step_module.b, "dp_vocab_workspace_bytes", lambda head: 256)
+    step._head_workspace(None, "side")
+    assert recorded == []
+    monkeypatch.setattr(step_module.b, "dp_vocab_workspace_bytes", lambda head: 512)
+    assert step._head_workspace(None, "side").numel() == 512
+    assert recorded == ["side"]
