@@ -332,6 +332,39 @@ def test_cross_term_of_many_examples(d):
     Case(70001, 1, d, 50, BF16, dead=0.2).check_cross(2)
 
 
+# the widest rows and rows of one element; many short examples, one long; few words and very many; one example a microbatch
+EXTREMES = [(2, 3, 65536, 40), (2, 70, 65536, 5), (3, 5, 1, 300), (70000, 1, 8, 9), (9000, 3, 24, 33), (1, 5000, 16, 40), (2, 3, 8, 200003),
+            (1, 257, 72, 2049)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", EXTREMES)
+def test_the_largest_and_the_smallest_sizes(shape, dtype):
+    c = Case(*shape, dtype)
+    c.check_loss()
+    c.check_backward()
+    c.check_sum()
+    c.check_cross(5)
+    assert dp.dp_poll_status() == 0
+
+
+def test_a_gradient_without_norms_and_norms_without_a_gradient():
+    c = Case(5, 20, 200, 3000, BF16)
+    head = c.head()
+    dx, sq = c.check_backward()
+    one, two = torch.full_like(dx, float("nan")), torch.full_like(sq, float("nan"))
+    dp.dp_vocab_loss_backward(head, c.lse, one, None, workspace=workspace(head))
+    dp.dp_vocab_loss_backward(head, c.lse, None, two, workspace=workspace(head))
+    assert torch.equal(one, dx) and torch.equal(two, sq)
+
+
+def test_rows_around_a_strided_gradient_stay_as_they_were():
+    c = Case(3, 7, 40, 300, BF16)
+    whole = torch.full((3, 7, 64), 5.0, dtype=BF16, device=DEV)
+    c.check_backward(out=whole[..., 8:48])
+    assert bool((whole[..., :8] == 5.0).all()) and bool((whole[..., 48:] == 5.0).all())
+
+
 def test_parts_of_the_log_sum_exp_are_joined_in_pieces():
     B, T, d, V = 700, 100, 8, 70000
     g = torch.Generator(device=DEV).manual_seed(0)
