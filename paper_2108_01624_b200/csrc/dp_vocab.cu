@@ -639,13 +639,15 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
 // Squared norms of short examples (at most 128 rows of planes): |G_i^T X_i|^2 = sum over rows r, s of the example of
 // (<x_r, x_s> + bias) <g_r, g_s>.  A CTA takes as many whole examples as 128 rows hold and some blocks of G; both Grams are
 // 128 x 128 x 16 UMMAs of a tile with itself, of which the epilogue uses each row's own example.  The Gram of G is taken
-// over by the epilogue every kNormSeg columns and added in registers: its squares are one large (the label's) and a
-// vocabulary of small ones, which a longer sum on the tensor core would lose.  Bound by reading G: 110 us for 625 MB, where the
-// layers' kernel with one example at a time took 318.
+// over by the epilogue every kNormSeg stages and added in registers: its squares are one large (the label's) and a
+// vocabulary of small ones, which a longer sum on the tensor core would lose.  What it drops makes norms too small: at 256 x 20
+// tokens and 30522 words squares are off by -3.5e-6 in the mean with 8 stages, -2.7e-6 with 4, -2.4e-6 with 2, -2.2e-6 with 1 (in fp32
+// throughout 2e-7), and the norms take 473, 476, 479 and 497 us of back to back calls with GRAD; dX hides the first step.
+// Bound by reading G: 110 us for 625 MB, where the layers' kernel with one example at a time took 318.
 // =================================================================================================
 constexpr int N_STAGES = 6, N_STAGE_BYTES = 2 * V_BOX_BYTES;    // 128 rows x 128 columns
 constexpr int N_THREADS = 192;                                  // warp 0 TMA, warp 1 UMMA, warps 2..5 epilogue
-constexpr int kNormSeg = 8;                                     // stages
+constexpr int kNormSeg = 4;                                     // stages of 128 columns
 struct NCtl {
   uint64_t full[N_STAGES], empty[N_STAGES], tmem_full[3], tmem_empty[2], drain;
   uint32_t tmem_base;
