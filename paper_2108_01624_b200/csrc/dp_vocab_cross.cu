@@ -31,7 +31,8 @@ struct CrossArgs {
   const int32_t* ids;
   float* out;                    // sqnorm, or partial sums [B][chunks]
   long long ldx, ldw, lde;
-  int B, T, Tu, d, V, chunks, t_chunks, all;   // all: (128-input x 8 NT-token) tasks of an example, shared by `chunks` blocks
+  int B, T, Tu, d, V;
+  unsigned chunks, t_chunks, all;   // all: (128-input x 8 NT-token) tasks of an example, shared by `chunks` blocks
   int vec;
   int* status;
 };
@@ -163,8 +164,8 @@ __global__ void __launch_bounds__(256) k_vocab_cross(const __grid_constant__ Cro
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   for (long long i = blockIdx.y; i < a.B; i += gridDim.y) {
     float sum = 0.0f;
-    for (int task = blockIdx.x; task < a.all; task += a.chunks) {
-      const int u0 = (task / a.t_chunks) * 128 + warp * 16, t0 = (task % a.t_chunks) * (NT * 8);
+    for (unsigned task = blockIdx.x; task < a.all; task += a.chunks) {
+      const int u0 = (int)(task / a.t_chunks) * 128 + warp * 16, t0 = (int)(task % a.t_chunks) * (NT * 8);
       if (u0 >= a.Tu) continue;
       const int2 id = cross_words(a, i, u0 + g);
       // rows that do not count are read from a place that exists; their columns or rows of the products are left out below
@@ -230,8 +231,8 @@ __global__ void __launch_bounds__(256) k_vocab_cross_lines(const __grid_constant
   };
   for (long long i = blockIdx.y; i < a.B; i += gridDim.y) {
     float sum = 0.0f;
-    for (int task = blockIdx.x; task < a.all; task += a.chunks) {
-      const int u0 = (task / a.t_chunks) * 128 + warp * 16, t0 = (task % a.t_chunks) * (NT * 8);
+    for (unsigned task = blockIdx.x; task < a.all; task += a.chunks) {
+      const int u0 = (int)(task / a.t_chunks) * 128 + warp * 16, t0 = (int)(task % a.t_chunks) * (NT * 8);
       const bool busy = u0 < a.Tu;
       __syncthreads();                             // the tokens' rows of the task before have been read
       for (int c = threadIdx.x; c < 8 * NT * lines * 8; c += 256) {
@@ -324,7 +325,7 @@ static int cross_chunks(int B, long long all) {
 
 template <typename T>
 static cudaError_t launch_cross(const CrossArgs& a, int nt, cudaStream_t s) {
-  const dim3 grid((unsigned)a.chunks, (unsigned)std::min(a.B, 65535));
+  const dim3 grid(a.chunks, (unsigned)std::min(a.B, 65535));
   return nt == 1 ? launch_chained(k_vocab_cross<T, 1>, grid, 256, 0, s, a)
        : nt == 3 ? launch_chained(k_vocab_cross<T, 3>, grid, 256, 0, s, a)
                  : launch_chained(k_vocab_cross<T, 4>, grid, 256, 0, s, a);
@@ -343,7 +344,7 @@ static cudaError_t launch_lines(const CrossArgs& a, int nt, cudaStream_t s) {
     ready[dev] = ok ? 1 : -1;
   }
   if (ready[dev] < 0) return cudaErrorInvalidValue;
-  const dim3 grid((unsigned)a.chunks, (unsigned)std::min(a.B, 65535));
+  const dim3 grid(a.chunks, (unsigned)std::min(a.B, 65535));
   const size_t smem = lines_smem(nt, a.d);
   return nt == 1 ? launch_chained(k_vocab_cross_lines<1>, grid, 256, smem, s, a)
        : nt == 3 ? launch_chained(k_vocab_cross_lines<3>, grid, 256, smem, s, a)
@@ -355,11 +356,11 @@ int launch_vocab_cross(const dp_vocab_head& h, const float* lse, const int32_t* 
   const bool f32 = h.dtype == DP_F32;
   const int nt = h.T <= 8 ? 1 : h.T <= 24 ? 3 : 4;        // 8, 24 or 32 tokens a pass over the inputs' rows
   CrossArgs a = {h.X, h.W, G_emb, h.bias, h.labels, h.weights, lse, ids, sqnorm, h.ldx, h.ldw, ld_emb, h.B, h.T, Tu, h.d, h.V};
-  a.t_chunks = ceil_div(h.T, 8 * nt);
+  a.t_chunks = (unsigned)ceil_div(h.T, 8 * nt);
   const long long all = (long long)ceil_div(Tu, 128) * a.t_chunks;
   if (all > 0x7fffffffll) return DP_ERR_UNSUPPORTED;
-  a.all = (int)all;
-  a.chunks = cross_chunks(h.B, all);
+  a.all = (unsigned)all;
+  a.chunks = (unsigned)cross_chunks(h.B, all);
   if (a.chunks > 1) a.out = partial;
   const int e = f32 ? 4 : 8;
   a.vec = !misaligned(h.X, 16) && !misaligned(h.W, 16) && !misaligned(G_emb, 16) && h.ldx % e == 0 && h.ldw % e == 0 && ld_emb % e == 0;

@@ -23,3 +23,12 @@ def test_strides_over_a_grid_fit_their_counters():
     for m in loops:
         step = int(m[3]) if m[3].isdigit() else 1
         assert MOST_WORDS + MOST_TOKENS + blocks * step <= LIMIT[m[1]], m[0]
+
+
+def test_the_cross_terms_tasks_fit_their_counter():
+    """Up to 2^31 - 1 tasks of an example (more are refused), in steps of up to 64 blocks: the last step ends behind them."""
+    text = source("dp_vocab_cross.cu")
+    loops = re.findall(r"for \(([\w ]+) task = blockIdx\.x; task < a\.all; task \+= a\.chunks\)", text)
+    assert len(loops) == 2 and "all > 0x7fffffffll" in text
+    limit = {"unsigned": 2 ** 32 - 1, **LIMIT}
+    assert all(2 ** 31 - 1 + 64 <= limit[t] for t in loops)
