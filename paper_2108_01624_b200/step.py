@@ -201,17 +201,20 @@ class DPStep:
             raise ValueError(f"spec {li} is no HEAD")
         if tuple(head.weight.shape) != (sp.d_in, sp.d_out) or (head.bias is not None) != sp.has_bias:
             raise ValueError(f"spec {li}: a head [{sp.d_in}, {sp.d_out}] {'with' if sp.has_bias else 'without'} bias expected")
-        if li in self._heads or any(h.B != head.B for h, _ in self._heads.values()):
-            self._heads = {}
+        begun, self._heads = self._heads, {}          # norms that a call fails to add to are not added to again
+        if li in begun or any(h.B != head.B for h, _ in begun.values()):
+            begun = {}
         self._batch(head.B)
-        b.dp_vocab_loss_backward(head, lse, dx, self._sqnorm, bool(self._heads), self._head_workspace(head, stream), stream)
-        self._heads[li] = (head, lse)
+        b.dp_vocab_loss_backward(head, lse, dx, self._sqnorm, bool(begun), self._head_workspace(head, stream), stream)
+        self._heads = {**begun, li: (head, lse)}
 
     def accumulate_microbatch(self, layers, stream=None, rows=None):
         """norms -> clip factors -> clipped accumulate for one microbatch (all enqueued, no sync).
         `layers` is a LayerList, or a list of them (layer_lists) when token counts differ between layers; `rows` is the
         row_list of the microbatch, needed exactly when there are ROWS specs (an example's norm runs over ALL its
-        tensors: one left out would break the bound that the noise is calibrated to)."""
+        tensors: one left out would break the bound that the noise is calibrated to).
+        What does not fit together is refused before the first norm, and can be passed again corrected; a call that fails later
+        leaves norms half summed, and the microbatch begins anew with the HEAD specs' head_backward."""
         lists = [layers] if isinstance(layers, b.LayerList) else list(layers)
         lists = [ll for ll in lists if len(ll)]
         heads = dict(sorted(self._heads.items()))
@@ -227,6 +230,22 @@ class DPStep:
             raise ValueError(f"heads of other numbers of examples than {B}")
         if rows is not None and rows.B != B:
             raise ValueError(f"rows of {rows.B} examples, layers of {B}")
+        if any(ll.B != B for ll in lists):
+            raise ValueError(f"layers of other numbers of examples than {B}")
+        by_acc = {}                                   # layers by the accumulator of their weight
+        for ll in lists if self.shared_tables else ():
+            for L in ll.layers:
+                by_acc.setdefault(L.acc_w.data_ptr(), []).append(L)
+        tables = {}                                   # the embedding that shares its table with a head
+        for li, (head, _) in heads.items():
+            if li in self.shared_tables:
+                emb = by_acc.get(self.view(self.acc, li, 0).data_ptr(), [])
+                if len(emb) != 1 or emb[0].kind != EMBEDDING:
+                    raise ValueError(f"the embedding that shares its table with head {li} is missing")
+                if emb[0].G.dtype != head.x.dtype or emb[0].G.shape[2] != head.x.shape[2]:
+                    raise ValueError(f"the embedding's G and the states of head {li} that shares its table differ in dtype or width")
+                tables[li] = emb[0]
+        self._heads = {}                              # what follows adds to their norms: after a failure they are wanted anew
         self._batch(B)
         if self._ws is None or len(self._ws) != len(lists):
             self._ws = [None] * len(lists)
@@ -235,21 +254,13 @@ class DPStep:
             if self._ws[k] is None or self._ws[k].numel() < need:
                 self._ws[k] = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             b.dp_per_example_sqnorms(ll, self._sqnorm, k > 0 or bool(heads), self._ws[k], stream)
-        if self.shared_tables:
-            by_acc = {}
-            for ll in lists:
-                for L in ll.layers:
-                    by_acc.setdefault(L.acc_w.data_ptr(), []).append(L)
-            for pair in by_acc.values():          # an embedding and the projection that shares its accumulator
-                if len(pair) == 2:
-                    emb, proj = (pair[0], pair[1]) if pair[0].kind == EMBEDDING else (pair[1], pair[0])
-                    b.dp_shared_table_cross_sqnorms(emb, proj, self._sqnorm, stream)
-            for li, (head, lse) in heads.items():
-                if li in self.shared_tables:
-                    emb = by_acc.get(self.view(self.acc, li, 0).data_ptr(), [])
-                    if len(emb) != 1:
-                        raise ValueError(f"the embedding that shares its table with head {li} is missing")
-                    b.dp_vocab_loss_cross_sqnorms(head, lse, emb[0].ids, emb[0].G, self._sqnorm, self._head_workspace(head, stream), stream)
+        for pair in by_acc.values():                  # an embedding and the projection that shares its accumulator
+            if len(pair) == 2:
+                emb, proj = (pair[0], pair[1]) if pair[0].kind == EMBEDDING else (pair[1], pair[0])
+                b.dp_shared_table_cross_sqnorms(emb, proj, self._sqnorm, stream)
+        for li, emb in tables.items():
+            head, lse = heads[li]
+            b.dp_vocab_loss_cross_sqnorms(head, lse, emb.ids, emb.G, self._sqnorm, self._head_workspace(head, stream), stream)
         if rows is not None:
             b.dp_rows_sqnorms(rows, self._sqnorm, bool(lists) or bool(heads), stream)
         b.dp_clip_factors(self._sqnorm, self.C, self._clip, stream)
@@ -259,7 +270,6 @@ class DPStep:
             b.dp_vocab_loss_clipped_accumulate(head, lse, self._clip, self.view(self.acc, li, 0),
                                                self.view(self.acc, li, 1) if head.bias is not None else None,
                                                self._head_workspace(head, stream), stream)
-        self._heads = {}
         if rows is not None:
             b.dp_rows_clipped_accumulate(rows, self._clip, stream)
         self.examples_seen += B

@@ -1,0 +1,107 @@
+"""DPStep with a vocabulary head, without a GPU: a microbatch that is refused or fails leaves no norms behind that a later one
+would add to.  The library's calls are stand-ins that do their sums on the host."""
+import pytest
+import torch
+
+from paper_2108_01624_b200 import step as step_module
+from paper_2108_01624_b200.binding import Layer
+from paper_2108_01624_b200.synth import EMBEDDING, HEAD, LINEAR, LayerSpec
+
+SPECS = [LayerSpec(EMBEDDING, 50, 8, False, "emb"), LayerSpec(LINEAR, 8, 6, False, "fc"), LayerSpec(HEAD, 50, 8, False, "mlm")]
+
+
+class Head:
+    def __init__(self, B=4, V=50, d=8):
+        self.B, self.weight, self.bias, self.x = B, torch.zeros(V, d), None, torch.zeros(B, 3, d)
+
+
+class Layers:
+    def __init__(self, layers, B=4):
+        self.layers, self.B = layers, B
+
+    def __len__(self):
+        return len(self.layers)
+
+
+class Calls:
+    """Layers' norms of 10 an example, a head's of 1, a cross term of -2; clip factors keep what they were given."""
+
+    def __init__(self, monkeypatch):
+        self.names, self.fails, self.seen = [], None, None
+        for name in ("dp_workspace_bytes", "dp_vocab_workspace_bytes"):
+            monkeypatch.setattr(step_module.b, name, lambda x: 256)
+        monkeypatch.setattr(step_module.b, "LayerList", Layers)
+        norms = lambda value: lambda a, sq, add, *rest: sq.copy_(sq * bool(add) + value)
+        self.put(monkeypatch, "dp_per_example_sqnorms", norms(10.0))
+        self.put(monkeypatch, "dp_vocab_loss_backward", lambda h, lse, dx, sq, add, *rest: sq.copy_(sq * bool(add) + 1.0))
+        self.put(monkeypatch, "dp_vocab_loss_cross_sqnorms", lambda h, lse, ids, g, sq, *rest: sq.sub_(2.0))
+        self.put(monkeypatch, "dp_clip_factors", lambda sq, *rest: setattr(self, "seen", sq.clone()))
+        for name in ("dp_clipped_accumulate_after_sqnorms", "dp_vocab_loss_clipped_accumulate"):
+            self.put(monkeypatch, name, lambda *a: None)
+
+    def put(self, monkeypatch, name, act):
+        def call(*a):
+            self.names.append(name)
+            act(*a)
+            if name == self.fails:
+                raise RuntimeError(name)
+        monkeypatch.setattr(step_module.b, name, call)
+
+
+def make(monkeypatch):
+    calls = Calls(monkeypatch)
+    step = step_module.DPStep(SPECS, "cpu", C=1.0, sigma=1.0, lr=1e-3, beta1=0.9, beta2=0.999, xi=1e-11, weight_decay=0.0, shared_tables={2: 0})
+    emb = Layer(kind=EMBEDDING, G=torch.zeros(4, 5, 8), ids=torch.zeros(4, 5, dtype=torch.int32), acc_w=step.view(step.acc, 0, 0))
+    fc = Layer(kind=LINEAR, G=torch.zeros(4, 5, 6), A=torch.zeros(4, 5, 8), acc_w=step.view(step.acc, 1, 0))
+    return step, calls, emb, fc
+
+
+def begun_anew(step, calls, layers, norm=9.0):
+    """The microbatch, whole: head 1, layers 10, cross term -2."""
+    step.head_backward(2, Head(), None, None)
+    step.accumulate_microbatch(layers)
+    return torch.equal(calls.seen, torch.full((4,), norm))
+
+
+def test_what_is_refused_is_refused_before_the_first_norm(monkeypatch):
+    step, calls, emb, fc = make(monkeypatch)
+    step.head_backward(2, Head(), None, None)
+    calls.names.clear()
+    other = Layer(kind=EMBEDDING, G=emb.G.bfloat16(), ids=emb.ids, acc_w=emb.acc_w)
+    wide = Layer(kind=EMBEDDING, G=torch.zeros(4, 5, 16), ids=emb.ids, acc_w=emb.acc_w)
+    for bad in (Layers([fc]), Layers([other, fc]), Layers([wide, fc]), Layers([emb, emb, fc]), [Layers([emb]), Layers([fc], B=5)]):
+        with pytest.raises(ValueError):
+            step.accumulate_microbatch(bad)
+    assert calls.names == [] and step.examples_seen == 0
+    step.accumulate_microbatch(Layers([emb, fc]))              # corrected, the head's norms still there
+    assert torch.equal(calls.seen, torch.full((4,), 9.0)) and step.examples_seen == 4
+
+
+@pytest.mark.parametrize("name", ["dp_per_example_sqnorms", "dp_vocab_loss_cross_sqnorms", "dp_clip_factors", "dp_vocab_loss_clipped_accumulate"])
+def test_a_microbatch_that_fails_midway_wants_its_heads_again(monkeypatch, name):
+    step, calls, emb, fc = make(monkeypatch)
+    step.head_backward(2, Head(), None, None)
+    calls.fails = name
+    with pytest.raises(RuntimeError, match=name):
+        step.accumulate_microbatch(Layers([emb, fc]))
+    calls.fails = None
+    with pytest.raises(ValueError, match="every HEAD"):
+        step.accumulate_microbatch(Layers([emb, fc]))
+    assert begun_anew(step, calls, Layers([emb, fc]))
+
+
+def test_a_heads_backward_that_fails_drops_the_heads_before_it(monkeypatch):
+    specs = [LayerSpec(HEAD, 50, 8, False, "a"), LayerSpec(HEAD, 50, 8, False, "b")]
+    calls = Calls(monkeypatch)
+    step = step_module.DPStep(specs, "cpu", C=1.0, sigma=1.0, lr=1e-3, beta1=0.9, beta2=0.999, xi=1e-11, weight_decay=0.0)
+    step.head_backward(0, Head(), None, None)
+    calls.fails = "dp_vocab_loss_backward"                     # after it has added to the norms
+    with pytest.raises(RuntimeError):
+        step.head_backward(1, Head(), None, None)
+    calls.fails = None
+    step.head_backward(1, Head(), None, None)
+    with pytest.raises(ValueError, match="every HEAD"):
+        step.accumulate_microbatch([])
+    step.head_backward(0, Head(), None, None)
+    step.accumulate_microbatch([])
+    assert torch.equal(calls.seen, torch.full((4,), 2.0))
