@@ -181,8 +181,11 @@ class ShardedUpdate:
         code = self._agreed_status()
         if code != 0:
             s = self.state
-            s.acc.zero_()
-            s.examples_seen = 0
+            if hasattr(s, "discard_macro_batch"):
+                s.discard_macro_batch()
+            else:
+                s.acc.zero_()
+                s.examples_seen = 0
             raise DeviceStatusError(code)
 
     def _mark(self, k: int):

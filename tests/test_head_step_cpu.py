@@ -5,6 +5,7 @@ import torch
 
 from paper_2108_01624_b200 import step as step_module
 from paper_2108_01624_b200.binding import Layer
+from paper_2108_01624_b200.parallel import ShardedUpdate
 from paper_2108_01624_b200.synth import EMBEDDING, HEAD, LINEAR, LayerSpec
 
 SPECS = [LayerSpec(EMBEDDING, 50, 8, False, "emb"), LayerSpec(LINEAR, 8, 6, False, "fc"), LayerSpec(HEAD, 50, 8, False, "mlm")]
@@ -105,3 +106,25 @@ def test_a_heads_backward_that_fails_drops_the_heads_before_it(monkeypatch):
     step.head_backward(0, Head(), None, None)
     step.accumulate_microbatch([])
     assert torch.equal(calls.seen, torch.full((4,), 2.0))
+
+
+def test_a_macro_batch_that_the_ranks_discard_takes_its_heads_along(monkeypatch):
+    """The status that made them discard it may be that of a head's norms."""
+    class Dist:
+        ReduceOp = torch.distributed.ReduceOp
+
+        def get_backend(self):
+            return "gloo"
+
+        def all_reduce(self, t, op=None):
+            return None
+    step, calls, emb, fc = make(monkeypatch)
+    step.acc.fill_(1.0)
+    update = ShardedUpdate(step, Dist(), 1, 0, poll_fn=lambda: -5)
+    step.head_backward(2, Head(), None, None)
+    step.examples_seen = 4
+    with pytest.raises(step_module.DeviceStatusError):
+        update.finish_macro_batch()
+    assert step.examples_seen == 0 and not step.acc.any()
+    with pytest.raises(ValueError, match="every HEAD"):
+        step.accumulate_microbatch(Layers([emb, fc]))
