@@ -6,6 +6,7 @@ the macro-batch size and the AdamW update run once per macro-batch (Section 5.3)
 """
 from __future__ import annotations
 
+import contextlib
 import math
 from typing import List, Optional, Sequence
 
@@ -121,6 +122,7 @@ class DPStep:
         self._clip = None
         self._heads: dict = {}          # heads of the microbatch under way: spec index -> (head, lse)
         self._head_ws = None
+        self._streams: dict = {}        # buffers -> the streams whose calls have used them
 
     def view(self, flat: torch.Tensor, li: int, k: int) -> torch.Tensor:
         shp = self.shapes[li][k]
@@ -177,18 +179,53 @@ class DPStep:
             groups.setdefault(int(L.G.shape[1]), []).append(L)
         return [b.LayerList(ls) for ls in groups.values()]
 
-    def _batch(self, B: int) -> None:
+    # Buffers of the calls.  Each is allocated for the stream of the calls that use it (the one they are given, or else the current
+    # one), and one that is replaced is kept from the allocator until every stream that used it is past it.
+    def _on(self, stream):
+        return torch.cuda.stream(stream) if stream is not None and self.device.type == "cuda" else contextlib.nullcontext()
+
+    def _used(self, what, stream) -> None:
+        """A call on `stream` is about to use the buffers `what`."""
+        if stream is None and self.device.type == "cuda":
+            stream = torch.cuda.current_stream(self.device)
+        if stream is not None:
+            self._streams.setdefault(what, set()).add(stream)
+
+    def _replaced(self, what, *buffers) -> None:
+        for stream in self._streams.pop(what, ()):
+            for t in buffers:
+                t.record_stream(stream)
+
+    def _batch(self, B: int, stream=None) -> None:
         """Norms and factors of a microbatch of B examples."""
         if self._sqnorm is None or self._sqnorm.numel() != B:
-            self._sqnorm = torch.empty(B, dtype=torch.float32, device=self.device)
-            self._clip = torch.empty(B, dtype=torch.float32, device=self.device)
+            if self._sqnorm is not None:
+                self._replaced("batch", self._sqnorm, self._clip)
+            with self._on(stream):
+                self._sqnorm, self._clip = (torch.empty(B, dtype=torch.float32, device=self.device) for _ in range(2))
+        self._used("batch", stream)
+
+    def _at_least(self, old: Optional[torch.Tensor], need: int, what, stream) -> torch.Tensor:
+        """A workspace of `need` bytes or more: the old one, or another in its place."""
+        if old is None or old.numel() < need:
+            if old is not None:
+                self._replaced(what, old)
+            with self._on(stream):
+                old = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self._used(what, stream)
+        return old
+
+    def _workspaces(self, lists, stream=None) -> None:
+        """A workspace for each of the microbatch's lists of layers."""
+        if self._ws is None or len(self._ws) != len(lists):
+            for k, ws in enumerate(self._ws or ()):
+                self._replaced(k, ws)
+            self._ws = [None] * len(lists)
+        for k, ll in enumerate(lists):
+            self._ws[k] = self._at_least(self._ws[k], max(b.dp_workspace_bytes(ll), 256), k, stream)
 
     def _head_workspace(self, head: b.VocabHead, stream=None) -> torch.Tensor:
-        need = b.dp_vocab_workspace_bytes(head)
-        if self._head_ws is None or self._head_ws.numel() < need:
-            if self._head_ws is not None and stream is not None:
-                self._head_ws.record_stream(stream)      # calls on it may still be at work there
-            self._head_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self._head_ws = self._at_least(self._head_ws, b.dp_vocab_workspace_bytes(head), "head", stream)
         return self._head_ws
 
     def head_backward(self, li: int, head: b.VocabHead, lse: torch.Tensor, dx: Optional[torch.Tensor], stream=None) -> None:
@@ -204,7 +241,7 @@ class DPStep:
         begun, self._heads = self._heads, {}          # norms that a call fails to add to are not added to again
         if li in begun or any(h.B != head.B for h, _ in begun.values()):
             begun = {}
-        self._batch(head.B)
+        self._batch(head.B, stream)
         b.dp_vocab_loss_backward(head, lse, dx, self._sqnorm, bool(begun), self._head_workspace(head, stream), stream)
         self._heads = {**begun, li: (head, lse)}
 
@@ -246,13 +283,9 @@ class DPStep:
                     raise ValueError(f"the embedding's G and the states of head {li} that shares its table differ in dtype or width")
                 tables[li] = emb[0]
         self._heads = {}                              # what follows adds to their norms: after a failure they are wanted anew
-        self._batch(B)
-        if self._ws is None or len(self._ws) != len(lists):
-            self._ws = [None] * len(lists)
+        self._batch(B, stream)
+        self._workspaces(lists, stream)
         for k, ll in enumerate(lists):
-            need = b.dp_workspace_bytes(ll)
-            if self._ws[k] is None or self._ws[k].numel() < need:
-                self._ws[k] = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             b.dp_per_example_sqnorms(ll, self._sqnorm, k > 0 or bool(heads), self._ws[k], stream)
         for pair in by_acc.values():                  # an embedding and the projection that shares its accumulator
             if len(pair) == 2:

@@ -128,3 +128,72 @@ def test_a_macro_batch_that_the_ranks_discard_takes_its_heads_along(monkeypatch)
     assert step.examples_seen == 0 and not step.acc.any()
     with pytest.raises(ValueError, match="every HEAD"):
         step.accumulate_microbatch(Layers([emb, fc]))
+
+
+class Buffer:
+    """Stands for a buffer on the device: its size, and the streams that it was recorded for."""
+
+    def __init__(self, n):
+        self.n, self.recorded = n, []
+
+    def numel(self):
+        return self.n
+
+    def record_stream(self, stream):
+        self.recorded.append(stream)
+
+
+def test_buffers_that_are_replaced_outlive_every_stream_that_used_them(monkeypatch):
+    for name in ("dp_workspace_bytes", "dp_vocab_workspace_bytes"):
+        monkeypatch.setattr(step_module.b, name, lambda x: x.B * 64)
+    monkeypatch.setattr(step_module.b, "LayerList", Layers)
+    for name in ("dp_per_example_sqnorms", "dp_vocab_loss_backward", "dp_clip_factors", "dp_clipped_accumulate_after_sqnorms",
+                 "dp_vocab_loss_clipped_accumulate"):
+        monkeypatch.setattr(step_module.b, name, lambda *a: None)
+    step = step_module.DPStep(SPECS[1:], "cpu", C=1.0, sigma=1.0, lr=1e-3, beta1=0.9, beta2=0.999, xi=1e-11, weight_decay=0.0)
+
+    def microbatch(B, stream, lists=1):
+        step.head_backward(1, Head(B=B), None, None, stream=stream)
+        step.accumulate_microbatch([Layers([None], B=B)] * lists, stream=stream)
+    old = step._sqnorm, step._clip, step._ws, step._head_ws = Buffer(4), Buffer(4), [Buffer(256)], Buffer(256)
+    microbatch(4, "a")
+    microbatch(4, "b")
+    assert all(t.recorded == [] for t in (old[0], old[1], old[2][0], old[3]))
+    ws = old[2][0]
+    microbatch(5, "c")                                         # more of everything
+    for t in (old[0], old[1], ws, old[3]):
+        assert {"a", "b"} <= set(t.recorded) <= {"a", "b", "c"}
+    assert step._sqnorm.numel() == step._clip.numel() == 5 and step._ws[0].numel() == step._head_ws.numel() == 320
+    step._sqnorm, step._clip, step._ws, step._head_ws = new = Buffer(5), Buffer(5), [Buffer(320)], Buffer(320)
+    microbatch(5, "d")
+    other = new[2][0]
+    microbatch(3, "d", lists=2)                                # fewer examples, another number of lists
+    assert set(new[0].recorded) == set(new[1].recorded) == {"c", "d"} and set(other.recorded) == {"c", "d"}
+    assert new[3].recorded == [] and step._head_ws is new[3]   # large enough
+
+
+def test_buffers_are_allocated_for_the_stream_that_uses_them(monkeypatch):
+    """What torch allocates or fills for a call on a stream of the caller's goes to that stream."""
+    calls = Calls(monkeypatch)
+    entered = []
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            entered.append(self.stream)
+
+        def __exit__(self, *a):
+            entered.append(None)
+    empty = torch.empty
+
+    def watched(*a, **k):
+        assert entered and entered[-1] == "s"
+        return empty(*a, **k)
+    step = step_module.DPStep(SPECS[1:], "cpu", C=1.0, sigma=1.0, lr=1e-3, beta1=0.9, beta2=0.999, xi=1e-11, weight_decay=0.0)
+    monkeypatch.setattr(step, "_on", On, raising=False)
+    monkeypatch.setattr(step_module.torch, "empty", watched)
+    step.head_backward(1, Head(), None, None, stream="s")
+    step.accumulate_microbatch([Layers([None])], stream="s")
+    assert entered.count("s") >= 3 and calls.seen is not None
