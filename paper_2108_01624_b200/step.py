@@ -308,9 +308,10 @@ class DPStep:
         self.examples_seen += B
         return self._sqnorm, self._clip
 
-    def discard_macro_batch(self) -> None:
+    def discard_macro_batch(self, stream=None) -> None:
         """Drops the partly accumulated macro-batch: the accumulator is cleared, theta, m, v and t stay as they are."""
-        self.acc.zero_()
+        with self._on(stream):
+            self.acc.zero_()
         self._heads = {}
         self.examples_seen = 0
 
@@ -321,7 +322,7 @@ class DPStep:
         Algorithm 1 is calibrated to.  In that case the macro-batch is discarded and DeviceStatusError raised."""
         code = b.dp_poll_status(stream)
         if code != b.DP_OK:
-            self.discard_macro_batch()
+            self.discard_macro_batch(stream)
             raise DeviceStatusError(code)
 
     def finish_macro_batch(self, batch_size: Optional[int] = None, fused: bool = True, stream=None,
@@ -338,7 +339,8 @@ class DPStep:
             self.noised_sqnorm(self.acc, 0, N, stream)
             self.clipped_update(self.theta, self.m, self.v, self.acc, stream)
         elif fused and self.sq_sums is not None:
-            self.sq_sums.zero_()
+            with self._on(stream):
+                self.sq_sums.zero_()
             b.dp_noise_scale_adamw_step_snr(self.theta, self.m, self.v, self.acc, True, self.sigma, self.C, N,
                                             self.seed, self.t, self.lr, self.beta1, self.beta2, self.xi,
                                             self.weight_decay, self.t, self.sq_sums, 0, stream)
@@ -350,16 +352,18 @@ class DPStep:
             b.dp_add_noise_and_scale(self.acc, self.sigma, self.C, N, self.seed, self.t, 0, stream)
             b.dp_adamw_step(self.theta, self.m, self.v, self.acc, self.lr, self.beta1, self.beta2, self.xi,
                             self.weight_decay, self.t, stream)
-            self.acc.zero_()
+            with self._on(stream):
+                self.acc.zero_()
         self.examples_seen = 0
 
     def noised_sqnorm(self, acc: torch.Tensor, elem_offset: int, batch_size: int, stream=None) -> torch.Tensor:
         """acc (the flat vector from element elem_offset on) <- (acc + noise) / batch_size in place; returns the squared
         norm of its tensors' elements in grad_sqsum."""
-        if self.grad_sqsum is None:
-            self.grad_sqsum = torch.zeros(1, dtype=torch.float64, device=self.device)
-        if self._norm_ws is None:       # after an end of a macro-batch with an empty shard there is a sum, but no workspace
-            self._norm_ws = torch.empty(b.dp_global_norm_workspace_bytes(), dtype=torch.uint8, device=self.device)
+        with self._on(stream):
+            if self.grad_sqsum is None:
+                self.grad_sqsum = torch.zeros(1, dtype=torch.float64, device=self.device)
+            if self._norm_ws is None:   # after an end of a macro-batch with an empty shard there is a sum, but no workspace
+                self._norm_ws = torch.empty(b.dp_global_norm_workspace_bytes(), dtype=torch.uint8, device=self.device)
         b.dp_add_noise_and_scale(acc, self.sigma, self.C, batch_size, self.seed, self.t, elem_offset, stream)
         b.dp_global_sqnorm(self.tensor_pieces(acc, elem_offset, elem_offset + acc.numel()), self.grad_sqsum, False,
                            self._norm_ws, stream)

@@ -197,3 +197,43 @@ def test_buffers_are_allocated_for_the_stream_that_uses_them(monkeypatch):
     step.head_backward(1, Head(), None, None, stream="s")
     step.accumulate_microbatch([Layers([None])], stream="s")
     assert entered.count("s") >= 3 and calls.seen is not None
+
+
+def test_what_ends_a_macro_batch_stays_on_its_stream(monkeypatch):
+    """Fills by torch, of the accumulator, the sums of squares and what is allocated for them, are in the order of the calls' stream."""
+    inside, outside = [], []
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            inside.append(self.stream)
+
+        def __exit__(self, *a):
+            inside.pop()
+    zero, zeros = torch.Tensor.zero_, torch.zeros
+
+    def watched(act):
+        def call(*a, **k):
+            if inside != ["s"]:
+                outside.append(act)
+            return act(*a, **k)
+        return call
+    for name in ("dp_noise_scale_adamw_step_snr", "dp_add_noise_and_scale", "dp_adamw_step", "dp_global_sqnorm", "dp_clip_adamw_step"):
+        monkeypatch.setattr(step_module.b, name, lambda *a: None)
+    monkeypatch.setattr(step_module.b, "dp_global_norm_workspace_bytes", lambda: 256)
+    monkeypatch.setattr(step_module.b, "dp_poll_status", lambda stream: -5 if stream == "s" and failing else 0)
+    failing = False
+    hyper = dict(C=1.0, sigma=1.0, lr=1e-3, beta1=0.9, beta2=0.999, xi=1e-11, weight_decay=0.0)
+    steps = [step_module.DPStep(SPECS, "cpu", track_snr=True, **hyper), step_module.DPStep(SPECS, "cpu", **hyper),
+             step_module.DPStep(SPECS, "cpu", max_grad_norm=1.0, **hyper)]
+    monkeypatch.setattr(step_module.DPStep, "_on", lambda self, stream: On(stream))
+    monkeypatch.setattr(torch.Tensor, "zero_", watched(zero))
+    monkeypatch.setattr(step_module.torch, "zeros", watched(zeros))
+    for step, fused in zip(steps, (True, False, True)):
+        step.finish_macro_batch(4, fused=fused, stream="s")
+    failing = True
+    with pytest.raises(step_module.DeviceStatusError):
+        steps[0].finish_macro_batch(4, stream="s")
+    assert outside == []
