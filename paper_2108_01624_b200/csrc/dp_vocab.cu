@@ -638,18 +638,19 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
 // =================================================================================================
 // Squared norms of short examples (at most 128 rows of planes): |G_i^T X_i|^2 = sum over rows r, s of the example of
 // (<x_r, x_s> + bias) <g_r, g_s>.  A CTA takes as many whole examples as 128 rows hold and some blocks of G; both Grams are
-// 128 x 128 x 16 UMMAs of a tile with itself, of which the epilogue uses each row's own example.  The Gram of G is taken
-// over by the epilogue every kNormSeg stages and added in registers: its squares are one large (the label's) and a
-// vocabulary of small ones, which a longer sum on the tensor core would lose.  What it drops makes norms too small: at 256 x 20
-// tokens and 30522 words squares are off by -3.5e-6 in the mean with 8 stages, -2.7e-6 with 4, -2.4e-6 with 2, -2.2e-6 with 1 (in fp32
-// throughout 2e-7), and the norms take 473, 476, 479 and 497 us of back to back calls with GRAD; dX hides the first step.
+// 128 x 128 x 16 UMMAs of a tile with itself, of which the epilogue uses each row's own example.  Both are taken over by
+// the epilogue every kNormSeg stages: the parts of G's are added in registers (its squares are one large, the label's, and a
+// vocabulary of small ones, which a longer sum on the tensor core would lose), then those of X's are multiplied by it as they come, so
+// that no width makes a sum longer (one sum of X's: 2.8e-4 of a squared norm lost at width 65536, 4e-6 now).  What the tensor core
+// drops makes norms too small: at 256 x 20 tokens of width 1024 and 30522 words by 3.2e-6 in the mean with 8 stages, 1.6e-6 with 4, 0.8e-6 with
+// 2, 0.4e-6 with 1 (in fp32 throughout 2e-7 to either side), and the norms with GRAD take 416, 418, 423 and 431 us replayed.
 // Bound by reading G: 110 us for 625 MB, where the layers' kernel with one example at a time took 318.
 // =================================================================================================
 constexpr int N_STAGES = 6, N_STAGE_BYTES = 2 * V_BOX_BYTES;    // 128 rows x 128 columns
 constexpr int N_THREADS = 192;                                  // warp 0 TMA, warp 1 UMMA, warps 2..5 epilogue
 constexpr int kNormSeg = 4;                                     // stages of 128 columns
 struct NCtl {
-  uint64_t full[N_STAGES], empty[N_STAGES], tmem_full[3], tmem_empty[2], drain;
+  uint64_t full[N_STAGES], empty[N_STAGES], tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base;
   int abort;
   float row[128];
@@ -674,17 +675,16 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
   volatile int* abort_flag = &S->abort;
   if (threadIdx.x == 0) {
     for (int s = 0; s < N_STAGES; ++s) { mbar_init(&S->full[s], 1); mbar_init(&S->empty[s], 1); }
-    for (int b = 0; b < 3; ++b) mbar_init(&S->tmem_full[b], 1);
-    for (int b = 0; b < 2; ++b) mbar_init(&S->tmem_empty[b], 4);
+    for (int b = 0; b < 2; ++b) { mbar_init(&S->tmem_full[b], 1); mbar_init(&S->tmem_empty[b], 4); }
     mbar_init(&S->drain, 1);
     S->abort = 0;
     fence_mbar_init();
   }
-  if (warp == 1) { tmem_alloc(&S->tmem_base, 512); tmem_relinquish(); }
+  if (warp == 1) { tmem_alloc(&S->tmem_base, 256); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_base = S->tmem_base;        // columns 0, 128: G, in turn; 256: X
+  const uint32_t tmem_base = S->tmem_base;        // columns 0, 128: the parts in turn
   const int px = (P.dp + 127) / 128;              // stages of X
   const int items = P.groups * P.splits;
 
@@ -696,19 +696,19 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
         const int grp = item % P.groups, split = item / P.groups;
         const int y = grp * P.examples * P.rows;
         const int s0 = (int)((long long)P.subs * split / P.splits), s1 = (int)((long long)P.subs * (split + 1) / P.splits);
-        const int pg = P.sub / 128, all = px + (s1 - s0) * pg;
+        const int sub_stages = P.sub / 128, pg = (s1 - s0) * sub_stages, all = pg + px;
         for (int j = 0; j < all; ++j, ++it) {
           const uint32_t slot = it % N_STAGES, ph = (it / N_STAGES) & 1u;
           if (!mbar_wait(&S->empty[slot], ph ^ 1u, abort_flag, P.status, 71, (int)it)) { alive = false; break; }
           uint8_t* st = tiles + slot * N_STAGE_BYTES;
           mbar_arrive_expect_tx(&S->full[slot], (uint32_t)N_STAGE_BYTES);
-          if (j < px) {                           // columns beyond X's arrive as zeros
-            load2(st, &P.x, &S->full[slot], 128 * j, y);
-            load2(st + V_BOX_BYTES, &P.x, &S->full[slot], 128 * j + 64, y);
-          } else {
-            const int z = s0 + (j - px) / pg, x = (j - px) % pg * 128;
+          if (j < pg) {
+            const int z = s0 + j / sub_stages, x = j % sub_stages * 128;
             tma_load_3d(st, &P.g, &S->full[slot], x, y, z);
             tma_load_3d(st + V_BOX_BYTES, &P.g, &S->full[slot], x + 64, y, z);
+          } else {                                // columns beyond X's arrive as zeros
+            load2(st, &P.x, &S->full[slot], 128 * (j - pg), y);
+            load2(st + V_BOX_BYTES, &P.x, &S->full[slot], 128 * (j - pg) + 64, y);
           }
         }
       }
@@ -727,16 +727,13 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
       for (int item = blockIdx.x; item < items && alive; item += gridDim.x) {
         const int split = item / P.groups;
         const int s0 = (int)((long long)P.subs * split / P.splits), s1 = (int)((long long)P.subs * (split + 1) / P.splits);
-        const int all = px + (s1 - s0) * (P.sub / 128);
-        // X first (the epilogue has read the X of the item before: it gave back that item's last part of G after it)
-        for (int j0 = 0; j0 < all && alive;) {
-          const bool isx = j0 == 0;
-          const int j1 = isx ? px : j0 + kNormSeg < all ? j0 + kNormSeg : all;
+        const int pg = (s1 - s0) * (P.sub / 128), all = pg + px;
+        for (int j0 = 0; j0 < all && alive; ++part) {
+          const int end = j0 < pg ? pg : all, j1 = j0 + kNormSeg < end ? j0 + kNormSeg : end;
           const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
           if (!mbar_wait(&S->tmem_empty[buf], tph ^ 1u, abort_flag, P.status, 72, (int)part)) { alive = false; break; }
-          if (isx && part > 0 && !mbar_wait(&S->tmem_empty[buf ^ 1u], ((part - 1) >> 1) & 1u, abort_flag, P.status, 73, (int)part)) { alive = false; break; }
           tc_fence_after();
-          const uint32_t d_tmem = tmem_base + (isx ? 256u : buf * 128u);
+          const uint32_t d_tmem = tmem_base + buf * 128u;
           for (int j = j0; j < j1; ++j, ++it) {
             const uint32_t slot = it % N_STAGES, ph = (it / N_STAGES) & 1u;
             if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 74, (int)it)) { alive = false; break; }
@@ -749,8 +746,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
             }
             umma_commit(&S->empty[slot]);
           }
-          if (alive) umma_commit(&S->tmem_full[isx ? 2 : buf]);
-          if (!isx) ++part;
+          if (alive) umma_commit(&S->tmem_full[buf]);
           j0 = j1;
         }
       }
@@ -760,19 +756,18 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
   } else {   // ---------------- epilogue warps 2..5: a row each ----------------
     const int q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem_base + ((uint32_t)(q * 32) << 16);
-    uint32_t part = 0, xs = 0;
+    uint32_t part = 0;
     bool alive = true;
-    for (int item = blockIdx.x; item < items; item += gridDim.x, ++xs) {
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
       const int grp = item % P.groups, split = item / P.groups;
       const int s0 = (int)((long long)P.subs * split / P.splits), s1 = (int)((long long)P.subs * (split + 1) / P.splits);
-      const int parts = ((s1 - s0) * (P.sub / 128) + kNormSeg - 1) / kNormSeg;
-      if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[2], xs & 1u, abort_flag, P.status, 75, (int)xs));
+      const int parts_g = ((s1 - s0) * (P.sub / 128) + kNormSeg - 1) / kNormSeg, parts_x = (px + kNormSeg - 1) / kNormSeg;
       float acc[128];
 #pragma unroll
       for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
-      float sum = 0.0f;
+      float sum = 0.0f, one = P.bias ? 1.0f : 0.0f;
       const int c0 = r / P.rows * P.rows, c1 = c0 + P.rows;       // this row's example
-      for (int k = 0; k < parts; ++k, ++part) {
+      for (int k = 0; k < parts_g + parts_x; ++k, ++part) {
         const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
         if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[buf], tph, abort_flag, P.status, 76, (int)part));
         if (!alive) continue;
@@ -782,16 +777,10 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
           uint32_t v[32];
           tmem_ld_32x32(lane_base + buf * 128u + (uint32_t)ch * 32u, v);
           tmem_ld_wait();
+          if (k < parts_g) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) acc[ch * 32 + j] += __uint_as_float(v[j]);
-        }
-        if (k == parts - 1) {                     // before this part's columns are given back, so is X's Gram
-          const float one = P.bias ? 1.0f : 0.0f;
-#pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            uint32_t v[32];
-            tmem_ld_32x32(lane_base + 256u + (uint32_t)ch * 32u, v);
-            tmem_ld_wait();
+            for (int j = 0; j < 32; ++j) acc[ch * 32 + j] += __uint_as_float(v[j]);
+          } else {
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
               const bool own = ch * 32 + j >= c0 && ch * 32 + j < c1;
@@ -799,6 +788,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
             }
           }
         }
+        if (k == parts_g) one = 0.0f;             // the bias' part has come with the first of X's
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&S->tmem_empty[buf]);
@@ -819,7 +809,7 @@ __global__ void __launch_bounds__(N_THREADS, 1) k_vocab_norms(const __grid_const
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc(tmem_base, 512);
+    tmem_dealloc(tmem_base, 256);
   }
 }
 

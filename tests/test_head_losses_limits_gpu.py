@@ -38,3 +38,34 @@ def test_microbatches_of_changing_size_on_a_stream_of_the_callers():
     torch.cuda.synchronize()
     assert torch.equal(want.acc, got.acc) and bool(want.acc.any())
     assert all(bool((t == 7.0).all()) for t in kept)
+
+
+def norm_errors(B, T, d, V, dtype, bias=True, seed=0):
+    """Signed errors of the squared norms relative to the definition from the same lse, one per example."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn(B, T, d, generator=g, device=DEV).to(dtype)
+    w = (torch.randn(V, d, generator=g, device=DEV) * (2.0 / math.sqrt(d))).to(dtype)
+    y = torch.randint(0, V, (B, T), generator=g, device=DEV, dtype=torch.int32)
+    b = torch.randn(V, generator=g, device=DEV) if bias else None
+    head = dp.VocabHead(x, w, y, bias=b)
+    ws, loss, lse, sq = workspace(head), torch.empty(B, T, device=DEV), torch.empty(B, T, device=DEV), torch.empty(B, device=DEV)
+    dp.dp_vocab_loss(head, loss, lse, workspace=ws)
+    dp.dp_vocab_loss_backward(head, lse, None, sq, workspace=ws)
+    ref = torch.empty(B, dtype=torch.float64, device=DEV)
+    for i in range(B):
+        xd = x[i].double()
+        G = (xd @ w.double().t() + (b.double() if bias else 0.0) - lse[i].double()[:, None]).exp()
+        G[torch.arange(T, device=DEV), y[i].long()] -= 1.0
+        ref[i] = (G.t() @ xd).pow(2).sum() + (G.sum(0).pow(2).sum() if bias else 0.0)
+    return (sq.double() - ref) / ref
+
+
+# What the tensor cores drop makes norms too small, so an example could add more than C: less than 2^-23 of what has been summed
+# at each step of 16, and no sum is longer than 32 steps: 2 * 32 * 2^-23 of the squares, which are products of two such sums.
+# Exponentials take 2 * 2^-20; G in two bf16 numbers 2 * 2^-17 for a token alone, to either side, less in the mean over examples
+# and tokens (4 sigma of 100 single tokens: 2^-18).  Together 2^-16 of a squared norm in the mean, whatever the sizes.
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B, T, d, V", [(100, 1, 1024, 40), (100, 1, 65536, 40), (64, 20, 8192, 300), (64, 32, 768, 3000)])
+def test_norms_of_short_examples_are_right_in_the_mean(B, T, d, V, dtype):
+    r = norm_errors(B, T, d, V, dtype)
+    assert abs(float(r.mean())) <= 2.0 ** -16, (float(r.mean()), float(r.min()), float(r.max()))
