@@ -908,7 +908,8 @@ k_vocab_tokens(const __grid_constant__ VHead H, const float* lse, const float* c
   wait_for_predecessor();
   let_successor_in();
   const int n = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  for (long long v = (long long)blockIdx.x * 256 + threadIdx.x; v < columns; v += (long long)gridDim.x * 256)   // of 2^26 tokens: 2^31 a step
+  // without sign: of 2^26 tokens a step is 2^31
+  for (unsigned v = blockIdx.x * 256 + threadIdx.x; v < (unsigned)columns; v += gridDim.x * 256)
     bias[v] = v >= H.V ? -INFINITY : H.bias ? H.bias[v] : 0.0f;
   if (n >= H.N) return;
   const int y = label_of(H, n, status);
