@@ -380,8 +380,9 @@ DP_API int dp_vocab_loss(const dp_vocab_head* head /*HOST*/, float* loss, float*
 /* From the lse of dp_vocab_loss: dX = G W (rows of leading dimension ld_dx; of dtype; may not overlap X), and
  *   sqnorm[i] = or += |G_i^T X_i|^2 + (with bias) |sum_t G_i|^2,
  * the squared norm of example i's gradients of W and bias.  dX or sqnorm may be NULL.  Tensor-core sums drop low bits: a
- * squared norm comes out too small, for examples of up to 64 bf16 or 32 fp32 tokens by 1 to 5 10^-6 of itself at any width (1.6e-6 at
- * 256 x 20 tokens of width 1024 and 30522 words). */
+ * squared norm comes out too small in the mean over examples, by 1 to 5 10^-6 of itself (1.6e-6 at 256 x 20 tokens of width 1024 and 30522
+ * words).  No such sum is longer than 512 terms, so that does not grow with widths (65536 measured) or with the tokens of an example
+ * (200000 measured; 3e-5 at a million, from the fp32 sums after them).  To that come 10^-5 to either side for an example of one token. */
 DP_API int dp_vocab_loss_backward(const dp_vocab_head* head /*HOST*/, const float* lse, void* dX, int64_t ld_dx, float* sqnorm,
                                   int accumulate_into, void* workspace, size_t workspace_bytes, void* cuda_stream);
 

@@ -103,8 +103,9 @@ bool umma_supported(const dp_layer& L);
 // Number of fp32 partial sums the squared-norm kernels write for these layers (per example).
 // The partial buffer is [B][count] and is summed by launch_reduce_partials.
 size_t umma_sqnorm_partials_per_example(const dp_layer* layers, const int* idx, int n, const int* use_gram);
+// parts: examples of more than 128 tokens are summed by parts, so that no sum on the tensor core grows with tokens or widths.
 int launch_umma_sqnorms(const dp_layer* layers, const int* idx, int n, const int* use_gram, float* partial,
-                        int partial_stride, int partial_base, int* status, cudaStream_t s);
+                        int partial_stride, int partial_base, int* status, cudaStream_t s, bool parts = false);
 // Host-side schedule of one accumulate launch (at most kUmmaMaxLayers layers): splits of the example range, first
 // work item per layer; returns the number of item slots (waves x units).
 constexpr int kUmmaMaxLayers = 96;

@@ -479,6 +479,7 @@ constexpr int W_BARS = 16;                              // stage barriers (more 
 static_assert(W_UNITS >= 3 && W_UNITS < W_BARS, "a stage of three units must fit, and every stage in flight needs a barrier");
 constexpr int W_THREADS = 320;                          // warp 0 TMA, warp 1 UMMA issue, warps 2..9 epilogue
 constexpr int kWideMaxLayers = 48;
+constexpr int kPartSteps = 32;                          // steps of 16 that a sum by parts takes on the tensor core
 
 struct alignas(64) WideLayer {
   CUtensorMap rowA, colA, rowG, colG;   // [B, T, d] bf16 as (feature, token, example); boxes 64 x 128 and 64 x 256
@@ -530,6 +531,12 @@ __device__ __forceinline__ WideItem wide_decode(const WideParams& P, int item, i
   return t;
 }
 
+// PARTS: no sum on the tensor core is longer than kPartSteps steps.  G's columns come first, in parts that the epilogue adds in
+// registers, then A's, whose parts it multiplies by that sum as they come; the two accumulators take the parts in turn.
+// (Without: whole sums, A's in the first accumulator and G's in the second.  What the tensor core drops at every step makes squared norms
+// too small: a vocabulary head's, blocks of 2048 columns, by 4 to 8e-6 of themselves at width 768 and 2.8e-4 at 65536, where parts leave
+// 1 to 4e-6.  4 examples of 512 tokens, width 768, 30522 words: 277 us for 264 with the product before; 16 of 65: 141 for 134.)
+template <bool PARTS>
 __global__ void __launch_bounds__(W_THREADS, 1) k_gram_sqnorm_wide(const __grid_constant__ WideParams P) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = align1024(smem_raw);
@@ -568,7 +575,8 @@ __global__ void __launch_bounds__(W_THREADS, 1) k_gram_sqnorm_wide(const __grid_
         const bool diag = t.c0 == t.r;
         // a lone column block is fetched with the 128-token box; rows beyond T arrive as zeros either way
         const int u = (diag ? 0 : 1) + (t.ncol == 2 ? 2 : 1);
-        for (int which = 0; which < 2 && alive; ++which) {
+        for (int turn = 0; turn < 2 && alive; ++turn) {
+          const int which = PARTS ? 1 - turn : turn;
           const CUtensorMap* rowmap = which ? &L.rowG : &L.rowA;
           const CUtensorMap* colmap = t.ncol == 2 ? (which ? &L.colG : &L.colA) : rowmap;
           const int d = which ? L.d_out : L.d_in;
@@ -604,7 +612,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) k_gram_sqnorm_wide(const __grid_
     if (lane == 0) {   // ---------------- MMA issuer ----------------
       constexpr uint32_t IDESC_N256 = idesc_bf16_f32(128, 256, false, false);
       constexpr uint32_t IDESC_N128 = idesc_bf16_f32(128, 128, false, false);
-      uint32_t n = 0, tile_it = 0;
+      uint32_t n = 0, tile_it = 0, part = 0;
       int pos = 0;
       bool alive = true;
       for (int item = blockIdx.x; item < P.total_items && alive; item += gridDim.x, ++tile_it) {
@@ -613,32 +621,36 @@ __global__ void __launch_bounds__(W_THREADS, 1) k_gram_sqnorm_wide(const __grid_
         const bool diag = t.c0 == t.r;
         const int u = (diag ? 0 : 1) + (t.ncol == 2 ? 2 : 1);
         const uint32_t idesc = t.ncol == 2 ? IDESC_N256 : IDESC_N128;
-        const uint32_t tph = tile_it & 1u;
-        for (int which = 0; which < 2 && alive; ++which) {
-          if (!mbar_wait(which ? &S->y_empty : &S->x_empty, tph ^ 1u, abort_flag, P.status, 22, (int)tile_it)) {
-            alive = false;
-            break;
-          }
-          tc_fence_after();
-          const int d = which ? L.d_out : L.d_in;
-          const uint32_t d_tmem = tmem_base + (uint32_t)which * 256u;
-          for (int k0 = 0; k0 < d; k0 += 64) {
-            if (pos + u > W_UNITS) pos = 0;              // the same walk over the unit ring as the producer's
-            const uint32_t rowb = smem_u32(tiles + pos * W_UNIT_BYTES);
-            const uint32_t colb = diag ? rowb : rowb + W_UNIT_BYTES;
-            pos += u;
-            if (pos == W_UNITS) pos = 0;
-            const uint32_t b = n % W_BARS, ph = (n / W_BARS) & 1u;
-            ++n;
-            if (!mbar_wait(&S->full[b], ph, abort_flag, P.status, 23, (int)n)) { alive = false; break; }
+        for (int turn = 0; turn < 2 && alive; ++turn) {
+          const int which = PARTS ? 1 - turn : turn;
+          const int d = which ? L.d_out : L.d_in, step = PARTS ? 16 * kPartSteps : d;
+          for (int first = 0; first < d && alive; first += step, ++part) {
+            const uint32_t buf = PARTS ? part & 1u : (uint32_t)which, tph = (PARTS ? part >> 1 : tile_it) & 1u;
+            if (!mbar_wait(buf ? &S->y_empty : &S->x_empty, tph ^ 1u, abort_flag, P.status, 22, (int)tile_it)) {
+              alive = false;
+              break;
+            }
             tc_fence_after();
+            const uint32_t d_tmem = tmem_base + buf * 256u;
+            const int end = d - first < step ? d : first + step;
+            for (int k0 = first; k0 < end; k0 += 64) {
+              if (pos + u > W_UNITS) pos = 0;              // the same walk over the unit ring as the producer's
+              const uint32_t rowb = smem_u32(tiles + pos * W_UNIT_BYTES);
+              const uint32_t colb = diag ? rowb : rowb + W_UNIT_BYTES;
+              pos += u;
+              if (pos == W_UNITS) pos = 0;
+              const uint32_t b = n % W_BARS, ph = (n / W_BARS) & 1u;
+              ++n;
+              if (!mbar_wait(&S->full[b], ph, abort_flag, P.status, 23, (int)n)) { alive = false; break; }
+              tc_fence_after();
 #pragma unroll
-            for (int k4 = 0; k4 < 4; ++k4)
-              umma_bf16(d_tmem, smem_desc_sw128(rowb + k4 * 32, 16, 1024), smem_desc_sw128(colb + k4 * 32, 16, 1024),
-                        idesc, (k0 | k4) ? 1u : 0u);
-            umma_commit(&S->empty[b]);
+              for (int k4 = 0; k4 < 4; ++k4)
+                umma_bf16(d_tmem, smem_desc_sw128(rowb + k4 * 32, 16, 1024), smem_desc_sw128(colb + k4 * 32, 16, 1024),
+                          idesc, (k0 > first || k4) ? 1u : 0u);
+              umma_commit(&S->empty[b]);
+            }
+            if (alive) umma_commit(buf ? &S->y_full : &S->x_full);
           }
-          if (alive) umma_commit(which ? &S->y_full : &S->x_full);
         }
       }
       umma_commit(&S->drain);
@@ -647,44 +659,76 @@ __global__ void __launch_bounds__(W_THREADS, 1) k_gram_sqnorm_wide(const __grid_
   } else {   // ---------------- epilogue warps 2..9: lanes [32 q, +32), column block h of the pair ----------------
     const uint32_t q = (uint32_t)warp & 3u;
     const int h = warp >= 6 ? 1 : 0;
-    uint32_t tile_it = 0;
+    uint32_t tile_it = 0, part = 0;
     bool alive = true;
     for (int item = blockIdx.x; item < P.total_items; item += gridDim.x, ++tile_it) {
       const WideItem t = wide_decode(P, item, per_example, nblk);
       const WideLayer& L = P.L[t.l];
-      const uint32_t tph = tile_it & 1u;
       const bool active = h < t.ncol;
       const uint32_t tsrc = tmem_base + ((q * 32u) << 16) + (uint32_t)h * 128u;
-      if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->x_full, tph, abort_flag, P.status, 24, (int)tile_it));
-      if (!alive) continue;
-      tc_fence_after();
-      uint32_t pv[4][32];
-      if (active) {
+      float bias1 = L.has_bias ? 1.0f : 0.0f, sum = 0.0f;
+      if constexpr (PARTS) {
+        const int parts_g = (L.d_out + 16 * kPartSteps - 1) / (16 * kPartSteps), parts_a = (L.d_in + 16 * kPartSteps - 1) / (16 * kPartSteps);
+        float acc[128];
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) tmem_ld_32x32(tsrc + (uint32_t)ch * 32u, pv[ch]);
-        tmem_ld_wait();
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&S->x_empty);
-      alive = __all_sync(0xffffffffu, mbar_wait(&S->y_full, tph, abort_flag, P.status, 25, (int)tile_it));
-      if (!alive) continue;
-      tc_fence_after();
-      const float bias1 = L.has_bias ? 1.0f : 0.0f;
-      float sum = 0.0f;
-      if (active) {
+        for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+        for (int k = 0; k < parts_g + parts_a; ++k, ++part) {
+          const uint32_t buf = part & 1u;
+          if (alive) alive = __all_sync(0xffffffffu, mbar_wait(buf ? &S->y_full : &S->x_full, (part >> 1) & 1u, abort_flag, P.status, 24, (int)tile_it));
+          if (!alive) continue;
+          tc_fence_after();
+          if (active) {
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {
-          uint32_t qv[32];
-          tmem_ld_32x32(tsrc + 256u + (uint32_t)ch * 32u, qv);
-          tmem_ld_wait();
+            for (int ch = 0; ch < 4; ++ch) {
+              uint32_t v[32];
+              tmem_ld_32x32(tsrc + buf * 256u + (uint32_t)ch * 32u, v);
+              tmem_ld_wait();
+              if (k < parts_g) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) sum = fmaf(__uint_as_float(pv[ch][j]) + bias1, __uint_as_float(qv[j]), sum);
+                for (int j = 0; j < 32; ++j) acc[ch * 32 + j] += __uint_as_float(v[j]);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) sum = fmaf(__uint_as_float(v[j]) + bias1, acc[ch * 32 + j], sum);
+              }
+            }
+          }
+          if (k == parts_g) bias1 = 0.0f;         // the bias' part has come with the first of A's
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(buf ? &S->y_empty : &S->x_empty);
         }
+        if (!alive) continue;
+      } else {
+        const uint32_t tph = tile_it & 1u;
+        if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->x_full, tph, abort_flag, P.status, 24, (int)tile_it));
+        if (!alive) continue;
+        tc_fence_after();
+        uint32_t pv[4][32];
+        if (active) {
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) tmem_ld_32x32(tsrc + (uint32_t)ch * 32u, pv[ch]);
+          tmem_ld_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S->x_empty);
+        alive = __all_sync(0xffffffffu, mbar_wait(&S->y_full, tph, abort_flag, P.status, 25, (int)tile_it));
+        if (!alive) continue;
+        tc_fence_after();
+        if (active) {
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) {
+            uint32_t qv[32];
+            tmem_ld_32x32(tsrc + 256u + (uint32_t)ch * 32u, qv);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum = fmaf(__uint_as_float(pv[ch][j]) + bias1, __uint_as_float(qv[j]), sum);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S->y_empty);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&S->y_empty);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
       if (lane == 0)
@@ -741,6 +785,10 @@ __device__ __forceinline__ TileItem tile_pair_decode(const UmmaParams& P, int it
   return t;
 }
 
+// PARTS: no sum on the tensor core is longer than kPartSteps steps (4 stages); the epilogue adds the parts of a tile in registers.  (Whole
+// sums make squared norms too small, by 1.7e-5 of themselves at 10000 rows and 1.6e-4 at 100000; parts by 1.2e-6.  5000 tokens, width 1024,
+// 10000 words: 1229 us for 1246 with the product before.)
+template <bool PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(T_THREADS, 1)
 k_tile_sqnorm_pair(const __grid_constant__ UmmaParams P) {
   extern __shared__ uint8_t smem_raw[];
@@ -764,7 +812,7 @@ k_tile_sqnorm_pair(const __grid_constant__ UmmaParams P) {
   cluster_sync_all();           // the peer's barriers are initialised before anyone signals them
   tc_fence_after();
   const uint32_t tmem_base = S->tmem_base;
-  const int n_tb = (P.T + Q_BK - 1) / Q_BK;
+  const int n_tb = (P.T + Q_BK - 1) / Q_BK, part_tb = PARTS ? 16 * kPartSteps / Q_BK : n_tb;
 
   if (warp == 0) {
     if (lane == 0) {   // ---------------- TMA producer (each CTA, its own slices) ----------------
@@ -805,61 +853,91 @@ k_tile_sqnorm_pair(const __grid_constant__ UmmaParams P) {
       }
     } else if (lane == 0) {   // ---------------- even CTA: UMMA issuer ----------------
       constexpr uint32_t IDESC = idesc_bf16_f32(256, 256, true, true);
-      uint32_t it = 0, tile_it = 0;
+      uint32_t it = 0, part = 0;                              // part: all of a tile's tokens, or some of them
       bool alive = true;
-      for (int item = first_item; item < P.total_items && alive; item += item_stride, ++tile_it) {
-        const uint32_t buf = tile_it & 1u, tph = (tile_it >> 1) & 1u;
-        if (!mbar_wait(&S->tmem_empty[buf], tph ^ 1u, abort_flag, P.status, 42, (int)tile_it)) { alive = false; break; }
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + buf * 256u;
-        uint32_t first = 0;
-        for (int tb = 0; tb < n_tb; ++tb) {
-          const uint32_t slot = it % Q_STAGES, ph = (it / Q_STAGES) & 1u;
-          ++it;
-          if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 43, (int)it) ||
-              !mbar_wait(&S->ready[slot], ph, abort_flag, P.status, 47, (int)it)) {
-            alive = false;
-            break;
-          }
+      for (int item = first_item; item < P.total_items && alive; item += item_stride) {
+        for (int tb0 = 0; tb0 < n_tb && alive; tb0 += part_tb, ++part) {
+          const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
+          if (!mbar_wait(&S->tmem_empty[buf], tph ^ 1u, abort_flag, P.status, 42, (int)part)) { alive = false; break; }
           tc_fence_after();
-          const uint32_t am = smem_u32(tiles + slot * Q_STAGE_BYTES), an = am + Q_HALF_BYTES;
-          const int left = P.T - tb * Q_BK, nk = left >= Q_BK ? Q_BK / 16 : (left + 15) >> 4;   // k-steps that hold tokens
+          const uint32_t d_tmem = tmem_base + buf * 256u;
+          const int tb1 = n_tb - tb0 < part_tb ? n_tb : tb0 + part_tb;
+          uint32_t first = 0;
+          for (int tb = tb0; tb < tb1; ++tb) {
+            const uint32_t slot = it % Q_STAGES, ph = (it / Q_STAGES) & 1u;
+            ++it;
+            if (!mbar_wait(&S->full[slot], ph, abort_flag, P.status, 43, (int)it) ||
+                !mbar_wait(&S->ready[slot], ph, abort_flag, P.status, 47, (int)it)) {
+              alive = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t am = smem_u32(tiles + slot * Q_STAGE_BYTES), an = am + Q_HALF_BYTES;
+            const int left = P.T - tb * Q_BK, nk = left >= Q_BK ? Q_BK / 16 : (left + 15) >> 4;   // k-steps that hold tokens
 #pragma unroll
-          for (int k8 = 0; k8 < Q_BK / 16; ++k8) {
-            if (k8 < nk)
-              umma_bf16_pair(d_tmem, smem_desc_sw128(am + k8 * 2048, Q_ATOM_BYTES, 1024),
-                             smem_desc_sw128(an + k8 * 2048, Q_ATOM_BYTES, 1024), IDESC, first | (uint32_t)k8);
+            for (int k8 = 0; k8 < Q_BK / 16; ++k8) {
+              if (k8 < nk)
+                umma_bf16_pair(d_tmem, smem_desc_sw128(am + k8 * 2048, Q_ATOM_BYTES, 1024),
+                               smem_desc_sw128(an + k8 * 2048, Q_ATOM_BYTES, 1024), IDESC, first | (uint32_t)k8);
+            }
+            first = 1;
+            umma_commit_pair(&S->empty[slot], (uint16_t)3);
           }
-          first = 1;
-          umma_commit_pair(&S->empty[slot], (uint16_t)3);
+          if (alive) umma_commit_pair(&S->tmem_full[buf], (uint16_t)3);
         }
-        if (alive) umma_commit_pair(&S->tmem_full[buf], (uint16_t)3);
       }
       umma_commit_pair(&S->drain, (uint16_t)1);
       mbar_wait_drain(&S->drain, 0u, P.status);
     }
   } else {   // ---------------- epilogue warps 2..9: lanes [32 q, +32), accumulator columns [128 h, +128) ----------------
     const uint32_t q = (uint32_t)warp & 3u, h = warp >= 6 ? 1u : 0u;
-    uint32_t tile_it = 0;
+    uint32_t part = 0;
     bool alive = true;
-    for (int item = first_item; item < P.total_items; item += item_stride, ++tile_it) {
+    for (int item = first_item; item < P.total_items; item += item_stride) {
       const TileItem t = tile_pair_decode(P, item);
-      const uint32_t buf = tile_it & 1u, tph = (tile_it >> 1) & 1u;
-      if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[buf], tph, abort_flag, P.status, 44, (int)tile_it));
-      if (!alive) continue;
-      tc_fence_after();
       float sum = 0.0f;
-#pragma unroll 1
-      for (int ch = 0; ch < 4; ++ch) {
-        uint32_t v[32];
-        tmem_ld_32x32(tmem_base + ((q * 32u) << 16) + buf * 256u + h * 128u + (uint32_t)ch * 32u, v);
-        tmem_ld_wait();
+      if constexpr (PARTS) {
+        float acc[128];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) sum = fmaf(__uint_as_float(v[j]), __uint_as_float(v[j]), sum);
+        for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+        for (int tb0 = 0; tb0 < n_tb; tb0 += part_tb, ++part) {
+          const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
+          if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[buf], tph, abort_flag, P.status, 44, (int)part));
+          if (!alive) continue;
+          tc_fence_after();
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) {
+            uint32_t v[32];
+            tmem_ld_32x32(tmem_base + ((q * 32u) << 16) + buf * 256u + h * 128u + (uint32_t)ch * 32u, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[ch * 32 + j] += __uint_as_float(v[j]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(&S->tmem_empty[buf], 0u);
+        }
+        if (!alive) continue;
+#pragma unroll
+        for (int j = 0; j < 128; ++j) sum = fmaf(acc[j], acc[j], sum);
+      } else {
+        const uint32_t buf = part & 1u, tph = (part >> 1) & 1u;
+        ++part;
+        if (alive) alive = __all_sync(0xffffffffu, mbar_wait(&S->tmem_full[buf], tph, abort_flag, P.status, 44, (int)part));
+        if (!alive) continue;
+        tc_fence_after();
+#pragma unroll 1
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t v[32];
+          tmem_ld_32x32(tmem_base + ((q * 32u) << 16) + buf * 256u + h * 128u + (uint32_t)ch * 32u, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum = fmaf(__uint_as_float(v[j]), __uint_as_float(v[j]), sum);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(&S->tmem_empty[buf], 0u);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(&S->tmem_empty[buf], 0u);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
       if (lane == 0) P.partial[(size_t)t.e * P.partial_stride + t.slot + (int)(rank * 8u + h * 4u + q)] = sum;
@@ -1325,8 +1403,8 @@ static bool sqnorm_kernels_ready() {
   if (dev < 0) return false;
   if (!state[dev])
     state[dev] = (ensure_smem(k_gram_sqnorm, G_SMEM) && ensure_smem(k_gram_sqnorm_short, G_SMEM_SHORT) &&
-                  ensure_smem(k_gram_sqnorm_wide, W_SMEM) &&
-                  ensure_smem(k_tile_sqnorm_pair, Q_SMEM)) ? 1 : -1;
+                  ensure_smem(k_gram_sqnorm_wide<false>, W_SMEM) && ensure_smem(k_gram_sqnorm_wide<true>, W_SMEM) &&
+                  ensure_smem(k_tile_sqnorm_pair<false>, Q_SMEM) && ensure_smem(k_tile_sqnorm_pair<true>, Q_SMEM)) ? 1 : -1;
   return state[dev] > 0;
 }
 
@@ -1339,7 +1417,7 @@ static bool accum_kernel_ready() {
 }
 
 int launch_umma_sqnorms(const dp_layer* layers, const int* idx, int n, const int* use_gram, float* partial,
-                        int partial_stride, int partial_base, int* status, cudaStream_t s) {
+                        int partial_stride, int partial_base, int* status, cudaStream_t s, bool parts) {
   if (n <= 0) return DP_OK;
   const int B = layers[idx[0]].B, T = layers[idx[0]].T;
   if (!sqnorm_kernels_ready()) return DP_ERR_CUDA;
@@ -1352,10 +1430,10 @@ int launch_umma_sqnorms(const dp_layer* layers, const int* idx, int n, const int
   }
   {   // Gram layers with several token blocks, widest first: items go to the CTAs round-robin, so the last,
       // partly filled round then holds the shortest items
-    const int per_example = wide_items((T + 127) / 128);
     std::vector<int> wide;
     for (int k = 0; k < n; ++k)
       if (use_gram[k] && gram_wide(layers[idx[k]])) wide.push_back(k);
+    const int per_example = wide.empty() ? 0 : wide_items((T + 127) / 128);
     std::stable_sort(wide.begin(), wide.end(), [&](int a, int b) {
       return layers[idx[a]].d_in + layers[idx[a]].d_out > layers[idx[b]].d_in + layers[idx[b]].d_out;
     });
@@ -1391,7 +1469,7 @@ int launch_umma_sqnorms(const dp_layer* layers, const int* idx, int n, const int
       P.partial = partial;
       P.status = status;
       const int grid = P.total_items < sm_count() ? P.total_items : sm_count();
-      k_gram_sqnorm_wide<<<grid, W_THREADS, W_SMEM, s>>>(P);
+      (parts ? k_gram_sqnorm_wide<true> : k_gram_sqnorm_wide<false>)<<<grid, W_THREADS, W_SMEM, s>>>(P);
       if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
     }
   }
@@ -1446,7 +1524,7 @@ int launch_umma_sqnorms(const dp_layer* layers, const int* idx, int n, const int
         k_gram_sqnorm<<<grid, G_THREADS, G_SMEM, s>>>(P);
       } else {
         const int units = sm_count() / 2;
-        k_tile_sqnorm_pair<<<2 * (P.total_items < units ? P.total_items : units), T_THREADS, Q_SMEM, s>>>(P);
+        (parts ? k_tile_sqnorm_pair<true> : k_tile_sqnorm_pair<false>)<<<2 * (P.total_items < units ? P.total_items : units), T_THREADS, Q_SMEM, s>>>(P);
       }
       if (counted(1) != cudaSuccess) return DP_ERR_CUDA;
     }

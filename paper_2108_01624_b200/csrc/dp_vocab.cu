@@ -1453,7 +1453,7 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
         }
         float* partial = r.at<float>(p.gram);
         const int count = (int)umma_sqnorm_partials_per_example(layers.data(), idx.data(), subs, way.data());
-        if ((rc = launch_umma_sqnorms(layers.data(), idx.data(), subs, way.data(), partial, count, 0, status, r.s)) != DP_OK) return rc;
+        if ((rc = launch_umma_sqnorms(layers.data(), idx.data(), subs, way.data(), partial, count, 0, status, r.s, true)) != DP_OK) return rc;
         VOCAB_CUDA(launch_chained(k_vocab_norm_sum, (unsigned)ceil_div(h.B, 8), 256, 0, r.s, partial, h.B, count, sqnorm, add));
         if (!p.gram_way && h.bias && p.R == 2) {
           for (int k = 0; k < subs; ++k) cols.push_back({&layers[k], false, r.at<float>(p.cols) + (size_t)k * h.B * p.sub});

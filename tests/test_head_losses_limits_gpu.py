@@ -69,3 +69,12 @@ def norm_errors(B, T, d, V, dtype, bias=True, seed=0):
 def test_norms_of_short_examples_are_right_in_the_mean(B, T, d, V, dtype):
     r = norm_errors(B, T, d, V, dtype)
     assert abs(float(r.mean())) <= 2.0 ** -16, (float(r.mean()), float(r.min()), float(r.max()))
+
+
+# Longer examples: rows of planes beyond 128 go through the layers' norm kernels, whose sums are of the same length here: Grams of
+# both operands (their widths in parts), or the gradient itself (its rows in parts).
+@pytest.mark.parametrize("B, T, d, V, dtype", [(32, 70, 768, 3000, BF16), (32, 33, 768, 3000, F32), (8, 512, 8192, 300, BF16), (3, 70, 65536, 40, F32),
+                                               (8, 512, 96, 3000, BF16), (4, 5000, 64, 500, BF16), (4, 5000, 64, 500, F32), (2, 100000, 16, 40, BF16)])
+def test_norms_of_long_examples_are_right_in_the_mean(B, T, d, V, dtype):
+    r = norm_errors(B, T, d, V, dtype)
+    assert abs(float(r.mean())) <= 2.0 ** -16, (float(r.mean()), float(r.min()), float(r.max()))
