@@ -413,7 +413,8 @@ typedef struct dp_distill {
   int32_t dtype;               /* dp_dtype of logits and dlogits */
   int32_t teacher_dtype;       /* of top_logits */
   int32_t N, V, K;             /* tokens, vocabulary, words of the teacher per token (1 .. 1024) */
-  double temperature;          /* 1e-30 to 1e30 */
+  double temperature;          /* 1e-30 to 1e30.  A loss beyond fp32 is infinite (from 1e19 on, where V > K); its logarithms are held to
+                                  about 10^-6, so where p and q differ by little it has an absolute error of temperature^2 times that */
   const void* logits;          /* row n begins at logits + n * ld (elements) */
   int64_t ld;                  /* >= V; 0 allowed with N = 1 */
   const int32_t* top_ids;      /* [N, K] */

@@ -15,6 +15,7 @@
 
 #include "dp_chain.cuh"
 #include "dp_internal.h"
+#include "dp_ptx.cuh"
 
 namespace dpk {
 
@@ -190,7 +191,7 @@ __global__ void __launch_bounds__(kDistillThreads) k_distill(const __grid_consta
       }
     }
     over_row<WARP, 3>(sum, red_sum, [](int, float x, float y) { return x + y; });
-    if (tid == 0) a.loss[n] = live ? w * a.tau * a.tau * (sum[2] / sum[1] + (logf(sum[0]) - logf(sum[1]))) : 0.0f;
+    if (tid == 0) a.loss[n] = live ? w * a.tau * (a.tau * (sum[2] / sum[1] + (logf(sum[0]) - logf(sum[1])))) : 0.0f;
     if (out) {
       const float c = w * a.tau, cp = c / sum[0], cq = c / sum[1];
       for (int k = tid; k < a.K; k += threads) {
@@ -242,6 +243,16 @@ template <typename T> __device__ __forceinline__ float vector_max(const uint4& d
     const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&d);
     const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
     return fmaxf(__low2float(m), __high2float(m));
+  }
+}
+
+// 2^((x + less) scale) of the elements of a vector, two at a time.
+template <typename T>
+__device__ __forceinline__ void vector_powers(const uint4& d, ptx::f32x2 less, ptx::f32x2 scale, ptx::f32x2 (&e)[8 / sizeof(T)]) {
+#pragma unroll
+  for (int u = 0; u < (int)(8 / sizeof(T)); ++u) {
+    const float2 y = ptx::unpack2(ptx::mul2(ptx::add2(ptx::pack2(lane_of<T>(d, 2 * u), lane_of<T>(d, 2 * u + 1)), less), scale));
+    e[u] = ptx::pack2(exp2_fast(y.x), exp2_fast(y.y));
   }
 }
 
@@ -337,15 +348,19 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
     top = warp_max(lane < warps ? red_max[lane][0] : -INFINITY);
     top_t = warp_max(lane < warps ? red_max[lane][1] : -INFINITY);
     const bool live = top_t != -INFINITY;
-    // powers of two of x log2(e) / tau, less the maximum's, rounded: what it was rounded by is common to a row and falls out
-    const float sub = top == -INFINITY ? 0.0f : -top * a.scale2, sub_t = -top_t * a.scale2;
+    // powers of two of (x - the maximum) log2(e) / tau: the difference first, since the exponents of small temperatures are
+    // large numbers, whose own rounding would be more than fp32 holds as a power
+    const float base = top == -INFINITY ? 0.0f : top;
+    const auto exponent = [&](float x) { return (x - base) * a.scale2; };
+    const ptx::f32x2 less = ptx::pack2(-base, -base), scale = ptx::pack2(a.scale2, a.scale2);
+    const auto exponent_t = [&](float t) { return (t - top_t) * a.scale2; };
     const float w = live ? (a.weights ? a.weights[n] : 1.0f) : 0.0f;
     // sums: of the student's powers, the teacher's, and the teacher's weight times the gap of the two exponents
     float sum_t = 0.0f, gap = 0.0f;
     for (int k = tid; k < a.K; k += threads) {
       const int id = s_id[k];
       if (id < 0) continue;
-      const float y = fmaf(to_float(z[id]), a.scale2, sub), t = fmaf(s_t[k], a.scale2, sub_t), e = exp2_fast(t);
+      const float y = exponent(to_float(z[id])), t = exponent_t(s_t[k]), e = exp2_fast(t);
       sum_t += e;
       if (e != 0.0f) gap += e * (t - y);
       // the same word again adds to its first place (s_q < 0: not the first)
@@ -359,21 +374,24 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
         for (int o = 0; o < a.K; ++o) {
           if (s_id[o] != id) continue;
           first = first && o >= k;
-          q += exp2_fast(fmaf(s_t[o], a.scale2, sub_t));
+          q += exp2_fast(exponent_t(s_t[o]));
         }
         if (!first) q = -1.0f;
       }
       s_y[k] = y;
       s_q[k] = q;
     }
-    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    ptx::f32x2 part[2] = {0ull, 0ull};
 #pragma unroll 2
     for (int v = tid; v < nv; v += threads) {
       const uint4 d = *reinterpret_cast<const uint4*>(rows + v * 16);
+      ptx::f32x2 e[E / 2];
+      vector_powers<T>(d, less, scale, e);
 #pragma unroll
-      for (int u = 0; u < E; ++u) part[u & 3] += exp2_fast(fmaf(lane_of<T>(d, u), a.scale2, sub));
+      for (int u = 0; u < E / 2; ++u) part[u & 1] = ptx::add2(part[u & 1], e[u]);
     }
-    float sum = (part[0] + part[1]) + (part[2] + part[3]);
+    const float2 halves = ptx::unpack2(ptx::add2(part[0], part[1]));
+    float sum = halves.x + halves.y;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (32 * warp < a.K) {
@@ -395,7 +413,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
     if (warp == 0) {
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) gap += __shfl_xor_sync(0xffffffffu, gap, o);
-      if (lane == 0) a.loss[n] = live ? w * a.tau * a.tau * 0.693147181f * (gap / sum_t + (log2f(sum) - log2f(sum_t))) : 0.0f;
+      if (lane == 0) a.loss[n] = live ? w * a.tau * (a.tau * (0.693147181f * (gap / sum_t + (log2f(sum) - log2f(sum_t))))) : 0.0f;
     }
     const Row after = row_of(n + gridDim.x);
     const int nv2 = after.inside ? after.nv : 0;
@@ -412,7 +430,7 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
 #pragma unroll
         for (int u = 0; u < E; ++u) {
           const int e = v * E - off + u;
-          if (e >= 0 && e < a.V) out[e] = from_float<T>(live ? cp * exp2_fast(fmaf(to_float(reinterpret_cast<const T*>(rows + v * 16)[u]), a.scale2, sub)) : 0.0f);
+          if (e >= 0 && e < a.V) out[e] = from_float<T>(live ? cp * exp2_fast(exponent(to_float(reinterpret_cast<const T*>(rows + v * 16)[u]))) : 0.0f);
         }
       };
       if (!same) {
@@ -426,14 +444,21 @@ __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __gri
     int v = tid;
     if (live) {
       uint4* to = reinterpret_cast<uint4*>(out - off);
+      const ptx::f32x2 cp2 = ptx::pack2(cp, cp);
 #pragma unroll 2
       for (; v < nv; v += threads) {
         const uint4 d = *reinterpret_cast<const uint4*>(there + v * 16);
         if (v < nv2) copy(v, from + (size_t)v * 16);   // its place is free: the words have been read, and this was its last time
         if (v >= lo && v < hi) {
+          ptx::f32x2 e[E / 2];
           float g[E];
+          vector_powers<T>(d, less, scale, e);
 #pragma unroll
-          for (int u = 0; u < E; ++u) g[u] = cp * exp2_fast(fmaf(lane_of<T>(d, u), a.scale2, sub));
+          for (int u = 0; u < E / 2; ++u) {
+            const float2 x = ptx::unpack2(ptx::mul2(e[u], cp2));
+            g[2 * u] = x.x;
+            g[2 * u + 1] = x.y;
+          }
           to[v] = packed<T>(g);
         }
       }

@@ -7,7 +7,7 @@ import torch
 import paper_2108_01624_b200 as dp
 from paper_2108_01624_b200.synth import HEAD, LayerSpec
 
-from .test_head_losses_gpu import BF16, DEV, F32, Case, workspace
+from .test_head_losses_gpu import BF16, DEV, F32, Case, check_distill, distill_case, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,12 @@ def test_norms_of_short_examples_are_right_in_the_mean(B, T, d, V, dtype):
 def test_norms_of_long_examples_are_right_in_the_mean(B, T, d, V, dtype):
     r = norm_errors(B, T, d, V, dtype)
     assert abs(float(r.mean())) <= 2.0 ** -16, (float(r.mean()), float(r.min()), float(r.max()))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [300, 5003, 130001])
+@pytest.mark.parametrize("tau", [1e-30, 1e-20, 1e-12, 1e-8, 1e-4, 1e6, 1e15])
+def test_distillation_over_the_range_of_temperatures(tau, V, dtype):
+    """Rows of every form: a warp's, shared memory's, those beyond.  Exponents of up to 10^31, losses from 10^-29 to 10^31."""
+    z, ids, t, w = distill_case(2, 3, V, 6, dtype)
+    check_distill(z, ids, t, tau, w, torch.full_like(z, float("nan")))
