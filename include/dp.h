@@ -421,7 +421,8 @@ typedef struct dp_distill {
   const void* top_logits;      /* [N, K] */
   const float* weights;        /* [N] or NULL for ones */
 } dp_distill;
-/* loss [N] fp32.  dlogits: rows ld_out apart, or NULL where only the loss is wanted; may be logits itself (ld_out = ld). */
+/* loss [N] fp32.  dlogits: rows ld_out apart, or NULL where only the loss is wanted; may be logits itself (ld_out = ld), and otherwise
+ * has no element in common with it (DP_ERR_ARG). */
 DP_API int dp_distill_loss(const dp_distill* p /*HOST*/, float* loss, void* dlogits, int64_t ld_out, void* cuda_stream);
 
 /* Test utility: out[k] = the raw Philox word of element elem_offset + k (lane (e & 3) of block e >> 2). */

@@ -654,7 +654,7 @@ def dp_distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: tor
                     loss: torch.Tensor, dlogits: Optional[torch.Tensor], token_weights: Optional[torch.Tensor] = None,
                     stream=None) -> torch.Tensor:
     """Distillation of logits [B, T, V] from the teacher's K top logits (top_ids int32, top_logits fp32 or bf16, [B, T, K];
-    negative ids are empty places): loss [B, T] fp32 and, unless None, dlogits like logits (which may be logits itself)."""
+    negative ids are empty places): loss [B, T] fp32 and, unless None, dlogits like logits (which may be logits itself, but not overlap it otherwise)."""
     rc = (_module or _native()).distill_loss(logits, top_ids, top_logits, temperature, loss, dlogits, token_weights,
                                              None if stream is None else stream.cuda_stream)
     if rc:

@@ -1,8 +1,12 @@
 """The vocabulary head's losses at the ends of their ranges, without a GPU: index arithmetic of the kernels at the largest sizes
 that the calls take (which are not run), by their source and the limits of the calls."""
+import ctypes as C
 import os
 import re
 
+import pytest
+
+from paper_2108_01624_b200 import binding as b
 from paper_2108_01624_b200 import build as builder
 
 MOST_TOKENS, MOST_WORDS = 1 << 26, 1 << 26           # of a head; its calls refuse more
@@ -31,3 +35,14 @@ def test_the_cross_terms_tasks_fit_their_counter():
     loops = re.findall(r"for \(([\w ]+) task = blockIdx\.x; task < a\.all; task \+= a\.chunks\)", text)
     assert len(loops) == 2 and "all > 0x7fffffffll" in text
     assert all(2 ** 31 - 1 + 64 <= LIMIT[t] for t in loops)
+
+
+@pytest.mark.parametrize("N, ld, at, ld_out", [
+    (6, 500, 2, 500), (6, 500, 998, 500), (6, 500, 500 * 10 + 998, 500), (6, 512, 1024 - 998, 512), (6, 512, -2, 512),   # a row ahead or behind
+    (6, 1100, 1202, 1100), (6, 1100, 1200, 550), (1, 0, 998, 0), (1, 7000, -998, 9000), (6, 500, 0, 1000), (6, 1000, 2 * 500 * 5, 500)])
+def test_distillation_refuses_rows_that_overlap_others(N, ld, at, ld_out):
+    """Rows of 500 bf16 words; dlogits `at` bytes behind logits.  In place, or beside them, is allowed; in part over them is not."""
+    builder.build()
+    P = 1 << 20
+    p = b.dp_distill(1, 0, N, 500, 8, 2.0, P, ld, P, P, P)
+    assert b.lib().dp_distill_loss(C.byref(p), P, P + at, ld_out, None) == -1

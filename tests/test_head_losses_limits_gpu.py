@@ -87,3 +87,18 @@ def test_distillation_over_the_range_of_temperatures(tau, V, dtype):
     """Rows of every form: a warp's, shared memory's, those beyond.  Exponents of up to 10^31, losses from 10^-29 to 10^31."""
     z, ids, t, w = distill_case(2, 3, V, 6, dtype)
     check_distill(z, ids, t, tau, w, torch.full_like(z, float("nan")))
+
+
+@pytest.mark.parametrize("V", [300, 6000, 130001])
+def test_distilled_rows_beside_the_logits(V):
+    """Logits and their gradient as columns of one buffer, and in every other row of one: no element in common."""
+    z, ids, t, w = distill_case(2, 3, V, 7, BF16)
+    wide = torch.full((2, 3, 2 * V), 5.0, dtype=BF16, device=DEV)
+    wide[..., V:] = z
+    check_distill(wide[..., V:], ids, t, 2.0, w, wide[..., :V])
+    rows = torch.full((2, 6, V), 5.0, dtype=BF16, device=DEV)
+    rows[:, ::2] = z
+    check_distill(rows[:, ::2], ids, t, 2.0, w, rows[:, 1::2])
+    assert torch.equal(rows[:, ::2].nan_to_num(), z.nan_to_num()) and torch.equal(wide[..., V:].nan_to_num(), z.nan_to_num())
+    with pytest.raises(dp.binding.DpError):
+        dp.dp_distill_loss(wide[..., V:], ids, t, 2.0, torch.empty(2, 3, device=DEV), wide[..., 1:V + 1])
