@@ -262,7 +262,7 @@ __device__ __forceinline__ void vector_powers(const uint4& d, ptx::f32x2 less, p
 template <typename T>
 __global__ void __launch_bounds__(kDistillThreads, 3) k_distill_rows(const __grid_constant__ DistillArgs a, int row_bytes) {
   constexpr int E = 16 / sizeof(T);              // elements of a vector
-  extern __shared__ uint8_t rows[];
+  extern __shared__ __align__(16) uint8_t rows[];
   __shared__ float red_max[16][2];
   __shared__ float red_sum[16][4];
   wait_for_predecessor();

@@ -199,8 +199,8 @@ __global__ void __launch_bounds__(256) k_vocab_cross(const __grid_constant__ Cro
           }
       }
       sum += cross_finish<NT>(a, i, id, t0, q, cz, ck);
-  }
-  cross_store(a, i, sum, red);
+    }
+    cross_store(a, i, sum, red);
   }
 }
 
@@ -215,7 +215,7 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
 
 template <int NT>
 __global__ void __launch_bounds__(256) k_vocab_cross_lines(const __grid_constant__ CrossArgs a) {
-  extern __shared__ uint8_t smem[];
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float red[8];
   wait_for_predecessor();
   let_successor_in();
@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(256) k_vocab_cross_lines(const __grid_constant
           }
       }
       sum += cross_finish<NT>(a, i, id, t0, q, cz, ck);
-  }
-  cross_store(a, i, sum, red);
+    }
+    cross_store(a, i, sum, red);
   }
 }
 

@@ -46,3 +46,10 @@ def test_distillation_refuses_rows_that_overlap_others(N, ld, at, ld_out):
     P = 1 << 20
     p = b.dp_distill(1, 0, N, 500, 8, 2.0, P, ld, P, P, P)
     assert b.lib().dp_distill_loss(C.byref(p), P, P + at, ld_out, None) == -1
+
+
+def test_shared_arrays_that_are_copied_to_by_16_bytes_say_so():
+    """cp.async writes 16 aligned bytes; bulk copies into swizzled tiles start where the kernel has aligned to 1024 bytes itself."""
+    for f in ("dp_vocab.cu", "dp_vocab_cross.cu", "dp_distill.cu"):
+        for align, name, after in re.findall(r"extern __shared__ (.*?)uint8_t (\w+)\[\];(.{600})", source(f), re.S):
+            assert "__align__(16)" in align or f"({name}) + 1023) & ~uintptr_t(1023)" in after, (f, name)
