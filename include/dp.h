@@ -352,7 +352,9 @@ DP_API int dp_qknorm_rope_backward(const dp_qknorm* p /*HOST*/, const dp_heads* 
  * more counts as none and is reported by dp_poll_status (DP_ERR_BAD_ID).
  * bias and weights are fp32; entries of bias may be -inf (a word that cannot occur).  Infinite or NaN logits of a
  * token with a label make what depends on it NaN.
- * Sums are fp32, in an order that only the sizes and the device decide; the label's logit is formed in fp64.  With bf16 X
+ * Sums are fp32, in an order that only the sizes and the device decide; the label's logit is formed in fp64 (in
+ * dp_vocab_loss_cross_sqnorms in fp32 like the others).  G follows from the lse that is handed over, an fp32 number: its rounding moves
+ * every exponential by up to ulp(lse) / 2 of itself, and so G at the label, however sure the model is, by that times the weight.  With bf16 X
  * and W the products are exact; G is rounded to 2^-16 of each element before it is summed over tokens, to 2^-8 where it
  * forms a bf16 dX.  With fp32 X and W operands carry 24 bits in z and 16 in the products with G. */
 typedef struct dp_vocab_head {

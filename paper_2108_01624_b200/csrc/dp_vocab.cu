@@ -16,9 +16,10 @@
 //
 // Exactness.  A product of bf16 numbers is exact in fp32 and the tensor cores sum in fp32, but drop low bits at every
 // step of 16: a sum of 64 steps comes out 7e-7 too small.  So
-//   - a sum longer than `seg` blocks is taken over by the epilogue, which adds its parts in registers;
-//   - the label's own logit is formed by itself, in fp64: loss = w log1p(exp(lse of the others - z_label)) and
-//     G_label = w expm1(z_label - lse) keep their relative error where the model is sure of the label;
+//   - a sum longer than `seg` blocks is taken over by the epilogue, which adds its parts in registers (norms: every 32 steps);
+//   - the label's own logit is formed by itself, in fp64: loss = w log1p(exp(lse of the others - z_label)) keeps its relative error
+//     where the model is sure of the label.  G_label = w expm1(z_label - lse) does so for the lse that it is given, an fp32 number:
+//     with one that dp_vocab_loss has rounded, every G is off by up to ulp(lse) / 2 of its exponential, G_label by that times w;
 //   - G is held as two bf16 numbers, hi + lo, to 2^-16 of it: rows (token, plane) of G meet rows (token, plane) of X in the
 //     sums over tokens, whose results are fp32.  dX in bf16 reads hi alone: its own rounding is as large.
 //   - fp32 X and W are split into three bf16 numbers each for the logits (24 bits; six products, the smallest first) and

@@ -102,3 +102,34 @@ def test_distilled_rows_beside_the_logits(V):
     assert torch.equal(rows[:, ::2].nan_to_num(), z.nan_to_num()) and torch.equal(wide[..., V:].nan_to_num(), z.nan_to_num())
     with pytest.raises(dp.binding.DpError):
         dp.dp_distill_loss(wide[..., V:], ids, t, 2.0, torch.empty(2, 3, device=DEV), wide[..., 1:V + 1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_gradient_from_the_losss_own_lse(dtype):
+    """Chained through an fp32 lse, every exponential moves by what that is off, G at the label of a token that the model is sure of by
+    as much in absolute terms: against the definition from the logits alone."""
+    c = Case(4, 16, 256, 500, dtype, sure=6.0, dead=0.1, bias=False, weights=False)
+    head = c.head()
+    ws, loss, lse = workspace(head), torch.empty(4, 16, device=DEV), torch.empty(4, 16, device=DEV)
+    dx, sq = torch.empty_like(c.x), torch.empty(4, device=DEV)
+    acc_w = torch.zeros(500, 256, device=DEV)
+    dp.dp_vocab_loss(head, loss, lse, workspace=ws)
+    dp.dp_vocab_loss_backward(head, lse, dx, sq, workspace=ws)
+    dp.dp_vocab_loss_clipped_accumulate(head, lse, torch.ones(4, device=DEV), acc_w, workspace=ws)
+    p = (c.z - c.lse64[..., None]).exp()
+    y = torch.zeros_like(p).scatter_(-1, c.labels.clamp(min=0).long()[..., None], 1.0)
+    # 1 - p at the label as the sum of the others
+    others = torch.where(y > 0, 0.0, p).sum(-1, keepdim=True)
+    G = c.w[..., None] * torch.where(y > 0, -others, p)
+    assert 0 < float(others[c.live].min()) < 1e-7
+    moved = (c.dz.amax(-1) + 2.0 ** -20 + 2.0 ** -23 * c.lse64.abs()).expm1()[..., None]          # of the lse, as its own test bounds it
+    dG = c.w[..., None] * p * (moved + torch.where(y > 0, 2.0 ** -20, c.dz.expm1() + 2.0 ** -20))
+    w, x = c.weight.double(), c.xd.flatten(0, 1)
+    r = 2 * 2.0 ** -16 if dtype == F32 else 2.0 ** -8
+    ref = G @ w
+    tol = dG @ w.abs() + (r + 2.0 ** -15) * ((G.abs() + dG) @ w.abs()) + (2.0 ** -24 if dtype == F32 else 2.0 ** -8) * ref.abs()
+    assert bool(((dx.double() - ref).abs() <= 1.02 * tol + 1e-37).all())
+    G, dG = G.flatten(0, 1), dG.flatten(0, 1)
+    ref = G.t() @ x
+    tol = dG.t() @ x.abs() + ((2 if dtype == F32 else 1) * 2.0 ** -16 + 2.0 ** -15) * ((G.abs() + dG).t() @ x.abs()) + 2.0 ** -23 * ref.abs()
+    assert bool(((acc_w.double() - ref).abs() <= 1.02 * tol).all())
