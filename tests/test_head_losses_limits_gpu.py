@@ -133,3 +133,18 @@ def test_a_gradient_from_the_losss_own_lse(dtype):
     ref = G.t() @ x
     tol = dG.t() @ x.abs() + ((2 if dtype == F32 else 1) * 2.0 ** -16 + 2.0 ** -15) * ((G.abs() + dG).t() @ x.abs()) + 2.0 ** -23 * ref.abs()
     assert bool(((acc_w.double() - ref).abs() <= 1.02 * tol).all())
+
+
+# Three blocks of G, two of which fill a piece of at most 1 GiB, the last piece one: dX, norms and sums over unequal pieces.  Short
+# examples, and long ones by either kernel with their bias apart (bf16) or as a column (fp32); widths that are no multiple of 4 and 8.
+@pytest.mark.parametrize("B, T, d, dtype, bias", [(2800, 9, 18, F32, True), (252, 100, 24, F32, True), (2500, 20, 20, BF16, False), (500, 100, 18, BF16, True),
+                                                  (715, 70, 264, BF16, True)])
+def test_unequal_pieces_of_the_vocabulary(B, T, d, dtype, bias):
+    c = Case(B, T, d, 6000, dtype, bias=bias, dead=0.2)
+    head = c.head()
+    rows = (4 if dtype == F32 else 2) * B * T
+    assert 2 <= (1 << 30) // (rows * 2048 * 2) < 3 and dp.dp_vocab_workspace_bytes(head) < 2 << 30
+    c.check_backward(sq0=torch.rand(B, device=DEV))
+    c.check_backward(out=torch.zeros(B, T, d + 3, dtype=dtype, device=DEV)[..., :d])
+    c.check_sum()
+    assert dp.dp_poll_status() == 0
