@@ -372,7 +372,8 @@ typedef struct dp_vocab_head {
  * are copied into the workspace first. */
 
 /* Bytes of scratch for the calls below; 0 on invalid sizes.  It holds G for a piece of the vocabulary (1 GiB at most, more only
- * where B * T * 2048 entries of G take more) and, where X or W are copied, their copies. */
+ * where B * T * 2048 entries of G take more), X in rows of planes, parts of the tiles that several SMs share (37 MiB, also of the smallest head)
+ * and, where X or W are copied, their copies: of W 2 bytes an entry in bf16, 6 in fp32, written anew by every call. */
 DP_API size_t dp_vocab_workspace_bytes(const dp_vocab_head* head /*HOST*/);
 
 /* loss[B, T] = weights * (lse - z[label]), lse[B, T] = log of the sum over v of exp z; fp32. */

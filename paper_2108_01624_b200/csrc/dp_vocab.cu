@@ -567,8 +567,9 @@ __global__ void __launch_bounds__(V_THREADS, 1) k_vocab_gemm(const __grid_consta
 // The tiles of a DX or DW launch that several pairs shared: their parts are added, in an order that the sizes decide.  Block (t, r):
 // tile t of those that were shared, 16 / STRANDS rows from (r / 4) of them on, columns [64 (r % 4), +64).  Strands of threads take a run
 // of the parts each; a warp reads 4 rows, 8 groups of four columns (64 bytes of a slot, 128 of a result at a time).  One strand where
-// a tile has few parts (two or three each: four strands are four times the blocks, most of whose threads idle), four where many (37:
-// 9.9 us, one strand 11.8).
+// a tile has up to eight parts (four strands are four times the blocks, most of whose threads idle), four where more: gradients of width
+// 1024, 10000 words with one / four strands, replayed: 256 tokens (18 parts a tile) 51 / 44 us, 512 (9 parts) 55.5 / 55.3, 768 (6 parts) 60.4 /
+// 61.1, 2048 (2 parts) 104 / 112.
 template <int MODE, int STRANDS>
 __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VParams P) {
   constexpr int OUTPUTS = 256 / STRANDS, ROWS = 16 / STRANDS;
@@ -1051,7 +1052,10 @@ static bool encode_blocks(CUtensorMap* map, const void* base, long long rows, in
   return encode(map, base, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-constexpr size_t kPartBytes = (size_t)256 << 20;    // maxima and sums of the column blocks that are joined at a time
+// Maxima and sums of the column blocks that are joined at a time.  Beyond it a product ends and begins, and its tail waits for the join:
+// the loss of 2000 x 100 tokens of width 64, 30522 words (all of it 765 MB) takes 3909 us with 64 MiB, 3728 with 128, 3658 with 256, 3594 with
+// 512, 3598 in one.
+constexpr size_t kPartBytes = (size_t)256 << 20;
 constexpr int kSubColumns = 2048;               // columns of one block of G, at most
 // G of one piece, unless one block alone is larger.  Every piece costs the start and the end of three kernels and another pass
 // over the sums of dX: 256 x 20 tokens of width 1024, 30522 words, gradient / clipped sum with pieces of 128 MiB 1048 / 987 us, 256 MiB
@@ -1217,7 +1221,10 @@ static int logits_operands(const VRun& r, VParams& P, int v0, int rows) {
   return DP_OK;
 }
 
-// Pairs that share a line of K blocks: all, or fewer where a share would be shorter than four (one pair for fewer).
+// Pairs that share a line of K blocks: all, or fewer where a share would be shorter than four (one pair for fewer).  Small heads only, and
+// no length is best for all: with shares of 1 / 2 / 4 / 8 blocks at least, replayed, the gradient of 16 x 20 bf16 tokens of width 512, 5003
+// words takes 35 / 35 / 31 / 33 us, of 30 x 20 of width 1024, 300 words 35 / 38 / 48 / 50, the sum of 4 x 20 of width 256, 2000 words
+// 29 / 25 / 29 / 38, of 2 x 60 of width 64, 20011 words 38 / 34 / 34 / 43.
 static int share_units(long long line) {
   const long long most = sm_count() / 2;
   return (int)std::max<long long>(1, std::min<long long>(most, line / 4));

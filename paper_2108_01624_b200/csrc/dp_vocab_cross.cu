@@ -354,7 +354,11 @@ static cudaError_t launch_lines(const CrossArgs& a, int nt, cudaStream_t s) {
 int launch_vocab_cross(const dp_vocab_head& h, const float* lse, const int32_t* ids, const void* G_emb, long long ld_emb, int Tu,
                        float* sqnorm, float* partial, int* status, cudaStream_t s) {
   const bool f32 = h.dtype == DP_F32;
-  const int nt = h.T <= 8 ? 1 : h.T <= 24 ? 3 : 4;        // 8, 24 or 32 tokens a pass over the inputs' rows
+  // 8, 24 or 32 tokens a pass over the inputs' rows: as few passes as registers allow, no more columns than they need.  256 x 128 inputs,
+  // width 1024, bf16, us with 8 / 24 / 32 a pass, replayed: 8 tokens 22 / 25 / 32, 9 tokens 41 / 26 / 32, 24 tokens 62 / 30 / 35, 25 tokens
+  // 80 / 54 / 36, 64 tokens 142 / 84 / 73; from 33 to 48 twice 24 would be better than twice 32 (57 for 69).  In fp32 8 a pass would also be
+  // where blocks are few (64 x 128 inputs, width 256: 9 tokens 16 / 21 / 23, 32 tokens 17 / 24 / 27).
+  const int nt = h.T <= 8 ? 1 : h.T <= 24 ? 3 : 4;
   CrossArgs a = {h.X, h.W, G_emb, h.bias, h.labels, h.weights, lse, ids, sqnorm, h.ldx, h.ldw, ld_emb, h.B, h.T, Tu, h.d, h.V};
   a.t_chunks = (unsigned)ceil_div(h.T, 8 * nt);
   const long long all = (long long)ceil_div(Tu, 128) * a.t_chunks;
