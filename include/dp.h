@@ -380,7 +380,7 @@ DP_API size_t dp_vocab_workspace_bytes(const dp_vocab_head* head /*HOST*/);
 DP_API int dp_vocab_loss(const dp_vocab_head* head /*HOST*/, float* loss, float* lse, void* workspace, size_t workspace_bytes,
                          void* cuda_stream);
 
-/* From the lse of dp_vocab_loss: dX = G W (rows of leading dimension ld_dx; of dtype; may not overlap X), and
+/* From the lse of dp_vocab_loss: dX = G W (rows of leading dimension ld_dx; of dtype; no element in common with X: DP_ERR_ARG), and
  *   sqnorm[i] = or += |G_i^T X_i|^2 + (with bias) |sum_t G_i|^2,
  * the squared norm of example i's gradients of W and bias.  dX or sqnorm may be NULL.  Tensor-core sums drop low bits: a
  * squared norm comes out too small in the mean over examples, by 1 to 5 10^-6 of itself (1.6e-6 at 256 x 20 tokens of width 1024 and 30522

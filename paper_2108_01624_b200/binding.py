@@ -621,7 +621,7 @@ def dp_vocab_loss(head: VocabHead, loss: torch.Tensor, lse: torch.Tensor, worksp
 
 def dp_vocab_loss_backward(head: VocabHead, lse: torch.Tensor, dx: Optional[torch.Tensor], sqnorm: Optional[torch.Tensor],
                            accumulate_into: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    """dx like x (may be a view with evenly spaced rows) and sqnorm [B] = or += every example's squared norm of the gradients
+    """dx like x (may be a view with evenly spaced rows, but not lie over x) and sqnorm [B] = or += every example's squared norm of the gradients
     of table and bias; either may be None."""
     rc = (_module or _native()).vocab_loss_backward(head.native, lse, dx, sqnorm, accumulate_into, workspace,
                                                     None if stream is None else stream.cuda_stream)

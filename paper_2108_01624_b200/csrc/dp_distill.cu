@@ -511,23 +511,6 @@ static cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s) {
   return launch_chained(k_distill_rows<T>, grid, threads, smem, s, a, (int)row_bytes);
 }
 
-// Whether a row [a + n lda, + width) meets a row [b + m ldb, + width), n, m < N (bytes).  Rows beside one another, of one buffer's columns
-// say, do not.
-static bool rows_meet(const void* first, __int128 lda, const void* second, __int128 ldb, long long N, long long width) {
-  const __int128 a = (intptr_t)first, b = (intptr_t)second;
-  if (a + (N - 1) * lda + width <= b || b + (N - 1) * ldb + width <= a) return false;
-  if (lda == ldb) {                              // the nearest row before and behind
-    const __int128 d = b - a, k = (d >= 0 ? d : d - lda + 1) / lda, left = d - k * lda;
-    return (left < width && k < N && k > -N) || (lda - left < width && k + 1 < N && k + 1 > -N);
-  }
-  for (long long n = 0, m = 0; n < N && m < N;) {
-    if (a + n * lda + width <= b + m * ldb) ++n;
-    else if (b + m * ldb + width <= a + n * lda) ++m;
-    else return true;
-  }
-  return false;
-}
-
 }  // namespace dpk
 
 using namespace dpk;
@@ -544,9 +527,7 @@ extern "C" int dp_distill_loss(const dp_distill* p, float* loss, void* dlogits, 
   const size_t e = p->dtype == DP_F32 ? 4 : 2;
   if (misaligned(p->logits, e) || misaligned(dlogits, e) || misaligned(p->top_ids, 4) || misaligned(loss, 4) ||
       misaligned(p->weights, 4) || misaligned(p->top_logits, p->teacher_dtype == DP_F32 ? 4 : 2)) return DP_ERR_ALIGN;
-  const long long size = (long long)e;
-  if (dlogits && dlogits != p->logits &&
-      rows_meet(p->logits, (__int128)ld * size, dlogits, (__int128)ldo * size, p->N, p->V * size)) return DP_ERR_ARG;
+  if (dlogits && dlogits != p->logits && rows_meet(p->logits, ld, dlogits, ldo, p->N, p->V, (int)e)) return DP_ERR_ARG;
   int* status = status_ptr();
   if (!status) return DP_ERR_CUDA;
   const DistillArgs a = {p->logits, p->top_ids, p->top_logits, p->weights, loss, dlogits, ld, ldo, p->N, p->V, p->K,

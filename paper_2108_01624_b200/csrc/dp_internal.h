@@ -127,6 +127,24 @@ int* status_ptr();
 bool use_gram(const dp_layer& L);
 static inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
+// Whether one of the N rows of so many elements of `size` bytes that lie ld_first elements apart from `first` on meets one of those ld_second apart
+// from `second` on.  Rows beside one another, of one buffer's columns say, do not.
+static inline bool rows_meet(const void* first, long long ld_first, const void* second, long long ld_second, long long N, long long elements, int size) {
+  const __int128 a = (intptr_t)first, b = (intptr_t)second, lda = (__int128)ld_first * size, ldb = (__int128)ld_second * size;
+  const long long width = elements * size;
+  if (a + (N - 1) * lda + width <= b || b + (N - 1) * ldb + width <= a) return false;
+  if (lda == ldb) {                              // the nearest row before and behind
+    const __int128 d = b - a, k = (d >= 0 ? d : d - lda + 1) / lda, left = d - k * lda;
+    return (left < width && k < N && k > -N) || (lda - left < width && k + 1 < N && k + 1 > -N);
+  }
+  for (long long n = 0, m = 0; n < N && m < N;) {
+    if (a + n * lda + width <= b + m * ldb) ++n;
+    else if (b + m * ldb + width <= a + n * lda) ++m;
+    else return true;
+  }
+  return false;
+}
+
 // The cross term of a shared table (dp_vocab_cross.cu); partial: B * kCrossChunks floats.
 constexpr int kCrossChunks = 64;
 int launch_vocab_cross(const dp_vocab_head& h, const float* lse, const int32_t* ids, const void* G_emb, long long ld_emb, int Tu,

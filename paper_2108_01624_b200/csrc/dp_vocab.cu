@@ -1357,6 +1357,7 @@ int dp_vocab_loss_backward(const dp_vocab_head* head, const float* lse, void* dx
   if (misaligned(lse, 4) || misaligned(sqnorm, 4) || misaligned(dx, h.dtype == DP_F32 ? 4 : 2)) return DP_ERR_ALIGN;
   VPlan p;
   if ((rc = check_call(head, 1, workspace, workspace_bytes, &p)) != DP_OK) return rc;
+  if (dx && rows_meet(h.X, h.ldx, dx, ld_dx, (long long)h.B * h.T, h.d, h.dtype == DP_F32 ? 4 : 2)) return DP_ERR_ARG;
   int* status = status_ptr();
   if (!status || !vocab_kernels_ready()) return DP_ERR_CUDA;
   const VRun r = {h, p, static_cast<char*>(workspace), static_cast<cudaStream_t>(cuda_stream), status};

@@ -53,3 +53,12 @@ def test_shared_arrays_that_are_copied_to_by_16_bytes_say_so():
     for f in ("dp_vocab.cu", "dp_vocab_cross.cu", "dp_distill.cu"):
         for align, name, after in re.findall(r"extern __shared__ (.*?)uint8_t (\w+)\[\];(.{600})", source(f), re.S):
             assert "__align__(16)" in align or f"({name}) + 1023) & ~uintptr_t(1023)" in after, (f, name)
+
+
+@pytest.mark.parametrize("at, ld", [(0, 64), (0, 80), (64, 64), (-2, 64), (30 * 128, 64), (126, 128)])
+def test_the_states_gradient_may_not_lie_over_them(at, ld):
+    """The clipped sum reads the states again.  31 rows of 64 bf16 numbers, dX `at` bytes behind X."""
+    builder.build()
+    P = 1 << 20
+    h = b.dp_vocab_head(1, 31, 1, 64, 1000, P, 64, P, 64, None, P, None)
+    assert b.lib().dp_vocab_loss_backward(C.byref(h), P, P + at, ld, P, 0, P, 1 << 40, None) == -1
