@@ -348,8 +348,9 @@ DP_API int dp_qknorm_rope_backward(const dp_qknorm* p /*HOST*/, const dp_heads* 
  * (accumulate_into = 1) before dp_clip_factors; dp_vocab_loss_clipped_accumulate.  Where the table is the token
  * embedding too, dp_vocab_loss_cross_sqnorms adds the inner product of the two parts of its gradient, and acc_w is the
  * accumulator of the embedding layer.
- * A token whose label is negative has no loss: its rows of X may hold anything, its loss, lse and dX are 0.  A label of V or
- * more counts as none and is reported by dp_poll_status (DP_ERR_BAD_ID).
+ * A token whose label is negative has no loss: its rows of X may hold anything, its loss, lse and dX are 0 (it is computed like the
+ * others: a head with few labels is best given those positions alone).  A label of V or more counts as none and is
+ * reported by dp_poll_status (DP_ERR_BAD_ID).
  * bias and weights are fp32; entries of bias may be -inf (a word that cannot occur).  Infinite or NaN logits of a
  * token with a label make what depends on it NaN.
  * Sums are fp32, in an order that only the sizes and the device decide; the label's logit is formed in fp64 (in

@@ -11,7 +11,7 @@
 // All are bound by the tensor cores where there are enough tokens (256 x 20 tokens of width 1024 and 30522 words are 0.32
 // TFLOP a product), and by reading the table where there are few.  There, alone: LSE 204 us (1.57 PFLOP/s, tensor pipe 86 % of the
 // time), GRAD 272 (it writes 625 MB of G besides: without its stores 221), DX 210 (1.52 PFLOP/s), DW 417 (both planes of G: 1.53), the norms
-// 110 (6.2 TB/s); back to back under the power cap 10 to 25 % longer.  Copies of 128 columns: stages of 64 with twice as many in
+// 113 (6.1 TB/s); back to back under the power cap 10 to 25 % longer.  Copies of 128 columns: stages of 64 with twice as many in
 // flight took 230 us in LSE, and a forwarding warp in the odd CTA instead of one barrier for the pair's copies 10 more.
 //
 // Exactness.  A product of bf16 numbers is exact in fp32 and the tensor cores sum in fp32, but drop low bits at every
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(256) k_vocab_join(const __grid_constant__ VPar
 // that no width makes a sum longer (one sum of X's: 2.8e-4 of a squared norm lost at width 65536, 4e-6 now).  What the tensor core
 // drops makes norms too small: at 256 x 20 tokens of width 1024 and 30522 words by 3.2e-6 in the mean with 8 stages, 1.6e-6 with 4, 0.8e-6 with
 // 2, 0.4e-6 with 1 (in fp32 throughout 2e-7 to either side), and the norms with GRAD take 416, 418, 423 and 431 us replayed.
-// Bound by reading G: 110 us for 625 MB, where the layers' kernel with one example at a time took 318.
+// Bound by reading G: 113 us for 625 MB, where the layers' kernel with one example at a time took 318.
 // =================================================================================================
 constexpr int N_STAGES = 6, N_STAGE_BYTES = 2 * V_BOX_BYTES;    // 128 rows x 128 columns
 constexpr int N_THREADS = 192;                                  // warp 0 TMA, warp 1 UMMA, warps 2..5 epilogue
