@@ -169,9 +169,10 @@ class ShardedUpdate:
             torch.cuda.synchronize(self.state.acc.device)
 
     def _agreed_status(self) -> int:
-        """This rank's device status, then the worst over all ranks, so that every rank takes the same branch
-        (a rank that stopped alone would leave the others waiting in the collectives)."""
-        code = int(self.poll_fn())
+        """This rank's device status (DP_ERR_CUDA where a microbatch failed among its clipped sums), then the worst over all
+        ranks, so that every rank takes the same branch (a rank that stopped alone would leave the others waiting in
+        the collectives)."""
+        code = int(self.poll_fn()) or (-4 if getattr(self.state, "spoilt", False) else 0)
         t = torch.tensor([code], dtype=torch.int32, device=self.state.acc.device if self.nccl else "cpu")
         self.dist.all_reduce(t, op=self.dist.ReduceOp.MIN)       # status codes are <= 0
         return int(t.item())
@@ -275,9 +276,11 @@ class ShardedUpdate:
     def finish_macro_batch(self, check_status: bool = True):
         """Ends the macro-batch on every rank (collective call).  With check_status, a device-side error on ANY
         rank since the last poll makes every rank discard its accumulator and raise before anything is applied."""
+        s = self.state
         if check_status:
             self._check_or_discard()
-        s = self.state
+        elif hasattr(s, "refuse_if_spoilt"):
+            s.refuse_if_spoilt()
         s.t += 1
         if self.peer_acc is not None:
             self._finish_fused()

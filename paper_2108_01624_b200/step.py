@@ -115,6 +115,7 @@ class DPStep:
         self.theta = self.theta_store[:pos] if theta is None else theta
         self.t = 0
         self.examples_seen = 0
+        self.spoilt = False             # a microbatch failed while its clipped sums were added: some are in acc
         # gradient-SNR of Section 5.2.1: (sum acc^2, sum noise^2) of the last macro-batch, filled by the fused pass
         self.sq_sums = torch.zeros(2, dtype=torch.float64, device=self.device) if track_snr else None
         self._ws = None
@@ -233,6 +234,7 @@ class DPStep:
         gradients for the clip.  accumulate_microbatch, which wants every HEAD spec's call before it, adds its clipped sum, so
         the head's tensors and lse stay as they are until then.  Again for the same spec, or with another number of examples: the
         microbatch begins anew."""
+        self.refuse_if_spoilt()
         sp = self.specs[li]
         if sp.kind != HEAD:
             raise ValueError(f"spec {li} is no HEAD")
@@ -250,8 +252,11 @@ class DPStep:
         `layers` is a LayerList, or a list of them (layer_lists) when token counts differ between layers; `rows` is the
         row_list of the microbatch, needed exactly when there are ROWS specs (an example's norm runs over ALL its
         tensors: one left out would break the bound that the noise is calibrated to).
-        What does not fit together is refused before the first norm, and can be passed again corrected; a call that fails later
-        leaves norms half summed, and the microbatch begins anew with the HEAD specs' head_backward."""
+        What does not fit together is refused before the first norm, and can be passed again corrected.  A call that fails later
+        leaves norms half summed: the microbatch begins anew with the HEAD specs' head_backward.  One that fails among the clipped
+        sums leaves some of them in the accumulator, where a second try would add them again, beyond C: nothing but
+        discard_macro_batch is taken then."""
+        self.refuse_if_spoilt()
         lists = [layers] if isinstance(layers, b.LayerList) else list(layers)
         lists = [ll for ll in lists if len(ll)]
         heads = dict(sorted(self._heads.items()))
@@ -297,6 +302,7 @@ class DPStep:
         if rows is not None:
             b.dp_rows_sqnorms(rows, self._sqnorm, bool(lists) or bool(heads), stream)
         b.dp_clip_factors(self._sqnorm, self.C, self._clip, stream)
+        self.spoilt = True                            # until all of the sums are added
         for k, ll in enumerate(lists):
             b.dp_clipped_accumulate_after_sqnorms(ll, self._clip, self._ws[k], stream)
         for li, (head, lse) in heads.items():
@@ -305,6 +311,7 @@ class DPStep:
                                                self._head_workspace(head, stream), stream)
         if rows is not None:
             b.dp_rows_clipped_accumulate(rows, self._clip, stream)
+        self.spoilt = False
         self.examples_seen += B
         return self._sqnorm, self._clip
 
@@ -314,6 +321,11 @@ class DPStep:
             self.acc.zero_()
         self._heads = {}
         self.examples_seen = 0
+        self.spoilt = False
+
+    def refuse_if_spoilt(self) -> None:
+        if self.spoilt:
+            raise RuntimeError("a microbatch failed while its clipped sums were added to the accumulator: discard_macro_batch() first")
 
     def check_device_status(self, stream=None) -> None:
         """Waits for the stream and reads the library's sticky status word.  A bounded wait that ran out or a token
@@ -333,6 +345,7 @@ class DPStep:
         accumulator is cleared."""
         if check_status:
             self.check_device_status(stream)
+        self.refuse_if_spoilt()
         N = self.examples_seen if batch_size is None else batch_size
         self.t += 1
         if self.max_grad_norm is not None:

@@ -78,7 +78,7 @@ def test_what_is_refused_is_refused_before_the_first_norm(monkeypatch):
     assert torch.equal(calls.seen, torch.full((4,), 9.0)) and step.examples_seen == 4
 
 
-@pytest.mark.parametrize("name", ["dp_per_example_sqnorms", "dp_vocab_loss_cross_sqnorms", "dp_clip_factors", "dp_vocab_loss_clipped_accumulate"])
+@pytest.mark.parametrize("name", ["dp_per_example_sqnorms", "dp_vocab_loss_cross_sqnorms", "dp_clip_factors"])
 def test_a_microbatch_that_fails_midway_wants_its_heads_again(monkeypatch, name):
     step, calls, emb, fc = make(monkeypatch)
     step.head_backward(2, Head(), None, None)
@@ -237,3 +237,47 @@ def test_what_ends_a_macro_batch_stays_on_its_stream(monkeypatch):
     with pytest.raises(step_module.DeviceStatusError):
         steps[0].finish_macro_batch(4, stream="s")
     assert outside == []
+
+
+def test_a_microbatch_that_fails_while_its_sums_are_added_spoils_the_macro_batch(monkeypatch):
+    """Some of its contributions are in the accumulator: passed again they would be there twice, beyond C."""
+    step, calls, emb, fc = make(monkeypatch)
+    for name in ("dp_clipped_accumulate_after_sqnorms", "dp_vocab_loss_clipped_accumulate"):
+        step.head_backward(2, Head(), None, None)
+        calls.fails = name
+        with pytest.raises(RuntimeError, match=name):
+            step.accumulate_microbatch(Layers([emb, fc]))
+        calls.fails = None
+        with pytest.raises(RuntimeError, match="discard_macro_batch"):
+            step.head_backward(2, Head(), None, None)
+        with pytest.raises(RuntimeError, match="discard_macro_batch"):
+            step.accumulate_microbatch(Layers([emb, fc]))
+        with pytest.raises(RuntimeError, match="discard_macro_batch"):
+            step.finish_macro_batch(4, check_status=False)
+        assert step.t == 0
+        step.discard_macro_batch()
+        assert begun_anew(step, calls, Layers([emb, fc])) and step.examples_seen == 4
+
+
+def test_ranks_discard_a_macro_batch_that_one_of_them_has_spoilt(monkeypatch):
+    agreed = []
+
+    class Dist:
+        ReduceOp = torch.distributed.ReduceOp
+
+        def get_backend(self):
+            return "gloo"
+
+        def all_reduce(self, t, op=None):
+            agreed.append(int(t))
+    step, calls, emb, fc = make(monkeypatch)
+    update = ShardedUpdate(step, Dist(), 1, 0, poll_fn=lambda: 0)
+    step.head_backward(2, Head(), None, None)
+    calls.fails = "dp_vocab_loss_clipped_accumulate"
+    with pytest.raises(RuntimeError):
+        step.accumulate_microbatch(Layers([emb, fc]))
+    calls.fails = None
+    with pytest.raises(step_module.DeviceStatusError):
+        update.finish_macro_batch()
+    assert agreed and agreed[0] < 0 and step.t == 0
+    assert begun_anew(step, calls, Layers([emb, fc]))
